@@ -192,6 +192,69 @@ int spion_attn_bwd(const void *Q, const void *K, const void *V, const void *O, c
                    void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
+ * The attention with what a Transformer adds inside its softmax: a learned relative position bias by buckets, dropout of the
+ * probabilities, and sequences shorter than the batch's length.  NULL and zero members leave a part out.
+ *   S_qk = scale * Q_q K_k + table[bucket_of[k - q + L - 1]][head] on the kept blocks, for keys k < lengths[b];
+ *   P = softmax over those, LSE its log-sum-exp;  O_q = sum_k c M_qk P_qk V_k, c = 1 / (1 - p).
+ *   M_qk is 0 where the 16-bit draw of (batch item and head, q, k) is below t = rint(65536 p), else 1; c = 65536 / (65536 - t).
+ *   The draw is half q % 2 of word k % 4 of the Philox4x32 call (7 rounds) with key seed and counter
+ *   ((q / 2) * 2^14 + k / 4, batch * H + head + 2^31, offset mod 2^32, stream): the same for any block size and kernel.
+ * A row that keeps nothing (no key below the length, biases that mask) gives O = 0, LSE = -inf and no gradient.  Rows and keys from
+ * the length on: O = 0, LSE = -inf, gradients 0; what Q, K, V and dO hold there, NaN included, does not enter any other result.
+ * A bias of -infinity, or down from -1e30, masks; up to a few thousand in magnitude biases keep the full accuracy.
+ */
+typedef struct {
+    const void *table;         /* [n_buckets, H], or NULL: no bias */
+    const uint8_t *bucket_of;  /* [2 L - 1], bucket of each k - q; an entry from n_buckets on counts as the last bucket */
+    const int32_t *lengths;    /* [B], clipped to 0 .. L, or NULL: all L */
+    const int64_t *rng;        /* {seed, offset}, read when the kernels run; may be NULL where dropout is 0 */
+    int64_t *rng_used;         /* spion_attn_fwd_with: receives a copy of rng (for the backward call), or NULL */
+    double dropout;            /* p, 0 <= p < 1 */
+    int32_t n_buckets;         /* 1 .. 256 where there is a table */
+    int32_t table_dtype;       /* spion_dtype of table and dtable */
+    uint32_t stream;           /* tells apart the dropouts that share an rng */
+    uint32_t reserved;         /* must be 0 */
+} spion_attn_extras;
+
+/* Bytes of device scratch of the two calls below; (size_t)-1 if the parameters are unsupported.  table_grad: whether the backward
+ * call gets a dtable. */
+size_t spion_attn_with_workspace_bytes(const spion_attn_params *p, const spion_attn_extras *x, int32_t nnzb, int32_t is_bwd,
+                                       int32_t table_grad);
+/* As spion_attn_fwd; flags must be 0.  x, p: HOST pointers. */
+int spion_attn_fwd_with(const void *Q, const void *K, const void *V, void *O, float *LSE, const int32_t *row_ptr,
+                        const int32_t *col_idx, int32_t nnzb, const spion_attn_params *p, const spion_attn_extras *x,
+                        void *workspace, size_t workspace_bytes, void *hip_stream);
+/* Gradient of spion_attn_fwd_with (same rng): dQ, dK, dV as spion_attn_bwd, and
+ *   dtable[b][head] = sum of dS_qk over all (batch, q, k) of bucket b, dS = P .* (c M .* (dO V^T) - delta);
+ * fp32 sums in a fixed order.  dtable [n_buckets, H] in table_dtype, or NULL.  flags must be 0. */
+int spion_attn_bwd_with(const void *Q, const void *K, const void *V, const void *O, const void *dO, const float *LSE,
+                        void *dQ, void *dK, void *dV, void *dtable, const int32_t *row_ptr, const int32_t *col_idx,
+                        const int32_t *col_ptr, const int32_t *row_idx, const int32_t *bsr_pos, int32_t nnzb,
+                        const spion_attn_params *p, const spion_attn_extras *x, void *workspace, size_t workspace_bytes,
+                        void *hip_stream);
+
+/*
+ * The same bias as a dense tensor, for the dense-attention phase that precedes a pattern (Section 4.1), and its gradient.
+ *   bias [H, q_len, k_len] = table[bucket_of[j - i - q_start + reach - 1]][h], table [n_buckets, H], both of `dtype`;
+ *   bucket_of [2 reach - 1]; q_start + q_len <= reach and k_len <= reach.  Query i has position q_start + i.
+ *   dtable[b][h] = sum of dbias[h][i][j] over the elements of bucket b; fp32 sums in a fixed order.
+ */
+int spion_relative_bias(const void *table, const uint8_t *bucket_of, void *bias, int32_t reach, int32_t n_buckets, int32_t H,
+                        int32_t q_len, int32_t k_len, int32_t q_start, int32_t dtype, void *hip_stream);
+size_t spion_relative_bias_workspace_bytes(int32_t n_buckets, int32_t H, int32_t q_len, int32_t k_len);
+int spion_relative_bias_grad(const void *dbias, const uint8_t *bucket_of, void *dtable, int32_t reach, int32_t n_buckets,
+                             int32_t H, int32_t q_len, int32_t k_len, int32_t q_start, int32_t dtype, void *workspace,
+                             size_t workspace_bytes, void *hip_stream);
+
+/*
+ * The end of the sub-layer (Algorithm 5: dropout, residual): y_i = residual_i + c M_i x_i for n elements of `dtype`; residual may
+ * be NULL.  M and c as above; the draw of element i is half i % 2 of word (i / 2) % 4 of the call with counter (i / 8 mod 2^32,
+ * i / 8 / 2^32, offset mod 2^32, stream).  The gradient with respect to x is the same call on dy without a residual.
+ */
+int spion_dropout_add(const void *x, const void *residual, void *y, int64_t n, int32_t dtype, double dropout, const int64_t *rng,
+                      int64_t *rng_used, uint32_t stream, void *hip_stream);
+
+/*
  * Producers of the pattern input.
  *
  * spion_score_mean: the score maps of the heads (and batch items) of a layer are averaged into the

@@ -15,4 +15,5 @@ from .binding import (  # noqa: F401
     frobenius_distance, spion_index_check, index_is_well_formed, spion_copy_yardstick,
 )
 from .autograd import sparse_attention  # noqa: E402,F401
+from .extras import RelativeBuckets, dropout_add, relative_bias, relative_buckets  # noqa: E402,F401
 from .sublayer import SparseMHA  # noqa: E402,F401

@@ -1,0 +1,94 @@
+// What the attention kernels with a relative position bias, dropout and sequence lengths have in common.
+//
+// Bias: score(q, k) += T[bucket_of[k - q + L - 1]][head].  The kernels add it as the value an MFMA accumulator starts from,
+// divided by the score scale, so that it costs no instruction beside its reading.
+//
+// Dropout: Philox4x32 with 7 rounds (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011: the
+// fewest that pass BigCrush).  Query q and key k of head bh have half q % 2 of word k % 4 of the call with counter
+// ((q / 2) 2^14 + k / 4, bh + 2^31, offset, stream) and key seed: 16 bits, so that p is taken in steps of 2^-16.  The
+// mask depends on the element's place alone, not on which kernel, side or block size computes it, and is never stored.
+// A call serves two queries by four keys: the lanes of a query-side tile (one query, four keys each) share it in pairs, those
+// of a key-side tile (one key, four queries each) in fours.
+#ifndef SPION_ATTN_EXTRAS_H_
+#define SPION_ATTN_EXTRAS_H_
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "attn_common.h"
+#include "philox.h"
+#include "spion_internal.h"
+
+namespace spion {
+
+constexpr float kMaskedBias = -1e30f;   // a bias from here down masks, as -infinity does
+
+__device__ __forceinline__ int length_of(const Extras& x, int bh, int L) {
+    if (!x.lengths) return L;
+    const int n = x.lengths[bh / x.H];
+    return n < 0 ? 0 : n > L ? L : n;
+}
+
+// The head's column of the table into LDS, as what the accumulators start from; all threads of the workgroup, which has to
+// meet before it is read.  Entries of the map beyond the table read its last bucket (the table is never read past its end).
+__device__ __forceinline__ void load_bias_table(float* tab, const Extras& x, int h, int tid, int threads) {
+    for (int b = tid; b < x.n_buckets; b += threads) {
+        const size_t at = (size_t)b * x.H + h;
+        const float v = x.table_bf16 ? (float)static_cast<const bf16_t*>(x.table)[at] : static_cast<const float*>(x.table)[at];
+        tab[b] = v <= kMaskedBias ? -INFINITY : v * x.inv_scale;
+    }
+}
+__device__ __forceinline__ int bucket_index(const Extras& x, unsigned b) { return (int)min(b, (unsigned)x.n_buckets - 1u); }
+
+struct ScoreDraws {
+    PhiloxKey key;
+    unsigned bh;
+    __device__ __forceinline__ ScoreDraws(const Extras& x, int bh_) : key(x.rng, x.stream), bh((unsigned)bh_ | 0x80000000u) {}
+    // queries q, q ^ 1 and keys k .. k + 3 (k a multiple of 4)
+    __device__ __forceinline__ uint4 call(int q, int k) const { return key.words((unsigned)(q >> 1) << 14 | (unsigned)k >> 2, bh); }
+};
+
+// Draws of query q and the keys k .. k + 3, one call a lane.
+__device__ __forceinline__ void query_draws(const ScoreDraws& d, int q, int k, unsigned (&u)[4]) {
+    const uint4 w = d.call(q, k);
+    const int s = (q & 1) * 16;
+    u[0] = w.x >> s & 0xffffu;
+    u[1] = w.y >> s & 0xffffu;
+    u[2] = w.z >> s & 0xffffu;
+    u[3] = w.w >> s & 0xffffu;
+}
+// Draws of the queries q .. q + 3 (q a multiple of 4) and key k.
+__device__ __forceinline__ void key_draws(const ScoreDraws& d, int q, int k, unsigned (&u)[4]) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const uint4 w = d.call(q + 2 * e, k & ~3);
+        const unsigned lo = (k & 1) ? w.y : w.x, hi = (k & 1) ? w.w : w.z, v = (k & 2) ? hi : lo;
+        u[2 * e] = v & 0xffffu;
+        u[2 * e + 1] = v >> 16;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// Sums over the diagonals (equal key - query) of dS tiles.  Lane (r, g) holds dS of query r and keys 16 kt + 4 g + i, i.e. of
+// distance d = 16 kt + 4 g + i - r.  Element i moved i lanes down the row of 16 lies in the lane p = r - i of distance 16 kt + 4 g - p
+// whatever i; those that leave the row at its lower end come in again at its upper one, one tile of 16 keys further on.
+// Six additions with a lane shift for each tile of 16 keys leave u[0 .. NKT], of distance 16 kt + 4 g - p.
+// ------------------------------------------------------------------------------------------------
+template <int CTRL>
+__device__ __forceinline__ float row_moved(float v) {   // 0 from beyond the row of 16 lanes
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+template <int NKT>
+__device__ __forceinline__ void diagonal_sums(const f32x4 (&ds)[NKT], float (&u)[NKT + 1]) {
+    float carry = 0.f;
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt) {
+        const f32x4 x = ds[kt];
+        u[kt] = carry + (x[0] + row_moved<0x101>(x[1]) + row_moved<0x102>(x[2]) + row_moved<0x103>(x[3]));   // row_shl:1, 2, 3
+        carry = row_moved<0x11f>(x[1]) + row_moved<0x11e>(x[2]) + row_moved<0x11d>(x[3]);                    // row_shr:15, 14, 13
+    }
+    u[NKT] = carry;
+}
+
+}  // namespace spion
+#endif

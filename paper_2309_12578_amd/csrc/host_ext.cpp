@@ -7,6 +7,8 @@
 // parsing by format strings.
 #include <Python.h>
 
+#include <cmath>
+
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <ATen/autocast_mode.h>
@@ -691,6 +693,370 @@ PyObject* py_projection(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ------------------------------------------------------------------------------------------------
+// Attention with extras, the dense bias, dropout: nodes that save what their backward entry points take.
+// ------------------------------------------------------------------------------------------------
+[[noreturn]] void not_implemented(const char* what) {
+    PyErr_SetString(PyExc_NotImplementedError, what);
+    throw python_error();
+}
+
+// A tensor that the kernels may read and an autograd node of this file may differentiate; `device`: the call's, once known.
+void check_operand(const at::Tensor& t, const std::optional<at::Device>& device) {
+    using c10::DispatchKey;
+    for (DispatchKey k : {DispatchKey::Functionalize, DispatchKey::FuncTorchBatched, DispatchKey::Batched, DispatchKey::FuncTorchGradWrapper,
+                          DispatchKey::Negative, DispatchKey::ZeroTensor})
+        if (t.key_set().has(k)) not_implemented("libspion's operators take plain tensors, none that a transform or a lazy view has made");
+    if (t._fw_grad(0).defined()) not_implemented("libspion's operators have no forward-mode derivative");
+    if (!t.is_cuda() || t.layout() != at::kStrided) bad_value("libspion needs device tensors");
+    if (device && t.device() != *device) bad_value("the tensors of a call must be on one device");
+}
+void not_traced() {
+    if (torch::jit::tracer::isTracing()) not_implemented("libspion's operators of this kind cannot be traced");
+}
+int dtype_code(const at::Tensor& t) {
+    if (t.scalar_type() == at::kFloat) return SPION_F32;
+    if (t.scalar_type() == at::kBFloat16) return SPION_BF16;
+    bad_value("unsupported dtype");
+}
+// Contiguous, and aligned to the 16 bytes that the attention kernels load at once.
+at::Tensor dense(const at::Tensor& t) {
+    const at::Tensor c = t.contiguous();
+    return (uintptr_t)c.data_ptr() % 16 == 0 ? c : c.clone();
+}
+int64_t long_arg(PyObject* o) {
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) throw python_error();
+    return v;
+}
+// {seed, offset} on the call's device
+at::Tensor rng_arg(PyObject* o, const at::Device& device) {
+    if (o == Py_None) bad_value("dropout needs rng, an int64 tensor {seed, offset}");
+    const at::Tensor& t = tensor_arg(o);
+    check_operand(t, device);
+    if (t.scalar_type() != at::kLong || t.numel() != 2 || !t.is_contiguous()) bad_value("rng must be a contiguous int64 tensor {seed, offset}");
+    return t;
+}
+unsigned stream_arg(PyObject* o) {
+    const int64_t v = long_arg(o);
+    if (v < 0 || v > 0xffffffffll) bad_value("stream must be a number of 32 bits");
+    return (unsigned)v;
+}
+double dropout_arg(PyObject* o) {
+    const double p = double_arg(o);
+    if (!(p >= 0.0 && p < 1.0) || std::nearbyint(65536.0 * p) > 65535.0) bad_value("dropout must be a probability below 1 (steps of 2^-16)");
+    return p;
+}
+at::Tensor new_longs(int64_t n, const at::Tensor& like) {
+    return at::Tensor(at::detail::empty_cuda({n}, at::kLong, like.device(), std::nullopt));
+}
+// What a node of this kind does about exceptions and second derivatives.
+template <class F>
+torch::autograd::variable_list differentiate(const char* twice, F&& f) {
+    TORCH_CHECK_NOT_IMPLEMENTED(!at::GradMode::is_enabled(), twice);
+    try {
+        return f();
+    } catch (const SpionFailure& e) {
+        PyGILState_STATE gil = PyGILState_Ensure();
+        spion_error(e.code, e.what);
+        python_error err;
+        err.persist();
+        PyGILState_Release(gil);
+        throw err;
+    } catch (const BadValue& e) {
+        TORCH_CHECK_VALUE(false, e.msg);
+    }
+}
+
+struct AttentionExtras {
+    at::Tensor bucket_of, lengths;
+    int n_buckets = 0;
+    double dropout = 0.0;
+    unsigned stream = 0;
+    spion_attn_extras params(const at::Tensor& table, const at::Tensor& rng) const {
+        spion_attn_extras x = {};
+        x.table = table.defined() ? table.data_ptr() : nullptr;
+        x.bucket_of = table.defined() ? (const uint8_t*)bucket_of.data_ptr() : nullptr;
+        x.lengths = lengths.defined() ? (const int32_t*)lengths.data_ptr() : nullptr;
+        x.rng = rng.defined() ? (const int64_t*)rng.data_ptr() : nullptr;
+        x.dropout = dropout;
+        x.n_buckets = n_buckets;
+        x.table_dtype = table.defined() ? dtype_code(table) : SPION_F32;
+        x.stream = stream;
+        return x;
+    }
+};
+
+at::Tensor with_workspace(const spion_attn_params& p, const spion_attn_extras& x, const Index& ix, bool is_bwd, bool table_grad, const at::Tensor& like) {
+    const size_t n = spion_attn_with_workspace_bytes(&p, &x, ix.nnzb, is_bwd, table_grad);
+    return new_bytes(n == (size_t)-1 ? 0 : n, like);   // what is unsupported the call itself tells
+}
+
+struct AttentionWithBackward : public torch::autograd::Node {
+    torch::autograd::SavedVariable q, k, v, o, lse, table, lengths, rng;
+    Index ix;
+    AttentionExtras extras;
+
+    std::string name() const override { return "SparseAttentionWithBackward"; }
+
+    void release_variables() override {
+        for (torch::autograd::SavedVariable* s : {&q, &k, &v, &o, &lse, &table, &lengths, &rng}) s->reset_data();
+    }
+
+    torch::autograd::variable_list apply(torch::autograd::variable_list&& grads) override {
+        torch::autograd::variable_list out(extras.n_buckets ? 4 : 3);
+        if (!grads[0].defined()) return out;
+        return differentiate("sparse_attention cannot be differentiated twice", [&] {
+            const at::Tensor Q = q.unpack(), K = k.unpack(), V = v.unpack(), O = o.unpack(shared_from_this()), stat = lse.unpack();
+            const at::Tensor T = table.unpack(), R = rng.unpack();
+            AttentionExtras with = extras;
+            with.lengths = lengths.unpack();
+            const c10::DeviceGuard guard(Q.device());
+            const at::Tensor g = dense(grads[0]);
+            const spion_attn_params p = params_of(Q, ix);
+            for (const at::Tensor* t : {&K, &V, &O, &g}) room_for(Q, *t);
+            room_for_rows(Q, stat);
+            const spion_attn_extras x = with.params(T, R);
+            const bool table_grad = T.defined() && task_should_compute_output(3);
+            for (int i = 0; i < 3; ++i) out[i] = new_like(Q);
+            if (table_grad) out[3] = new_like(T);
+            const at::Tensor ws = with_workspace(p, x, ix, true, table_grad, Q);
+            const int rc = spion_attn_bwd_with(
+                device_ptr(Q), device_ptr(K), device_ptr(V), device_ptr(O), device_ptr(g), (const float*)device_ptr(stat), device_ptr(out[0]),
+                device_ptr(out[1]), device_ptr(out[2]), table_grad ? device_ptr(out[3]) : nullptr, (const int32_t*)device_ptr(ix.row_ptr),
+                (const int32_t*)device_ptr(ix.col_idx), (const int32_t*)device_ptr(ix.col_ptr), (const int32_t*)device_ptr(ix.row_idx),
+                (const int32_t*)device_ptr(ix.bsr_pos), ix.nnzb, &p, &x, device_ptr(ws), (size_t)ws.nbytes(), current_stream());
+            if (rc != SPION_OK) throw SpionFailure{rc, "spion_attn_bwd_with"};
+            return out;
+        });
+    }
+};
+
+// sparse_attention_with(Q, K, V, row_ptr, col_idx, col_ptr, row_idx, bsr_pos, nnzb, block, scale, table | None, bucket_of | None,
+//                       lengths | None, dropout, rng | None, stream) -> O
+PyObject* py_sparse_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!arg_count(n, 17, "sparse_attention_with")) return nullptr;
+    return guarded([&]() -> PyObject* {
+        not_traced();
+        const at::Tensor &q = tensor_arg(a[0]), &k = tensor_arg(a[1]), &v = tensor_arg(a[2]);
+        check_operand(q, std::nullopt);
+        const at::Device device = q.device();
+        check_operand(k, device);
+        check_operand(v, device);
+        if (q.dim() != 4 || k.sizes() != q.sizes() || v.sizes() != q.sizes() || k.scalar_type() != q.scalar_type() ||
+            v.scalar_type() != q.scalar_type())
+            bad_value("Q, K and V must have one shape [B, H, L, 64] and one dtype");
+        Index ix;
+        ix.row_ptr = tensor_arg(a[3]);
+        ix.col_idx = tensor_arg(a[4]);
+        ix.nnzb = int_arg(a[8]);
+        ix.block = int_arg(a[9]);
+        ix.scale = (float)double_arg(a[10]);
+        for (const at::Tensor* t : {&ix.row_ptr, &ix.col_idx}) check_operand(*t, device);
+        AttentionExtras extras;
+        at::Tensor table = optional_arg(a[11]);
+        extras.lengths = optional_arg(a[13]);
+        extras.dropout = dropout_arg(a[14]);
+        extras.stream = stream_arg(a[16]);
+        if (table.defined()) {
+            check_operand(table, device);
+            extras.bucket_of = tensor_arg(a[12]);
+            check_operand(extras.bucket_of, device);
+            dtype_code(table);
+            if (table.dim() != 2 || table.size(1) != q.size(1)) bad_value("the bias table must be [buckets, H]");
+            if (table.size(0) < 1 || table.size(0) > 256) bad_value("the bias table must have 1 to 256 buckets");
+            if (extras.bucket_of.scalar_type() != at::kByte || !extras.bucket_of.is_contiguous() || extras.bucket_of.numel() != 2 * q.size(2) - 1)
+                bad_value("the buckets must be a contiguous uint8 map of 2 L - 1 distances");
+            extras.n_buckets = (int)table.size(0);
+        }
+        if (extras.lengths.defined()) {
+            check_operand(extras.lengths, device);
+            if (extras.lengths.scalar_type() != at::kInt || extras.lengths.numel() != q.size(0) || !extras.lengths.is_contiguous())
+                bad_value("lengths must be a contiguous int32 tensor [B]");
+        }
+        const bool drop = std::nearbyint(65536.0 * extras.dropout) > 0.0;
+        at::Tensor rng, used;
+        if (drop) rng = rng_arg(a[15], device);
+        const c10::DeviceGuard guard(device);
+        const bool grad = table.defined() ? torch::autograd::compute_requires_grad(q, k, v, table) : torch::autograd::compute_requires_grad(q, k, v);
+        at::Tensor o, lse, qc, kc, vc, tc;
+        {
+            at::NoGradGuard no_grad;
+            qc = dense(q);
+            kc = dense(k);
+            vc = dense(v);
+            if (table.defined()) tc = table.contiguous();
+            const spion_attn_params p = params_of(qc, ix);
+            o = new_like(qc);
+            lse = at::Tensor(at::detail::empty_cuda({q.size(0), q.size(1), q.size(2)}, at::kFloat, device, std::nullopt));
+            if (drop && grad) used = new_longs(2, qc);
+            spion_attn_extras x = extras.params(tc, rng);
+            if (used.defined()) x.rng_used = (int64_t*)used.data_ptr();
+            const at::Tensor ws = with_workspace(p, x, ix, false, false, qc);
+            const int rc = spion_attn_fwd_with(device_ptr(qc), device_ptr(kc), device_ptr(vc), device_ptr(o), (float*)device_ptr(lse),
+                                               (const int32_t*)device_ptr(ix.row_ptr), (const int32_t*)device_ptr(ix.col_idx), ix.nnzb, &p, &x,
+                                               device_ptr(ws), (size_t)ws.nbytes(), current_stream());
+            if (rc != SPION_OK) throw SpionFailure{rc, "spion_attn_fwd_with"};
+        }
+        if (grad) {
+            ix.col_ptr = tensor_arg(a[5]);
+            ix.row_idx = tensor_arg(a[6]);
+            ix.bsr_pos = tensor_arg(a[7]);
+            for (const at::Tensor* t : {&ix.col_ptr, &ix.row_idx, &ix.bsr_pos}) check_operand(*t, device);
+            auto node = std::shared_ptr<AttentionWithBackward>(new AttentionWithBackward(), torch::autograd::deleteNode);
+            node->set_next_edges(table.defined() ? torch::autograd::collect_next_edges(q, k, v, table) : torch::autograd::collect_next_edges(q, k, v));
+            node->q = torch::autograd::SavedVariable(qc, false);
+            node->k = torch::autograd::SavedVariable(kc, false);
+            node->v = torch::autograd::SavedVariable(vc, false);
+            node->lse = torch::autograd::SavedVariable(lse, false);
+            node->table = torch::autograd::SavedVariable(tc, false);
+            node->lengths = torch::autograd::SavedVariable(extras.lengths, false);
+            node->rng = torch::autograd::SavedVariable(used, false);
+            extras.lengths.reset();
+            node->extras = std::move(extras);
+            node->ix = std::move(ix);
+            torch::autograd::set_history(o, node);
+            node->o = torch::autograd::SavedVariable(o, true);
+        }
+        return wrap(o);
+    });
+}
+
+struct RelativeBiasBackward : public torch::autograd::Node {
+    at::Tensor bucket_of;
+    at::ScalarType type = at::kFloat;
+    int reach = 0, n_buckets = 0, H = 0, q_len = 0, k_len = 0, q_start = 0;
+
+    std::string name() const override { return "RelativeBiasBackward"; }
+
+    torch::autograd::variable_list apply(torch::autograd::variable_list&& grads) override {
+        torch::autograd::variable_list out(1);
+        if (!grads[0].defined()) return out;
+        return differentiate("relative_bias cannot be differentiated twice", [&] {
+            const c10::DeviceGuard guard(bucket_of.device());
+            const at::Tensor g = grads[0].contiguous();
+            if (g.scalar_type() != type || g.numel() != (int64_t)H * q_len * k_len) bad_value("relative_bias: a gradient of another shape");
+            out[0] = at::Tensor(at::detail::empty_cuda({n_buckets, H}, type, g.device(), std::nullopt));
+            const at::Tensor ws = new_bytes(spion_relative_bias_workspace_bytes(n_buckets, H, q_len, k_len), g);
+            const int rc = spion_relative_bias_grad(device_ptr(g), (const uint8_t*)device_ptr(bucket_of), device_ptr(out[0]), reach, n_buckets, H, q_len,
+                                                    k_len, q_start, dtype_code(g), device_ptr(ws), (size_t)ws.nbytes(), current_stream());
+            if (rc != SPION_OK) throw SpionFailure{rc, "spion_relative_bias_grad"};
+            return out;
+        });
+    }
+};
+
+// relative_bias(table, bucket_of, q_len, k_len, q_start) -> [H, q_len, k_len]
+PyObject* py_relative_bias(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!arg_count(n, 5, "relative_bias")) return nullptr;
+    return guarded([&]() -> PyObject* {
+        not_traced();
+        const at::Tensor &table = tensor_arg(a[0]), &bucket_of = tensor_arg(a[1]);
+        check_operand(table, std::nullopt);
+        check_operand(bucket_of, table.device());
+        const int64_t q_len = long_arg(a[2]), k_len = long_arg(a[3]), q_start = long_arg(a[4]);
+        if (table.dim() != 2 || table.size(0) < 1 || table.size(0) > 256 || table.size(1) < 1) bad_value("the bias table must be [buckets, H], 1 to 256 buckets");
+        if (bucket_of.scalar_type() != at::kByte || !bucket_of.is_contiguous() || bucket_of.numel() % 2 != 1)
+            bad_value("the buckets must be a contiguous uint8 map of 2 L - 1 distances");
+        const int64_t reach = (bucket_of.numel() + 1) / 2;
+        if (q_len < 1 || k_len < 1 || q_start < 0 || q_len > reach || q_start > reach - q_len || k_len > reach)
+            bad_value("the buckets do not reach over the positions asked for");
+        const c10::DeviceGuard guard(table.device());
+        const at::Tensor tc = table.contiguous();
+        const int code = dtype_code(tc);
+        at::Tensor bias(at::detail::empty_cuda({table.size(1), q_len, k_len}, tc.scalar_type(), tc.device(), std::nullopt));
+        const int rc = spion_relative_bias(device_ptr(tc), (const uint8_t*)device_ptr(bucket_of), device_ptr(bias), (int)reach, (int)table.size(0),
+                                           (int)table.size(1), (int)q_len, (int)k_len, (int)q_start, code, current_stream());
+        if (rc != SPION_OK) throw SpionFailure{rc, "spion_relative_bias"};
+        if (torch::autograd::compute_requires_grad(table)) {
+            auto node = std::shared_ptr<RelativeBiasBackward>(new RelativeBiasBackward(), torch::autograd::deleteNode);
+            node->set_next_edges(torch::autograd::collect_next_edges(table));
+            node->bucket_of = bucket_of;
+            node->type = tc.scalar_type();
+            node->reach = (int)reach;
+            node->n_buckets = (int)table.size(0);
+            node->H = (int)table.size(1);
+            node->q_len = (int)q_len;
+            node->k_len = (int)k_len;
+            node->q_start = (int)q_start;
+            torch::autograd::set_history(bias, node);
+        }
+        return wrap(bias);
+    });
+}
+
+void dropout_call(const at::Tensor& x, const at::Tensor& residual, const at::Tensor& y, double p, const at::Tensor& rng, const at::Tensor& used, unsigned stream) {
+    if (x.numel() == 0) return;
+    const int rc = spion_dropout_add(device_ptr(x), residual.defined() ? device_ptr(residual) : nullptr, device_ptr(y), x.numel(), dtype_code(x), p,
+                                     (const int64_t*)device_ptr(rng), used.defined() ? (int64_t*)device_ptr(used) : nullptr, stream, current_stream());
+    if (rc != SPION_OK) throw SpionFailure{rc, "spion_dropout_add"};
+}
+
+struct DropoutAddBackward : public torch::autograd::Node {
+    torch::autograd::SavedVariable rng;
+    double p = 0.0;
+    unsigned stream = 0;
+    bool has_residual = false;
+
+    std::string name() const override { return "DropoutAddBackward"; }
+
+    void release_variables() override { rng.reset_data(); }
+
+    torch::autograd::variable_list apply(torch::autograd::variable_list&& grads) override {
+        torch::autograd::variable_list out(has_residual ? 2 : 1);
+        if (!grads[0].defined()) return out;
+        return differentiate("dropout_add cannot be differentiated twice", [&] {
+            const c10::DeviceGuard guard(grads[0].device());
+            if (has_residual && task_should_compute_output(1)) out[1] = grads[0];
+            if (task_should_compute_output(0)) {
+                const at::Tensor g = grads[0].contiguous();
+                out[0] = new_like(g);
+                dropout_call(g, at::Tensor(), out[0], p, rng.unpack(), at::Tensor(), stream);
+            }
+            return out;
+        });
+    }
+};
+
+// dropout_add(x, residual | None, p, rng, stream) -> residual + dropout(x)
+PyObject* py_dropout_add(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!arg_count(n, 5, "dropout_add")) return nullptr;
+    return guarded([&]() -> PyObject* {
+        not_traced();
+        const at::Tensor& x = tensor_arg(a[0]);
+        const at::Tensor residual = optional_arg(a[1]);
+        check_operand(x, std::nullopt);
+        dtype_code(x);
+        if (residual.defined()) {
+            check_operand(residual, x.device());
+            if (residual.sizes() != x.sizes() || residual.scalar_type() != x.scalar_type()) bad_value("residual must have x's shape and dtype");
+        }
+        const double p = dropout_arg(a[2]);
+        const at::Tensor rng = rng_arg(a[3], x.device());
+        const unsigned stream = stream_arg(a[4]);
+        const c10::DeviceGuard guard(x.device());
+        const bool grad = residual.defined() ? torch::autograd::compute_requires_grad(x, residual) : torch::autograd::compute_requires_grad(x);
+        at::Tensor y, used;
+        {
+            at::NoGradGuard no_grad;
+            const at::Tensor xc = x.contiguous();
+            y = new_like(xc);
+            if (grad) used = new_longs(2, xc);
+            dropout_call(xc, residual.defined() ? residual.contiguous() : at::Tensor(), y, p, rng, used, stream);
+        }
+        if (grad) {
+            auto node = std::shared_ptr<DropoutAddBackward>(new DropoutAddBackward(), torch::autograd::deleteNode);
+            node->set_next_edges(residual.defined() ? torch::autograd::collect_next_edges(x, residual) : torch::autograd::collect_next_edges(x));
+            node->rng = torch::autograd::SavedVariable(used, false);
+            node->p = p;
+            node->stream = stream;
+            node->has_residual = residual.defined();
+            torch::autograd::set_history(y, node);
+        }
+        return wrap(y);
+    });
+}
+
 // generate_pattern(A_s, L, block, filter, mode, value, flags, fl_out, row_ptr, col_idx, col_ptr, row_idx, bsr_pos,
 //                  nnzb, pool_sum, workspace | None) -> nnzb, after the pattern is complete
 PyObject* py_generate_pattern(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -738,6 +1104,9 @@ PyMethodDef kMethods[] = {
     {"layer_norm", (PyCFunction)(void*)py_layer_norm, METH_FASTCALL, nullptr},
     {"residual", (PyCFunction)(void*)py_residual, METH_FASTCALL, nullptr},
     {"projection", (PyCFunction)(void*)py_projection, METH_FASTCALL, nullptr},
+    {"sparse_attention_with", (PyCFunction)(void*)py_sparse_attention_with, METH_FASTCALL, nullptr},
+    {"relative_bias", (PyCFunction)(void*)py_relative_bias, METH_FASTCALL, nullptr},
+    {"dropout_add", (PyCFunction)(void*)py_dropout_add, METH_FASTCALL, nullptr},
     {"generate_pattern", (PyCFunction)(void*)py_generate_pattern, METH_FASTCALL, nullptr},
     {"set_error_class", py_set_error_class, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},

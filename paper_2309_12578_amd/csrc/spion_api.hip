@@ -109,6 +109,18 @@ int attn_params_ok(const spion_attn_params* p, int32_t nnzb) {
 // that memory is likely to hold.
 std::atomic<unsigned long long> g_tag{1};
 
+unsigned long long next_tag() {
+    return g_tag.fetch_add(1, std::memory_order_relaxed) * 0x9e3779b97f4a7bull & ((1ull << (64 - spion::kArriveBits)) - 1ull);
+}
+
+// Draws of 16 bits below the threshold are dropped; false: not a probability below 1.
+bool dropout_threshold(double p, unsigned& threshold) {
+    if (!(p >= 0.0 && p < 1.0) || rint(65536.0 * p) > 65535.0) return false;
+    threshold = (unsigned)rint(65536.0 * p);
+    return true;
+}
+float keep_scale(unsigned threshold) { return (float)(65536.0 / (65536.0 - threshold)); }
+
 spion::AttnShape make_shape(const spion_attn_params* p) {
     spion::AttnShape s;
     s.BH = p->B * p->H;
@@ -123,7 +135,7 @@ spion::AttnShape make_shape(const spion_attn_params* p) {
     s.heads_beside = 0;
     s.fwd_room = nullptr;
     s.bwd_room = false;
-    s.tag = g_tag.fetch_add(1, std::memory_order_relaxed) * 0x9e3779b97f4a7bull & ((1ull << (64 - spion::kArriveBits)) - 1ull);
+    s.tag = next_tag();
     return s;
 }
 
@@ -480,6 +492,126 @@ int spion_attn_bwd(const void* Q, const void* K, const void* V, const void* O, c
                                nnzb, workspace, static_cast<hipStream_t>(hip_stream)) != hipSuccess)
         return SPION_ERR_HIP;
     return SPION_OK;
+}
+
+// Whether the parameters of a call with extras are supported, and the extras as the kernels take them.
+static int take_extras(const spion_attn_params* p, const spion_attn_extras* x, int32_t nnzb, spion::Extras& out) {
+    const int rc = attn_params_ok(p, nnzb);
+    if (rc != SPION_OK) return rc;
+    if (p->flags != 0 || x->reserved != 0) return SPION_ERR_PARAM;
+    unsigned threshold = 0;
+    if (!dropout_threshold(x->dropout, threshold)) return SPION_ERR_PARAM;
+    if (p->L > 65536) return SPION_ERR_SHAPE;   // positions in a draw's counter (and SPION_MAX_NB blocks of 64)
+    if (x->table) {
+        if (x->table_dtype != SPION_F32 && x->table_dtype != SPION_BF16) return SPION_ERR_DTYPE;
+        if (x->n_buckets < 1 || x->n_buckets > spion::Extras::kMaxBuckets) return SPION_ERR_PARAM;
+        if (!x->bucket_of) return SPION_ERR_NULL;
+    }
+    if (threshold && !x->rng) return SPION_ERR_NULL;
+    const spion::AttnShape s = make_shape(p);
+    out.table = x->table;
+    out.bucket_of = x->bucket_of;
+    out.lengths = x->lengths;
+    out.rng = reinterpret_cast<const long long*>(x->rng);
+    out.rng_used = reinterpret_cast<long long*>(x->rng_used);
+    out.n_buckets = x->table ? x->n_buckets : 0;
+    out.H = p->H;
+    out.table_bf16 = x->table_dtype == SPION_BF16;
+    out.inv_scale = 1.f / s.scale;
+    out.threshold = threshold;
+    out.stream = x->stream;
+    out.keep_scale = keep_scale(threshold);
+    out.slices = nullptr;
+    return SPION_OK;
+}
+
+size_t spion_attn_with_workspace_bytes(const spion_attn_params* p, const spion_attn_extras* x, int32_t nnzb, int32_t is_bwd,
+                                       int32_t table_grad) {
+    spion::Extras extras;
+    if (!p || !x || take_extras(p, x, nnzb, extras) != SPION_OK) return (size_t)-1;
+    return spion::attn_with_workspace_bytes(make_shape(p), table_grad && extras.table, extras.n_buckets, p->H, nnzb, is_bwd != 0);
+}
+
+int spion_attn_fwd_with(const void* Q, const void* K, const void* V, void* O, float* LSE, const int32_t* row_ptr,
+                        const int32_t* col_idx, int32_t nnzb, const spion_attn_params* p, const spion_attn_extras* x, void* workspace,
+                        size_t workspace_bytes, void* hip_stream) {
+    if (!Q || !K || !V || !O || !LSE || !row_ptr || !col_idx || !p || !x) return SPION_ERR_NULL;
+    spion::Extras extras;
+    const int rc = take_extras(p, x, nnzb, extras);
+    if (rc != SPION_OK) return rc;
+    if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)O) % 16 != 0) return SPION_ERR_PARAM;
+    const spion::AttnShape s = make_shape(p);
+    const size_t need = spion::attn_with_workspace_bytes(s, false, extras.n_buckets, p->H, nnzb, false);
+    if (need && (!workspace || (uintptr_t)workspace % kAlign != 0 || workspace_bytes < need)) return SPION_ERR_WORKSPACE;
+    return spion::launch_attn_fwd_with(s, extras, Q, K, V, O, LSE, row_ptr, col_idx, nnzb, static_cast<hipStream_t>(hip_stream)) ==
+                   hipSuccess ? SPION_OK : SPION_ERR_HIP;
+}
+
+int spion_attn_bwd_with(const void* Q, const void* K, const void* V, const void* O, const void* dO, const float* LSE, void* dQ, void* dK,
+                        void* dV, void* dtable, const int32_t* row_ptr, const int32_t* col_idx, const int32_t* col_ptr,
+                        const int32_t* row_idx, const int32_t* bsr_pos, int32_t nnzb, const spion_attn_params* p,
+                        const spion_attn_extras* x, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (!Q || !K || !V || !O || !dO || !LSE || !dQ || !dK || !dV || !row_ptr || !col_idx || !col_ptr || !row_idx || !bsr_pos || !p || !x)
+        return SPION_ERR_NULL;
+    spion::Extras extras;
+    const int rc = take_extras(p, x, nnzb, extras);
+    if (rc != SPION_OK) return rc;
+    if (dtable && !extras.table) return SPION_ERR_NULL;
+    if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)O | (uintptr_t)dO | (uintptr_t)dQ | (uintptr_t)dK | (uintptr_t)dV) % 16 != 0)
+        return SPION_ERR_PARAM;
+    if (!spion::attn_bwd_grids_fit(p->B * p->H, p->block, p->L / p->block, nnzb)) return SPION_ERR_SHAPE;
+    const spion::AttnShape s = make_shape(p);
+    const size_t need = spion::attn_with_workspace_bytes(s, dtable != nullptr, extras.n_buckets, p->H, nnzb, true);
+    if (need && (!workspace || (uintptr_t)workspace % kAlign != 0 || workspace_bytes < need)) return SPION_ERR_WORKSPACE;
+    return spion::launch_attn_bwd_with(s, extras, Q, K, V, O, dO, LSE, dQ, dK, dV, dtable, row_ptr, col_idx, col_ptr, row_idx, nnzb,
+                                       workspace, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? SPION_OK : SPION_ERR_HIP;
+}
+
+static int relative_bias_args_ok(int32_t reach, int32_t n_buckets, int32_t H, int32_t q_len, int32_t k_len, int32_t q_start, int32_t dtype) {
+    if (dtype != SPION_F32 && dtype != SPION_BF16) return SPION_ERR_DTYPE;
+    if (n_buckets < 1 || n_buckets > spion::Extras::kMaxBuckets) return SPION_ERR_PARAM;
+    if (H < 1 || H > 65535 || q_len < 1 || k_len < 1 || q_start < 0 || reach < 1 || reach > 1 << 20) return SPION_ERR_SHAPE;
+    if ((int64_t)q_start + q_len > reach || k_len > reach) return SPION_ERR_SHAPE;
+    return SPION_OK;
+}
+
+int spion_relative_bias(const void* table, const uint8_t* bucket_of, void* bias, int32_t reach, int32_t n_buckets, int32_t H, int32_t q_len,
+                        int32_t k_len, int32_t q_start, int32_t dtype, void* hip_stream) {
+    if (!table || !bucket_of || !bias) return SPION_ERR_NULL;
+    const int rc = relative_bias_args_ok(reach, n_buckets, H, q_len, k_len, q_start, dtype);
+    if (rc != SPION_OK) return rc;
+    return spion::launch_relative_bias(table, bucket_of, bias, reach, n_buckets, H, q_len, k_len, q_start, dtype == SPION_BF16,
+                                       static_cast<hipStream_t>(hip_stream)) == hipSuccess ? SPION_OK : SPION_ERR_HIP;
+}
+
+size_t spion_relative_bias_workspace_bytes(int32_t n_buckets, int32_t H, int32_t q_len, int32_t k_len) {
+    const int32_t reach = q_len > k_len ? q_len : k_len;
+    if (relative_bias_args_ok(reach, n_buckets, H, q_len, k_len, 0, SPION_F32) != SPION_OK) return (size_t)-1;
+    return spion::relative_bias_grad_workspace_bytes(H, q_len, k_len, n_buckets);
+}
+
+int spion_relative_bias_grad(const void* dbias, const uint8_t* bucket_of, void* dtable, int32_t reach, int32_t n_buckets, int32_t H,
+                             int32_t q_len, int32_t k_len, int32_t q_start, int32_t dtype, void* workspace, size_t workspace_bytes,
+                             void* hip_stream) {
+    if (!dbias || !bucket_of || !dtable) return SPION_ERR_NULL;
+    const int rc = relative_bias_args_ok(reach, n_buckets, H, q_len, k_len, q_start, dtype);
+    if (rc != SPION_OK) return rc;
+    if (!workspace || (uintptr_t)workspace % kAlign != 0 || workspace_bytes < spion_relative_bias_workspace_bytes(n_buckets, H, q_len, k_len))
+        return SPION_ERR_WORKSPACE;
+    return spion::launch_relative_bias_grad(dbias, bucket_of, dtable, reach, n_buckets, H, q_len, k_len, q_start, dtype == SPION_BF16, next_tag(),
+                                            workspace, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? SPION_OK : SPION_ERR_HIP;
+}
+
+int spion_dropout_add(const void* x, const void* residual, void* y, int64_t n, int32_t dtype, double dropout, const int64_t* rng,
+                      int64_t* rng_used, uint32_t stream, void* hip_stream) {
+    if (!x || !y || !rng) return SPION_ERR_NULL;
+    if (dtype != SPION_F32 && dtype != SPION_BF16) return SPION_ERR_DTYPE;
+    if (n < 1) return SPION_ERR_SHAPE;
+    unsigned threshold = 0;
+    if (!dropout_threshold(dropout, threshold)) return SPION_ERR_PARAM;
+    return spion::launch_dropout(x, residual, y, n, reinterpret_cast<const long long*>(rng), reinterpret_cast<long long*>(rng_used), stream,
+                                 threshold, keep_scale(threshold), dtype == SPION_BF16, static_cast<hipStream_t>(hip_stream)) == hipSuccess
+               ? SPION_OK : SPION_ERR_HIP;
 }
 
 int spion_heads_attn_fwd(const void* qkv, void* S, float* LSE, const int32_t* row_ptr, const int32_t* col_idx, int32_t nnzb,

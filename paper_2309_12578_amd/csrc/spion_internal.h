@@ -49,6 +49,21 @@ struct AttnShape {
     unsigned long long tag;       // of this call alone, below 2^(64 - kArriveBits) (see last_to_arrive)
 };
 
+// What spion_attn_fwd_with / _bwd_with add to the attention, as the kernels take it (attn_extras.h).
+struct Extras {
+    const void* table;                // [n_buckets, H] or nullptr
+    const uint8_t* bucket_of;         // [2 L - 1]
+    const int* lengths;               // [B] or nullptr
+    const long long* rng;             // {seed, offset}, where there is dropout
+    long long* rng_used;              // forward: receives a copy of them, or nullptr
+    int n_buckets, H, table_bf16;
+    float inv_scale;                  // 1 / score scale
+    unsigned threshold, stream;       // draws below are dropped; 0: no dropout
+    float keep_scale;                 // 65536 / (65536 - threshold)
+    float* slices;                    // backward: sums of dS over diagonals, or nullptr: no gradient of the table
+    static constexpr int kMaxBuckets = 256;
+};
+
 // How the kernels cut long block rows (see attn_bf16_tiles.h), from what the host knows of a pattern.
 struct RowCut {
     int piece = 0;     // kept blocks of a piece, at most, unless there are too many pieces (row_pieces())
@@ -101,6 +116,24 @@ struct BwdWorkspace {
 BwdWorkspace attn_bwd_workspace(const AttnShape& s, int nnzb);   // its sizes
 // false when a backward launch for this shape would need more workgroups than a 1-D grid can hold
 bool attn_bwd_grids_fit(int BH, int bs, int nb, int nnzb);
+
+// attn_extras_kernels.hip: the attention with a relative position bias, dropout and lengths (fp32, bf16), and the gradient of
+// the bias table from the diagonal sums that the backward pass leaves
+hipError_t launch_attn_fwd_with(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, void* O, float* LSE,
+                                const int* row_ptr, const int* col_idx, int nnzb, hipStream_t st);
+hipError_t launch_attn_bwd_with(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, const void* O,
+                                const void* dO, const float* LSE, void* dQ, void* dK, void* dV, void* dtable, const int* row_ptr,
+                                const int* col_idx, const int* col_ptr, const int* row_idx, int nnzb, void* workspace, hipStream_t st);
+size_t attn_with_workspace_bytes(const AttnShape& s, bool table_grad, int n_buckets, int H, int nnzb, bool is_bwd);
+
+// dropout_kernels.hip: y = residual + dropout(x) (residual nullptr: without), the dense bias and its table's gradient
+hipError_t launch_dropout(const void* x, const void* residual, void* y, long long n, const long long* rng, long long* rng_used, unsigned stream,
+                          unsigned threshold, float keep_scale, bool is_bf16, hipStream_t st);
+hipError_t launch_relative_bias(const void* table, const uint8_t* bucket_of, void* bias, int reach, int n_buckets, int H, int q_len, int k_len,
+                                int q_start, bool is_bf16, hipStream_t st);
+size_t relative_bias_grad_workspace_bytes(int H, int q_len, int k_len, int n_buckets);
+hipError_t launch_relative_bias_grad(const void* dbias, const uint8_t* bucket_of, void* dtable, int reach, int n_buckets, int H, int q_len, int k_len,
+                                     int q_start, bool is_bf16, unsigned long long tag, void* workspace, hipStream_t st);
 
 // norm_kernels.hip: LayerNorm over rows of D = 64 k <= 2048 elements
 size_t layer_norm_workspace_bytes(int rows, int D);
