@@ -68,6 +68,60 @@ __device__ __forceinline__ void key_draws(const ScoreDraws& d, int q, int k, uns
     }
 }
 
+// Two 16-bit draws or factors in a word.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+
+// Lane l's word of lane l ^ 1, and of l ^ 2.
+__device__ __forceinline__ unsigned from_pair(unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true); }
+__device__ __forceinline__ unsigned from_other_pair(unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true); }
+
+// Factors 0 (dropped) and 1 of two draws; `below` = threshold - 1 in both halves (the threshold is not 0).
+__device__ __forceinline__ u16x2 kept(unsigned draws, u16x2 below) {
+    return __builtin_elementwise_min(__builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, draws), below), (u16x2){1, 1});
+}
+__device__ __forceinline__ u16x2 both_halves(unsigned v) { return (u16x2){(unsigned short)v, (unsigned short)v}; }
+
+// Probabilities with the dropped ones 0: factors as bit patterns, so that nothing is rounded.
+__device__ __forceinline__ bf16x4 drop(bf16x4 p, const u16x2 (&k)[2]) {
+    struct Bits { u16x2 h[2]; } b = __builtin_bit_cast(Bits, p);
+    b.h[0] *= k[0];
+    b.h[1] *= k[1];
+    return __builtin_bit_cast(bf16x4, b);
+}
+
+// Query side: factors of this lane's query q = 16-row tile + r and the keys k0 + 16 kt + 4 g + i, two to a word, NKT even.  A call
+// has two queries' draws: lane r makes those of tile kt = 2 j + r % 2 for itself and its neighbour r ^ 1, which makes the other tile's.
+template <int NKT>
+__device__ __forceinline__ void query_factors(const ScoreDraws& d, int q, int k0, int g, u16x2 below, u16x2 (&f)[NKT][2]) {
+    const bool odd = q & 1;
+    const unsigned mine = odd ? 0x07060302u : 0x05040100u, other = odd ? 0x05040100u : 0x07060302u;   // high or low halves of two words
+#pragma unroll
+    for (int j = 0; j < NKT / 2; ++j) {
+        const uint4 w = d.call(q, k0 + 16 * (2 * j + (q & 1)) + 4 * g);
+        const unsigned a0 = __builtin_amdgcn_perm(w.y, w.x, mine), a1 = __builtin_amdgcn_perm(w.w, w.z, mine);
+        const unsigned b0 = from_pair(__builtin_amdgcn_perm(w.y, w.x, other)), b1 = from_pair(__builtin_amdgcn_perm(w.w, w.z, other));
+        f[2 * j][0] = kept(odd ? b0 : a0, below);
+        f[2 * j][1] = kept(odd ? b1 : a1, below);
+        f[2 * j + 1][0] = kept(odd ? a0 : b0, below);
+        f[2 * j + 1][1] = kept(odd ? a1 : b1, below);
+    }
+}
+
+// Key side: draws of this lane's key k = 16-row tile + r and the queries q0 + 16 h + 4 g + i, h < 2: words [2 h] have i = 0, 1,
+// [2 h + 1] i = 2, 3.  Four calls serve the four keys of lanes 4 a .. 4 a + 3: lane r makes number r % 4 and gets word r % 4 of
+// each of the four (a 4 x 4 transpose in two steps).
+__device__ __forceinline__ void key_words(const ScoreDraws& d, int q0, int k, int g, unsigned (&u)[4]) {
+    const int c = k & 3;
+    const uint4 w = d.call(q0 + 16 * (c >> 1) + 4 * g + 2 * (c & 1), k & ~3);
+    const bool b0 = c & 1, b1 = c & 2;
+    const unsigned x0 = b0 ? from_pair(w.y) : w.x, x1 = b0 ? w.y : from_pair(w.x);
+    const unsigned x2 = b0 ? from_pair(w.w) : w.z, x3 = b0 ? w.w : from_pair(w.z);
+    u[0] = b1 ? from_other_pair(x2) : x0;
+    u[2] = b1 ? x2 : from_other_pair(x0);
+    u[1] = b1 ? from_other_pair(x3) : x1;
+    u[3] = b1 ? x3 : from_other_pair(x1);
+}
+
 // ------------------------------------------------------------------------------------------------
 // Sums over the diagonals (equal key - query) of dS tiles.  Lane (r, g) holds dS of query r and keys 16 kt + 4 g + i, i.e. of
 // distance d = 16 kt + 4 g + i - r.  Element i moved i lanes down the row of 16 lies in the lane p = r - i of distance 16 kt + 4 g - p

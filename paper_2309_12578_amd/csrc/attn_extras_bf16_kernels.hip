@@ -1,0 +1,445 @@
+// The attention of attn_extras_kernels.hip (relative position bias, dropout, lengths) for bf16 and block size 32 or 64: the tile
+// movement, work order and cuts of the plain bf16 kernels, with
+//   - the biases of a block, one for each of its 2 BS - 1 distances, in LDS: two stages, as the tiles; what an accumulator of
+//     S^T starts from is read from there (neighbouring lanes read neighbouring words);
+//   - dropout factors made while the tiles are on their way;
+//   - tiles whose rows from the sequence's length on come as zeros, whatever memory holds there: the loads' range ends with the sequence.
+#include <hip/hip_runtime.h>
+#include <limits.h>
+#include <stdint.h>
+
+#include "attn_bf16_tiles.h"
+#include "attn_common.h"
+#include "attn_extras.h"
+#include "attn_key_items.h"
+#include "spion_internal.h"
+
+namespace spion {
+
+namespace {
+
+template <int BS>
+struct KvTiles {
+    bf16_t k[BS * kD];
+    bf16_t v[BS * kD];
+};
+
+// Own loads landed (all, or all but the four youngest), previous LDS accesses done, then meet the other waves.
+__device__ __forceinline__ void meet(bool four_younger_in_flight) {
+    if (four_younger_in_flight) __builtin_amdgcn_s_waitcnt(kWaitVm4);
+    else __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void lds_meet() {
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Entries of an ascending list whose block starts below `length`, of the n from list on.
+template <int BS>
+__device__ __forceinline__ int blocks_below(const int* list, int n, int length, int L, int lane) {
+    if (length >= L) return n;
+    int count = 0;
+    for (int base = 0; base < n; base += 64) {
+        const int at = base + lane;
+        const int here = __popcll(__ballot(at < n && list[at < n ? at : n - 1] * BS < length));
+        count += here;
+        if (here < 64) break;
+    }
+    return count;
+}
+
+// The biases of a block's distances.  The first BS / 32 waves bring them, a distance a lane: the map's byte is
+// requested a step before it is looked up.
+template <int BS, bool BIAS>
+struct BlockBias {
+    const uint8_t* from;   // map entry of this lane's distance in a block on the diagonal
+    const float* tab;
+    int last;
+    bool mine;
+    __device__ __forceinline__ BlockBias(const Extras& x, const float* tab_, int L, int tid, int wave)
+        : from(nullptr), tab(tab_), last(x.n_buckets - 1), mine(BIAS && wave < BS / 32) {
+        if (BIAS) from = x.bucket_of + (L - BS + (tid < 2 * BS - 2 ? tid : 2 * BS - 2));
+    }
+    __device__ __forceinline__ unsigned request(int blocks_off) const { return mine ? from[(ptrdiff_t)blocks_off * BS] : 0u; }   // key block - query block
+    __device__ __forceinline__ void put(float* slice, unsigned bucket, int tid) const {
+        if (mine) slice[tid] = tab[min((int)bucket, last)];
+    }
+};
+
+// The head's column of the bias table in registers (requested before anything else is), then in LDS.
+template <int BS, bool BIAS>
+struct TableColumn {
+    static constexpr int N = Extras::kMaxBuckets / (BS * 4);
+    float v[N];
+    __device__ __forceinline__ TableColumn(const Extras& x, int h, int tid) {
+        if constexpr (BIAS) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int b = tid + i * BS * 4;
+                v[i] = 0.f;
+                if (b < x.n_buckets) {
+                    const size_t at = (size_t)b * x.H + h;
+                    v[i] = x.table_bf16 ? (float)static_cast<const bf16_t*>(x.table)[at] : static_cast<const float*>(x.table)[at];
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void put(float* tab, const Extras& x, int tid) const {
+        if constexpr (BIAS) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) tab[tid + i * BS * 4] = v[i] <= kMaskedBias ? -INFINITY : v[i] * x.inv_scale;
+        }
+    }
+};
+
+// Where rows of head bh are, see HeadRows.
+struct Rows {
+    int H, beside;
+    __device__ __forceinline__ int in_row() const { return beside ? 3 * H * kD : kD; }
+    __device__ __forceinline__ int out_row() const { return beside ? H * kD : kD; }
+    __device__ __forceinline__ size_t in_head(int bh, int L) const {
+        return beside ? ((size_t)(bh / H) * L * 3 * H + bh % H) * kD : (size_t)bh * L * kD;
+    }
+    __device__ __forceinline__ size_t out_head(int bh, int L) const {
+        return beside ? ((size_t)(bh / H) * L * H + bh % H) * kD : (size_t)bh * L * kD;
+    }
+};
+
+// Bytes of a tile that starts at row `row0` up to the sequence's end.
+template <int BS>
+__device__ __forceinline__ unsigned tile_range(int row0, int length, int row_len) {
+    const int rows = length - row0;
+    return rows >= BS ? 0xffffffffu : rows <= 0 ? 0u : (unsigned)rows * (unsigned)row_len * (unsigned)sizeof(bf16_t);
+}
+
+}  // namespace
+
+// ------------------------------------------------------------------------------------------------
+// forward
+// ------------------------------------------------------------------------------------------------
+struct FwdWith {
+    const bf16_t *Q, *K, *V;
+    bf16_t* O;
+    float* LSE;
+    const int *row_ptr, *col_idx;
+    Rows at;
+    Extras x;
+    RowCut cut;
+    int L, nb, heads, order;
+    float scale_log2;
+};
+
+// The kernel's arguments once more, from memory: what is used at its end only would otherwise sit in scalar registers over the
+// loop, of which there are too few (7 to 61 of them were spilled).
+template <typename Args>
+__device__ __forceinline__ const __attribute__((address_space(4))) Args& args_again() {
+    auto p = reinterpret_cast<const __attribute__((address_space(4))) Args*>(reinterpret_cast<uintptr_t>(__builtin_amdgcn_kernarg_segment_ptr()));
+    asm volatile("" : "+s"(p));
+    return *p;
+}
+
+// In which order block rows start, see the launcher.
+enum WithOrder { kInOrder, kDealtHeads, kLongestFirst };
+
+template <int BS, bool BIAS, bool DROP>
+__global__ __launch_bounds__(BS * 4, BS == 64 ? 3 : 4) void attn_fwd_with_bf16_kernel(FwdWith a) {
+    constexpr int NKT = BS / 16;
+    __shared__ __attribute__((aligned(16))) KvTiles<BS> sm0, sm1;
+    __shared__ float bias0[2 * BS], bias1[2 * BS], tab[BIAS ? Extras::kMaxBuckets : 1];
+
+    const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int L = a.L;
+    if (DROP && blockIdx.x == 0 && tid < 2 && a.x.rng_used) a.x.rng_used[tid] = a.x.rng[tid];
+
+    // which block row, or piece of a long one
+    int id = blockIdx.x;
+    const bool helper = id < a.cut.groups;
+    RowPieces cuts = {0, 1, 0, 0};
+    int bh, I, piece = 0;
+    if (helper) {
+        const int all = a.heads * a.cut.helpers;
+        if (id >= all) return;
+        const int l = xcd_deal(id, 0, all), p = l % a.cut.helpers;
+        cuts = row_pieces<false>(a.row_ptr, a.nb, a.cut, p, lane);
+        if (cuts.row < 0) return;
+        bh = l / a.cut.helpers;
+        I = cuts.row;
+        piece = p - cuts.first + 1;
+    } else {
+        id -= a.cut.groups;
+        ItemOfHead mine;
+        if (a.order == kInOrder) {
+            const int vid = xcd_deal(id, 0, a.heads * a.nb);
+            mine = {vid / a.nb, vid % a.nb};
+        } else {
+            mine = deal_heads(id, a.heads, false);
+            if (mine.item >= a.nb) return;
+            if (a.order == kLongestFirst) mine.item = row_by_length(a.row_ptr, a.nb, mine.item, lane);
+        }
+        bh = mine.head;
+        I = mine.item;
+    }
+
+    const TableColumn<BS, BIAS> column(a.x, bh % a.x.H, tid);
+    const BlockBias<BS, BIAS> biases(a.x, tab, L, tid, wave);
+    unsigned bucket = biases.request(0);
+    const size_t head = a.at.in_head(bh, L);
+    const int row_len = a.at.in_row(), length = length_of(a.x, bh, L);
+    const int qrow = I * BS + wave * 16 + r;
+    const SwzLane sl(r, g);
+    const TileLoadLane tl(wave, lane, row_len);
+    const bf16_t *const Kh = a.K + head, *const Vh = a.V + head;
+    auto issue = [&](KvTiles<BS>& st, int J) {
+        const unsigned range = tile_range<BS>(J * BS, length, row_len);
+        tile_load_async(Kh + (size_t)J * BS * row_len, st.k, wave, tl, range);
+        tile_load_async(Vh + (size_t)J * BS * row_len, st.v, wave, tl, range);
+    };
+    if (!helper) issue(sm0, I);   // the diagonal block, before any index is known
+    bf16x8 qf[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        qf[c] = *reinterpret_cast<const bf16x8*>(a.Q + head + (size_t)qrow * row_len + c * 32 + g * 8);
+        if (qrow >= length) qf[c] = bf16x8{};
+    }
+    int jb = a.row_ptr[I], n = a.row_ptr[I + 1] - jb;   // blocks of this workgroup
+    if (n > a.cut.longest) {
+        if (!helper) cuts = row_pieces<true>(a.row_ptr, a.nb, a.cut, I, lane);
+        const int from = piece * n / cuts.count;
+        n = (piece + 1) * n / cuts.count - from;
+        jb += from;
+    }
+    const int* cols = a.col_idx + jb;
+    n = I * BS < length ? blocks_below<BS>(cols, n, length, L, lane) : 0;
+    const int last = n > 0 ? n - 1 : 0;
+    int first[8];
+    int pd = n > 0 ? find_in_row(cols, n, I, first) : -1;
+    if (helper) pd = -1;   // in index order, the diagonal block where it comes
+    // block visited at step t (clamped reads stay inside this row's entries; an empty row reads nothing)
+    auto col_at = [&](int t) {
+        const int j = walk_index(t < last ? t : last, pd);
+        return j < 8 ? pick8(first, j) : cols[j];
+    };
+    int walk_v = 0;   // the first 64 blocks of the walk, one per lane
+    if (n > 2) walk_v = cols[walk_index(lane < last ? lane : last, pd)];
+    auto later_col = [&](int t) {
+        const int u = t < last ? t : last;
+        return u < 64 ? __builtin_amdgcn_readlane(walk_v, u) : cols[walk_index(u, pd)];
+    };
+    int jcur = n > 0 ? col_at(0) : I, jnext = n > 0 ? col_at(1) : I;
+    column.put(tab, a.x, tid);
+    if (pd < 0 && n > 0) {
+        // no diagonal block in this row (piece): once everyone's early load has landed, load block 0 over it
+        if (BIAS) bucket = biases.request(jcur - I);
+        if (!helper) {
+            __builtin_amdgcn_s_waitcnt(kWaitVm0);
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        }
+        issue(sm0, jcur);
+    }
+    // the second block goes out as soon as its index is known; it is the youngest load from here on
+    if (n > 0) {
+        const unsigned second = biases.request(jnext - I);
+        issue(sm1, jnext);   // (a one-block row loads its block twice: keeps the wait below uniform)
+        if constexpr (BIAS) {
+            lds_meet();   // the table is there
+            biases.put(bias0, bucket, tid);
+            biases.put(bias1, second, tid);
+        }
+    }
+    [[maybe_unused]] const ScoreDraws draws(a.x, bh);
+    [[maybe_unused]] const u16x2 below = both_halves(a.x.threshold - 1u);
+    const float scale_log2 = a.scale_log2;
+
+    float m = kLowest;   // what the row's exponentials are taken against, log2 units
+    f32x4 lacc = f32x4{0.f, 0.f, 0.f, 0.f};   // running row sum, replicated in its 4 elements
+    f32x4 oacc[4];
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) oacc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    bf16x8 ones;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = (bf16_t)1.0f;
+    const int slice_at = 4 * g - wave * 16 - r + BS - 1;   // of key 4 g of the block
+
+    auto step = [&](const KvTiles<BS>& cur, KvTiles<BS>& tgt, const float* bias_c, float* bias_n, int it) {
+        [[maybe_unused]] u16x2 factors[NKT][2];
+        if constexpr (DROP) query_factors<NKT>(draws, qrow, jcur * BS, g, below, factors);
+        meet(it == 0);
+        if (it > 0) {
+            jnext = later_col(it + 1);
+            if constexpr (BIAS) biases.put(bias_n, bucket, tid);
+            if (it + 1 < n) issue(tgt, jnext);
+        }
+        if constexpr (BIAS) bucket = biases.request(later_col(it + 2) - I);
+        // S^T tile kt: [key 16 kt + 4 g + i][query r]; all K fragments are requested up front
+        bf16x8 kfr[NKT][2];
+#pragma unroll
+        for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+                kfr[kt][c] = *reinterpret_cast<const bf16x8*>(cur.k + kt * 16 * kD + sl.frag[c]);
+        f32x4 s[NKT];
+#pragma unroll
+        for (int kt = 0; kt < NKT; ++kt) {
+            if constexpr (BIAS) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[kt][i] = bias_c[slice_at + 16 * kt + i];
+            } else {
+                s[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) s[kt] = mma_d(s[kt], kfr[kt][c], qf[c]);
+        }
+        if (jcur * BS + BS > length) {   // the block that the sequence ends in
+#pragma unroll
+            for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (jcur * BS + kt * 16 + 4 * g + i >= length) s[kt][i] = -INFINITY;
+        }
+        constexpr int NM = (BS / 32) * 4;
+        bf16x8 vop[NM];
+#pragma unroll
+        for (int j = 0; j < NM; ++j) {
+            const int o = sl.tr(j & 3) + (j >> 2) * 32 * kD;
+            vop[j] = join(lds_read_tr(cur.v + o), lds_read_tr(cur.v + 16 * kD + o));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        bf16x4 pq[NKT];
+        f32x4 sums;
+        auto probabilities = [&]() {   // and their sums, see the plain kernel
+#pragma unroll
+            for (int kt = 0; kt < NKT; ++kt) {
+                f32x4 p;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[i] = fast_exp2(fmaf(s[kt][i], scale_log2, -m));
+                pq[kt] = to_quad<bf16_t>(p);
+            }
+            sums = lacc;
+#pragma unroll
+            for (int pc = 0; pc < BS / 32; ++pc) sums = mma_d(sums, ones, join(pq[2 * pc], pq[2 * pc + 1]));
+        };
+        if (it > 0) probabilities();
+        if (it == 0 || __any(!(sums[0] <= kSumLimit))) {
+            float mx = s[0][0];
+#pragma unroll
+            for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[kt][i]);
+            float m_new = fmaxf(m, group_max(mx) * scale_log2);
+            if (lacc[0] > 1.f) m_new = fmaxf(m_new, m + log2f(lacc[0]));   // a sum that many blocks have added up to
+            const float alpha = fast_exp2(m - m_new);
+            m = m_new;
+            lacc *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt) oacc[dt] *= alpha;
+            probabilities();
+        }
+        lacc = sums;
+        if constexpr (DROP) {   // behind the sums: the softmax is over all of them
+#pragma unroll
+            for (int kt = 0; kt < NKT; ++kt) pq[kt] = drop(pq[kt], factors[kt]);
+        }
+#pragma unroll
+        for (int j = 0; j < NM; ++j) {
+            const int pc = j >> 2;
+            oacc[j & 3] = mma_d(oacc[j & 3], vop[j], join(pq[2 * pc], pq[2 * pc + 1]));   // O^T[d][query] += V^T P^T
+        }
+        jcur = jnext;
+    };
+
+    for (int it = 0; it < n; it += 2) {
+        step(sm0, sm1, bias0, bias1, it);
+        if (it + 1 < n) step(sm1, sm0, bias1, bias0, it + 1);
+    }
+
+    // an empty row never waited for its early load: it must land before this workgroup's LDS is freed
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);
+
+    const auto& z = args_again<FwdWith>();
+    if (cuts.count > 1) {   // a long row in pieces: see attn_bf16_tiles.h
+        constexpr int kPart = 64 * 18;   // floats of a wave: nine pairs a lane, its accumulators, then reference and sum
+        const size_t slot = (size_t)bh * z.cut.slots + cuts.slot;
+        float* const parts = z.cut.parts + (slot * (BS / 16) + wave) * kPart + lane * 2;
+        float* const mine = parts + (size_t)piece * (BS / 16) * kPart;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) put_shared(mine + i * 128, oacc[i / 2][i % 2 * 2], oacc[i / 2][i % 2 * 2 + 1]);
+        put_shared(mine + 1024, m, lacc[0]);
+        if (!last_to_arrive(z.cut.counters + slot, z.cut.tag, cuts.count, reinterpret_cast<int*>(sm0.v))) return;
+        m = -INFINITY;
+        lacc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) oacc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int c = 0; c < cuts.count; ++c) {
+            const float* const part = parts + (size_t)c * (BS / 16) * kPart;
+            float2 v[9];
+#pragma unroll
+            for (int i = 0; i < 9; ++i) v[i] = get_shared(part + i * 128);
+            const float m_new = fmaxf(m, v[8].x), down = fast_exp2(m - m_new), up = fast_exp2(v[8].x - m_new);
+            m = m_new;
+            lacc = lacc * down + v[8].y * up;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int e = i % 2 * 2;
+                oacc[i / 2][e] = oacc[i / 2][e] * down + v[i].x * up;
+                oacc[i / 2][e + 1] = oacc[i / 2][e + 1] * down + v[i].y * up;
+            }
+        }
+    }
+    const float lsum = lacc[0];
+    const bool none = lsum == 0.f || qrow >= length;
+    const float inv = none ? 0.f : (DROP ? z.x.keep_scale : 1.f) / lsum;
+    // the stage that the last block did not use is free, see the plain kernel
+    bf16_t* patch = ((n & 1) ? sm1.k : sm0.k) + wave * (16 * kD);
+    const Rows at = {z.at.H, z.at.beside};
+    store_rows_coalesced(patch, z.O + at.out_head(bh, L) + (size_t)(I * BS + wave * 16) * at.out_row(), at.out_row(), oacc, inv, lane);
+    if (g == 0) z.LSE[(size_t)bh * L + qrow] = none ? -INFINITY : (m + log2f(lsum)) * kLn2;
+}
+
+static int resident(int bs) { return 256 * (bs == 64 ? 4 : 8); }
+
+// Order of the rows and their cuts: the plain kernel's rules.
+template <int BS>
+hipError_t fwd_with_bf16(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, void* O, float* LSE,
+                         const int* row_ptr, const int* col_idx, int nnzb, hipStream_t st) {
+    const int total = s.nb * s.BH;
+    RowCut cut;
+    if (s.fwd_room) cut = RowCut(s, nnzb);
+    if (cut.slots) {   // a helper for each piece
+        cut.helpers = cut.slots - 1;
+        cut.groups = (s.BH * cut.helpers + 7) & ~7;
+    } else {
+        cut = RowCut{};
+        cut.longest = INT_MAX;
+    }
+    const bool short_rows = BS == 32 ? nnzb < 6 * s.nb && 4 * total >= 5 * resident(BS) : nnzb < 4 * s.nb && total >= 2 * resident(BS);
+    const WithOrder order = !short_rows && (total > resident(BS) || (total > 256 && nnzb >= 6 * s.nb)) ? kLongestFirst
+                            : !short_rows && total > (BS == 64 ? 512 : 768) && 2 * nnzb >= 3 * s.nb   ? kDealtHeads
+                                                                                                        : kInOrder;
+    const long long grid = cut.groups + (order == kInOrder ? total : dealt(s.BH, s.nb, false));
+    if (grid > 0x7fffffffll) return hipErrorInvalidValue;
+    const FwdWith args = {static_cast<const bf16_t*>(Q), static_cast<const bf16_t*>(K), static_cast<const bf16_t*>(V), static_cast<bf16_t*>(O), LSE,
+                          row_ptr, col_idx, Rows{x.H, s.heads_beside != 0}, x, cut, s.L, s.nb, s.BH, order, s.scale * kLog2e};
+    auto launch = [&](auto kernel) { kernel<<<dim3((unsigned)grid), dim3(BS * 4), 0, st>>>(args); };
+    if (x.table) {
+        if (x.threshold) launch(attn_fwd_with_bf16_kernel<BS, true, true>);
+        else launch(attn_fwd_with_bf16_kernel<BS, true, false>);
+    } else {
+        if (x.threshold) launch(attn_fwd_with_bf16_kernel<BS, false, true>);
+        else launch(attn_fwd_with_bf16_kernel<BS, false, false>);
+    }
+    return hipGetLastError();
+}
+template hipError_t fwd_with_bf16<32>(const AttnShape&, const Extras&, const void*, const void*, const void*, void*, float*, const int*, const int*,
+                                      int, hipStream_t);
+template hipError_t fwd_with_bf16<64>(const AttnShape&, const Extras&, const void*, const void*, const void*, void*, float*, const int*, const int*,
+                                      int, hipStream_t);
+
+}  // namespace spion

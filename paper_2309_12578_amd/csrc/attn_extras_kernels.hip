@@ -456,17 +456,21 @@ struct WithWorkspace {
 
 template <typename T, int BS>
 hipError_t fwd_with(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, void* O, float* LSE,
-                    const int* row_ptr, const int* col_idx, hipStream_t st) {
-    const long long total = (long long)s.BH * s.nb * (BS / 16), grid = group_grid(total);
-    if (grid > 0x7fffffffll) return hipErrorInvalidValue;
-    auto launch = [&](auto kernel) {
-        kernel<<<dim3((unsigned)grid), dim3(kWaves * 64), 0, st>>>(
-            static_cast<const T*>(Q), static_cast<const T*>(K), static_cast<const T*>(V), static_cast<T*>(O), LSE, row_ptr, col_idx, x,
-            s.L, s.nb, (int)total, s.scale * kLog2e);
-    };
-    if (x.threshold) launch(attn_fwd_with_kernel<T, BS, true>);
-    else launch(attn_fwd_with_kernel<T, BS, false>);
-    return hipGetLastError();
+                    const int* row_ptr, const int* col_idx, int nnzb, hipStream_t st) {
+    if constexpr (sizeof(T) == 2 && BS > 16) {
+        return fwd_with_bf16<BS>(s, x, Q, K, V, O, LSE, row_ptr, col_idx, nnzb, st);
+    } else {
+        const long long total = (long long)s.BH * s.nb * (BS / 16), grid = group_grid(total);
+        if (grid > 0x7fffffffll) return hipErrorInvalidValue;
+        auto launch = [&](auto kernel) {
+            kernel<<<dim3((unsigned)grid), dim3(kWaves * 64), 0, st>>>(
+                static_cast<const T*>(Q), static_cast<const T*>(K), static_cast<const T*>(V), static_cast<T*>(O), LSE, row_ptr, col_idx, x,
+                s.L, s.nb, (int)total, s.scale * kLog2e);
+        };
+        if (x.threshold) launch(attn_fwd_with_kernel<T, BS, true>);
+        else launch(attn_fwd_with_kernel<T, BS, false>);
+        return hipGetLastError();
+    }
 }
 
 template <typename T, int BS>
@@ -489,7 +493,7 @@ hipError_t bwd_with(const AttnShape& s, const Extras& x, const void* Q, const vo
 }  // namespace
 
 size_t attn_with_workspace_bytes(const AttnShape& s, bool table_grad, int n_buckets, int H, int nnzb, bool is_bwd) {
-    if (!is_bwd) return 0;
+    if (!is_bwd) return s.is_bf16 && s.bs > 16 ? RowCut(s, nnzb).room_bytes(s.BH, s.bs) : 0;
     return WithWorkspace(s, table_grad, n_buckets, H, nnzb).total;
 }
 
@@ -507,8 +511,7 @@ size_t attn_with_workspace_bytes(const AttnShape& s, bool table_grad, int n_buck
 
 hipError_t launch_attn_fwd_with(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, void* O, float* LSE,
                                 const int* row_ptr, const int* col_idx, int nnzb, hipStream_t st) {
-    (void)nnzb;
-    SPION_DISPATCH(fwd_with, s, x, Q, K, V, O, LSE, row_ptr, col_idx, st);
+    SPION_DISPATCH(fwd_with, s, x, Q, K, V, O, LSE, row_ptr, col_idx, nnzb, st);
 }
 
 static hipError_t launch_bwd(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, const void* O,

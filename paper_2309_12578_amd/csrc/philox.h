@@ -15,6 +15,8 @@ struct PhiloxKey {
     static __device__ __forceinline__ unsigned uniform(unsigned v) { return (unsigned)__builtin_amdgcn_readfirstlane((int)v); }
     __device__ __forceinline__ uint4 words(unsigned c0, unsigned c1) const {
         unsigned a = c0, b = c1, c = c2, d = c3, x = k0, y = k1;
+        // the rounds' keys are made again for each call, by scalar additions beside the vector work: kept, they take 14 registers
+        asm volatile("" : "+s"(x), "+s"(y));
 #pragma unroll
         for (int r = 0; r < 7; ++r) {
             const unsigned long long p = (unsigned long long)a * 0xD2511F53u, q = (unsigned long long)c * 0xCD9E8D57u;

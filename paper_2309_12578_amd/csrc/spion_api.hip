@@ -540,9 +540,10 @@ int spion_attn_fwd_with(const void* Q, const void* K, const void* V, void* O, fl
     const int rc = take_extras(p, x, nnzb, extras);
     if (rc != SPION_OK) return rc;
     if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)O) % 16 != 0) return SPION_ERR_PARAM;
-    const spion::AttnShape s = make_shape(p);
+    spion::AttnShape s = make_shape(p);
     const size_t need = spion::attn_with_workspace_bytes(s, false, extras.n_buckets, p->H, nnzb, false);
     if (need && (!workspace || (uintptr_t)workspace % kAlign != 0 || workspace_bytes < need)) return SPION_ERR_WORKSPACE;
+    if (need) s.fwd_room = workspace;
     return spion::launch_attn_fwd_with(s, extras, Q, K, V, O, LSE, row_ptr, col_idx, nnzb, static_cast<hipStream_t>(hip_stream)) ==
                    hipSuccess ? SPION_OK : SPION_ERR_HIP;
 }

@@ -124,6 +124,10 @@ hipError_t launch_attn_fwd_with(const AttnShape& s, const Extras& x, const void*
 hipError_t launch_attn_bwd_with(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, const void* O,
                                 const void* dO, const float* LSE, void* dQ, void* dK, void* dV, void* dtable, const int* row_ptr,
                                 const int* col_idx, const int* col_ptr, const int* row_idx, int nnzb, void* workspace, hipStream_t st);
+// attn_extras_bf16_kernels.hip: bf16, BS in {32, 64}
+template <int BS>
+hipError_t fwd_with_bf16(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, void* O, float* LSE,
+                         const int* row_ptr, const int* col_idx, int nnzb, hipStream_t st);
 size_t attn_with_workspace_bytes(const AttnShape& s, bool table_grad, int n_buckets, int H, int nnzb, bool is_bwd);
 
 // dropout_kernels.hip: y = residual + dropout(x) (residual nullptr: without), the dense bias and its table's gradient
