@@ -34,6 +34,7 @@ SOURCES = [
     ("attn_bwd_bf16_kernels.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form"]),
     ("attn_extras_kernels.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form"]),
     ("attn_extras_bf16_kernels.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form"]),
+    ("attn_extras_bwd_bf16_kernels.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form"]),
     ("dropout_kernels.hip", []),
     ("norm_kernels.hip", []),
     ("projection_kernels.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form"]),

@@ -114,12 +114,14 @@ __device__ __forceinline__ void key_words(const ScoreDraws& d, int q0, int k, in
     const int c = k & 3;
     const uint4 w = d.call(q0 + 16 * (c >> 1) + 4 * g + 2 * (c & 1), k & ~3);
     const bool b0 = c & 1, b1 = c & 2;
-    const unsigned x0 = b0 ? from_pair(w.y) : w.x, x1 = b0 ? w.y : from_pair(w.x);
-    const unsigned x2 = b0 ? from_pair(w.w) : w.z, x3 = b0 ? w.w : from_pair(w.z);
-    u[0] = b1 ? from_other_pair(x2) : x0;
-    u[2] = b1 ? x2 : from_other_pair(x0);
-    u[1] = b1 ? from_other_pair(x3) : x1;
-    u[3] = b1 ? x3 : from_other_pair(x1);
+    // every lane takes part in every exchange, whichever of the two it then keeps
+    const unsigned px = from_pair(w.x), py = from_pair(w.y), pz = from_pair(w.z), pw = from_pair(w.w);
+    const unsigned x0 = b0 ? py : w.x, x1 = b0 ? w.y : px, x2 = b0 ? pw : w.z, x3 = b0 ? w.w : pz;
+    const unsigned o0 = from_other_pair(x0), o1 = from_other_pair(x1), o2 = from_other_pair(x2), o3 = from_other_pair(x3);
+    u[0] = b1 ? o2 : x0;
+    u[2] = b1 ? x2 : o0;
+    u[1] = b1 ? o3 : x1;
+    u[3] = b1 ? x3 : o1;
 }
 
 // ------------------------------------------------------------------------------------------------

@@ -11,7 +11,7 @@
 #include "attn_bf16_tiles.h"
 #include "attn_common.h"
 #include "attn_extras.h"
-#include "attn_key_items.h"
+#include "attn_extras_bf16.h"
 #include "spion_internal.h"
 
 namespace spion {
@@ -23,100 +23,6 @@ struct KvTiles {
     bf16_t k[BS * kD];
     bf16_t v[BS * kD];
 };
-
-// Own loads landed (all, or all but the four youngest), previous LDS accesses done, then meet the other waves.
-__device__ __forceinline__ void meet(bool four_younger_in_flight) {
-    if (four_younger_in_flight) __builtin_amdgcn_s_waitcnt(kWaitVm4);
-    else __builtin_amdgcn_s_waitcnt(kWaitVm0);
-    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
-__device__ __forceinline__ void lds_meet() {
-    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
-
-// Entries of an ascending list whose block starts below `length`, of the n from list on.
-template <int BS>
-__device__ __forceinline__ int blocks_below(const int* list, int n, int length, int L, int lane) {
-    if (length >= L) return n;
-    int count = 0;
-    for (int base = 0; base < n; base += 64) {
-        const int at = base + lane;
-        const int here = __popcll(__ballot(at < n && list[at < n ? at : n - 1] * BS < length));
-        count += here;
-        if (here < 64) break;
-    }
-    return count;
-}
-
-// The biases of a block's distances.  The first BS / 32 waves bring them, a distance a lane: the map's byte is
-// requested a step before it is looked up.
-template <int BS, bool BIAS>
-struct BlockBias {
-    const uint8_t* from;   // map entry of this lane's distance in a block on the diagonal
-    const float* tab;
-    int last;
-    bool mine;
-    __device__ __forceinline__ BlockBias(const Extras& x, const float* tab_, int L, int tid, int wave)
-        : from(nullptr), tab(tab_), last(x.n_buckets - 1), mine(BIAS && wave < BS / 32) {
-        if (BIAS) from = x.bucket_of + (L - BS + (tid < 2 * BS - 2 ? tid : 2 * BS - 2));
-    }
-    __device__ __forceinline__ unsigned request(int blocks_off) const { return mine ? from[(ptrdiff_t)blocks_off * BS] : 0u; }   // key block - query block
-    __device__ __forceinline__ void put(float* slice, unsigned bucket, int tid) const {
-        if (mine) slice[tid] = tab[min((int)bucket, last)];
-    }
-};
-
-// The head's column of the bias table in registers (requested before anything else is), then in LDS.
-template <int BS, bool BIAS>
-struct TableColumn {
-    static constexpr int N = Extras::kMaxBuckets / (BS * 4);
-    float v[N];
-    __device__ __forceinline__ TableColumn(const Extras& x, int h, int tid) {
-        if constexpr (BIAS) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int b = tid + i * BS * 4;
-                v[i] = 0.f;
-                if (b < x.n_buckets) {
-                    const size_t at = (size_t)b * x.H + h;
-                    v[i] = x.table_bf16 ? (float)static_cast<const bf16_t*>(x.table)[at] : static_cast<const float*>(x.table)[at];
-                }
-            }
-        }
-    }
-    __device__ __forceinline__ void put(float* tab, const Extras& x, int tid) const {
-        if constexpr (BIAS) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) tab[tid + i * BS * 4] = v[i] <= kMaskedBias ? -INFINITY : v[i] * x.inv_scale;
-        }
-    }
-};
-
-// Where rows of head bh are, see HeadRows.
-struct Rows {
-    int H, beside;
-    __device__ __forceinline__ int in_row() const { return beside ? 3 * H * kD : kD; }
-    __device__ __forceinline__ int out_row() const { return beside ? H * kD : kD; }
-    __device__ __forceinline__ size_t in_head(int bh, int L) const {
-        return beside ? ((size_t)(bh / H) * L * 3 * H + bh % H) * kD : (size_t)bh * L * kD;
-    }
-    __device__ __forceinline__ size_t out_head(int bh, int L) const {
-        return beside ? ((size_t)(bh / H) * L * H + bh % H) * kD : (size_t)bh * L * kD;
-    }
-};
-
-// Bytes of a tile that starts at row `row0` up to the sequence's end.
-template <int BS>
-__device__ __forceinline__ unsigned tile_range(int row0, int length, int row_len) {
-    const int rows = length - row0;
-    return rows >= BS ? 0xffffffffu : rows <= 0 ? 0u : (unsigned)rows * (unsigned)row_len * (unsigned)sizeof(bf16_t);
-}
 
 }  // namespace
 
@@ -134,15 +40,6 @@ struct FwdWith {
     int L, nb, heads, order;
     float scale_log2;
 };
-
-// The kernel's arguments once more, from memory: what is used at its end only would otherwise sit in scalar registers over the
-// loop, of which there are too few (7 to 61 of them were spilled).
-template <typename Args>
-__device__ __forceinline__ const __attribute__((address_space(4))) Args& args_again() {
-    auto p = reinterpret_cast<const __attribute__((address_space(4))) Args*>(reinterpret_cast<uintptr_t>(__builtin_amdgcn_kernarg_segment_ptr()));
-    asm volatile("" : "+s"(p));
-    return *p;
-}
 
 // In which order block rows start, see the launcher.
 enum WithOrder { kInOrder, kDealtHeads, kLongestFirst };

@@ -212,6 +212,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_bwd_with_kernel(
 
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (blockIdx.x == 0 && x.counters)
+        for (int h = tid; h < x.H; h += kWaves * 64) x.counters[h * Extras::kCounterStride] = 0u;
     const int half = (total + 7) / 8 * 8;   // workgroups of a side
     const bool key_side = (int)blockIdx.x >= half;
     const int item = item_of_group(key_side ? blockIdx.x - half : blockIdx.x, total);
@@ -398,40 +400,69 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_bwd_with_kernel(
 }
 
 // ------------------------------------------------------------------------------------------------
-// The table's gradient from the slices: diagonal t of a tile (query tile a, key tile b) of block (I, J) has distance
-// (J - I) BS + (b - a) TS + t - (TS - 1).  Workgroup = (head, part of its batch's block rows); every thread adds into
-// its own copy of the buckets in LDS, the copies are added up in a fixed order, and so are the parts, by the last workgroup of
-// the head to arrive.
+// The table's gradient from the slices: number t of a tile (query tile a, key tile b, of ts rows) of block (I, J) is of distance
+// (J - I) bs + (b - a) ts + t - (ts - 1).  Workgroup = (head, part of its batch's kept blocks); every thread adds into its own
+// copy of the buckets in LDS, the copies are added up in a fixed order, and so are the parts, by the last workgroup of the head
+// to arrive.  The counters of arrivals, a line each, are 0 from the backward kernel on: counting by compare and swap, as where a few pieces of
+// a row meet, hundreds of workgroups took 500 to 1500 us.
 // ------------------------------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void table_grad_kernel(const float* __restrict__ slices, const int* __restrict__ row_ptr,
                                                          const int* __restrict__ col_idx, Extras x, int B, int L, int nb, int nnzb, int bs,
-                                                         int ts, int parts, float* __restrict__ partial,
-                                                         unsigned long long* __restrict__ counters, unsigned long long tag,
+                                                         int ts, int parts, float* partial, unsigned* __restrict__ counters,
                                                          void* __restrict__ dtable) {
     extern __shared__ float hist[];   // [n_buckets][threads]
+    constexpr int kAtOnce = 64;       // blocks whose places are found together, a lane each
+    __shared__ long long slice_s[kAtOnce];
+    __shared__ int map_s[kAtOnce], tiles_s[kAtOnce];
     const int h = blockIdx.x % x.H, part = blockIdx.x / x.H, tid = threadIdx.x, threads = blockDim.x;
-    const int nbk = x.n_buckets, tpb = bs / ts, per_block = tpb * tpb * 2 * ts;
-    for (int b = 0; b < nbk; ++b) hist[b * threads + tid] = 0.f;
-    const long long rows = (long long)B * nb;
-    const long long first = part * rows / parts, end = (part + 1) * rows / parts;
-    for (long long row = first; row < end; ++row) {
-        const int b = (int)(row / nb), I = (int)(row % nb), bh = b * x.H + h;
-        const int length = length_of(x, bh, L);
-        if (I * bs >= length) continue;
-        const int jb = row_ptr[I], je = row_ptr[I + 1];
-        for (int j = jb; j < je; ++j) {
-            const int J = col_idx[j];
-            if (J * bs >= length) break;
-            const float* const from = slices + ((size_t)bh * nnzb + j) * per_block;
-            for (int e = tid; e < per_block; e += threads) {
-                const int tile = e / (2 * ts), t = e % (2 * ts), a = tile / tpb, c = tile % tpb;
-                if (t == 2 * ts - 1 || I * bs + a * ts >= length) continue;
-                const int at = (J - I) * bs + (c - a) * ts + t - (ts - 1) + L - 1;
-                hist[bucket_index(x, x.bucket_of[at]) * threads + tid] += from[e];
+    for (int b = 0; b < x.n_buckets; ++b) hist[b * threads + tid] = 0.f;
+    const int tpb = bs / ts, per_block = tpb * tpb * 2 * ts;   // powers of two
+    const int shift = __ffs(per_block) - 1, tile_shift = __ffs(2 * ts) - 1;
+    const long long all = (long long)B * nnzb, end = (part + 1) * all / parts;
+    for (long long c0 = part * all / parts; c0 < end; c0 += kAtOnce) {
+        __syncthreads();
+        if (tid < kAtOnce) {
+            const long long e = c0 + tid;
+            int map = 0, tiles = 0;
+            if (e < end) {
+                const int b = (int)(e / nnzb), j = (int)(e % nnzb);
+                int lo = 0, hi = nb;   // the last row that starts at j or before
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if (row_ptr[mid] <= j) lo = mid;
+                    else hi = mid;
+                }
+                const int J = col_idx[j], length = length_of(x, b * x.H + h, L);
+                slice_s[tid] = ((long long)(b * x.H + h) * nnzb + j) << shift;
+                map = (J - lo) * bs + L - ts;
+                // query tiles that were computed: rows and blocks from the length on were not
+                tiles = J * bs < length ? min(tpb, (length - lo * bs + ts - 1) / ts) : 0;
             }
+            map_s[tid] = map;
+            tiles_s[tid] = tiles;
+        }
+        __syncthreads();
+        const int n = (int)min((long long)kAtOnce, end - c0) << shift;
+#pragma unroll 4
+        for (int f = tid; f < n; f += threads) {
+            const int entry = f >> shift, e = f & (per_block - 1), t = e & (2 * ts - 1), tile = e >> tile_shift;
+            const int q = tile / tpb, k = tile % tpb;
+            if (t == 2 * ts - 1 || q >= tiles_s[entry]) continue;
+            const int bucket = bucket_index(x, x.bucket_of[map_s[entry] + (k - q) * ts + t]);
+            __hip_atomic_fetch_add(&hist[bucket * threads + tid], slices[slice_s[entry] + e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
         }
     }
-    finish_table_grad(hist, x.n_buckets, part, parts, h, x.H, partial, counters, tag, dtable, x.table_bf16 != 0);
+    leave_partial(hist, x.n_buckets, part, parts, h, partial);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's stores are done, at device scope
+    __syncthreads();                                   // and those of the others, and every wave is done with the copies
+    int* const flag = reinterpret_cast<int*>(hist);
+    if (tid == 0) {
+        const unsigned before = __hip_atomic_fetch_add(counters + h * Extras::kCounterStride, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        *flag = before == (unsigned)parts - 1u;
+    }
+    __syncthreads();
+    asm volatile("" ::: "memory");   // nothing of the others' is read before
+    if (*flag) write_table_column(partial, x.n_buckets, parts, h, x.H, dtable, x.table_bf16 != 0);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -439,18 +470,25 @@ __global__ __launch_bounds__(256) void table_grad_kernel(const float* __restrict
 // ------------------------------------------------------------------------------------------------
 namespace {
 
+// The backward's: of the bf16 kernels of block 32 and 64 first, then what the table's gradient takes.
 struct WithWorkspace {
-    int tile, parts;
-    size_t slices = 0, partial, counters, total;   // offsets, and the end
+    int tile, parts;                           // rows of a tile that has its own slice; workgroups per head
+    size_t slices, partial, counters, total;   // offsets, and the end
     WithWorkspace(const AttnShape& s, bool table_grad, int n_buckets, int H, int nnzb) {
         auto up = [](size_t n) { return (n + 255) / 256 * 256; };
-        tile = 16;
-        const long long rows = (long long)s.BH / (H ? H : 1) * s.nb;
-        parts = (int)std::min<long long>(std::min<long long>(rows, 255), std::max(1, 1024 / (H ? H : 1)));
-        const size_t per_block = (size_t)(s.bs / tile) * (s.bs / tile) * 2 * tile;
-        partial = up(table_grad ? (size_t)s.BH * nnzb * per_block * sizeof(float) : 0);
-        counters = up(partial + (table_grad ? (size_t)H * parts * n_buckets * sizeof(float) : 0));
-        total = up(counters + (table_grad ? (size_t)H * 8 : 0));
+        const bool tiled = s.is_bf16 && s.bs > 16;
+        tile = tiled ? s.bs : 16;
+        slices = tiled ? up(attn_bwd_workspace(s, nnzb).with_rows) : 0;
+        if (!table_grad) {
+            total = slices;
+            return;
+        }
+        // eight blocks a workgroup or more, and about two workgroups a compute unit
+        const long long blocks = (long long)s.BH / H * nnzb;
+        parts = (int)std::max<long long>(1, std::min<long long>(blocks / 8, 512 / H));
+        partial = up(slices + (size_t)s.BH * nnzb * (s.bs / tile) * (s.bs / tile) * 2 * tile * sizeof(float));
+        counters = up(partial + (size_t)H * parts * n_buckets * sizeof(float));
+        total = up(counters + (size_t)H * Extras::kCounterStride * 4);
     }
 };
 
@@ -476,18 +514,22 @@ hipError_t fwd_with(const AttnShape& s, const Extras& x, const void* Q, const vo
 template <typename T, int BS>
 hipError_t bwd_with(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, const void* O, const void* dO,
                     const float* LSE, void* dQ, void* dK, void* dV, const int* row_ptr, const int* col_idx, const int* col_ptr,
-                    const int* row_idx, int nnzb, hipStream_t st) {
-    const long long total = (long long)s.BH * s.nb * (BS / 16), grid = 2 * group_grid(total);
-    if (grid > 0x7fffffffll) return hipErrorInvalidValue;
-    auto launch = [&](auto kernel) {
-        kernel<<<dim3((unsigned)grid), dim3(kWaves * 64), 0, st>>>(
-            static_cast<const T*>(Q), static_cast<const T*>(K), static_cast<const T*>(V), static_cast<const T*>(O),
-            static_cast<const T*>(dO), LSE, static_cast<T*>(dQ), static_cast<T*>(dK), static_cast<T*>(dV), row_ptr, col_idx, col_ptr,
-            row_idx, x, s.L, s.nb, nnzb, (int)total, s.scale, s.scale * kLog2e);
-    };
-    if (x.threshold) launch(attn_bwd_with_kernel<T, BS, true>);
-    else launch(attn_bwd_with_kernel<T, BS, false>);
-    return hipGetLastError();
+                    const int* row_idx, int nnzb, void* workspace, hipStream_t st) {
+    if constexpr (sizeof(T) == 2 && BS > 16) {
+        return bwd_with_bf16<BS>(s, x, Q, K, V, O, dO, LSE, dQ, dK, dV, row_ptr, col_idx, col_ptr, row_idx, nnzb, workspace, st);
+    } else {
+        const long long total = (long long)s.BH * s.nb * (BS / 16), grid = 2 * group_grid(total);
+        if (grid > 0x7fffffffll) return hipErrorInvalidValue;
+        auto launch = [&](auto kernel) {
+            kernel<<<dim3((unsigned)grid), dim3(kWaves * 64), 0, st>>>(
+                static_cast<const T*>(Q), static_cast<const T*>(K), static_cast<const T*>(V), static_cast<const T*>(O),
+                static_cast<const T*>(dO), LSE, static_cast<T*>(dQ), static_cast<T*>(dK), static_cast<T*>(dV), row_ptr, col_idx, col_ptr,
+                row_idx, x, s.L, s.nb, nnzb, (int)total, s.scale, s.scale * kLog2e);
+        };
+        if (x.threshold) launch(attn_bwd_with_kernel<T, BS, true>);
+        else launch(attn_bwd_with_kernel<T, BS, false>);
+        return hipGetLastError();
+    }
 }
 
 }  // namespace
@@ -516,8 +558,8 @@ hipError_t launch_attn_fwd_with(const AttnShape& s, const Extras& x, const void*
 
 static hipError_t launch_bwd(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, const void* O,
                              const void* dO, const float* LSE, void* dQ, void* dK, void* dV, const int* row_ptr, const int* col_idx,
-                             const int* col_ptr, const int* row_idx, int nnzb, hipStream_t st) {
-    SPION_DISPATCH(bwd_with, s, x, Q, K, V, O, dO, LSE, dQ, dK, dV, row_ptr, col_idx, col_ptr, row_idx, nnzb, st);
+                             const int* col_ptr, const int* row_idx, int nnzb, void* workspace, hipStream_t st) {
+    SPION_DISPATCH(bwd_with, s, x, Q, K, V, O, dO, LSE, dQ, dK, dV, row_ptr, col_idx, col_ptr, row_idx, nnzb, workspace, st);
 }
 
 hipError_t launch_attn_bwd_with(const AttnShape& s, const Extras& extras, const void* Q, const void* K, const void* V, const void* O,
@@ -527,12 +569,13 @@ hipError_t launch_attn_bwd_with(const AttnShape& s, const Extras& extras, const 
     const WithWorkspace ws(s, dtable != nullptr, x.n_buckets, x.H, nnzb);
     char* const base = static_cast<char*>(workspace);
     x.slices = dtable ? reinterpret_cast<float*>(base + ws.slices) : nullptr;
-    hipError_t e = launch_bwd(s, x, Q, K, V, O, dO, LSE, dQ, dK, dV, row_ptr, col_idx, col_ptr, row_idx, nnzb, st);
+    x.counters = dtable ? reinterpret_cast<unsigned*>(base + ws.counters) : nullptr;
+    hipError_t e = launch_bwd(s, x, Q, K, V, O, dO, LSE, dQ, dK, dV, row_ptr, col_idx, col_ptr, row_idx, nnzb, workspace, st);
     if (e != hipSuccess || !dtable) return e;
     const int threads = table_grad_threads(x.n_buckets);
     table_grad_kernel<<<dim3((unsigned)(x.H * ws.parts)), dim3(threads), (size_t)x.n_buckets * threads * sizeof(float), st>>>(
         x.slices, row_ptr, col_idx, x, s.BH / x.H, s.L, s.nb, nnzb, s.bs, ws.tile, ws.parts,
-        reinterpret_cast<float*>(base + ws.partial), reinterpret_cast<unsigned long long*>(base + ws.counters), s.tag, dtable);
+        reinterpret_cast<float*>(base + ws.partial), x.counters, dtable);
     return hipGetLastError();
 }
 

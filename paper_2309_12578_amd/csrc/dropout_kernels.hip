@@ -133,9 +133,7 @@ hipError_t launch_relative_bias(const void* table, const uint8_t* bucket_of, voi
 // ------------------------------------------------------------------------------------------------
 template <typename T>
 __global__ __launch_bounds__(256) void relative_bias_grad_kernel(const T* __restrict__ dbias, const uint8_t* __restrict__ bucket_of,
-                                                                 void* __restrict__ dtable, int reach, int n_buckets, int H, int q_len, int k_len,
-                                                                 int q_start, int parts, int band, float* __restrict__ partial,
-                                                                 unsigned long long* __restrict__ counters, unsigned long long tag) {
+                                                                 int reach, int n_buckets, int H, int q_len, int k_len, int q_start, int parts, int band, float* partial) {
     extern __shared__ float hist[];   // [n_buckets][threads]
     const int h = blockIdx.x % H, part = blockIdx.x / H, tid = threadIdx.x, threads = blockDim.x;
     for (int b = 0; b < n_buckets; ++b) hist[b * threads + tid] = 0.f;
@@ -153,18 +151,21 @@ __global__ __launch_bounds__(256) void relative_bias_grad_kernel(const T* __rest
         const unsigned b = bucket_of[d - q_start + reach - 1];
         hist[min(b, (unsigned)n_buckets - 1u) * threads + tid] += sum;
     }
-    finish_table_grad(hist, n_buckets, part, parts, h, H, partial, counters, tag, dtable, sizeof(T) == 2);
+    leave_partial(hist, n_buckets, part, parts, h, partial);
+}
+
+__global__ __launch_bounds__(256) void relative_bias_sum_kernel(const float* partial, void* __restrict__ dtable, int n_buckets, int H, int parts, int is_bf16) {
+    write_table_column(partial, n_buckets, parts, blockIdx.x, H, dtable, is_bf16 != 0);
 }
 
 namespace {
 struct BiasGradPlan {
     int band = 256, parts;
-    size_t counters, total;
+    size_t total;
     BiasGradPlan(int H, int q_len, int k_len, int n_buckets) {
         const long long tiles = (long long)((q_len + k_len) / table_grad_threads(n_buckets) + 1) * ((q_len + band - 1) / band);
-        parts = (int)std::min<long long>(std::min<long long>(tiles, 255), std::max(1, 2048 / H));
-        counters = ((size_t)H * parts * n_buckets * sizeof(float) + 255) / 256 * 256;
-        total = (counters + (size_t)H * 8 + 255) / 256 * 256;
+        parts = (int)std::min<long long>(tiles, std::max(1, 2048 / H));
+        total = ((size_t)H * parts * n_buckets * sizeof(float) + 255) / 256 * 256;
     }
 };
 }  // namespace
@@ -172,20 +173,20 @@ struct BiasGradPlan {
 size_t relative_bias_grad_workspace_bytes(int H, int q_len, int k_len, int n_buckets) { return BiasGradPlan(H, q_len, k_len, n_buckets).total; }
 
 hipError_t launch_relative_bias_grad(const void* dbias, const uint8_t* bucket_of, void* dtable, int reach, int n_buckets, int H, int q_len, int k_len,
-                                     int q_start, bool is_bf16, unsigned long long tag, void* workspace, hipStream_t st) {
+                                     int q_start, bool is_bf16, void* workspace, hipStream_t st) {
     const BiasGradPlan plan(H, q_len, k_len, n_buckets);
     const int threads = table_grad_threads(n_buckets);
-    auto* const counters = reinterpret_cast<unsigned long long*>(static_cast<char*>(workspace) + plan.counters);
-    const size_t lds = (size_t)n_buckets * threads * sizeof(float);
-    const dim3 grid((unsigned)(H * plan.parts));
-    if (is_bf16)
-        relative_bias_grad_kernel<bf16_t><<<grid, dim3(threads), lds, st>>>(static_cast<const bf16_t*>(dbias), bucket_of, dtable, reach, n_buckets, H, q_len,
-                                                                           k_len, q_start, plan.parts, plan.band, static_cast<float*>(workspace),
-                                                                           counters, tag);
-    else
-        relative_bias_grad_kernel<float><<<grid, dim3(threads), lds, st>>>(static_cast<const float*>(dbias), bucket_of, dtable, reach, n_buckets, H, q_len,
-                                                                          k_len, q_start, plan.parts, plan.band, static_cast<float*>(workspace),
-                                                                          counters, tag);
+    float* const partial = static_cast<float*>(workspace);
+    auto launch = [&](auto kernel, auto type) {
+        typedef decltype(type) T;
+        kernel<<<dim3((unsigned)(H * plan.parts)), dim3(threads), (size_t)n_buckets * threads * sizeof(float), st>>>(
+            static_cast<const T*>(dbias), bucket_of, reach, n_buckets, H, q_len, k_len, q_start, plan.parts, plan.band, partial);
+    };
+    if (is_bf16) launch(relative_bias_grad_kernel<bf16_t>, bf16_t{});
+    else launch(relative_bias_grad_kernel<float>, float{});
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    relative_bias_sum_kernel<<<dim3((unsigned)H), dim3(256), 0, st>>>(partial, dtable, n_buckets, H, plan.parts, is_bf16);
     return hipGetLastError();
 }
 

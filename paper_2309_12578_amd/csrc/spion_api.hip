@@ -522,6 +522,7 @@ static int take_extras(const spion_attn_params* p, const spion_attn_extras* x, i
     out.stream = x->stream;
     out.keep_scale = keep_scale(threshold);
     out.slices = nullptr;
+    out.counters = nullptr;
     return SPION_OK;
 }
 
@@ -599,8 +600,8 @@ int spion_relative_bias_grad(const void* dbias, const uint8_t* bucket_of, void* 
     if (rc != SPION_OK) return rc;
     if (!workspace || (uintptr_t)workspace % kAlign != 0 || workspace_bytes < spion_relative_bias_workspace_bytes(n_buckets, H, q_len, k_len))
         return SPION_ERR_WORKSPACE;
-    return spion::launch_relative_bias_grad(dbias, bucket_of, dtable, reach, n_buckets, H, q_len, k_len, q_start, dtype == SPION_BF16, next_tag(),
-                                            workspace, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? SPION_OK : SPION_ERR_HIP;
+    return spion::launch_relative_bias_grad(dbias, bucket_of, dtable, reach, n_buckets, H, q_len, k_len, q_start, dtype == SPION_BF16, workspace,
+                                            static_cast<hipStream_t>(hip_stream)) == hipSuccess ? SPION_OK : SPION_ERR_HIP;
 }
 
 int spion_dropout_add(const void* x, const void* residual, void* y, int64_t n, int32_t dtype, double dropout, const int64_t* rng,

@@ -61,7 +61,8 @@ struct Extras {
     unsigned threshold, stream;       // draws below are dropped; 0: no dropout
     float keep_scale;                 // 65536 / (65536 - threshold)
     float* slices;                    // backward: sums of dS over diagonals, or nullptr: no gradient of the table
-    static constexpr int kMaxBuckets = 256;
+    unsigned* counters;               // with them: [H], kCounterStride words apart, which the backward kernels set to 0
+    static constexpr int kMaxBuckets = 256, kCounterStride = 64;
 };
 
 // How the kernels cut long block rows (see attn_bf16_tiles.h), from what the host knows of a pattern.
@@ -128,6 +129,10 @@ hipError_t launch_attn_bwd_with(const AttnShape& s, const Extras& x, const void*
 template <int BS>
 hipError_t fwd_with_bf16(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, void* O, float* LSE,
                          const int* row_ptr, const int* col_idx, int nnzb, hipStream_t st);
+template <int BS>
+hipError_t bwd_with_bf16(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, const void* O, const void* dO,
+                         const float* LSE, void* dQ, void* dK, void* dV, const int* row_ptr, const int* col_idx, const int* col_ptr,
+                         const int* row_idx, int nnzb, void* workspace, hipStream_t st);
 size_t attn_with_workspace_bytes(const AttnShape& s, bool table_grad, int n_buckets, int H, int nnzb, bool is_bwd);
 
 // dropout_kernels.hip: y = residual + dropout(x) (residual nullptr: without), the dense bias and its table's gradient
@@ -137,7 +142,7 @@ hipError_t launch_relative_bias(const void* table, const uint8_t* bucket_of, voi
                                 int q_start, bool is_bf16, hipStream_t st);
 size_t relative_bias_grad_workspace_bytes(int H, int q_len, int k_len, int n_buckets);
 hipError_t launch_relative_bias_grad(const void* dbias, const uint8_t* bucket_of, void* dtable, int reach, int n_buckets, int H, int q_len, int k_len,
-                                     int q_start, bool is_bf16, unsigned long long tag, void* workspace, hipStream_t st);
+                                     int q_start, bool is_bf16, void* workspace, hipStream_t st);
 
 // norm_kernels.hip: LayerNorm over rows of D = 64 k <= 2048 elements
 size_t layer_norm_workspace_bytes(int rows, int D);
@@ -161,6 +166,7 @@ hipError_t fwd_bf16(const AttnShape& s, const void* Q, const void* K, const void
 
 // attn_bwd_bf16_kernels.hip: tuned bf16 backward, BS in {32, 64}; both sides in one launch; pieces of long rows per head, at most
 int bwd_bf16_row_slots(const AttnShape& s, int nnzb);
+void bwd_bf16_decide_row_cut(RowCut& cut, const AttnShape& s, int nnzb);   // which they are
 template <int BS>
 hipError_t bwd_bf16(const AttnShape& s, const void* Q, const void* K, const void* V, const void* O,
                     const void* dO, const float* LSE, void* dQ, void* dK, void* dV, const int* row_ptr,
