@@ -13,6 +13,7 @@
 #define SPION_ATTN_EXTRAS_H_
 
 #include <hip/hip_runtime.h>
+#include <limits.h>
 #include <stdint.h>
 
 #include "attn_common.h"
@@ -21,6 +22,7 @@
 
 namespace spion {
 
+constexpr int kNoSlice = INT_MIN;       // in place of a slice's distance: nothing was computed
 constexpr float kMaskedBias = -1e30f;   // a bias from here down masks, as -infinity does
 
 __device__ __forceinline__ int length_of(const Extras& x, int bh, int L) {

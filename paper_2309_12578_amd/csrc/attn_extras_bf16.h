@@ -57,10 +57,33 @@ struct BlockBias {
         if (BIAS) from = x.bucket_of + (L - BS + (tid < 2 * BS - 2 ? tid : 2 * BS - 2));
     }
     __device__ __forceinline__ unsigned request(int blocks_off) const { return mine ? from[(ptrdiff_t)blocks_off * BS] : 0u; }   // key block - query block
+    // Behind the biases, for either half of the distances: the bucket they are all of, or -1, and its bias.
     __device__ __forceinline__ void put(float* slice, unsigned bucket, int tid) const {
-        if (mine) slice[tid] = tab[min((int)bucket, last)];
+        if (mine) {
+            const int b = min((int)bucket, last);
+            const float v = tab[b];
+            slice[tid] = v;
+            const bool alike = __all(b == __builtin_amdgcn_readfirstlane(b));
+            const float2 all = make_float2(__builtin_bit_cast(float, alike ? b : -1), v);
+            if ((tid & 63) == 0) {
+                *reinterpret_cast<float2*>(slice + 2 * BS + (tid >> 6) * 2) = all;
+                if (BS == 32) *reinterpret_cast<float2*>(slice + 2 * BS + 2) = all;
+            }
+        }
     }
 };
+template <int BS>
+constexpr int kSlice = 2 * BS + 4;   // floats
+
+// Whether all distances of a block are of one bucket (it is far off the diagonal, as most are), and its bias: then no lane needs to
+// look up its own.
+template <int BS>
+__device__ __forceinline__ bool one_bucket(const float* slice, float& bias) {
+    const float4 all = *reinterpret_cast<const float4*>(slice + 2 * BS);
+    const int first = __builtin_amdgcn_readfirstlane(__float_as_int(all.x));
+    bias = all.y;
+    return first >= 0 && first == __builtin_amdgcn_readfirstlane(__float_as_int(all.z));
+}
 
 // The head's column of the bias table in registers (requested before anything else is), then in LDS.
 template <int BS, bool BIAS>

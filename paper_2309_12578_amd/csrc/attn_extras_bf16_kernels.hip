@@ -48,7 +48,8 @@ template <int BS, bool BIAS, bool DROP>
 __global__ __launch_bounds__(BS * 4, BS == 64 ? 3 : 4) void attn_fwd_with_bf16_kernel(FwdWith a) {
     constexpr int NKT = BS / 16;
     __shared__ __attribute__((aligned(16))) KvTiles<BS> sm0, sm1;
-    __shared__ float bias0[2 * BS], bias1[2 * BS], tab[BIAS ? Extras::kMaxBuckets : 1];
+    __shared__ __attribute__((aligned(16))) float bias0[kSlice<BS>], bias1[kSlice<BS>];
+    __shared__ float tab[BIAS ? Extras::kMaxBuckets : 1];
 
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -123,13 +124,14 @@ __global__ __launch_bounds__(BS * 4, BS == 64 ? 3 : 4) void attn_fwd_with_bf16_k
         const int j = walk_index(t < last ? t : last, pd);
         return j < 8 ? pick8(first, j) : cols[j];
     };
-    int walk_v = 0;   // the first 64 blocks of the walk, one per lane
+    int walk_v = 0;   // 64 blocks of the walk, one per lane
     if (n > 2) walk_v = cols[walk_index(lane < last ? lane : last, pd)];
-    auto later_col = [&](int t) {
+    auto later_col = [&](int t) {   // t >= 2, one after the other
         const int u = t < last ? t : last;
-        return u < 64 ? __builtin_amdgcn_readlane(walk_v, u) : cols[walk_index(u, pd)];
+        if (u >= 64 && (u & 63) == 0) walk_v = args_again<FwdWith>().col_idx[jb + walk_index(u + lane < last ? u + lane : last, pd)];
+        return __builtin_amdgcn_readlane(walk_v, u & 63);
     };
-    int jcur = n > 0 ? col_at(0) : I, jnext = n > 0 ? col_at(1) : I;
+    int jcur = __builtin_amdgcn_readfirstlane(n > 0 ? col_at(0) : I), jnext = __builtin_amdgcn_readfirstlane(n > 0 ? col_at(1) : I);
     column.put(tab, a.x, tid);
     if (pd < 0 && n > 0) {
         // no diagonal block in this row (piece): once everyone's early load has landed, load block 0 over it
@@ -170,11 +172,11 @@ __global__ __launch_bounds__(BS * 4, BS == 64 ? 3 : 4) void attn_fwd_with_bf16_k
         if constexpr (DROP) query_factors<NKT>(draws, qrow, jcur * BS, g, below, factors);
         meet(it == 0);
         if (it > 0) {
-            jnext = later_col(it + 1);
             if constexpr (BIAS) biases.put(bias_n, bucket, tid);
             if (it + 1 < n) issue(tgt, jnext);
         }
-        if constexpr (BIAS) bucket = biases.request(later_col(it + 2) - I);
+        const int jafter = later_col(it + 2);
+        if constexpr (BIAS) bucket = biases.request(jafter - I);
         // S^T tile kt: [key 16 kt + 4 g + i][query r]; all K fragments are requested up front
         bf16x8 kfr[NKT][2];
 #pragma unroll
@@ -183,17 +185,20 @@ __global__ __launch_bounds__(BS * 4, BS == 64 ? 3 : 4) void attn_fwd_with_bf16_k
             for (int c = 0; c < 2; ++c)
                 kfr[kt][c] = *reinterpret_cast<const bf16x8*>(cur.k + kt * 16 * kD + sl.frag[c]);
         f32x4 s[NKT];
+        float bias = 0.f;
+        const bool one = !BIAS || one_bucket<BS>(bias_c, bias);
 #pragma unroll
-        for (int kt = 0; kt < NKT; ++kt) {
-            if constexpr (BIAS) {
+        for (int kt = 0; kt < NKT; ++kt) s[kt] = f32x4{bias, bias, bias, bias};
+        if (BIAS && !one) {
+#pragma unroll
+            for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[kt][i] = bias_c[slice_at + 16 * kt + i];
-            } else {
-                s[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
-            }
+        }
+#pragma unroll
+        for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
             for (int c = 0; c < 2; ++c) s[kt] = mma_d(s[kt], kfr[kt][c], qf[c]);
-        }
         if (jcur * BS + BS > length) {   // the block that the sequence ends in
 #pragma unroll
             for (int kt = 0; kt < NKT; ++kt)
@@ -250,6 +255,7 @@ __global__ __launch_bounds__(BS * 4, BS == 64 ? 3 : 4) void attn_fwd_with_bf16_k
             oacc[j & 3] = mma_d(oacc[j & 3], vop[j], join(pq[2 * pc], pq[2 * pc + 1]));   // O^T[d][query] += V^T P^T
         }
         jcur = jnext;
+        jnext = jafter;
     };
 
     for (int it = 0; it < n; it += 2) {

@@ -52,7 +52,8 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
     __shared__ __attribute__((aligned(16))) bf16_t ta0[BS * kD], tb0[BS * kD], tc0[BS * kD];
     __shared__ __attribute__((aligned(16))) bf16_t ta1[BS * kD], tb1[BS * kD], tc1[BS * kD];
     __shared__ __attribute__((aligned(16))) float lse0[BS], del0[BS], lse1[BS], del1[BS];
-    __shared__ float bias0[2 * BS], bias1[2 * BS], tab[BIAS ? Extras::kMaxBuckets : 1];
+    __shared__ __attribute__((aligned(16))) float bias0[kSlice<BS>], bias1[kSlice<BS>];
+    __shared__ float tab[BIAS ? Extras::kMaxBuckets : 1];
 
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -147,6 +148,7 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
             jb += from;
         }
         const int* cols = b.col_idx + jb;
+        const int n_all = n;
         n = I * BS < length ? blocks_below<BS>(cols, n, length, L, lane) : 0;
         const int last = n > 0 ? n - 1 : 0;
         int first[8];
@@ -157,13 +159,14 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
             const int j = walk_index(t < last ? t : last, pd);
             return j < 8 ? pick8(first, j) : cols[j];
         };
-        int walk_v = 0;   // the first 64 blocks of the walk, one per lane
+        int walk_v = 0;   // 64 blocks of the walk, one per lane
         if (n > 2) walk_v = cols[walk_index(lane < last ? lane : last, pd)];
-        auto later_col = [&](int t) {
+        auto later_col = [&](int t) {   // t >= 2, one after the other
             const int u = t < last ? t : last;
-            return u < 64 ? __builtin_amdgcn_readlane(walk_v, u) : args_again<BwdWith>().col_idx[jb + walk_index(u, pd)];
+            if (u >= 64 && (u & 63) == 0) walk_v = args_again<BwdWith>().col_idx[jb + walk_index(u + lane < last ? u + lane : last, pd)];
+            return __builtin_amdgcn_readlane(walk_v, u & 63);
         };
-        int jcur = n > 0 ? col_at(0) : I, jnext = n > 0 ? col_at(1) : I;
+        int jcur = __builtin_amdgcn_readfirstlane(n > 0 ? col_at(0) : I), jnext = __builtin_amdgcn_readfirstlane(n > 0 ? col_at(1) : I);
         column.put(tab, a.x, tid);
         if (pd < 0 && n > 0) {
             // no diagonal block in this row (piece): once everyone's early load has landed, load block 0 over it
@@ -175,15 +178,17 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
             }
             issue(ta0, tb0, jcur);
         }
-        // Diagonals: this wave's places (lane group, distance), and for two steps each wave's sums of every distance of
-        // the block.  What a wave never writes stays 0.
+        // Diagonals: this wave's places (lane group, distance), of which those it never writes stay 0, and for two steps each
+        // wave's sums of every distance of the block.
         constexpr int kPlaces = 16 * NT + 32;
         float* const places = reinterpret_cast<float*>(tc0) + wave * (4 * kPlaces);
         float* const sums = reinterpret_cast<float*>(tc1);   // [step % 2][wave][2 BS]
         const bool by_distance = BIAS && b.x.slices != nullptr;
+        float* const my_slices = by_distance ? b.x.slices + ((size_t)bh * b.nnzb + jb) * (2 * BS) + tid : nullptr;   // of this row (piece)
         if (by_distance) {
             for (int i = tid; i < NT * 4 * kPlaces; i += BS * 4) reinterpret_cast<float*>(tc0)[i] = 0.f;
-            for (int i = tid; i < 2 * NT * 2 * BS; i += BS * 4) sums[i] = 0.f;
+            for (int e = n + tid; e < n_all; e += BS * 4)   // what is not computed
+                (my_slices - tid)[(size_t)e * (2 * BS) + 2 * BS - 1] = __builtin_bit_cast(float, kNoSlice);
         }
         if (n > 0) {
             const unsigned second = biases.request(jnext - I);
@@ -198,13 +203,14 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt) dq[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
         const int slice_at = 4 * g - wave * 16 - r + BS - 1;   // of key 4 g of the block
-        float* const my_slices = by_distance ? b.x.slices + ((size_t)bh * b.nnzb + jb) * (2 * BS) + tid : nullptr;   // of this row (piece)
-        // the distances of the block of step t, from the waves' sums
+        // the distances of the block of step t, from the waves' sums; the first wave's last number is where the block lies
         auto write_slice = [&](int t) {
             if (tid < 2 * BS) {
-                float v = 0.f;
+                const float* const from = sums + (t & 1) * (NT * 2 * BS) + tid;
+                float v = from[0];
 #pragma unroll
-                for (int w = 0; w < NT; ++w) v += sums[((t & 1) * NT + w) * (2 * BS) + tid];
+                for (int w = 1; w < NT; ++w) v += from[w * (2 * BS)];
+                if (tid == 2 * BS - 1) v = from[0];
                 my_slices[(size_t)(walk_index(t, pd) * (2 * BS))] = v;
             }
         };
@@ -215,11 +221,22 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
             meet(it == 0);
             if (BIAS && by_distance && it > 0) write_slice(it - 1);
             if (it > 0) {
-                jnext = later_col(it + 1);
-                if constexpr (BIAS) biases.put(bias_n, bucket, tid);
+                    if constexpr (BIAS) biases.put(bias_n, bucket, tid);
                 if (it + 1 < n) issue(tk, tv, jnext);
             }
-            if constexpr (BIAS) bucket = biases.request(later_col(it + 2) - I);
+            const int jafter = later_col(it + 2);
+            if constexpr (BIAS) bucket = biases.request(jafter - I);
+            f32x4 s[NT];
+            float bias = 0.f;
+            const bool one = !BIAS || one_bucket<BS>(bias_c, bias);
+#pragma unroll
+            for (int kt16 = 0; kt16 < NT; ++kt16) s[kt16] = f32x4{bias, bias, bias, bias};
+            if (BIAS && !one) {
+#pragma unroll
+                for (int kt16 = 0; kt16 < NT; ++kt16)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[kt16][i] = bias_c[slice_at + 16 * kt16 + i];
+            }
             bf16x8 kfr[NT][2], vfr[NT][2];
 #pragma unroll
             for (int kt16 = 0; kt16 < NT; ++kt16)
@@ -228,17 +245,11 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
                     kfr[kt16][c] = *reinterpret_cast<const bf16x8*>(kt + kt16 * 16 * kD + sl.frag[c]);
                     vfr[kt16][c] = *reinterpret_cast<const bf16x8*>(vt + kt16 * 16 * kD + sl.frag[c]);
                 }
-            f32x4 s[NT], dp[NT];
+            f32x4 dp[NT];
 #pragma unroll
             for (int kt16 = 0; kt16 < NT; ++kt16) {
                 // without dropout dP - delta comes out of the MFMA: the accumulator starts at -delta
                 dp[kt16] = DROP ? f32x4{0.f, 0.f, 0.f, 0.f} : f32x4{-delta, -delta, -delta, -delta};
-                if constexpr (BIAS) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[kt16][i] = bias_c[slice_at + 16 * kt16 + i];
-                } else {
-                    s[kt16] = f32x4{0.f, 0.f, 0.f, 0.f};
-                }
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     s[kt16] = mma_d(s[kt16], kfr[kt16][c], qf[c]);      // S^T = K Q^T
@@ -276,26 +287,46 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
                 dq[j & 3] = mma_d(dq[j & 3], kop[j], join(dsq[2 * pc], dsq[2 * pc + 1]));   // dQ^T[d][query] += K^T dS^T
             }
             if (BIAS && by_distance) {
-                float u[NT + 1];
-                diagonal_sums<NT>(s, u);
+                int l = lane;   // addresses that only this part uses are made here
+                asm volatile("" : "+v"(l));
+                float* const mine = sums + ((it & 1) * NT + wave) * (2 * BS) + l;   // numbers l, l + 64, .. of the block's 2 BS
+                const float place = l == 63 ? __int_as_float((jcur - I) * BS) : 0.f;   // for the last number
+                if (one) {   // of one bucket: it does not matter which distance has what
+                    f32x4 v = s[0];
 #pragma unroll
-                for (int kt16 = 0; kt16 <= NT; ++kt16) places[g * kPlaces + 16 * kt16 + 4 * g - r + 15] = u[kt16];
-                __builtin_amdgcn_wave_barrier();
-                // distance index (key - query of the block + BS - 1) of place e: e + BS - 16 - 16 wave
-                float* const mine = sums + ((it & 1) * NT + wave) * (2 * BS) + (BS - 16 - 16 * wave);
+                    for (int kt16 = 1; kt16 < NT; ++kt16) v += s[kt16];
+                    float sum = (v[0] + v[1]) + (v[2] + v[3]);
+                    if (BS == 64) {
+                        mine[0] = sum;
+                        mine[64] = place;
+                    } else {
+                        float lower, upper;
+                        swap_halves32(sum, lower, upper);
+                        mine[0] = l < 32 ? lower + upper : place;
+                    }
+                } else {
+                    float u[NT + 1];
+                    diagonal_sums<NT>(s, u);
+                    float* const of_lane = places + (l >> 4) * (kPlaces + 4) - (l & 15) + 15;   // of lane group g, distance 4 g - r
 #pragma unroll
-                for (int e0 = 0; e0 < 16 * NT + 15; e0 += 64) {
-                    const int e = e0 + lane;
-                    if (e < 16 * NT + 15) {
-                        float v = 0.f;
+                    for (int kt16 = 0; kt16 <= NT; ++kt16) of_lane[16 * kt16] = u[kt16];
+                    __builtin_amdgcn_wave_barrier();
 #pragma unroll
-                        for (int gg = 0; gg < 4; ++gg) v += places[gg * kPlaces + e];
-                        mine[e] = v;
+                    for (int t = 0; t < 2 * BS; t += 64) {
+                        const int e = t + l - (BS - 16 - 16 * wave);   // place of this distance; a wave has those of its queries
+                        float v = t + 64 == 2 * BS ? place : 0.f;
+                        if (e >= 0 && e < 16 * NT + 15) {
+                            v = places[e];
+#pragma unroll
+                            for (int gg = 1; gg < 4; ++gg) v += places[gg * kPlaces + e];
+                        }
+                        mine[t] = v;
                     }
                 }
                 __builtin_amdgcn_wave_barrier();
             }
             jcur = jnext;
+            jnext = jafter;
         };
 
         for (int it = 0; it < n; it += 2) {
@@ -445,6 +476,8 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
             const int o = sl.tr(j >> 1) + pc * 32 * kD;
             return join(lds_read_tr(tile + o), lds_read_tr(tile + 16 * kD + o));
         };
+        float bias = 0.f;
+        const bool one = !BIAS || one_bucket<BS>(bias_c, bias);
         frags(0);
 #pragma unroll
         for (int pc = 0; pc < NT / 2; ++pc) {
@@ -464,10 +497,10 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
                 const int qt16 = 2 * pc + h;
                 const f32x4 ndelta = *reinterpret_cast<const f32x4*>(&del_s[qt16 * 16 + 4 * g]);
                 const f32x4 lse4 = *reinterpret_cast<const f32x4*>(&lse_s[qt16 * 16 + 4 * g]);   // log2 units
-                f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f}, dp = DROP ? f32x4{0.f, 0.f, 0.f, 0.f} : ndelta;   // the MFMA returns dP - delta
-                if constexpr (BIAS) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[i] = bias_c[slice_at - 16 * qt16 - i];
+                f32x4 s = f32x4{bias, bias, bias, bias}, dp = DROP ? f32x4{0.f, 0.f, 0.f, 0.f} : ndelta;   // the MFMA returns dP - delta
+                if (BIAS && !one) {
+                    const float* const from = bias_c + slice_at - 16 * qt16;
+                    s = f32x4{from[0], from[-1], from[-2], from[-3]};
                 }
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {

@@ -264,6 +264,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_bwd_with_kernel(
             clear(dof);
         }
         delta = group_sum(delta);
+        if (x.slices)   // what is not computed
+            for (int e = n * TPB + tid; e < n_list * TPB; e += kWaves * 64)
+                x.slices[((((size_t)bh * nnzb + row_ptr[block] + e / TPB) * TPB + sub) * TPB + e % TPB) * 32 + 31] = __builtin_bit_cast(float, kNoSlice);
         f32x4 dq[1][4];
         clear_acc<1>(dq);
         for (int t = wave * KT; t < nt; t += STRIDE) {
@@ -310,7 +313,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_bwd_with_kernel(
                     if (lane < 32) {
                         const float v = diag_s[wave][0][lane] + diag_s[wave][1][lane] + diag_s[wave][2][lane] + diag_s[wave][3][lane];
                         const size_t entry = (size_t)bh * nnzb + row_ptr[block] + (t + u) / TPB;
-                        x.slices[((entry * TPB + sub) * TPB + (t + u) % TPB) * 32 + lane] = v;
+                        x.slices[((entry * TPB + sub) * TPB + (t + u) % TPB) * 32 + lane] = lane < 31 ? v : __builtin_bit_cast(float, k0 - row0);
                     }
                     __builtin_amdgcn_wave_barrier();
                 }
@@ -400,65 +403,62 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_bwd_with_kernel(
 }
 
 // ------------------------------------------------------------------------------------------------
-// The table's gradient from the slices: number t of a tile (query tile a, key tile b, of ts rows) of block (I, J) is of distance
-// (J - I) bs + (b - a) ts + t - (ts - 1).  Workgroup = (head, part of its batch's kept blocks); every thread adds into its own
-// copy of the buckets in LDS, the copies are added up in a fixed order, and so are the parts, by the last workgroup of the head
-// to arrive.  The counters of arrivals, a line each, are 0 from the backward kernel on: counting by compare and swap, as where a few pieces of
-// a row meet, hundreds of workgroups took 500 to 1500 us.
+// The table's gradient from the slices, 2 TS numbers each: number t < 2 TS - 1 is the sum of dS over distance base + t - (TS - 1) of
+// a TS x TS tile whose first key is `base` from its first query; the last has `base` as an integer, or kNoSlice where nothing was
+// computed.  Every thread adds into its own copy of the buckets in LDS, the copies are added up in a fixed order, and so
+// are the parts of a head, by the last of its workgroups to arrive.  The counters of arrivals, a line each, are 0 from the backward
+// kernel on: counting by compare and swap, as where a few pieces of a row meet, hundreds of workgroups took 500 to 1500 us.
+// kInFlight tiles a wave at a time, whose numbers are requested together, then their buckets: one by one, with the tile's place found from the
+// index, 4 x 8 heads x 4096, 851 blocks of 64, took 30 us.
 // ------------------------------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void table_grad_kernel(const float* __restrict__ slices, const int* __restrict__ row_ptr,
-                                                         const int* __restrict__ col_idx, Extras x, int B, int L, int nb, int nnzb, int bs,
-                                                         int ts, int parts, float* partial, unsigned* __restrict__ counters,
+template <int TS>
+__global__ __launch_bounds__(256) void table_grad_kernel(const float* __restrict__ slices, Extras x, int L, unsigned tiles_of_head,
+                                                         unsigned tiles_a_sequence, int parts, float* partial, unsigned long long* __restrict__ counters,
                                                          void* __restrict__ dtable) {
     extern __shared__ float hist[];   // [n_buckets][threads]
-    constexpr int kAtOnce = 64;       // blocks whose places are found together, a lane each
-    __shared__ long long slice_s[kAtOnce];
-    __shared__ int map_s[kAtOnce], tiles_s[kAtOnce];
-    const int h = blockIdx.x % x.H, part = blockIdx.x / x.H, tid = threadIdx.x, threads = blockDim.x;
+    constexpr int F = 2 * TS, LANES = F < 64 ? F : 64, PER = F / LANES, GROUP = 64 / LANES, kInFlight = 4;   // lanes of a tile, numbers a lane, tiles a wave
+    typedef float Numbers __attribute__((ext_vector_type(PER)));
+    const int h = blockIdx.x % x.H, part = blockIdx.x / x.H, tid = threadIdx.x, threads = blockDim.x, lane = tid & 63;
     for (int b = 0; b < x.n_buckets; ++b) hist[b * threads + tid] = 0.f;
-    const int tpb = bs / ts, per_block = tpb * tpb * 2 * ts;   // powers of two
-    const int shift = __ffs(per_block) - 1, tile_shift = __ffs(2 * ts) - 1;
-    const long long all = (long long)B * nnzb, end = (part + 1) * all / parts;
-    for (long long c0 = part * all / parts; c0 < end; c0 += kAtOnce) {
-        __syncthreads();
-        if (tid < kAtOnce) {
-            const long long e = c0 + tid;
-            int map = 0, tiles = 0;
-            if (e < end) {
-                const int b = (int)(e / nnzb), j = (int)(e % nnzb);
-                int lo = 0, hi = nb;   // the last row that starts at j or before
-                while (hi - lo > 1) {
-                    const int mid = (lo + hi) >> 1;
-                    if (row_ptr[mid] <= j) lo = mid;
-                    else hi = mid;
-                }
-                const int J = col_idx[j], length = length_of(x, b * x.H + h, L);
-                slice_s[tid] = ((long long)(b * x.H + h) * nnzb + j) << shift;
-                map = (J - lo) * bs + L - ts;
-                // query tiles that were computed: rows and blocks from the length on were not
-                tiles = J * bs < length ? min(tpb, (length - lo * bs + ts - 1) / ts) : 0;
-            }
-            map_s[tid] = map;
-            tiles_s[tid] = tiles;
+    const int t = lane % LANES * PER;
+    const unsigned first = (unsigned)((unsigned long long)part * tiles_of_head / parts);
+    const unsigned end = (unsigned)((unsigned long long)(part + 1) * tiles_of_head / parts);
+    const unsigned at_once = (threads >> 6) * GROUP, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    for (unsigned c0 = first + wave * GROUP; c0 < end; c0 += kInFlight * at_once) {
+        Numbers v[kInFlight];
+        int base[kInFlight];
+#pragma unroll
+        for (int u = 0; u < kInFlight; ++u) {
+            const unsigned tile = c0 + u * at_once + lane / LANES, at = tile < end ? tile : end - 1;
+            const unsigned b = at / tiles_a_sequence, e = at % tiles_a_sequence;
+            v[u] = *reinterpret_cast<const Numbers*>(slices + ((size_t)(b * x.H + h) * tiles_a_sequence + e) * F + t);
         }
-        __syncthreads();
-        const int n = (int)min((long long)kAtOnce, end - c0) << shift;
-#pragma unroll 4
-        for (int f = tid; f < n; f += threads) {
-            const int entry = f >> shift, e = f & (per_block - 1), t = e & (2 * ts - 1), tile = e >> tile_shift;
-            const int q = tile / tpb, k = tile % tpb;
-            if (t == 2 * ts - 1 || q >= tiles_s[entry]) continue;
-            const int bucket = bucket_index(x, x.bucket_of[map_s[entry] + (k - q) * ts + t]);
-            __hip_atomic_fetch_add(&hist[bucket * threads + tid], slices[slice_s[entry] + e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+#pragma unroll
+        for (int u = 0; u < kInFlight; ++u) {
+            const float place = v[u][PER - 1];   // (a bit cast of the element itself is one of the vector's first)
+            const int from = __shfl(__builtin_bit_cast(int, place), lane | (LANES - 1));
+            base[u] = c0 + u * at_once + lane / LANES < end ? from : kNoSlice;
         }
+        int bucket[kInFlight][PER];
+#pragma unroll
+        for (int u = 0; u < kInFlight; ++u)
+#pragma unroll
+            for (int i = 0; i < PER; ++i)   // (no place leads past the map)
+                bucket[u][i] = bucket_index(x, x.bucket_of[min((unsigned)(base[u] + L - TS + t + i), 2u * L - 2u)]);
+#pragma unroll
+        for (int u = 0; u < kInFlight; ++u)
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (base[u] != kNoSlice && t + i != F - 1)
+                    __hip_atomic_fetch_add(&hist[bucket[u][i] * threads + tid], v[u][i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     }
     leave_partial(hist, x.n_buckets, part, parts, h, partial);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's stores are done, at device scope
     __syncthreads();                                   // and those of the others, and every wave is done with the copies
     int* const flag = reinterpret_cast<int*>(hist);
     if (tid == 0) {
-        const unsigned before = __hip_atomic_fetch_add(counters + h * Extras::kCounterStride, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        *flag = before == (unsigned)parts - 1u;
+        const unsigned long long before = __hip_atomic_fetch_add(counters + h * Extras::kCounterStride, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        *flag = before == (unsigned long long)parts - 1ull;
     }
     __syncthreads();
     asm volatile("" ::: "memory");   // nothing of the others' is read before
@@ -483,12 +483,12 @@ struct WithWorkspace {
             total = slices;
             return;
         }
-        // eight blocks a workgroup or more, and about two workgroups a compute unit
-        const long long blocks = (long long)s.BH / H * nnzb;
-        parts = (int)std::max<long long>(1, std::min<long long>(blocks / 8, 512 / H));
+        // sixteen slices a workgroup or more, and about two workgroups a compute unit
+        const long long tiles = (long long)s.BH / H * nnzb * (s.bs / tile) * (s.bs / tile);
+        parts = (int)std::max<long long>(1, std::min<long long>(tiles / 16, 512 / H));
         partial = up(slices + (size_t)s.BH * nnzb * (s.bs / tile) * (s.bs / tile) * 2 * tile * sizeof(float));
         counters = up(partial + (size_t)H * parts * n_buckets * sizeof(float));
-        total = up(counters + (size_t)H * Extras::kCounterStride * 4);
+        total = up(counters + (size_t)H * Extras::kCounterStride * 8);
     }
 };
 
@@ -569,13 +569,19 @@ hipError_t launch_attn_bwd_with(const AttnShape& s, const Extras& extras, const 
     const WithWorkspace ws(s, dtable != nullptr, x.n_buckets, x.H, nnzb);
     char* const base = static_cast<char*>(workspace);
     x.slices = dtable ? reinterpret_cast<float*>(base + ws.slices) : nullptr;
-    x.counters = dtable ? reinterpret_cast<unsigned*>(base + ws.counters) : nullptr;
+    x.counters = dtable ? reinterpret_cast<unsigned long long*>(base + ws.counters) : nullptr;
     hipError_t e = launch_bwd(s, x, Q, K, V, O, dO, LSE, dQ, dK, dV, row_ptr, col_idx, col_ptr, row_idx, nnzb, workspace, st);
     if (e != hipSuccess || !dtable) return e;
+    const long long tiles = (long long)nnzb * (s.bs / ws.tile) * (s.bs / ws.tile);
+    if (s.BH / x.H * tiles > 0x7fffffffll) return hipErrorInvalidValue;   // (256 GB of slices and more)
     const int threads = table_grad_threads(x.n_buckets);
-    table_grad_kernel<<<dim3((unsigned)(x.H * ws.parts)), dim3(threads), (size_t)x.n_buckets * threads * sizeof(float), st>>>(
-        x.slices, row_ptr, col_idx, x, s.BH / x.H, s.L, s.nb, nnzb, s.bs, ws.tile, ws.parts,
-        reinterpret_cast<float*>(base + ws.partial), x.counters, dtable);
+    auto launch = [&](auto kernel) {
+        kernel<<<dim3((unsigned)(x.H * ws.parts)), dim3(threads), (size_t)x.n_buckets * threads * sizeof(float), st>>>(
+            x.slices, x, s.L, (unsigned)(s.BH / x.H * tiles), (unsigned)tiles, ws.parts, reinterpret_cast<float*>(base + ws.partial), x.counters, dtable);
+    };
+    if (ws.tile == 16) launch(table_grad_kernel<16>);
+    else if (ws.tile == 32) launch(table_grad_kernel<32>);
+    else launch(table_grad_kernel<64>);
     return hipGetLastError();
 }
 

@@ -8,6 +8,9 @@
 
 namespace spion {
 
+// a ^ b ^ c in one instruction
+__device__ __forceinline__ unsigned xor3(unsigned a, unsigned b, unsigned c) { return (unsigned)__builtin_amdgcn_bitop3_b32((int)a, (int)b, (int)c, 0x96); }
+
 struct PhiloxKey {
     unsigned k0, k1, c2, c3;   // the same for a whole launch: kept in scalar registers
     __device__ __forceinline__ PhiloxKey(const long long* __restrict__ rng, unsigned stream)
@@ -15,14 +18,14 @@ struct PhiloxKey {
     static __device__ __forceinline__ unsigned uniform(unsigned v) { return (unsigned)__builtin_amdgcn_readfirstlane((int)v); }
     __device__ __forceinline__ uint4 words(unsigned c0, unsigned c1) const {
         unsigned a = c0, b = c1, c = c2, d = c3, x = k0, y = k1;
-        // the rounds' keys are made again for each call, by scalar additions beside the vector work: kept, they take 14 registers
-        asm volatile("" : "+s"(x), "+s"(y));
+        // what is uniform is made again for each call, by scalar instructions beside the vector work: kept, it takes 20 registers
+        asm volatile("" : "+s"(x), "+s"(y), "+s"(c));
 #pragma unroll
         for (int r = 0; r < 7; ++r) {
             const unsigned long long p = (unsigned long long)a * 0xD2511F53u, q = (unsigned long long)c * 0xCD9E8D57u;
-            a = (unsigned)(q >> 32) ^ b ^ x;
+            a = xor3((unsigned)(q >> 32), b, x);
             b = (unsigned)q;
-            c = (unsigned)(p >> 32) ^ d ^ y;
+            c = xor3((unsigned)(p >> 32), d, y);
             d = (unsigned)p;
             x += 0x9E3779B9u;
             y += 0xBB67AE85u;

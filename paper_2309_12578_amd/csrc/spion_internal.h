@@ -61,8 +61,10 @@ struct Extras {
     unsigned threshold, stream;       // draws below are dropped; 0: no dropout
     float keep_scale;                 // 65536 / (65536 - threshold)
     float* slices;                    // backward: sums of dS over diagonals, or nullptr: no gradient of the table
-    unsigned* counters;               // with them: [H], kCounterStride words apart, which the backward kernels set to 0
-    static constexpr int kMaxBuckets = 256, kCounterStride = 64;
+    // With them: [H], kCounterStride numbers apart, which the backward kernels set to 0 first thing.  (Of a type that nothing of the
+    // index has: behind a store that might have changed the index the compiler keeps it, and all that comes from it, in vector registers.)
+    unsigned long long* counters;
+    static constexpr int kMaxBuckets = 256, kCounterStride = 32;
 };
 
 // How the kernels cut long block rows (see attn_bf16_tiles.h), from what the host knows of a pattern.
