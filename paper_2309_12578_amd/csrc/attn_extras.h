@@ -70,31 +70,35 @@ __device__ __forceinline__ void key_draws(const ScoreDraws& d, int q, int k, uns
     }
 }
 
-// Two 16-bit draws or factors in a word.
-typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-
 // Lane l's word of lane l ^ 1, and of l ^ 2.
 __device__ __forceinline__ unsigned from_pair(unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true); }
 __device__ __forceinline__ unsigned from_other_pair(unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true); }
 
-// Factors 0 (dropped) and 1 of two draws; `below` = threshold - 1 in both halves (the threshold is not 0).
-__device__ __forceinline__ u16x2 kept(unsigned draws, u16x2 below) {
-    return __builtin_elementwise_min(__builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, draws), below), (u16x2){1, 1});
+// Factors 0 (dropped) and 1 of two draws; `below` = threshold - 1 in both halves (the threshold is not 0): min(draw - below,
+// 1), the difference cut off at 0.  (Written with vector types, these become comparisons and selections of single halves, five
+// instructions for what takes three here.)
+__device__ __forceinline__ unsigned kept(unsigned draws, unsigned below) {
+    unsigned f;
+    asm("v_pk_sub_u16 %0, %1, %2 clamp" : "=v"(f) : "v"(draws), "v"(below));
+    asm("v_pk_min_u16 %0, %1, 1 op_sel_hi:[1,0]" : "=v"(f) : "v"(f));
+    return f;
 }
-__device__ __forceinline__ u16x2 both_halves(unsigned v) { return (u16x2){(unsigned short)v, (unsigned short)v}; }
+__device__ __forceinline__ unsigned both_halves(unsigned v) { return v << 16 | (v & 0xffffu); }
 
-// Probabilities with the dropped ones 0: factors as bit patterns, so that nothing is rounded.
-__device__ __forceinline__ bf16x4 drop(bf16x4 p, const u16x2 (&k)[2]) {
-    struct Bits { u16x2 h[2]; } b = __builtin_bit_cast(Bits, p);
-    b.h[0] *= k[0];
-    b.h[1] *= k[1];
-    return __builtin_bit_cast(bf16x4, b);
+// Probabilities with the dropped ones 0: their bit patterns times the factors, so that nothing is rounded.
+__device__ __forceinline__ bf16x4 drop(bf16x4 p, const unsigned (&f)[2]) {
+    typedef unsigned Words __attribute__((ext_vector_type(2)));
+    const Words w = __builtin_bit_cast(Words, p);
+    unsigned lo = w[0], hi = w[1];
+    asm("v_pk_mul_lo_u16 %0, %1, %2" : "=v"(lo) : "v"(lo), "v"(f[0]));
+    asm("v_pk_mul_lo_u16 %0, %1, %2" : "=v"(hi) : "v"(hi), "v"(f[1]));
+    return __builtin_bit_cast(bf16x4, (Words){lo, hi});
 }
 
 // Query side: factors of this lane's query q = 16-row tile + r and the keys k0 + 16 kt + 4 g + i, two to a word, NKT even.  A call
 // has two queries' draws: lane r makes those of tile kt = 2 j + r % 2 for itself and its neighbour r ^ 1, which makes the other tile's.
 template <int NKT>
-__device__ __forceinline__ void query_factors(const ScoreDraws& d, int q, int k0, int g, u16x2 below, u16x2 (&f)[NKT][2]) {
+__device__ __forceinline__ void query_factors(const ScoreDraws& d, int q, int k0, int g, unsigned below, unsigned (&f)[NKT][2]) {
     const bool odd = q & 1;
     const unsigned mine = odd ? 0x07060302u : 0x05040100u, other = odd ? 0x05040100u : 0x07060302u;   // high or low halves of two words
 #pragma unroll

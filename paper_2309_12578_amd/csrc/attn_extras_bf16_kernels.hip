@@ -154,7 +154,7 @@ __global__ __launch_bounds__(BS * 4, BS == 64 ? 3 : 4) void attn_fwd_with_bf16_k
         }
     }
     [[maybe_unused]] const ScoreDraws draws(a.x, bh);
-    [[maybe_unused]] const u16x2 below = both_halves(a.x.threshold - 1u);
+    [[maybe_unused]] const unsigned below = both_halves(a.x.threshold - 1u);
     const float scale_log2 = a.scale_log2;
 
     float m = kLowest;   // what the row's exponentials are taken against, log2 units
@@ -168,7 +168,7 @@ __global__ __launch_bounds__(BS * 4, BS == 64 ? 3 : 4) void attn_fwd_with_bf16_k
     const int slice_at = 4 * g - wave * 16 - r + BS - 1;   // of key 4 g of the block
 
     auto step = [&](const KvTiles<BS>& cur, KvTiles<BS>& tgt, const float* bias_c, float* bias_n, int it) {
-        [[maybe_unused]] u16x2 factors[NKT][2];
+        [[maybe_unused]] unsigned factors[NKT][2];
         if constexpr (DROP) query_factors<NKT>(draws, qrow, jcur * BS, g, below, factors);
         meet(it == 0);
         if (it > 0) {

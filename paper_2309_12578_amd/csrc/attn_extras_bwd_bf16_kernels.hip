@@ -37,8 +37,8 @@ struct BwdWith {
 namespace {
 
 // dp of the kept elements, 0 of the dropped ones: element i of four whose factors are f.
-__device__ __forceinline__ float where_kept(float v, const u16x2 (&f)[2], int i) {
-    const int mask = __builtin_amdgcn_sbfe(__builtin_bit_cast(int, f[i >> 1]), 16 * (i & 1), 1);
+__device__ __forceinline__ float where_kept(float v, const unsigned (&f)[2], int i) {
+    const int mask = __builtin_amdgcn_sbfe((int)f[i >> 1], 16 * (i & 1), 1);
     return __builtin_bit_cast(float, __builtin_bit_cast(int, v) & mask);
 }
 
@@ -101,7 +101,7 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
     const size_t head = a.at.in_head(bh, L), out_head = a.at.out_head(bh, L), vec = (size_t)bh * L;
     const int length = length_of(a.x, bh, L);
     [[maybe_unused]] const ScoreDraws draws(a.x, bh);
-    [[maybe_unused]] const u16x2 below = both_halves(a.x.threshold - 1u);
+    [[maybe_unused]] const unsigned below = both_halves(a.x.threshold - 1u);
     const float scale_log2 = a.scale_log2, log2_keep = DROP ? log2f(a.x.keep_scale) : 0.f;
     // a row that keeps nothing, or past the sequence's end, has no probabilities
     auto reference = [&](float lse) { return lse == -INFINITY ? INFINITY : fmaf(lse, kLog2e, -log2_keep); };
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
         };
 
         auto step = [&](const bf16_t* kt, const bf16_t* vt, bf16_t* tk, bf16_t* tv, const float* bias_c, float* bias_n, int it) {
-            [[maybe_unused]] u16x2 factors[NT][2];
+            [[maybe_unused]] unsigned factors[NT][2];
             if constexpr (DROP) query_factors<NT>(draws, qrow, jcur * BS, g, below, factors);
             meet(it == 0);
             if (BIAS && by_distance && it > 0) write_slice(it - 1);
@@ -481,7 +481,7 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
         frags(0);
 #pragma unroll
         for (int pc = 0; pc < NT / 2; ++pc) {
-            [[maybe_unused]] u16x2 factors[2][2];
+            [[maybe_unused]] unsigned factors[2][2];
             if constexpr (DROP) {
                 unsigned u[4];
                 key_words(draws, icur * BS + 32 * pc, krow, g, u);
