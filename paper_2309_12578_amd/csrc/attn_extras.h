@@ -79,7 +79,7 @@ __device__ __forceinline__ unsigned from_other_pair(unsigned v) { return (unsign
 // instructions for what takes three here.)
 __device__ __forceinline__ unsigned kept(unsigned draws, unsigned below) {
     unsigned f;
-    asm("v_pk_sub_u16 %0, %1, %2 clamp" : "=v"(f) : "v"(draws), "v"(below));
+    asm("v_pk_sub_u16 %0, %1, %2 clamp" : "=v"(f) : "v"(draws), "s"(below));
     asm("v_pk_min_u16 %0, %1, 1 op_sel_hi:[1,0]" : "=v"(f) : "v"(f));
     return f;
 }

@@ -30,6 +30,13 @@ __device__ __forceinline__ void lds_meet() {
     asm volatile("" ::: "memory");
 }
 
+// The lane's number where addresses are made from it that are used there alone: the compiler makes them there, and does not keep them
+// in registers over the loop.
+__device__ __forceinline__ int once(int lane) {
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+
 // Entries of an ascending list whose block starts below `length`, of the n from list on.
 template <int BS>
 __device__ __forceinline__ int blocks_below(const int* list, int n, int length, int L, int lane) {
@@ -48,15 +55,16 @@ __device__ __forceinline__ int blocks_below(const int* list, int n, int length, 
 // requested a step before it is looked up.
 template <int BS, bool BIAS>
 struct BlockBias {
-    const uint8_t* from;   // map entry of this lane's distance in a block on the diagonal
+    const uint8_t* map;
     const float* tab;
-    int last;
+    int last, first;   // map entry of the smallest distance in a block on the diagonal
     bool mine;
-    __device__ __forceinline__ BlockBias(const Extras& x, const float* tab_, int L, int tid, int wave)
-        : from(nullptr), tab(tab_), last(x.n_buckets - 1), mine(BIAS && wave < BS / 32) {
-        if (BIAS) from = x.bucket_of + (L - BS + (tid < 2 * BS - 2 ? tid : 2 * BS - 2));
+    __device__ __forceinline__ BlockBias(const Extras& x, const float* tab_, int L, int wave)
+        : map(x.bucket_of), tab(tab_), last(x.n_buckets - 1), first(L - BS), mine(BIAS && wave < BS / 32) {}
+    // Key block - query block.  (The last lane has no distance.)
+    __device__ __forceinline__ unsigned request(int blocks_off, int tid) const {
+        return mine ? map[(unsigned)(first + blocks_off * BS + min(once(tid), 2 * BS - 2))] : 0u;
     }
-    __device__ __forceinline__ unsigned request(int blocks_off) const { return mine ? from[(ptrdiff_t)blocks_off * BS] : 0u; }   // key block - query block
     // Behind the biases, for either half of the distances: the bucket they are all of, or -1, and its bias.
     __device__ __forceinline__ void put(float* slice, unsigned bucket, int tid) const {
         if (mine) {

@@ -45,7 +45,7 @@ struct FwdWith {
 enum WithOrder { kInOrder, kDealtHeads, kLongestFirst };
 
 template <int BS, bool BIAS, bool DROP>
-__global__ __launch_bounds__(BS * 4, BS == 64 ? 3 : 4) void attn_fwd_with_bf16_kernel(FwdWith a) {
+__global__ __launch_bounds__(BS * 4, 4) void attn_fwd_with_bf16_kernel(FwdWith a) {
     constexpr int NKT = BS / 16;
     __shared__ __attribute__((aligned(16))) KvTiles<BS> sm0, sm1;
     __shared__ __attribute__((aligned(16))) float bias0[kSlice<BS>], bias1[kSlice<BS>];
@@ -86,8 +86,8 @@ __global__ __launch_bounds__(BS * 4, BS == 64 ? 3 : 4) void attn_fwd_with_bf16_k
     }
 
     const TableColumn<BS, BIAS> column(a.x, bh % a.x.H, tid);
-    const BlockBias<BS, BIAS> biases(a.x, tab, L, tid, wave);
-    unsigned bucket = biases.request(0);
+    const BlockBias<BS, BIAS> biases(a.x, tab, L, wave);
+    unsigned bucket = biases.request(0, tid);
     const size_t head = a.at.in_head(bh, L);
     const int row_len = a.at.in_row(), length = length_of(a.x, bh, L);
     const int qrow = I * BS + wave * 16 + r;
@@ -135,7 +135,7 @@ __global__ __launch_bounds__(BS * 4, BS == 64 ? 3 : 4) void attn_fwd_with_bf16_k
     column.put(tab, a.x, tid);
     if (pd < 0 && n > 0) {
         // no diagonal block in this row (piece): once everyone's early load has landed, load block 0 over it
-        if (BIAS) bucket = biases.request(jcur - I);
+        if (BIAS) bucket = biases.request(jcur - I, tid);
         if (!helper) {
             __builtin_amdgcn_s_waitcnt(kWaitVm0);
             __builtin_amdgcn_s_barrier();
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(BS * 4, BS == 64 ? 3 : 4) void attn_fwd_with_bf16_k
     }
     // the second block goes out as soon as its index is known; it is the youngest load from here on
     if (n > 0) {
-        const unsigned second = biases.request(jnext - I);
+        const unsigned second = biases.request(jnext - I, tid);
         issue(sm1, jnext);   // (a one-block row loads its block twice: keeps the wait below uniform)
         if constexpr (BIAS) {
             lds_meet();   // the table is there
@@ -168,15 +168,13 @@ __global__ __launch_bounds__(BS * 4, BS == 64 ? 3 : 4) void attn_fwd_with_bf16_k
     const int slice_at = 4 * g - wave * 16 - r + BS - 1;   // of key 4 g of the block
 
     auto step = [&](const KvTiles<BS>& cur, KvTiles<BS>& tgt, const float* bias_c, float* bias_n, int it) {
-        [[maybe_unused]] unsigned factors[NKT][2];
-        if constexpr (DROP) query_factors<NKT>(draws, qrow, jcur * BS, g, below, factors);
         meet(it == 0);
         if (it > 0) {
             if constexpr (BIAS) biases.put(bias_n, bucket, tid);
             if (it + 1 < n) issue(tgt, jnext);
         }
         const int jafter = later_col(it + 2);
-        if constexpr (BIAS) bucket = biases.request(jafter - I);
+        if constexpr (BIAS) bucket = biases.request(jafter - I, tid);
         // S^T tile kt: [key 16 kt + 4 g + i][query r]; all K fragments are requested up front
         bf16x8 kfr[NKT][2];
 #pragma unroll
@@ -200,19 +198,30 @@ __global__ __launch_bounds__(BS * 4, BS == 64 ? 3 : 4) void attn_fwd_with_bf16_k
 #pragma unroll
             for (int c = 0; c < 2; ++c) s[kt] = mma_d(s[kt], kfr[kt][c], qf[c]);
         if (jcur * BS + BS > length) {   // the block that the sequence ends in
+            const int left = length - jcur * BS - 4 * (once(lane) >> 4);
 #pragma unroll
             for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (jcur * BS + kt * 16 + 4 * g + i >= length) s[kt][i] = -INFINITY;
+                    if (kt * 16 + i >= left) s[kt][i] = -INFINITY;
         }
-        constexpr int NM = (BS / 32) * 4;
-        bf16x8 vop[NM];
+        // the generator's turn: the matrix cores have the scores to do
+        [[maybe_unused]] unsigned factors[NKT][2];
+        if constexpr (DROP) {
+            __builtin_amdgcn_sched_barrier(0);
+            query_factors<NKT>(draws, qrow, jcur * BS, g, below, factors);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // the transposed V operands of O^T += V^T P^T for 32 keys: requested here, they land while the exponentials are computed
+        bf16x8 vop[4];
+        auto request_v = [&](int pc) {
 #pragma unroll
-        for (int j = 0; j < NM; ++j) {
-            const int o = sl.tr(j & 3) + (j >> 2) * 32 * kD;
-            vop[j] = join(lds_read_tr(cur.v + o), lds_read_tr(cur.v + 16 * kD + o));
-        }
+            for (int j = 0; j < 4; ++j) {
+                const int o = sl.tr(j) + pc * 32 * kD;
+                vop[j] = join(lds_read_tr(cur.v + o), lds_read_tr(cur.v + 16 * kD + o));
+            }
+        };
+        request_v(0);
         __builtin_amdgcn_sched_barrier(0);
         bf16x4 pq[NKT];
         f32x4 sums;
@@ -250,9 +259,11 @@ __global__ __launch_bounds__(BS * 4, BS == 64 ? 3 : 4) void attn_fwd_with_bf16_k
             for (int kt = 0; kt < NKT; ++kt) pq[kt] = drop(pq[kt], factors[kt]);
         }
 #pragma unroll
-        for (int j = 0; j < NM; ++j) {
-            const int pc = j >> 2;
-            oacc[j & 3] = mma_d(oacc[j & 3], vop[j], join(pq[2 * pc], pq[2 * pc + 1]));   // O^T[d][query] += V^T P^T
+        for (int pc = 0; pc < BS / 32; ++pc) {
+            const bf16x8 p = join(pq[2 * pc], pq[2 * pc + 1]);
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt) oacc[dt] = mma_d(oacc[dt], vop[dt], p);   // O^T[d][query] += V^T P^T
+            if (pc + 1 < BS / 32) request_v(pc + 1);
         }
         jcur = jnext;
         jnext = jafter;
@@ -267,10 +278,11 @@ __global__ __launch_bounds__(BS * 4, BS == 64 ? 3 : 4) void attn_fwd_with_bf16_k
     __builtin_amdgcn_s_waitcnt(kWaitVm0);
 
     const auto& z = args_again<FwdWith>();
+    const int l = once(lane), qrow_l = I * BS + wave * 16 + (l & 15);
     if (cuts.count > 1) {   // a long row in pieces: see attn_bf16_tiles.h
         constexpr int kPart = 64 * 18;   // floats of a wave: nine pairs a lane, its accumulators, then reference and sum
         const size_t slot = (size_t)bh * z.cut.slots + cuts.slot;
-        float* const parts = z.cut.parts + (slot * (BS / 16) + wave) * kPart + lane * 2;
+        float* const parts = z.cut.parts + (slot * (BS / 16) + wave) * kPart + l * 2;
         float* const mine = parts + (size_t)piece * (BS / 16) * kPart;
 #pragma unroll
         for (int i = 0; i < 8; ++i) put_shared(mine + i * 128, oacc[i / 2][i % 2 * 2], oacc[i / 2][i % 2 * 2 + 1]);
@@ -297,13 +309,13 @@ __global__ __launch_bounds__(BS * 4, BS == 64 ? 3 : 4) void attn_fwd_with_bf16_k
         }
     }
     const float lsum = lacc[0];
-    const bool none = lsum == 0.f || qrow >= length;
+    const bool none = lsum == 0.f || qrow_l >= length;
     const float inv = none ? 0.f : (DROP ? z.x.keep_scale : 1.f) / lsum;
     // the stage that the last block did not use is free, see the plain kernel
     bf16_t* patch = ((n & 1) ? sm1.k : sm0.k) + wave * (16 * kD);
     const Rows at = {z.at.H, z.at.beside};
-    store_rows_coalesced(patch, z.O + at.out_head(bh, L) + (size_t)(I * BS + wave * 16) * at.out_row(), at.out_row(), oacc, inv, lane);
-    if (g == 0) z.LSE[(size_t)bh * L + qrow] = none ? -INFINITY : (m + log2f(lsum)) * kLn2;
+    store_rows_coalesced(patch, z.O + at.out_head(bh, z.L) + (size_t)(I * BS + wave * 16) * at.out_row(), at.out_row(), oacc, inv, l);
+    if (l < 16) z.LSE[(size_t)bh * z.L + qrow_l] = none ? -INFINITY : (m + log2f(lsum)) * kLn2;
 }
 
 static int resident(int bs) { return 256 * (bs == 64 ? 4 : 8); }

@@ -94,7 +94,7 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
         }
     }
     const TableColumn<BS, BIAS> column(a.x, bh % a.x.H, tid);
-    const BlockBias<BS, BIAS> biases(a.x, tab, L, tid, wave);
+    const BlockBias<BS, BIAS> biases(a.x, tab, L, wave);
     const SwzLane sl(r, g);
     const int in_row = a.at.in_row(), out_row = a.at.out_row();   // elements between rows of Q, K, V and of O, dO
     const TileLoadLane tl(wave, lane, in_row);
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
         const auto& b = args_again<BwdWith>();   // this side's
         const int I = idx;
         const int qrow = I * BS + wave * 16 + r;
-        unsigned bucket = biases.request(0);
+        unsigned bucket = biases.request(0, tid);
         const bf16_t *const Kh = b.K + head, *const Vh = b.V + head;
         auto issue = [&](bf16_t* kt, bf16_t* vt, int J) {
             const unsigned range = tile_range<BS>(J * BS, length, in_row);
@@ -170,7 +170,7 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
         column.put(tab, a.x, tid);
         if (pd < 0 && n > 0) {
             // no diagonal block in this row (piece): once everyone's early load has landed, load block 0 over it
-            if (BIAS) bucket = biases.request(jcur - I);
+            if (BIAS) bucket = biases.request(jcur - I, tid);
             if (!helper) {
                 __builtin_amdgcn_s_waitcnt(kWaitVm0);
                 __builtin_amdgcn_s_barrier();
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
                 (my_slices - tid)[(size_t)e * (2 * BS) + 2 * BS - 1] = __builtin_bit_cast(float, kNoSlice);
         }
         if (n > 0) {
-            const unsigned second = biases.request(jnext - I);
+            const unsigned second = biases.request(jnext - I, tid);
             issue(ta1, tb1, jnext);   // the youngest load at step 0 (a one-block row loads its block twice)
             lds_meet();               // the table is there, the places are clear
             if constexpr (BIAS) {
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
                 if (it + 1 < n) issue(tk, tv, jnext);
             }
             const int jafter = later_col(it + 2);
-            if constexpr (BIAS) bucket = biases.request(jafter - I);
+            if constexpr (BIAS) bucket = biases.request(jafter - I, tid);
             f32x4 s[NT];
             float bias = 0.f;
             const bool one = !BIAS || one_bucket<BS>(bias_c, bias);
@@ -405,8 +405,8 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
     if (n > 0) {
         icur = row_at(0);
         inext = row_at(1);
-        const unsigned first = biases.request(J - icur);
-        bucket = biases.request(J - inext);
+        const unsigned first = biases.request(J - icur, tid);
+        bucket = biases.request(J - inext, tid);
         load_q(ta0, icur);
         load_do(tb0, icur);
         load_o(tc0, lse0, icur);
@@ -446,7 +446,7 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
                 load_o(no, nlse, inext);
             }
         }
-        if constexpr (BIAS) bucket = biases.request(J - row_at(it + 2));
+        if constexpr (BIAS) bucket = biases.request(J - row_at(it + 2), tid);
         // delta of the 16 query rows 16 wave .. + 15: the diagonal of dO O^T; stored negated (and divided by c)
         {
             f32x4 dd = f32x4{0.f, 0.f, 0.f, 0.f};
