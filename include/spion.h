@@ -216,10 +216,8 @@ typedef struct {
     uint32_t reserved;         /* must be 0 */
 } spion_attn_extras;
 
-/* Bytes of device scratch of the two calls below; (size_t)-1 if the parameters are unsupported.  table_grad: whether the backward
- * call gets a dtable. */
-size_t spion_attn_with_workspace_bytes(const spion_attn_params *p, const spion_attn_extras *x, int32_t nnzb, int32_t is_bwd,
-                                       int32_t table_grad);
+/* Bytes of device scratch of the two calls below; (size_t)-1 if the parameters are unsupported. */
+size_t spion_attn_with_workspace_bytes(const spion_attn_params *p, const spion_attn_extras *x, int32_t nnzb, int32_t is_bwd);
 /* As spion_attn_fwd; flags must be 0.  x, p: HOST pointers. */
 int spion_attn_fwd_with(const void *Q, const void *K, const void *V, void *O, float *LSE, const int32_t *row_ptr,
                         const int32_t *col_idx, int32_t nnzb, const spion_attn_params *p, const spion_attn_extras *x,

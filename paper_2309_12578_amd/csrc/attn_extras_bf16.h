@@ -68,6 +68,7 @@ struct BlockBias {
     // Behind the biases, for either half of the distances: the bucket they are all of, or -1, and its bias.
     __device__ __forceinline__ void put(float* slice, unsigned bucket, int tid) const {
         if (mine) {
+            tid = once(tid);
             const int b = min((int)bucket, last);
             const float v = tab[b];
             slice[tid] = v;
@@ -131,6 +132,14 @@ struct Rows {
         return beside ? ((size_t)(bh / H) * L * H + bh % H) * kD : (size_t)bh * L * kD;
     }
 };
+
+// What the end of a row's piece needs of its cut, in one register: at most RowCut::kSlots each.
+struct CutRow {
+    int count, slot, piece;
+};
+static_assert(RowCut::kSlots < 1024, "ten bits each");
+__device__ __forceinline__ int pack_cut(const RowPieces& cuts, int piece) { return cuts.count | cuts.slot << 10 | piece << 20; }
+__device__ __forceinline__ CutRow unpack_cut(int packed) { return {packed & 1023, packed >> 10 & 1023, packed >> 20}; }
 
 // Bytes of a tile that starts at row `row0` up to the sequence's end.
 template <int BS>

@@ -45,7 +45,7 @@ struct FwdWith {
 enum WithOrder { kInOrder, kDealtHeads, kLongestFirst };
 
 template <int BS, bool BIAS, bool DROP>
-__global__ __launch_bounds__(BS * 4, 4) void attn_fwd_with_bf16_kernel(FwdWith a) {
+__global__ __launch_bounds__(BS * 4, BS == 32 && DROP ? 5 : 4) void attn_fwd_with_bf16_kernel(FwdWith a) {
     constexpr int NKT = BS / 16;
     __shared__ __attribute__((aligned(16))) KvTiles<BS> sm0, sm1;
     __shared__ __attribute__((aligned(16))) float bias0[kSlice<BS>], bias1[kSlice<BS>];
@@ -144,13 +144,14 @@ __global__ __launch_bounds__(BS * 4, 4) void attn_fwd_with_bf16_kernel(FwdWith a
         issue(sm0, jcur);
     }
     // the second block goes out as soon as its index is known; it is the youngest load from here on
+    const int packed = pack_cut(cuts, piece);   // one register over the loop
     if (n > 0) {
-        const unsigned second = biases.request(jnext - I, tid);
+        const unsigned first = bucket;
+        bucket = biases.request(jnext - I, tid);
         issue(sm1, jnext);   // (a one-block row loads its block twice: keeps the wait below uniform)
         if constexpr (BIAS) {
             lds_meet();   // the table is there
-            biases.put(bias0, bucket, tid);
-            biases.put(bias1, second, tid);
+            biases.put(bias0, first, tid);
         }
     }
     [[maybe_unused]] const ScoreDraws draws(a.x, bh);
@@ -169,10 +170,8 @@ __global__ __launch_bounds__(BS * 4, 4) void attn_fwd_with_bf16_kernel(FwdWith a
 
     auto step = [&](const KvTiles<BS>& cur, KvTiles<BS>& tgt, const float* bias_c, float* bias_n, int it) {
         meet(it == 0);
-        if (it > 0) {
-            if constexpr (BIAS) biases.put(bias_n, bucket, tid);
-            if (it + 1 < n) issue(tgt, jnext);
-        }
+        if constexpr (BIAS) biases.put(bias_n, bucket, tid);
+        if (it > 0 && it + 1 < n) issue(tgt, jnext);
         const int jafter = later_col(it + 2);
         if constexpr (BIAS) bucket = biases.request(jafter - I, tid);
         // S^T tile kt: [key 16 kt + 4 g + i][query r]; all K fragments are requested up front
@@ -279,20 +278,21 @@ __global__ __launch_bounds__(BS * 4, 4) void attn_fwd_with_bf16_kernel(FwdWith a
 
     const auto& z = args_again<FwdWith>();
     const int l = once(lane), qrow_l = I * BS + wave * 16 + (l & 15);
-    if (cuts.count > 1) {   // a long row in pieces: see attn_bf16_tiles.h
+    const CutRow mine_of = unpack_cut(packed);
+    if (mine_of.count > 1) {   // a long row in pieces: see attn_bf16_tiles.h
         constexpr int kPart = 64 * 18;   // floats of a wave: nine pairs a lane, its accumulators, then reference and sum
-        const size_t slot = (size_t)bh * z.cut.slots + cuts.slot;
+        const size_t slot = (size_t)bh * z.cut.slots + mine_of.slot;
         float* const parts = z.cut.parts + (slot * (BS / 16) + wave) * kPart + l * 2;
-        float* const mine = parts + (size_t)piece * (BS / 16) * kPart;
+        float* const mine = parts + (size_t)mine_of.piece * (BS / 16) * kPart;
 #pragma unroll
         for (int i = 0; i < 8; ++i) put_shared(mine + i * 128, oacc[i / 2][i % 2 * 2], oacc[i / 2][i % 2 * 2 + 1]);
         put_shared(mine + 1024, m, lacc[0]);
-        if (!last_to_arrive(z.cut.counters + slot, z.cut.tag, cuts.count, reinterpret_cast<int*>(sm0.v))) return;
+        if (!last_to_arrive(z.cut.counters + slot, z.cut.tag, mine_of.count, reinterpret_cast<int*>(sm0.v))) return;
         m = -INFINITY;
         lacc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt) oacc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int c = 0; c < cuts.count; ++c) {
+        for (int c = 0; c < mine_of.count; ++c) {
             const float* const part = parts + (size_t)c * (BS / 16) * kPart;
             float2 v[9];
 #pragma unroll

@@ -58,7 +58,7 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int L = a.L, nb = a.nb;
-    if (BIAS && blockIdx.x == 0 && a.x.counters)
+    if (BIAS && blockIdx.x == 0)
         for (int h = tid; h < a.x.H; h += BS * 4) a.x.counters[h * Extras::kCounterStride] = 0u;
 
     // which workgroup am I
@@ -183,20 +183,22 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
         constexpr int kPlaces = 16 * NT + 32;
         float* const places = reinterpret_cast<float*>(tc0) + wave * (4 * kPlaces);
         float* const sums = reinterpret_cast<float*>(tc1);   // [step % 2][wave][2 BS]
-        const bool by_distance = BIAS && b.x.slices != nullptr;
-        float* const my_slices = by_distance ? b.x.slices + ((size_t)bh * b.nnzb + jb) * (2 * BS) + tid : nullptr;   // of this row (piece)
-        if (by_distance) {
+        float* const my_slices = BIAS ? b.x.slices + ((size_t)bh * b.nnzb + jb) * (2 * BS) + tid : nullptr;   // of this row (piece)
+        if constexpr (BIAS) {
             for (int i = tid; i < NT * 4 * kPlaces; i += BS * 4) reinterpret_cast<float*>(tc0)[i] = 0.f;
             for (int e = n + tid; e < n_all; e += BS * 4)   // what is not computed
                 (my_slices - tid)[(size_t)e * (2 * BS) + 2 * BS - 1] = __builtin_bit_cast(float, kNoSlice);
         }
+        const int packed = pack_cut(cuts, piece);   // one register over the loop
+        int pd_v = pd;   // (scalar registers are short)
+        asm volatile("" : "+v"(pd_v));
         if (n > 0) {
-            const unsigned second = biases.request(jnext - I, tid);
+            const unsigned first = bucket;
+            bucket = biases.request(jnext - I, tid);
             issue(ta1, tb1, jnext);   // the youngest load at step 0 (a one-block row loads its block twice)
-            lds_meet();               // the table is there, the places are clear
             if constexpr (BIAS) {
-                biases.put(bias0, bucket, tid);
-                biases.put(bias1, second, tid);
+                lds_meet();   // the table is there, the places are clear
+                biases.put(bias0, first, tid);
             }
         }
         f32x4 dq[4];
@@ -211,19 +213,15 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
 #pragma unroll
                 for (int w = 1; w < NT; ++w) v += from[w * (2 * BS)];
                 if (tid == 2 * BS - 1) v = from[0];
-                my_slices[(size_t)(walk_index(t, pd) * (2 * BS))] = v;
+                my_slices[(size_t)(walk_index(t, pd_v) * (2 * BS))] = v;
             }
         };
 
         auto step = [&](const bf16_t* kt, const bf16_t* vt, bf16_t* tk, bf16_t* tv, const float* bias_c, float* bias_n, int it) {
-            [[maybe_unused]] unsigned factors[NT][2];
-            if constexpr (DROP) query_factors<NT>(draws, qrow, jcur * BS, g, below, factors);
             meet(it == 0);
-            if (BIAS && by_distance && it > 0) write_slice(it - 1);
-            if (it > 0) {
-                    if constexpr (BIAS) biases.put(bias_n, bucket, tid);
-                if (it + 1 < n) issue(tk, tv, jnext);
-            }
+            if (BIAS && it > 0) write_slice(it - 1);
+            if constexpr (BIAS) biases.put(bias_n, bucket, tid);
+            if (it > 0 && it + 1 < n) issue(tk, tv, jnext);
             const int jafter = later_col(it + 2);
             if constexpr (BIAS) bucket = biases.request(jafter - I, tid);
             f32x4 s[NT];
@@ -257,19 +255,30 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
                 }
             }
             if (jcur * BS + BS > length) {   // the block that the sequence ends in
+                const int left = length - jcur * BS - 4 * (once(lane) >> 4);
 #pragma unroll
                 for (int kt16 = 0; kt16 < NT; ++kt16)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (jcur * BS + kt16 * 16 + 4 * g + i >= length) s[kt16][i] = -INFINITY;
+                        if (kt16 * 16 + i >= left) s[kt16][i] = -INFINITY;
             }
-            constexpr int NM = (BS / 32) * 4;
-            bf16x8 kop[NM];
+            // the generator's turn: the matrix cores have the scores to do
+            [[maybe_unused]] unsigned factors[NT][2];
+            if constexpr (DROP) {
+                __builtin_amdgcn_sched_barrier(0);
+                query_factors<NT>(draws, qrow, jcur * BS, g, below, factors);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            // the transposed K operands of dQ^T += K^T dS^T for 32 keys: they land while the exponentials are computed
+            bf16x8 kop[4];
+            auto request_k = [&](int pc) {
 #pragma unroll
-            for (int j = 0; j < NM; ++j) {
-                const int o = sl.tr(j & 3) + (j >> 2) * 32 * kD;
-                kop[j] = join(lds_read_tr(kt + o), lds_read_tr(kt + 16 * kD + o));
-            }
+                for (int j = 0; j < 4; ++j) {
+                    const int o = sl.tr(j) + pc * 32 * kD;
+                    kop[j] = join(lds_read_tr(kt + o), lds_read_tr(kt + 16 * kD + o));
+                }
+            };
+            request_k(0);
             __builtin_amdgcn_sched_barrier(0);
             bf16x4 dsq[NT];
 #pragma unroll
@@ -282,13 +291,14 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
                 dsq[kt16] = to_quad<bf16_t>(s[kt16]);
             }
 #pragma unroll
-            for (int j = 0; j < NM; ++j) {
-                const int pc = j >> 2;
-                dq[j & 3] = mma_d(dq[j & 3], kop[j], join(dsq[2 * pc], dsq[2 * pc + 1]));   // dQ^T[d][query] += K^T dS^T
+            for (int pc = 0; pc < BS / 32; ++pc) {
+                const bf16x8 ds = join(dsq[2 * pc], dsq[2 * pc + 1]);
+#pragma unroll
+                for (int dt = 0; dt < 4; ++dt) dq[dt] = mma_d(dq[dt], kop[dt], ds);   // dQ^T[d][query] += K^T dS^T
+                if (pc + 1 < BS / 32) request_k(pc + 1);
             }
-            if (BIAS && by_distance) {
-                int l = lane;   // addresses that only this part uses are made here
-                asm volatile("" : "+v"(l));
+            if constexpr (BIAS) {
+                const int l = once(lane);
                 float* const mine = sums + ((it & 1) * NT + wave) * (2 * BS) + l;   // numbers l, l + 64, .. of the block's 2 BS
                 const float place = l == 63 ? __int_as_float((jcur - I) * BS) : 0.f;   // for the last number
                 if (one) {   // of one bucket: it does not matter which distance has what
@@ -335,22 +345,23 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
         }
         // an empty row never waited for its early load: it must land before this workgroup's LDS is freed
         __builtin_amdgcn_s_waitcnt(kWaitVm0);
-        if (BIAS && by_distance && n > 0) {
+        if (BIAS && n > 0) {
             lds_meet();
             write_slice(n - 1);
         }
         const auto& z = args_again<BwdWith>();
-        if (cuts.count > 1) {   // a long row in pieces: see attn_bf16_tiles.h
+        const CutRow mine_of = unpack_cut(packed);
+        if (mine_of.count > 1) {   // a long row in pieces: see attn_bf16_tiles.h
             constexpr int kPart = 8 * 128;   // eight pairs a lane
-            const size_t first_slot = (size_t)bh * z.cut.slots + cuts.slot;
+            const size_t first_slot = (size_t)bh * z.cut.slots + mine_of.slot;
             float* const parts = z.cut.parts + (first_slot * NT + wave) * kPart + lane * 2;
-            float* const mine = parts + (size_t)piece * NT * kPart;
+            float* const mine = parts + (size_t)mine_of.piece * NT * kPart;
 #pragma unroll
             for (int i = 0; i < 8; ++i) put_shared(mine + i * 128, dq[i / 2][i % 2 * 2], dq[i / 2][i % 2 * 2 + 1]);
-            if (!last_to_arrive(z.cut.counters + first_slot, z.cut.tag, cuts.count, reinterpret_cast<int*>(lse0))) return;
+            if (!last_to_arrive(z.cut.counters + first_slot, z.cut.tag, mine_of.count, reinterpret_cast<int*>(lse0))) return;
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt) dq[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-            for (int c = 0; c < cuts.count; ++c) {
+            for (int c = 0; c < mine_of.count; ++c) {
                 float2 v[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] = get_shared(parts + (size_t)c * NT * kPart + i * 128);
@@ -483,6 +494,7 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
         for (int pc = 0; pc < NT / 2; ++pc) {
             [[maybe_unused]] unsigned factors[2][2];
             if constexpr (DROP) {
+                __builtin_amdgcn_sched_barrier(0);
                 unsigned u[4];
                 key_words(draws, icur * BS + 32 * pc, krow, g, u);
 #pragma unroll
@@ -490,6 +502,7 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
                     factors[h][0] = kept(u[2 * h], below);
                     factors[h][1] = kept(u[2 * h + 1], below);
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
             bf16x4 pq[2], dsq[2];
 #pragma unroll

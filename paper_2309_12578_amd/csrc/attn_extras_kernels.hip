@@ -474,12 +474,12 @@ namespace {
 struct WithWorkspace {
     int tile, parts;                           // rows of a tile that has its own slice; workgroups per head
     size_t slices, partial, counters, total;   // offsets, and the end
-    WithWorkspace(const AttnShape& s, bool table_grad, int n_buckets, int H, int nnzb) {
+    WithWorkspace(const AttnShape& s, int n_buckets, int H, int nnzb) {   // n_buckets 0: no table
         auto up = [](size_t n) { return (n + 255) / 256 * 256; };
         const bool tiled = s.is_bf16 && s.bs > 16;
         tile = tiled ? s.bs : 16;
         slices = tiled ? up(attn_bwd_workspace(s, nnzb).with_rows) : 0;
-        if (!table_grad) {
+        if (n_buckets == 0) {
             total = slices;
             return;
         }
@@ -534,9 +534,9 @@ hipError_t bwd_with(const AttnShape& s, const Extras& x, const void* Q, const vo
 
 }  // namespace
 
-size_t attn_with_workspace_bytes(const AttnShape& s, bool table_grad, int n_buckets, int H, int nnzb, bool is_bwd) {
+size_t attn_with_workspace_bytes(const AttnShape& s, int n_buckets, int H, int nnzb, bool is_bwd) {
     if (!is_bwd) return s.is_bf16 && s.bs > 16 ? RowCut(s, nnzb).room_bytes(s.BH, s.bs) : 0;
-    return WithWorkspace(s, table_grad, n_buckets, H, nnzb).total;
+    return WithWorkspace(s, n_buckets, H, nnzb).total;
 }
 
 #define SPION_DISPATCH(FN, ...)                                                   \
@@ -566,10 +566,10 @@ hipError_t launch_attn_bwd_with(const AttnShape& s, const Extras& extras, const 
                                 const void* dO, const float* LSE, void* dQ, void* dK, void* dV, void* dtable, const int* row_ptr,
                                 const int* col_idx, const int* col_ptr, const int* row_idx, int nnzb, void* workspace, hipStream_t st) {
     Extras x = extras;
-    const WithWorkspace ws(s, dtable != nullptr, x.n_buckets, x.H, nnzb);
+    const WithWorkspace ws(s, x.n_buckets, x.H, nnzb);
     char* const base = static_cast<char*>(workspace);
-    x.slices = dtable ? reinterpret_cast<float*>(base + ws.slices) : nullptr;
-    x.counters = dtable ? reinterpret_cast<unsigned long long*>(base + ws.counters) : nullptr;
+    x.slices = x.table ? reinterpret_cast<float*>(base + ws.slices) : nullptr;
+    x.counters = x.table ? reinterpret_cast<unsigned long long*>(base + ws.counters) : nullptr;
     hipError_t e = launch_bwd(s, x, Q, K, V, O, dO, LSE, dQ, dK, dV, row_ptr, col_idx, col_ptr, row_idx, nnzb, workspace, st);
     if (e != hipSuccess || !dtable) return e;
     const long long tiles = (long long)nnzb * (s.bs / ws.tile) * (s.bs / ws.tile);

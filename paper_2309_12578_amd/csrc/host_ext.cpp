@@ -787,8 +787,8 @@ struct AttentionExtras {
     }
 };
 
-at::Tensor with_workspace(const spion_attn_params& p, const spion_attn_extras& x, const Index& ix, bool is_bwd, bool table_grad, const at::Tensor& like) {
-    const size_t n = spion_attn_with_workspace_bytes(&p, &x, ix.nnzb, is_bwd, table_grad);
+at::Tensor with_workspace(const spion_attn_params& p, const spion_attn_extras& x, const Index& ix, bool is_bwd, const at::Tensor& like) {
+    const size_t n = spion_attn_with_workspace_bytes(&p, &x, ix.nnzb, is_bwd);
     return new_bytes(n == (size_t)-1 ? 0 : n, like);   // what is unsupported the call itself tells
 }
 
@@ -820,7 +820,7 @@ struct AttentionWithBackward : public torch::autograd::Node {
             const bool table_grad = T.defined() && task_should_compute_output(3);
             for (int i = 0; i < 3; ++i) out[i] = new_like(Q);
             if (table_grad) out[3] = new_like(T);
-            const at::Tensor ws = with_workspace(p, x, ix, true, table_grad, Q);
+            const at::Tensor ws = with_workspace(p, x, ix, true, Q);
             const int rc = spion_attn_bwd_with(
                 device_ptr(Q), device_ptr(K), device_ptr(V), device_ptr(O), device_ptr(g), (const float*)device_ptr(stat), device_ptr(out[0]),
                 device_ptr(out[1]), device_ptr(out[2]), table_grad ? device_ptr(out[3]) : nullptr, (const int32_t*)device_ptr(ix.row_ptr),
@@ -892,7 +892,7 @@ PyObject* py_sparse_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) 
             if (drop && grad) used = new_longs(2, qc);
             spion_attn_extras x = extras.params(tc, rng);
             if (used.defined()) x.rng_used = (int64_t*)used.data_ptr();
-            const at::Tensor ws = with_workspace(p, x, ix, false, false, qc);
+            const at::Tensor ws = with_workspace(p, x, ix, false, qc);
             const int rc = spion_attn_fwd_with(device_ptr(qc), device_ptr(kc), device_ptr(vc), device_ptr(o), (float*)device_ptr(lse),
                                                (const int32_t*)device_ptr(ix.row_ptr), (const int32_t*)device_ptr(ix.col_idx), ix.nnzb, &p, &x,
                                                device_ptr(ws), (size_t)ws.nbytes(), current_stream());

@@ -526,11 +526,10 @@ static int take_extras(const spion_attn_params* p, const spion_attn_extras* x, i
     return SPION_OK;
 }
 
-size_t spion_attn_with_workspace_bytes(const spion_attn_params* p, const spion_attn_extras* x, int32_t nnzb, int32_t is_bwd,
-                                       int32_t table_grad) {
+size_t spion_attn_with_workspace_bytes(const spion_attn_params* p, const spion_attn_extras* x, int32_t nnzb, int32_t is_bwd) {
     spion::Extras extras;
     if (!p || !x || take_extras(p, x, nnzb, extras) != SPION_OK) return (size_t)-1;
-    return spion::attn_with_workspace_bytes(make_shape(p), table_grad && extras.table, extras.n_buckets, p->H, nnzb, is_bwd != 0);
+    return spion::attn_with_workspace_bytes(make_shape(p), extras.n_buckets, p->H, nnzb, is_bwd != 0);
 }
 
 int spion_attn_fwd_with(const void* Q, const void* K, const void* V, void* O, float* LSE, const int32_t* row_ptr,
@@ -542,7 +541,7 @@ int spion_attn_fwd_with(const void* Q, const void* K, const void* V, void* O, fl
     if (rc != SPION_OK) return rc;
     if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)O) % 16 != 0) return SPION_ERR_PARAM;
     spion::AttnShape s = make_shape(p);
-    const size_t need = spion::attn_with_workspace_bytes(s, false, extras.n_buckets, p->H, nnzb, false);
+    const size_t need = spion::attn_with_workspace_bytes(s, extras.n_buckets, p->H, nnzb, false);
     if (need && (!workspace || (uintptr_t)workspace % kAlign != 0 || workspace_bytes < need)) return SPION_ERR_WORKSPACE;
     if (need) s.fwd_room = workspace;
     return spion::launch_attn_fwd_with(s, extras, Q, K, V, O, LSE, row_ptr, col_idx, nnzb, static_cast<hipStream_t>(hip_stream)) ==
@@ -563,7 +562,7 @@ int spion_attn_bwd_with(const void* Q, const void* K, const void* V, const void*
         return SPION_ERR_PARAM;
     if (!spion::attn_bwd_grids_fit(p->B * p->H, p->block, p->L / p->block, nnzb)) return SPION_ERR_SHAPE;
     const spion::AttnShape s = make_shape(p);
-    const size_t need = spion::attn_with_workspace_bytes(s, dtable != nullptr, extras.n_buckets, p->H, nnzb, true);
+    const size_t need = spion::attn_with_workspace_bytes(s, extras.n_buckets, p->H, nnzb, true);
     if (need && (!workspace || (uintptr_t)workspace % kAlign != 0 || workspace_bytes < need)) return SPION_ERR_WORKSPACE;
     return spion::launch_attn_bwd_with(s, extras, Q, K, V, O, dO, LSE, dQ, dK, dV, dtable, row_ptr, col_idx, col_ptr, row_idx, nnzb,
                                        workspace, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? SPION_OK : SPION_ERR_HIP;

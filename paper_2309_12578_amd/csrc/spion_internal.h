@@ -60,7 +60,7 @@ struct Extras {
     float inv_scale;                  // 1 / score scale
     unsigned threshold, stream;       // draws below are dropped; 0: no dropout
     float keep_scale;                 // 65536 / (65536 - threshold)
-    float* slices;                    // backward: sums of dS over diagonals, or nullptr: no gradient of the table
+    float* slices;                    // backward, with a table: sums of dS over diagonals
     // With them: [H], kCounterStride numbers apart, which the backward kernels set to 0 first thing.  (Of a type that nothing of the
     // index has: behind a store that might have changed the index the compiler keeps it, and all that comes from it, in vector registers.)
     unsigned long long* counters;
@@ -135,7 +135,7 @@ template <int BS>
 hipError_t bwd_with_bf16(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, const void* O, const void* dO,
                          const float* LSE, void* dQ, void* dK, void* dV, const int* row_ptr, const int* col_idx, const int* col_ptr,
                          const int* row_idx, int nnzb, void* workspace, hipStream_t st);
-size_t attn_with_workspace_bytes(const AttnShape& s, bool table_grad, int n_buckets, int H, int nnzb, bool is_bwd);
+size_t attn_with_workspace_bytes(const AttnShape& s, int n_buckets, int H, int nnzb, bool is_bwd);
 
 // dropout_kernels.hip: y = residual + dropout(x) (residual nullptr: without), the dense bias and its table's gradient
 hipError_t launch_dropout(const void* x, const void* residual, void* y, long long n, const long long* rng, long long* rng_used, unsigned stream,
