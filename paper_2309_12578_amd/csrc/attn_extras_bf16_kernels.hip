@@ -154,7 +154,7 @@ __global__ __launch_bounds__(BS * 4, BS == 32 && DROP ? 5 : 4) void attn_fwd_wit
             biases.put(bias0, first, tid);
         }
     }
-    [[maybe_unused]] const ScoreDraws draws(a.x, bh);
+    [[maybe_unused]] const ScoreDraws draws(a.x.rng, a.x.stream, bh);
     [[maybe_unused]] const unsigned below = both_halves(a.x.threshold - 1u);
     const float scale_log2 = a.scale_log2;
 

@@ -45,7 +45,7 @@ __device__ __forceinline__ float where_kept(float v, const unsigned (&f)[2], int
 }  // namespace
 
 template <int BS, bool BIAS, bool DROP>
-__global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_with_bf16_kernel(BwdWith a) {
+__global__ __launch_bounds__(BS * 4, 3) void attn_bwd_with_bf16_kernel(BwdWith a) {
     constexpr int NT = BS / 16;   // 16-row tiles per block = waves per workgroup
     // Query side: {ta, tb} hold {K, V} of a block, two stages; tc0 and tc1 what adds up diagonals.  Key side: {ta, tb, tc} hold
     // {Q, dO, O} of a block row, two stages.
@@ -96,25 +96,26 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
     const TableColumn<BS, BIAS> column(a.x, bh % a.x.H, tid);
     const BlockBias<BS, BIAS> biases(a.x, tab, L, wave);
     const SwzLane sl(r, g);
-    const int in_row = a.at.in_row(), out_row = a.at.out_row();   // elements between rows of Q, K, V and of O, dO
-    const TileLoadLane tl(wave, lane, in_row);
-    const size_t head = a.at.in_head(bh, L), out_head = a.at.out_head(bh, L), vec = (size_t)bh * L;
     const int length = length_of(a.x, bh, L);
-    [[maybe_unused]] const ScoreDraws draws(a.x, bh);
-    [[maybe_unused]] const unsigned below = both_halves(a.x.threshold - 1u);
-    const float scale_log2 = a.scale_log2, log2_keep = DROP ? log2f(a.x.keep_scale) : 0.f;
-    // a row that keeps nothing, or past the sequence's end, has no probabilities
-    auto reference = [&](float lse) { return lse == -INFINITY ? INFINITY : fmaf(lse, kLog2e, -log2_keep); };
+    // what a row's exponentials are taken against; a row that keeps nothing, or past the sequence's end, has no probabilities
+    auto reference = [](float lse, float log2_keep) { return lse == -INFINITY ? INFINITY : fmaf(lse, kLog2e, -log2_keep); };
 
     if (!key_side) {
         // ========================================================================================
         // query side: block row I
         // ========================================================================================
         const auto& b = args_again<BwdWith>();   // this side's
+        const Rows at = {b.at.H, b.at.beside};
+        const int in_row = at.in_row(), out_row = at.out_row();   // elements between rows of Q, K, V and of O, dO
+        const size_t head = at.in_head(bh, L), out_head = at.out_head(bh, L), vec = (size_t)bh * L;
+        [[maybe_unused]] const ScoreDraws draws(b.x.rng, b.x.stream, bh);
+        [[maybe_unused]] const unsigned below = both_halves(b.x.threshold - 1u);
+        const float scale_log2 = b.scale_log2, log2_keep = DROP ? log2f(b.x.keep_scale) : 0.f;
         const int I = idx;
         const int qrow = I * BS + wave * 16 + r;
         unsigned bucket = biases.request(0, tid);
         const bf16_t *const Kh = b.K + head, *const Vh = b.V + head;
+        const TileLoadLane tl(wave, lane, in_row);
         auto issue = [&](bf16_t* kt, bf16_t* vt, int J) {
             const unsigned range = tile_range<BS>(J * BS, length, in_row);
             tile_load_async(Kh + (size_t)J * BS * in_row, kt, wave, tl, range);
@@ -133,7 +134,7 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
                 of[c] = *reinterpret_cast<const bf16x8*>(b.O + out);
                 if (qrow >= length) qf[c] = dof[c] = of[c] = bf16x8{};
             }
-            if (qrow < length) lse2 = reference(b.LSE[vec + qrow]);
+            if (qrow < length) lse2 = reference(b.LSE[vec + qrow], log2_keep);
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -161,9 +162,11 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
         };
         int walk_v = 0;   // 64 blocks of the walk, one per lane
         if (n > 2) walk_v = cols[walk_index(lane < last ? lane : last, pd)];
+        int pd_v = pd, jb_v = jb;   // (scalar registers are short)
+        asm volatile("" : "+v"(pd_v), "+v"(jb_v));
         auto later_col = [&](int t) {   // t >= 2, one after the other
             const int u = t < last ? t : last;
-            if (u >= 64 && (u & 63) == 0) walk_v = args_again<BwdWith>().col_idx[jb + walk_index(u + lane < last ? u + lane : last, pd)];
+            if (u >= 64 && (u & 63) == 0) walk_v = args_again<BwdWith>().col_idx[jb_v + walk_index(u + lane < last ? u + lane : last, pd_v)];
             return __builtin_amdgcn_readlane(walk_v, u & 63);
         };
         int jcur = __builtin_amdgcn_readfirstlane(n > 0 ? col_at(0) : I), jnext = __builtin_amdgcn_readfirstlane(n > 0 ? col_at(1) : I);
@@ -190,8 +193,6 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
                 (my_slices - tid)[(size_t)e * (2 * BS) + 2 * BS - 1] = __builtin_bit_cast(float, kNoSlice);
         }
         const int packed = pack_cut(cuts, piece);   // one register over the loop
-        int pd_v = pd;   // (scalar registers are short)
-        asm volatile("" : "+v"(pd_v));
         if (n > 0) {
             const unsigned first = bucket;
             bucket = biases.request(jnext - I, tid);
@@ -350,11 +351,12 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
             write_slice(n - 1);
         }
         const auto& z = args_again<BwdWith>();
+        const int l = once(lane);
         const CutRow mine_of = unpack_cut(packed);
         if (mine_of.count > 1) {   // a long row in pieces: see attn_bf16_tiles.h
             constexpr int kPart = 8 * 128;   // eight pairs a lane
             const size_t first_slot = (size_t)bh * z.cut.slots + mine_of.slot;
-            float* const parts = z.cut.parts + (first_slot * NT + wave) * kPart + lane * 2;
+            float* const parts = z.cut.parts + (first_slot * NT + wave) * kPart + l * 2;
             float* const mine = parts + (size_t)mine_of.piece * NT * kPart;
 #pragma unroll
             for (int i = 0; i < 8; ++i) put_shared(mine + i * 128, dq[i / 2][i % 2 * 2], dq[i / 2][i % 2 * 2 + 1]);
@@ -375,8 +377,8 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
         // Through the K tile of the stage that the last block did not use: every wave is past the barrier of the last step,
         // and the wave's own 2 KB of it were only ever written by the wave's own loads, which have all landed.
         bf16_t* patch = ((n & 1) ? ta1 : ta0) + wave * (16 * kD);
-        const Rows at = {z.at.H, z.at.beside};
-        store_rows_coalesced(patch, z.dQ + at.in_head(bh, z.L) + (size_t)(I * BS + wave * 16) * at.in_row(), at.in_row(), dq, z.scale, lane);
+        const Rows out = {z.at.H, z.at.beside};
+        store_rows_coalesced(patch, z.dQ + out.in_head(bh, z.L) + (size_t)(I * BS + wave * 16) * out.in_row(), out.in_row(), dq, z.scale, l);
         return;
     }
 
@@ -384,6 +386,12 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
     // key side: work item idx of head bh.  {Q, dO, O} tiles and LSE of a block row in two stages.
     // ============================================================================================
     const auto& b = args_again<BwdWith>();   // this side's
+    const Rows at = {b.at.H, b.at.beside};
+    const int in_row = at.in_row(), out_row = at.out_row();   // elements between rows of Q, K, V and of O, dO
+    const size_t head = at.in_head(bh, L), out_head = at.out_head(bh, L), vec = (size_t)bh * L;
+    [[maybe_unused]] const ScoreDraws draws(b.x.rng, b.x.stream, bh);
+    [[maybe_unused]] const unsigned below = both_halves(b.x.threshold - 1u);
+    const float scale_log2 = b.scale_log2, log2_keep = DROP ? log2f(b.x.keep_scale) : 0.f;
     const KeyItem item = key_item_lookup(b.col_ptr, nb, b.chunk, b.finest, idx, lane);
     if (item.J < 0) return;
     const int J = item.J, slot = item.slot;
@@ -396,19 +404,21 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
     const int last = n > 0 ? n - 1 : 0;
     auto row_at = [&](int t) { return __builtin_amdgcn_readlane(rows_v, t < last ? t : last); };
 
-    const TileLoadLane tlo(wave, lane, out_row);
     const bf16_t *const Qh = b.Q + head, *const dOh = b.dO + out_head, *const Oh = b.O + out_head;
     const float* const LSEh = b.LSE + vec;
     // six tile loads per wave, plus one 4-byte-per-lane load of LSE in wave 0
-    auto load_q = [&](bf16_t* qt, int I) {
-        tile_load_async(Qh + (size_t)I * BS * in_row, qt, wave, tl, tile_range<BS>(I * BS, length, in_row));
+    auto load_q = [&](bf16_t* qt, int I) {   // (offsets of the lane made here each time: registers are short)
+        const TileLoadLane tli(wave, once(lane), in_row);
+        tile_load_async(Qh + (size_t)I * BS * in_row, qt, wave, tli, tile_range<BS>(I * BS, length, in_row));
     };
     auto load_do = [&](bf16_t* dt_, int I) {
+        const TileLoadLane tlo(wave, once(lane), out_row);
         tile_load_async(dOh + (size_t)I * BS * out_row, dt_, wave, tlo, tile_range<BS>(I * BS, length, out_row));
     };
     auto load_o = [&](bf16_t* ot, float* lse_s, int I) {
+        const TileLoadLane tlo(wave, once(lane), out_row);
         tile_load_async(Oh + (size_t)I * BS * out_row, ot, wave, tlo, tile_range<BS>(I * BS, length, out_row));
-        if (wave == 0 && lane < BS) __builtin_amdgcn_global_load_lds(LSEh + (size_t)I * BS + lane, (lds_void_ptr)lse_s, 4, 0, 0);
+        if (wave == 0 && lane < BS) __builtin_amdgcn_global_load_lds(LSEh + (size_t)I * BS + once(lane), (lds_void_ptr)lse_s, 4, 0, 0);
     };
     unsigned bucket = 0;
     int icur = 0, inext = 0;   // block row of steps it, it + 1
@@ -467,9 +477,10 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
                 dd = mma_d(dd, *reinterpret_cast<const bf16x8*>(dt_ + off), *reinterpret_cast<const bf16x8*>(ot + off));
             }
             // lane (r, g) holds (dO O^T)[4 g + i][r]: the diagonal entry of row r sits in lane group r / 4
-            const float d0 = (r & 1) ? dd[1] : dd[0], d1 = (r & 1) ? dd[3] : dd[2];
-            if (g == (r >> 2)) del_s[wave * 16 + r] = ((r & 2) ? d1 : d0) * delta_scale;
-            if (wave == 0 && lane < BS) lse_s[lane] = reference(lse_s[lane]);
+            const int l = once(lane), row = l & 15;
+            const float d0 = (row & 1) ? dd[1] : dd[0], d1 = (row & 1) ? dd[3] : dd[2];
+            if ((l >> 4) == (row >> 2)) del_s[wave * 16 + row] = ((row & 2) ? d1 : d0) * delta_scale;
+            if (wave == 0 && l < BS) lse_s[l] = reference(lse_s[l], log2_keep);
         }
         lds_meet();
         if (kSpread && more) load_do(nd, inext);
@@ -557,10 +568,11 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
     __builtin_amdgcn_s_waitcnt(kWaitVm0);   // the owned fragments of a column without kept rows
 
     const auto& z = args_again<BwdWith>();
+    const int l = once(lane);
     if (slot >= 0) {
         // a chunk of a column: the last of them to arrive adds all of them up, in their order
         constexpr int kPart = 16 * 128;
-        float* const parts = z.partial + (((size_t)bh * z.n_slots + item.first) * NT + wave) * kPart + lane * 2;
+        float* const parts = z.partial + (((size_t)bh * z.n_slots + item.first) * NT + wave) * kPart + l * 2;
         float* const mine = parts + (size_t)(slot - item.first) * NT * kPart;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -586,17 +598,17 @@ __global__ __launch_bounds__(BS * 4, BS == 64 && DROP ? 2 : 3) void attn_bwd_wit
             }
         }
     }
-    if (krow >= length)   // what memory holds there has gone into this key's sums alone
+    if (J * BS + wave * 16 + (l & 15) >= length)   // what memory holds there has gone into this key's sums alone
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt) dk[dt] = dv[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     // through the stage the last block did not use, see the plain kernel
     const bool odd = (n & 1) != 0;   // last block in stage 0 -> stage 1 is free
     bf16_t* pa = (odd ? ta1 : ta0) + wave * (16 * kD);
     bf16_t* pb = (odd ? tb1 : tb0) + wave * (16 * kD);
-    const Rows at = {z.at.H, z.at.beside};
-    const size_t row0 = at.in_head(bh, z.L) + (size_t)(J * BS + wave * 16) * at.in_row();
-    store_rows_coalesced(pa, z.dK + row0, at.in_row(), dk, z.scale, lane);
-    store_rows_coalesced(pb, z.dV + row0, at.in_row(), dv, 1.f, lane);
+    const Rows out = {z.at.H, z.at.beside};
+    const size_t row0 = out.in_head(bh, z.L) + (size_t)(J * BS + wave * 16) * out.in_row();
+    store_rows_coalesced(pa, z.dK + row0, out.in_row(), dk, z.scale, l);
+    store_rows_coalesced(pb, z.dV + row0, out.in_row(), dv, 1.f, l);
 }
 
 // The plan of the plain kernel: cuts, order and lengths of work items as there.

@@ -102,7 +102,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_fwd_with_kernel(
     const int query = row0 + r;
     if (query < length) load_rows<T>(qf, Q + head + (size_t)row0 * kD, r, g);
     else clear(qf);
-    [[maybe_unused]] ScoreDraws draws(x, bh);
+    [[maybe_unused]] ScoreDraws draws(x.rng, x.stream, bh);
 
     float m = kLowest, limit = -INFINITY, lsum = 0.f;
     f32x4 oacc[1][4];
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_bwd_with_kernel(
     if (!key_side && x.slices)
         for (int i = tid; i < kWaves * 4 * kDiag; i += kWaves * 64) (&diag_s[0][0][0])[i] = 0.f;
     __syncthreads();
-    [[maybe_unused]] ScoreDraws draws(x, bh);
+    [[maybe_unused]] ScoreDraws draws(x.rng, x.stream, bh);
     const float keep = DROP ? x.keep_scale : 1.f;
     const int own = row0 + r;
 
