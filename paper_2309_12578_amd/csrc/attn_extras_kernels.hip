@@ -406,63 +406,51 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_bwd_with_kernel(
 // The table's gradient from the slices, 2 TS numbers each: number t < 2 TS - 1 is the sum of dS over distance base + t - (TS - 1) of
 // a TS x TS tile whose first key is `base` from its first query; the last has `base` as an integer, or kNoSlice where nothing was
 // computed.  Every thread adds into its own copy of the buckets in LDS, the copies are added up in a fixed order, and so
-// are the parts of a head, by the last of its workgroups to arrive.  The counters of arrivals, a line each, are 0 from the backward
-// kernel on: counting by compare and swap, as where a few pieces of a row meet, hundreds of workgroups took 500 to 1500 us.
-// kInFlight tiles a wave at a time, whose numbers are requested together, then their buckets: one by one, with the tile's place found from the
-// index, 4 x 8 heads x 4096, 851 blocks of 64, took 30 us.
+// are the parts of a head, by the last of its workgroups to arrive; the counters of arrivals, a line each, are 0 from the backward kernel on.
+// kInFlight tiles a wave and share of it at a time, whose numbers are requested together, then their buckets: 4 x 8 heads x 4096, 851 blocks
+// of 64, 10.5 us; 2 x 8 heads x 16320, 13.5 us.
 // ------------------------------------------------------------------------------------------------
 template <int TS>
 __global__ __launch_bounds__(256) void table_grad_kernel(const float* __restrict__ slices, Extras x, int L, unsigned tiles_of_head,
                                                          unsigned tiles_a_sequence, int parts, float* partial, unsigned long long* __restrict__ counters,
                                                          void* __restrict__ dtable) {
     extern __shared__ float hist[];   // [n_buckets][threads]
-    constexpr int F = 2 * TS, LANES = F < 64 ? F : 64, PER = F / LANES, GROUP = 64 / LANES, kInFlight = 4;   // lanes of a tile, numbers a lane, tiles a wave
-    typedef float Numbers __attribute__((ext_vector_type(PER)));
+    constexpr int F = 2 * TS, LANES = F / 4, GROUP = 64 / LANES, kInFlight = 4;   // lanes of a tile, four numbers each; tiles of a wave
     const int h = blockIdx.x % x.H, part = blockIdx.x / x.H, tid = threadIdx.x, threads = blockDim.x, lane = tid & 63;
     for (int b = 0; b < x.n_buckets; ++b) hist[b * threads + tid] = 0.f;
-    const int t = lane % LANES * PER;
+    const int t = lane % LANES * 4;
     const unsigned first = (unsigned)((unsigned long long)part * tiles_of_head / parts);
     const unsigned end = (unsigned)((unsigned long long)(part + 1) * tiles_of_head / parts);
     const unsigned at_once = (threads >> 6) * GROUP, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     for (unsigned c0 = first + wave * GROUP; c0 < end; c0 += kInFlight * at_once) {
-        Numbers v[kInFlight];
+        float4 v[kInFlight];
         int base[kInFlight];
 #pragma unroll
         for (int u = 0; u < kInFlight; ++u) {
             const unsigned tile = c0 + u * at_once + lane / LANES, at = tile < end ? tile : end - 1;
             const unsigned b = at / tiles_a_sequence, e = at % tiles_a_sequence;
-            v[u] = *reinterpret_cast<const Numbers*>(slices + ((size_t)(b * x.H + h) * tiles_a_sequence + e) * F + t);
+            v[u] = *reinterpret_cast<const float4*>(slices + ((size_t)(b * x.H + h) * tiles_a_sequence + e) * F + t);
         }
 #pragma unroll
         for (int u = 0; u < kInFlight; ++u) {
-            const float place = v[u][PER - 1];   // (a bit cast of the element itself is one of the vector's first)
+            const float place = v[u].w;
             const int from = __shfl(__builtin_bit_cast(int, place), lane | (LANES - 1));
             base[u] = c0 + u * at_once + lane / LANES < end ? from : kNoSlice;
         }
-        int bucket[kInFlight][PER];
+        unsigned buckets[kInFlight];
+#pragma unroll
+        for (int u = 0; u < kInFlight; ++u) {   // (no place leads past the map's 2 L - 1; the last number of a tile belongs to no distance)
+            const unsigned at = (unsigned)(base[u] + L - TS + t), from = min(at, 2u * L - 5u);
+            buckets[u] = reinterpret_cast<const FourBuckets*>(x.bucket_of + from)->u >> (at == from ? 0 : 8);
+        }
 #pragma unroll
         for (int u = 0; u < kInFlight; ++u)
-#pragma unroll
-            for (int i = 0; i < PER; ++i)   // (no place leads past the map)
-                bucket[u][i] = bucket_index(x, x.bucket_of[min((unsigned)(base[u] + L - TS + t + i), 2u * L - 2u)]);
-#pragma unroll
-        for (int u = 0; u < kInFlight; ++u)
-#pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if (base[u] != kNoSlice && t + i != F - 1)
-                    __hip_atomic_fetch_add(&hist[bucket[u][i] * threads + tid], v[u][i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            if (base[u] != kNoSlice) {
+                const float four[4] = {v[u].x, v[u].y, v[u].z, t + 3 == F - 1 ? 0.f : v[u].w};
+                add_four(hist + tid, threads, four, buckets[u], x.n_buckets);
+            }
     }
-    leave_partial(hist, x.n_buckets, part, parts, h, partial);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's stores are done, at device scope
-    __syncthreads();                                   // and those of the others, and every wave is done with the copies
-    int* const flag = reinterpret_cast<int*>(hist);
-    if (tid == 0) {
-        const unsigned long long before = __hip_atomic_fetch_add(counters + h * Extras::kCounterStride, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        *flag = before == (unsigned long long)parts - 1ull;
-    }
-    __syncthreads();
-    asm volatile("" ::: "memory");   // nothing of the others' is read before
-    if (*flag) write_table_column(partial, x.n_buckets, parts, h, x.H, dtable, x.table_bf16 != 0);
+    finish_table_grad(hist, x.n_buckets, part, parts, h, x.H, partial, counters + h * Extras::kCounterStride, dtable, x.table_bf16 != 0);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -485,7 +473,7 @@ struct WithWorkspace {
         }
         // sixteen slices a workgroup or more, and about two workgroups a compute unit
         const long long tiles = (long long)s.BH / H * nnzb * (s.bs / tile) * (s.bs / tile);
-        parts = (int)std::max<long long>(1, std::min<long long>(tiles / 16, 512 / H));
+        parts = (int)std::max<long long>(1, std::min<long long>(tiles / 16, 1024 / H));
         partial = up(slices + (size_t)s.BH * nnzb * (s.bs / tile) * (s.bs / tile) * 2 * tile * sizeof(float));
         counters = up(partial + (size_t)H * parts * n_buckets * sizeof(float));
         total = up(counters + (size_t)H * Extras::kCounterStride * 8);
