@@ -13,6 +13,8 @@ from .binding import (  # noqa: F401
     spion_attn_fwd, spion_attn_bwd, generate_pattern, attn_fwd, attn_bwd,
     spion_score_mean, spion_frobenius_workspace_bytes, spion_frobenius_distance, score_mean,
     frobenius_distance, spion_index_check, index_is_well_formed, spion_copy_yardstick,
+    spion_attn_with_workspace_bytes, spion_attn_fwd_with, spion_attn_bwd_with, spion_relative_bias,
+    spion_relative_bias_workspace_bytes, spion_relative_bias_grad, spion_dropout_add,
 )
 from .autograd import sparse_attention  # noqa: E402,F401
 from .extras import RelativeBuckets, dropout_add, relative_bias, relative_buckets  # noqa: E402,F401

@@ -51,4 +51,4 @@ def sparse_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, pattern:
         raise ValueError("flags are not supported together with a bias, lengths or dropout")
     return (_b._host or _b._native()).sparse_attention_with(
         Q, K, V, pattern.row_ptr, pattern.col_idx, pattern.col_ptr, pattern.row_idx, pattern.bsr_pos, pattern.nnzb, pattern.block,
-        scale, bias, None if bias is None else _map_for(bias, buckets), lengths, dropout, rng, stream)
+        scale, bias, None if bias is None else _map_for(bias, buckets, Q.shape[-2]), lengths, dropout, rng, stream)

@@ -44,6 +44,13 @@ class _AttnParams(ctypes.Structure):
                 ("scale", ctypes.c_float), ("flags", ctypes.c_uint32)]
 
 
+class _AttnExtras(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("bucket_of", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+                ("rng", ctypes.c_void_p), ("rng_used", ctypes.c_void_p), ("dropout", ctypes.c_double),
+                ("n_buckets", ctypes.c_int32), ("table_dtype", ctypes.c_int32), ("stream", ctypes.c_uint32),
+                ("reserved", ctypes.c_uint32)]
+
+
 _lib: Optional[ctypes.CDLL] = None
 
 
@@ -87,6 +94,21 @@ def load() -> ctypes.CDLL:
     lib.spion_attn_fwd.argtypes = [vp] * 7 + [i32, ctypes.POINTER(_AttnParams), vp, sz, vp]
     lib.spion_attn_bwd.restype = ctypes.c_int
     lib.spion_attn_bwd.argtypes = [vp] * 14 + [i32, ctypes.POINTER(_AttnParams), vp, sz, vp]
+    params = ctypes.POINTER(_AttnParams), ctypes.POINTER(_AttnExtras)
+    lib.spion_attn_with_workspace_bytes.restype = sz
+    lib.spion_attn_with_workspace_bytes.argtypes = [*params, i32, i32]
+    lib.spion_attn_fwd_with.restype = ctypes.c_int
+    lib.spion_attn_fwd_with.argtypes = [vp] * 7 + [i32, *params, vp, sz, vp]
+    lib.spion_attn_bwd_with.restype = ctypes.c_int
+    lib.spion_attn_bwd_with.argtypes = [vp] * 15 + [i32, *params, vp, sz, vp]
+    lib.spion_relative_bias.restype = ctypes.c_int
+    lib.spion_relative_bias.argtypes = [vp] * 3 + [i32] * 7 + [vp]
+    lib.spion_relative_bias_workspace_bytes.restype = sz
+    lib.spion_relative_bias_workspace_bytes.argtypes = [i32] * 4
+    lib.spion_relative_bias_grad.restype = ctypes.c_int
+    lib.spion_relative_bias_grad.argtypes = [vp] * 3 + [i32] * 7 + [vp, sz, vp]
+    lib.spion_dropout_add.restype = ctypes.c_int
+    lib.spion_dropout_add.argtypes = [vp] * 3 + [ctypes.c_int64, i32, ctypes.c_double, vp, vp, ctypes.c_uint32, vp]
     _lib = lib
     return lib
 
@@ -228,6 +250,88 @@ def spion_attn_bwd(Q, K, V, O, dO, LSE, dQ, dK, dV, row_ptr, col_idx, col_ptr, r
                                _ptr(workspace), ws_bytes, _stream(stream))
     if rc != 0:
         raise SpionError(rc, "spion_attn_bwd")
+
+
+def _bytes(workspace: Optional[torch.Tensor]) -> int:
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def _attn_extras(H, L, table, bucket_of, lengths, rng, rng_used, dropout, dropout_stream) -> _AttnExtras:
+    n_buckets = 0 if table is None else int(table.shape[0])
+    if table is not None and (table.shape != (n_buckets, H) or bucket_of is None or bucket_of.numel() != 2 * L - 1 or
+                              bucket_of.dtype != torch.uint8):
+        raise ValueError("the bias table must be [n_buckets, H], its buckets uint8 [2 L - 1]")
+    if lengths is not None and lengths.dtype != torch.int32:
+        raise ValueError("lengths must be int32")
+    for t in (rng, rng_used):
+        if t is not None and (t.dtype != torch.int64 or t.numel() != 2):
+            raise ValueError("rng must be int64 {seed, offset}")
+    return _AttnExtras(_ptr(table), _ptr(bucket_of), _ptr(lengths), _ptr(rng), _ptr(rng_used), float(dropout), n_buckets,
+                       SPION_F32 if table is None else _dtype_code(table.dtype), dropout_stream, 0)
+
+
+def spion_attn_with_workspace_bytes(B, H, L, d, block, dtype, nnzb, is_bwd, scale=0.0, table=None, bucket_of=None, lengths=None,
+                                    rng=None, dropout=0.0) -> int:
+    p = _attn_params(B, H, L, d, block, dtype, scale, 0)
+    x = _attn_extras(H, L, table, bucket_of, lengths, rng, None, dropout, 0)
+    n = int(load().spion_attn_with_workspace_bytes(ctypes.byref(p), ctypes.byref(x), nnzb, int(is_bwd)))
+    if n == ctypes.c_size_t(-1).value:
+        raise SpionError(-2, "spion_attn_with_workspace_bytes")
+    return n
+
+
+def spion_attn_fwd_with(Q, K, V, O, LSE, row_ptr, col_idx, nnzb, B, H, L, d, block, dtype, scale=0.0, table=None, bucket_of=None,
+                        lengths=None, rng=None, rng_used=None, dropout=0.0, dropout_stream=0, workspace=None, stream=None) -> None:
+    p = _attn_params(B, H, L, d, block, dtype, scale, 0)
+    x = _attn_extras(H, L, table, bucket_of, lengths, rng, rng_used, dropout, dropout_stream)
+    rc = load().spion_attn_fwd_with(_ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(LSE), _ptr(row_ptr), _ptr(col_idx), int(nnzb),
+                                    ctypes.byref(p), ctypes.byref(x), _ptr(workspace), _bytes(workspace), _stream(stream))
+    if rc != 0:
+        raise SpionError(rc, "spion_attn_fwd_with")
+
+
+def spion_attn_bwd_with(Q, K, V, O, dO, LSE, dQ, dK, dV, dtable, row_ptr, col_idx, col_ptr, row_idx, bsr_pos, nnzb, B, H, L, d,
+                        block, dtype, scale=0.0, table=None, bucket_of=None, lengths=None, rng=None, dropout=0.0,
+                        dropout_stream=0, workspace=None, stream=None) -> None:
+    p = _attn_params(B, H, L, d, block, dtype, scale, 0)
+    x = _attn_extras(H, L, table, bucket_of, lengths, rng, None, dropout, dropout_stream)
+    rc = load().spion_attn_bwd_with(_ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(dO), _ptr(LSE), _ptr(dQ), _ptr(dK), _ptr(dV),
+                                    _ptr(dtable), _ptr(row_ptr), _ptr(col_idx), _ptr(col_ptr), _ptr(row_idx), _ptr(bsr_pos),
+                                    int(nnzb), ctypes.byref(p), ctypes.byref(x), _ptr(workspace), _bytes(workspace),
+                                    _stream(stream))
+    if rc != 0:
+        raise SpionError(rc, "spion_attn_bwd_with")
+
+
+def spion_relative_bias(table, bucket_of, bias, reach: int, n_buckets: int, H: int, q_len: int, k_len: int, q_start: int, dtype: int,
+                        stream=None) -> None:
+    rc = load().spion_relative_bias(_ptr(table), _ptr(bucket_of), _ptr(bias), reach, n_buckets, H, q_len, k_len, q_start, dtype,
+                                    _stream(stream))
+    if rc != 0:
+        raise SpionError(rc, "spion_relative_bias")
+
+
+def spion_relative_bias_workspace_bytes(n_buckets: int, H: int, q_len: int, k_len: int) -> int:
+    n = int(load().spion_relative_bias_workspace_bytes(n_buckets, H, q_len, k_len))
+    if n == ctypes.c_size_t(-1).value:
+        raise SpionError(-2, "spion_relative_bias_workspace_bytes")
+    return n
+
+
+def spion_relative_bias_grad(dbias, bucket_of, dtable, reach: int, n_buckets: int, H: int, q_len: int, k_len: int, q_start: int,
+                             dtype: int, workspace, stream=None) -> None:
+    rc = load().spion_relative_bias_grad(_ptr(dbias), _ptr(bucket_of), _ptr(dtable), reach, n_buckets, H, q_len, k_len, q_start,
+                                         dtype, _ptr(workspace), _bytes(workspace), _stream(stream))
+    if rc != 0:
+        raise SpionError(rc, "spion_relative_bias_grad")
+
+
+def spion_dropout_add(x, residual, y, n: int, dtype: int, dropout: float, rng, rng_used=None, dropout_stream: int = 0,
+                      stream=None) -> None:
+    rc = load().spion_dropout_add(_ptr(x), _ptr(residual), _ptr(y), n, dtype, float(dropout), _ptr(rng), _ptr(rng_used),
+                                  dropout_stream, _stream(stream))
+    if rc != 0:
+        raise SpionError(rc, "spion_dropout_add")
 
 
 # ------------------------------------------------------------------------------------------------

@@ -792,10 +792,12 @@ at::Tensor with_workspace(const spion_attn_params& p, const spion_attn_extras& x
     return new_bytes(n == (size_t)-1 ? 0 : n, like);   // what is unsupported the call itself tells
 }
 
+// The gradient of sparse_attention_with, and of heads_attention_with (q = qkv, no k and v).
 struct AttentionWithBackward : public torch::autograd::Node {
     torch::autograd::SavedVariable q, k, v, o, lse, table, lengths, rng;
     Index ix;
     AttentionExtras extras;
+    int64_t H = 0;   // of qkv's heads; 0: Q, K and V
 
     std::string name() const override { return "SparseAttentionWithBackward"; }
 
@@ -804,33 +806,95 @@ struct AttentionWithBackward : public torch::autograd::Node {
     }
 
     torch::autograd::variable_list apply(torch::autograd::variable_list&& grads) override {
-        torch::autograd::variable_list out(extras.n_buckets ? 4 : 3);
+        const int inputs = H ? 1 : 3;
+        torch::autograd::variable_list out(inputs + (extras.n_buckets ? 1 : 0));
         if (!grads[0].defined()) return out;
         return differentiate("sparse_attention cannot be differentiated twice", [&] {
-            const at::Tensor Q = q.unpack(), K = k.unpack(), V = v.unpack(), O = o.unpack(shared_from_this()), stat = lse.unpack();
-            const at::Tensor T = table.unpack(), R = rng.unpack();
+            const at::Tensor Q = q.unpack(), O = o.unpack(shared_from_this()), stat = lse.unpack(), T = table.unpack(), R = rng.unpack();
+            const at::Tensor K = H ? Q : k.unpack(), V = H ? Q : v.unpack();
             AttentionExtras with = extras;
             with.lengths = lengths.unpack();
             const c10::DeviceGuard guard(Q.device());
             const at::Tensor g = dense(grads[0]);
-            const spion_attn_params p = params_of(Q, ix);
-            for (const at::Tensor* t : {&K, &V, &O, &g}) room_for(Q, *t);
-            room_for_rows(Q, stat);
+            // what saved-tensor hooks hand back is looked at as the call's own tensors were
+            auto same = [&](bool ok) {
+                if (!ok) bad_value("sparse_attention: a saved tensor is not the one that was saved");
+            };
+            if (H) same(Q.dim() == 3 && Q.size(2) == 3 * H * 64 && Q.scalar_type() == at::kBFloat16 && Q.is_contiguous());
+            else same(Q.dim() == 4 && Q.is_contiguous());
+            const spion_attn_params p = H ? heads_params(Q, H, ix) : params_of(Q, ix);
+            for (const at::Tensor* t : {&K, &V}) same(t->numel() == Q.numel() && t->scalar_type() == Q.scalar_type() && t->is_contiguous());
+            for (const at::Tensor* t : {&O, &g}) same(t->numel() == Q.numel() / (H ? 3 : 1) && t->scalar_type() == Q.scalar_type() && t->is_contiguous());
+            same(stat.numel() == (int64_t)p.B * p.H * p.L && stat.scalar_type() == at::kFloat && stat.is_contiguous());
+            same(!extras.n_buckets || (T.numel() == (int64_t)extras.n_buckets * p.H && T.is_contiguous() && T.device() == Q.device()));
+            same(!with.lengths.defined() || (with.lengths.numel() == p.B && with.lengths.scalar_type() == at::kInt && with.lengths.is_contiguous()));
+            same(!R.defined() || (R.numel() == 2 && R.scalar_type() == at::kLong && R.is_contiguous()));
             const spion_attn_extras x = with.params(T, R);
-            const bool table_grad = T.defined() && task_should_compute_output(3);
-            for (int i = 0; i < 3; ++i) out[i] = new_like(Q);
-            if (table_grad) out[3] = new_like(T);
+            const bool table_grad = extras.n_buckets && task_should_compute_output(inputs);
+            for (int i = 0; i < inputs; ++i) out[i] = new_like(Q);
+            if (table_grad) out[inputs] = new_like(T);
+            void* const dtable = table_grad ? device_ptr(out[inputs]) : nullptr;
             const at::Tensor ws = with_workspace(p, x, ix, true, Q);
-            const int rc = spion_attn_bwd_with(
-                device_ptr(Q), device_ptr(K), device_ptr(V), device_ptr(O), device_ptr(g), (const float*)device_ptr(stat), device_ptr(out[0]),
-                device_ptr(out[1]), device_ptr(out[2]), table_grad ? device_ptr(out[3]) : nullptr, (const int32_t*)device_ptr(ix.row_ptr),
-                (const int32_t*)device_ptr(ix.col_idx), (const int32_t*)device_ptr(ix.col_ptr), (const int32_t*)device_ptr(ix.row_idx),
-                (const int32_t*)device_ptr(ix.bsr_pos), ix.nnzb, &p, &x, device_ptr(ws), (size_t)ws.nbytes(), current_stream());
+            auto index = [](const at::Tensor& t) { return (const int32_t*)device_ptr(t); };
+            if (H) {
+                const int rc = spion_heads_attn_bwd_with(device_ptr(Q), device_ptr(O), device_ptr(g), (const float*)device_ptr(stat), device_ptr(out[0]),
+                                                         dtable, index(ix.row_ptr), index(ix.col_idx), index(ix.col_ptr), index(ix.row_idx), ix.nnzb,
+                                                         &p, &x, device_ptr(ws), (size_t)ws.nbytes(), current_stream());
+                if (rc != SPION_OK) throw SpionFailure{rc, "spion_heads_attn_bwd_with"};
+                return out;
+            }
+            const int rc = spion_attn_bwd_with(device_ptr(Q), device_ptr(K), device_ptr(V), device_ptr(O), device_ptr(g), (const float*)device_ptr(stat),
+                                               device_ptr(out[0]), device_ptr(out[1]), device_ptr(out[2]), dtable, index(ix.row_ptr), index(ix.col_idx),
+                                               index(ix.col_ptr), index(ix.row_idx), index(ix.bsr_pos), ix.nnzb, &p, &x, device_ptr(ws),
+                                               (size_t)ws.nbytes(), current_stream());
             if (rc != SPION_OK) throw SpionFailure{rc, "spion_attn_bwd_with"};
             return out;
         });
     }
 };
+
+// The arguments table | None, bucket_of | None, lengths | None, dropout, rng | None, stream of a call on B sequences of L tokens.
+struct ExtrasArgs {
+    AttentionExtras extras;
+    at::Tensor table, rng;   // rng: only where there is something to draw
+
+    ExtrasArgs(PyObject* const* a, int64_t B, int64_t H, int64_t L, const at::Device& device) {
+        table = optional_arg(a[0]);
+        extras.lengths = optional_arg(a[2]);
+        extras.dropout = dropout_arg(a[3]);
+        extras.stream = stream_arg(a[5]);
+        if (table.defined()) {
+            check_operand(table, device);
+            extras.bucket_of = tensor_arg(a[1]);
+            check_operand(extras.bucket_of, device);
+            dtype_code(table);
+            if (table.dim() != 2 || table.size(1) != H) bad_value("the bias table must be [buckets, H]");
+            if (table.size(0) < 1 || table.size(0) > 256) bad_value("the bias table must have 1 to 256 buckets");
+            if (extras.bucket_of.scalar_type() != at::kByte || !extras.bucket_of.is_contiguous() || extras.bucket_of.numel() != 2 * L - 1)
+                bad_value("the buckets must be a contiguous uint8 map of 2 L - 1 distances");
+            extras.n_buckets = (int)table.size(0);
+        }
+        if (extras.lengths.defined()) {
+            check_operand(extras.lengths, device);
+            if (extras.lengths.scalar_type() != at::kInt || extras.lengths.numel() != B || !extras.lengths.is_contiguous())
+                bad_value("lengths must be a contiguous int32 tensor [B]");
+        }
+        if (std::nearbyint(65536.0 * extras.dropout) > 0.0) rng = rng_arg(a[4], device);
+    }
+};
+
+// The node of a call, but for q, k, v and o.
+std::shared_ptr<AttentionWithBackward> with_node(AttentionExtras&& extras, Index&& ix, const at::Tensor& lse, const at::Tensor& table, const at::Tensor& used) {
+    auto node = std::shared_ptr<AttentionWithBackward>(new AttentionWithBackward(), torch::autograd::deleteNode);
+    node->lse = torch::autograd::SavedVariable(lse, false);
+    node->table = torch::autograd::SavedVariable(table, false);
+    node->lengths = torch::autograd::SavedVariable(extras.lengths, false);
+    node->rng = torch::autograd::SavedVariable(used, false);
+    extras.lengths.reset();
+    node->extras = std::move(extras);
+    node->ix = std::move(ix);
+    return node;
+}
 
 // sparse_attention_with(Q, K, V, row_ptr, col_idx, col_ptr, row_idx, bsr_pos, nnzb, block, scale, table | None, bucket_of | None,
 //                       lengths | None, dropout, rng | None, stream) -> O
@@ -853,33 +917,11 @@ PyObject* py_sparse_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) 
         ix.block = int_arg(a[9]);
         ix.scale = (float)double_arg(a[10]);
         for (const at::Tensor* t : {&ix.row_ptr, &ix.col_idx}) check_operand(*t, device);
-        AttentionExtras extras;
-        at::Tensor table = optional_arg(a[11]);
-        extras.lengths = optional_arg(a[13]);
-        extras.dropout = dropout_arg(a[14]);
-        extras.stream = stream_arg(a[16]);
-        if (table.defined()) {
-            check_operand(table, device);
-            extras.bucket_of = tensor_arg(a[12]);
-            check_operand(extras.bucket_of, device);
-            dtype_code(table);
-            if (table.dim() != 2 || table.size(1) != q.size(1)) bad_value("the bias table must be [buckets, H]");
-            if (table.size(0) < 1 || table.size(0) > 256) bad_value("the bias table must have 1 to 256 buckets");
-            if (extras.bucket_of.scalar_type() != at::kByte || !extras.bucket_of.is_contiguous() || extras.bucket_of.numel() != 2 * q.size(2) - 1)
-                bad_value("the buckets must be a contiguous uint8 map of 2 L - 1 distances");
-            extras.n_buckets = (int)table.size(0);
-        }
-        if (extras.lengths.defined()) {
-            check_operand(extras.lengths, device);
-            if (extras.lengths.scalar_type() != at::kInt || extras.lengths.numel() != q.size(0) || !extras.lengths.is_contiguous())
-                bad_value("lengths must be a contiguous int32 tensor [B]");
-        }
-        const bool drop = std::nearbyint(65536.0 * extras.dropout) > 0.0;
-        at::Tensor rng, used;
-        if (drop) rng = rng_arg(a[15], device);
+        ExtrasArgs with(a + 11, q.size(0), q.size(1), q.size(2), device);
+        const at::Tensor& table = with.table;
         const c10::DeviceGuard guard(device);
         const bool grad = table.defined() ? torch::autograd::compute_requires_grad(q, k, v, table) : torch::autograd::compute_requires_grad(q, k, v);
-        at::Tensor o, lse, qc, kc, vc, tc;
+        at::Tensor o, lse, qc, kc, vc, tc, used;
         {
             at::NoGradGuard no_grad;
             qc = dense(q);
@@ -889,8 +931,8 @@ PyObject* py_sparse_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) 
             const spion_attn_params p = params_of(qc, ix);
             o = new_like(qc);
             lse = at::Tensor(at::detail::empty_cuda({q.size(0), q.size(1), q.size(2)}, at::kFloat, device, std::nullopt));
-            if (drop && grad) used = new_longs(2, qc);
-            spion_attn_extras x = extras.params(tc, rng);
+            if (with.rng.defined() && grad) used = new_longs(2, qc);
+            spion_attn_extras x = with.extras.params(tc, with.rng);
             if (used.defined()) x.rng_used = (int64_t*)used.data_ptr();
             const at::Tensor ws = with_workspace(p, x, ix, false, qc);
             const int rc = spion_attn_fwd_with(device_ptr(qc), device_ptr(kc), device_ptr(vc), device_ptr(o), (float*)device_ptr(lse),
@@ -903,22 +945,71 @@ PyObject* py_sparse_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) 
             ix.row_idx = tensor_arg(a[6]);
             ix.bsr_pos = tensor_arg(a[7]);
             for (const at::Tensor* t : {&ix.col_ptr, &ix.row_idx, &ix.bsr_pos}) check_operand(*t, device);
-            auto node = std::shared_ptr<AttentionWithBackward>(new AttentionWithBackward(), torch::autograd::deleteNode);
+            auto node = with_node(std::move(with.extras), std::move(ix), lse, tc, used);
             node->set_next_edges(table.defined() ? torch::autograd::collect_next_edges(q, k, v, table) : torch::autograd::collect_next_edges(q, k, v));
             node->q = torch::autograd::SavedVariable(qc, false);
             node->k = torch::autograd::SavedVariable(kc, false);
             node->v = torch::autograd::SavedVariable(vc, false);
-            node->lse = torch::autograd::SavedVariable(lse, false);
-            node->table = torch::autograd::SavedVariable(tc, false);
-            node->lengths = torch::autograd::SavedVariable(extras.lengths, false);
-            node->rng = torch::autograd::SavedVariable(used, false);
-            extras.lengths.reset();
-            node->extras = std::move(extras);
-            node->ix = std::move(ix);
             torch::autograd::set_history(o, node);
             node->o = torch::autograd::SavedVariable(o, true);
         }
         return wrap(o);
+    });
+}
+
+// heads_attention_with(qkv [B, L, 3 H 64], H, row_ptr, col_idx, col_ptr, row_idx, bsr_pos, nnzb, block, apart, table | None,
+//                      bucket_of | None, lengths | None, dropout, rng | None, stream) -> [B, L, H 64]
+// None where the steps are to be taken one by one (see heads_attention).
+PyObject* py_heads_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!arg_count(n, 16, "heads_attention_with")) return nullptr;
+    return guarded([&]() -> PyObject* {
+        if (!nothing_between() || !plain(a[0]) || a[9] == Py_True) Py_RETURN_NONE;
+        const at::Tensor& qkv = THPVariable_Unpack(a[0]);
+        const int64_t H = int_arg(a[1]);
+        Index ix;
+        ix.nnzb = int_arg(a[7]);
+        ix.block = int_arg(a[8]);
+        if (!heads_in_place(qkv, ix) || qkv.dim() != 3 || !qkv.is_contiguous() || H <= 0 || qkv.size(2) != 3 * H * 64 || qkv.numel() == 0 ||
+            (uintptr_t)qkv.data_ptr() % 16 != 0)
+            Py_RETURN_NONE;
+        const at::Device device = qkv.device();
+        const int64_t B = qkv.size(0), L = qkv.size(1);
+        ix.row_ptr = tensor_arg(a[2]);
+        ix.col_idx = tensor_arg(a[3]);
+        for (const at::Tensor* t : {&ix.row_ptr, &ix.col_idx}) check_operand(*t, device);
+        ExtrasArgs with(a + 10, B, H, L, device);
+        const at::Tensor& table = with.table;
+        const c10::DeviceGuard guard(device);
+        const bool grad = table.defined() ? torch::autograd::compute_requires_grad(qkv, table) : torch::autograd::compute_requires_grad(qkv);
+        at::Tensor tc, used;
+        at::Tensor s(at::detail::empty_cuda({B, L, H * 64}, qkv.scalar_type(), device, std::nullopt));
+        at::Tensor lse(at::detail::empty_cuda({B, H, L}, at::kFloat, device, std::nullopt));
+        {
+            at::NoGradGuard no_grad;
+            if (table.defined()) tc = table.contiguous();
+            const spion_attn_params p = heads_params(qkv, H, ix);
+            if (with.rng.defined() && grad) used = new_longs(2, qkv);
+            spion_attn_extras x = with.extras.params(tc, with.rng);
+            if (used.defined()) x.rng_used = (int64_t*)used.data_ptr();
+            const at::Tensor ws = with_workspace(p, x, ix, false, qkv);
+            const int rc = spion_heads_attn_fwd_with(device_ptr(qkv), device_ptr(s), (float*)device_ptr(lse), (const int32_t*)device_ptr(ix.row_ptr),
+                                                     (const int32_t*)device_ptr(ix.col_idx), ix.nnzb, &p, &x, device_ptr(ws), (size_t)ws.nbytes(),
+                                                     current_stream());
+            if (rc != SPION_OK) throw SpionFailure{rc, "spion_heads_attn_fwd_with"};
+        }
+        if (grad) {
+            ix.col_ptr = tensor_arg(a[4]);
+            ix.row_idx = tensor_arg(a[5]);
+            ix.bsr_pos = tensor_arg(a[6]);
+            for (const at::Tensor* t : {&ix.col_ptr, &ix.row_idx}) check_operand(*t, device);
+            auto node = with_node(std::move(with.extras), std::move(ix), lse, tc, used);
+            node->H = H;
+            node->set_next_edges(table.defined() ? torch::autograd::collect_next_edges(qkv, table) : torch::autograd::collect_next_edges(qkv));
+            node->q = torch::autograd::SavedVariable(qkv, false);
+            torch::autograd::set_history(s, node);
+            node->o = torch::autograd::SavedVariable(s, true);
+        }
+        return wrap(s);
     });
 }
 
@@ -1100,6 +1191,7 @@ PyMethodDef kMethods[] = {
     {"attn_fwd", (PyCFunction)(void*)py_attn_fwd, METH_FASTCALL, nullptr},
     {"attn_bwd", (PyCFunction)(void*)py_attn_bwd, METH_FASTCALL, nullptr},
     {"sparse_attention", (PyCFunction)(void*)py_sparse_attention, METH_FASTCALL, nullptr},
+    {"heads_attention_with", (PyCFunction)(void*)py_heads_attention_with, METH_FASTCALL, nullptr},
     {"heads_attention", (PyCFunction)(void*)py_heads_attention, METH_FASTCALL, nullptr},
     {"layer_norm", (PyCFunction)(void*)py_layer_norm, METH_FASTCALL, nullptr},
     {"residual", (PyCFunction)(void*)py_residual, METH_FASTCALL, nullptr},

@@ -648,4 +648,47 @@ int spion_heads_attn_bwd(const void* qkv, const void* S, const void* dS, const f
                                   nnzb, workspace, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? SPION_OK : SPION_ERR_HIP;
 }
 
+int spion_heads_attn_fwd_with(const void* qkv, void* S, float* LSE, const int32_t* row_ptr, const int32_t* col_idx, int32_t nnzb,
+                              const spion_attn_params* p, const spion_attn_extras* x, void* workspace, size_t workspace_bytes,
+                              void* hip_stream) {
+    if (!qkv || !S || !LSE || !row_ptr || !col_idx || !p || !x) return SPION_ERR_NULL;
+    const int rc = heads_beside_ok((uintptr_t)qkv | (uintptr_t)S, p, nnzb);
+    if (rc != SPION_OK) return rc;
+    spion::Extras extras;
+    const int with_rc = take_extras(p, x, nnzb, extras);
+    if (with_rc != SPION_OK) return with_rc;
+    spion::AttnShape s = make_shape(p);
+    const size_t need = spion::attn_with_workspace_bytes(s, extras.n_buckets, p->H, nnzb, false);
+    if (need && (!workspace || (uintptr_t)workspace % kAlign != 0 || workspace_bytes < need)) return SPION_ERR_WORKSPACE;
+    if (need) s.fwd_room = workspace;
+    s.heads_beside = p->H;
+    const uint16_t* const q = static_cast<const uint16_t*>(qkv);
+    const size_t D = (size_t)p->H * 64;
+    return spion::launch_attn_fwd_with(s, extras, q, q + D, q + 2 * D, S, LSE, row_ptr, col_idx, nnzb, static_cast<hipStream_t>(hip_stream)) ==
+                   hipSuccess ? SPION_OK : SPION_ERR_HIP;
+}
+
+int spion_heads_attn_bwd_with(const void* qkv, const void* S, const void* dS, const float* LSE, void* dqkv, void* dtable,
+                              const int32_t* row_ptr, const int32_t* col_idx, const int32_t* col_ptr, const int32_t* row_idx, int32_t nnzb,
+                              const spion_attn_params* p, const spion_attn_extras* x, void* workspace, size_t workspace_bytes,
+                              void* hip_stream) {
+    if (!qkv || !S || !dS || !LSE || !dqkv || !row_ptr || !col_idx || !col_ptr || !row_idx || !p || !x) return SPION_ERR_NULL;
+    const int rc = heads_beside_ok((uintptr_t)qkv | (uintptr_t)S | (uintptr_t)dS | (uintptr_t)dqkv, p, nnzb);
+    if (rc != SPION_OK) return rc;
+    spion::Extras extras;
+    const int with_rc = take_extras(p, x, nnzb, extras);
+    if (with_rc != SPION_OK) return with_rc;
+    if (dtable && !extras.table) return SPION_ERR_NULL;
+    if (!spion::attn_bwd_grids_fit(p->B * p->H, p->block, p->L / p->block, nnzb)) return SPION_ERR_SHAPE;
+    spion::AttnShape s = make_shape(p);
+    const size_t need = spion::attn_with_workspace_bytes(s, extras.n_buckets, p->H, nnzb, true);
+    if (need && (!workspace || (uintptr_t)workspace % kAlign != 0 || workspace_bytes < need)) return SPION_ERR_WORKSPACE;
+    s.heads_beside = p->H;
+    const uint16_t* const q = static_cast<const uint16_t*>(qkv);
+    uint16_t* const d = static_cast<uint16_t*>(dqkv);
+    const size_t D = (size_t)p->H * 64;
+    return spion::launch_attn_bwd_with(s, extras, q, q + D, q + 2 * D, S, dS, LSE, d, d + D, d + 2 * D, dtable, row_ptr, col_idx, col_ptr,
+                                       row_idx, nnzb, workspace, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? SPION_OK : SPION_ERR_HIP;
+}
+
 }  // extern "C"

@@ -52,6 +52,15 @@ int spion_heads_attn_bwd(const void* qkv, const void* S, const void* dS, const f
                          const int32_t* col_idx, const int32_t* col_ptr, const int32_t* row_idx, int32_t nnzb,
                          const spion_attn_params* p, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+// spion_attn_fwd_with / spion_attn_bwd_with (p, x, workspace and index as there) on the same tensors, under the same conditions.
+int spion_heads_attn_fwd_with(const void* qkv, void* S, float* LSE, const int32_t* row_ptr, const int32_t* col_idx, int32_t nnzb,
+                              const spion_attn_params* p, const spion_attn_extras* x, void* workspace, size_t workspace_bytes,
+                              void* hip_stream);
+int spion_heads_attn_bwd_with(const void* qkv, const void* S, const void* dS, const float* LSE, void* dqkv, void* dtable,
+                              const int32_t* row_ptr, const int32_t* col_idx, const int32_t* col_ptr, const int32_t* row_idx, int32_t nnzb,
+                              const spion_attn_params* p, const spion_attn_extras* x, void* workspace, size_t workspace_bytes,
+                              void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

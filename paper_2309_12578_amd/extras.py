@@ -15,7 +15,7 @@ from . import binding as _b
 @dataclasses.dataclass(frozen=True)
 class RelativeBuckets:
     """Which bucket of a bias table each distance key - query has: `map[d + length - 1]` for -length < d < length, uint8.  Any map
-    will do; `relative_buckets` makes the usual one.  A program makes it once for a length and keeps it."""
+    will do; `relative_buckets` makes the usual one.  A program makes it once, for its longest sequences, and keeps it."""
     length: int
     count: int
     map: torch.Tensor
@@ -67,12 +67,17 @@ def relative_buckets(length: int, count: int = 32, max_distance: int = 128, bidi
     return RelativeBuckets(length, count, torch.from_numpy(bucket.astype(np.uint8)).to(device))
 
 
-def _map_for(table: torch.Tensor, buckets: Optional[RelativeBuckets]) -> torch.Tensor:
+def _map_for(table: torch.Tensor, buckets: Optional[RelativeBuckets], length: Optional[int] = None) -> torch.Tensor:
+    """The buckets of the distances that sequences of `length` tokens have."""
     if not isinstance(buckets, RelativeBuckets):
         raise ValueError("a bias table needs its RelativeBuckets")
     if table.shape[:1] != (buckets.count,):
         raise ValueError("the bias table must have a row for each bucket")
-    return buckets.map
+    if length is None or length == buckets.length:
+        return buckets.map
+    if length > buckets.length:
+        raise ValueError("the buckets do not reach over sequences of %d tokens" % length)
+    return buckets.map[buckets.length - length:buckets.length + length - 1]
 
 
 def relative_bias(table: torch.Tensor, buckets: RelativeBuckets, q_len: int, k_len: int, q_start: int = 0) -> torch.Tensor:
