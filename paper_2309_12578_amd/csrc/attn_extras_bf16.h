@@ -148,15 +148,6 @@ __device__ __forceinline__ unsigned tile_range(int row0, int length, int row_len
     return rows >= BS ? 0xffffffffu : rows <= 0 ? 0u : (unsigned)rows * (unsigned)row_len * (unsigned)sizeof(bf16_t);
 }
 
-// The kernel's arguments once more, from memory: what is used at its end only would otherwise sit in scalar registers over the
-// loop, of which there are too few (7 to 61 of them were spilled).
-template <typename Args>
-__device__ __forceinline__ const __attribute__((address_space(4))) Args& args_again() {
-    auto p = reinterpret_cast<const __attribute__((address_space(4))) Args*>(reinterpret_cast<uintptr_t>(__builtin_amdgcn_kernarg_segment_ptr()));
-    asm volatile("" : "+s"(p));
-    return *p;
-}
-
 }  // namespace
 
 }  // namespace spion

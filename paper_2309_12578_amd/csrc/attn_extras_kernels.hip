@@ -5,16 +5,18 @@
 //   dV = (c M . P)^T dO, dQ = scale dS K, dK = scale dS^T Q, dT[b][head] = sum of dS over the elements of bucket b
 // Queries and keys from the length on: O = 0, LSE = -inf, gradients 0; nothing of theirs is added up.
 //
-// The kernels of this file take every type and block size: a workgroup of four waves has 16 rows, whose 16-row tiles of the other
-// side the waves take in turn, straight from memory into registers (layouts as in attn_kernels.hip).
+// The kernels of this file are for fp32 and block 16: a workgroup of four waves has 16 or 32 rows, whose 16-row tiles of the other
+// side the waves take in turn, straight from memory into registers (layouts, order and pieces as in attn_kernels.hip).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
 #include <algorithm>
+#include <climits>
 
 #include "attn_bf16_tiles.h"
 #include "attn_common.h"
 #include "attn_extras.h"
+#include "attn_key_items.h"
 #include "attn_register_tiles.h"
 #include "spion_internal.h"
 #include "table_grad.h"
@@ -48,319 +50,572 @@ __device__ __forceinline__ void zero_cols_from(typename Elem<T>::Quad (&v)[4], i
         if (row0 + i >= length) v[i] = typename Elem<T>::Quad{};
 }
 
-template <typename T>
+// A workgroup's 16 NQ rows, whose tiles its four waves share.
+template <typename T, int BS, int NQ>
 struct Tiles {
     static constexpr int KT = sizeof(T) == 2 ? 2 : 1;   // tiles per step: a bf16 MFMA contracts over 32 rows
-    static constexpr int NDC = kD / Elem<T>::KC;
+    static constexpr int NDC = kD / Elem<T>::KC, TPB = BS / 16, OWN = 16 * NQ, PARTS = BS / OWN;
 };
 
 constexpr int kWaves = 4;
 
-// bias / scale of query q and the keys k .. k + 3 (or, KEYS, of key k and the queries q .. q + 3)
+// The buckets of query q and the keys k .. k + 3 (or, KEYS, of key k and the queries q .. q + 3), and their biases / scale
 template <bool KEYS>
-__device__ __forceinline__ f32x4 bias_of(const Extras& x, const float* tab, int q, int k, int L) {
+__device__ __forceinline__ unsigned buckets_of(const Extras& x, int q, int k, int L) {
+    return x.table ? (unsigned)*reinterpret_cast<const u32_any*>(x.bucket_of + (k - q - (KEYS ? 3 : 0) + L - 1)) : 0u;
+}
+template <bool KEYS>
+__device__ __forceinline__ f32x4 bias_of(const Extras& x, const float* tab, unsigned b) {
     if (!x.table) return f32x4{0.f, 0.f, 0.f, 0.f};
-    const unsigned b = *reinterpret_cast<const u32_any*>(x.bucket_of + (k - q - (KEYS ? 3 : 0) + L - 1));
     f32x4 v;
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = tab[bucket_index(x, b >> (KEYS ? 24 - 8 * i : 8 * i) & 255u)];
     return v;
 }
 
+// The rows that a workgroup of the forward or of the query side has: of helpers (cut.groups, which come first) a piece of a long row, of the others a
+// row's first piece or all of it, by length where sort_rows.  false: none.
+template <int PARTS>
+__device__ __forceinline__ bool row_of_group(const int* __restrict__ row_ptr, int nb, int BH, const RowCut& cut, int sort_rows, int id, int lane, int& bh,
+                                             int& I, int& part, RowPieces& cuts, int& piece) {
+    cuts = {0, 1, 0, 0};
+    piece = 0;
+    const int at = (id >> 3) / PARTS * 8 + (id & 7);   // a row's workgroups on one XCD
+    part = (id >> 3) % PARTS;
+    if (id < cut.groups) {
+        const int want = at / BH;
+        if (want >= cut.helpers) return false;
+        cuts = row_pieces<false>(row_ptr, nb, cut, want, lane);
+        if (cuts.row < 0) return false;
+        bh = at % BH;
+        I = cuts.row;
+        piece = want - cuts.first + 1;
+        return true;
+    }
+    if (sort_rows) {
+        const int row = at - cut.groups / PARTS;   // (a multiple of 8)
+        if (row >= BH * nb) return false;
+        const ItemOfHead mine = rows_in_order(row_ptr, nb, BH, row, lane);
+        bh = mine.head;
+        I = mine.item;
+        return true;
+    }
+    const int item = item_of_group(id - cut.groups, BH * nb * PARTS);
+    if (item < 0) return false;
+    bh = item / (nb * PARTS);
+    I = item % (nb * PARTS) / PARTS;
+    part = item % PARTS;
+    return true;
+}
+// The piece of a row of more than cut.longest blocks from jb on: which blocks it has.
+__device__ __forceinline__ void piece_of_row(const int* __restrict__ row_ptr, int nb, const RowCut& cut, int I, int lane, RowPieces& cuts, int piece, int& jb,
+                                             int& n) {
+    if (piece == 0) cuts = row_pieces<true>(row_ptr, nb, cut, I, lane);
+    const int from = piece * n / cuts.count;
+    n = (piece + 1) * n / cuts.count - from;
+    jb += from;
+}
+
 }  // namespace
 
 // ------------------------------------------------------------------------------------------------
-// forward: workgroup = (head, 16 query rows)
+// forward: workgroup = (head, Tiles::OWN query rows)
 // ------------------------------------------------------------------------------------------------
-template <typename T, int BS, bool DROP>
+template <typename T, int BS, int NQ, bool DROP>
 __global__ __launch_bounds__(kWaves * 64, 2) void attn_fwd_with_kernel(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, T* __restrict__ O, float* __restrict__ LSE,
-    const int* __restrict__ row_ptr, const int* __restrict__ col_idx, Extras x, int L, int nb, int total, float scale_log2) {
+    const int* __restrict__ row_ptr, const int* __restrict__ col_idx, Extras x, RowCut cut, int BH, int L, int nb, int sort_rows, float scale_log2) {
     typedef typename Elem<T>::Frag Frag;
     typedef typename Elem<T>::Quad Quad;
-    constexpr int KT = Tiles<T>::KT, NDC = Tiles<T>::NDC, TPB = BS / 16, STRIDE = kWaves * KT;
-    __shared__ __attribute__((aligned(16))) float o_s[kWaves][16 * kPatchLd];
-    __shared__ float m_s[kWaves][16], l_s[kWaves][16], tab[Extras::kMaxBuckets];
+    typedef Tiles<T, BS, NQ> S;
+    constexpr int KT = S::KT, NDC = S::NDC, STRIDE = kWaves * KT;
+    __shared__ int flag;
+    __shared__ __attribute__((aligned(16))) float o_s[kWaves][S::OWN * kPatchLd];
+    __shared__ float m_s[kWaves][S::OWN], l_s[kWaves][S::OWN], tab[Extras::kMaxBuckets];
 
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     if (DROP && blockIdx.x == 0 && tid < 2 && x.rng_used) x.rng_used[tid] = x.rng[tid];
-    const int item = item_of_group(blockIdx.x, total);
-    if (item < 0) return;
-    const int bh = item / (nb * TPB), I = item % (nb * TPB) / TPB, row0 = I * BS + item % TPB * 16;
+    int bh, I, part, piece, id = blockIdx.x;
+    RowPieces cuts;
+    if (!row_of_group<S::PARTS>(row_ptr, nb, BH, cut, sort_rows, id, lane, bh, I, part, cuts, piece)) return;
+    const int row0 = I * BS + part * S::OWN;
     const size_t head = (size_t)bh * L * kD;
     const int length = length_of(x, bh, L);
     if (x.table) load_bias_table(tab, x, bh % x.H, tid, kWaves * 64);
     __syncthreads();
 
-    const int* cols = col_idx + row_ptr[I];
-    const int n = row0 < length ? blocks_below<BS>(cols, row_ptr[I + 1] - row_ptr[I], length, lane) : 0;
-    const int nt = n * TPB;
+    int jb = row_ptr[I], n = row_ptr[I + 1] - jb;
+    if (n > cut.longest) piece_of_row(row_ptr, nb, cut, I, lane, cuts, piece, jb, n);
+    const int* cols = col_idx + jb;
+    n = row0 < length ? blocks_below<BS>(cols, n, length, lane) : 0;
+    const int nt = n * S::TPB;
     const int cols64 = n > 0 ? cols[lane < n ? lane : n - 1] : 0;
-    auto key0 = [&](int t) { return list_at(cols, cols64, t / TPB) * BS + t % TPB * 16; };
-    Frag qf[NDC];
-    const int query = row0 + r;
-    if (query < length) load_rows<T>(qf, Q + head + (size_t)row0 * kD, r, g);
-    else clear(qf);
+    auto key0 = [&](int t) { return list_at(cols, cols64, t / S::TPB) * BS + t % S::TPB * 16; };
+    Frag qf[NQ][NDC];
+#pragma unroll
+    for (int h = 0; h < NQ; ++h) {
+        if (row0 + 16 * h + r < length) load_rows<T>(qf[h], Q + head + (size_t)(row0 + 16 * h) * kD, r, g);
+        else clear(qf[h]);
+    }
     [[maybe_unused]] ScoreDraws draws(x.rng, x.stream, bh);
+    // K of tiles t, t + 1, .. and the buckets (past the end: tile t once more, which counts nothing)
+    auto load_k = [&](Frag (&k)[KT][NDC], unsigned (&buckets)[NQ][KT], int t) {
+#pragma unroll
+        for (int u = 0; u < KT; ++u) {
+            const int k0 = key0(t + u < nt ? t + u : t);
+            load_rows<T>(k[u], K + head + (size_t)k0 * kD, r, g);
+#pragma unroll
+            for (int h = 0; h < NQ; ++h) buckets[h][u] = buckets_of<false>(x, row0 + 16 * h + r, k0 + 4 * g, L);
+        }
+    };
 
-    float m = kLowest, limit = -INFINITY, lsum = 0.f;
-    f32x4 oacc[1][4];
-    clear_acc<1>(oacc);
-    for (int t = wave * KT; t < nt; t += STRIDE) {
-        Frag kf[KT][NDC];
+    float m[NQ], limit[NQ], lsum[NQ];
+    f32x4 oacc[NQ][4];
+    clear_acc<NQ>(oacc);
+#pragma unroll
+    for (int h = 0; h < NQ; ++h) {
+        m[h] = kLowest;
+        limit[h] = -INFINITY;
+        lsum[h] = 0.f;
+    }
+    auto step = [&](Frag (&kf)[KT][NDC], const unsigned (&buckets)[NQ][KT], Frag (&knext)[KT][NDC], unsigned (&bnext)[NQ][KT], int t) {
         Quad vc[KT][4];
-        f32x4 s[KT];
+        f32x4 s[NQ][KT];
         int k0[KT];
 #pragma unroll
         for (int u = 0; u < KT; ++u) {
             k0[u] = key0(t + u < nt ? t + u : t);
-            const size_t at = head + (size_t)k0[u] * kD;
-            load_rows<T>(kf[u], K + at, r, g);
-            load_cols<T>(vc[u], V + at, r, g);
-            s[u] = bias_of<false>(x, tab, query, k0[u] + 4 * g, L);
+            load_cols<T>(vc[u], V + head + (size_t)k0[u] * kD, r, g);
+        }
+        if (t + STRIDE < nt) load_k(knext, bnext, t + STRIDE);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < KT; ++u) {
             if (k0[u] + 16 > length) {
                 zero_rows_from<T>(kf[u], k0[u] + r >= length);
                 zero_cols_from<T>(vc[u], k0[u] + 4 * g, length);
             }
             if (u > 0 && t + u >= nt) clear(vc[u]);
         }
-        float mx = -INFINITY;
+        float mx[NQ];
+        bool above = false;
 #pragma unroll
-        for (int u = 0; u < KT; ++u) {
+        for (int h = 0; h < NQ; ++h) {
+            mx[h] = -INFINITY;
 #pragma unroll
-            for (int c = 0; c < NDC; ++c) s[u] = mma_d(s[u], kf[u][c], qf[c]);   // S^T: [key 4 g + i][query r]
-            const bool there = u == 0 || t + u < nt;
+            for (int u = 0; u < KT; ++u) {
+                s[h][u] = bias_of<false>(x, tab, buckets[h][u]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (!there || k0[u] + 4 * g + i >= length) s[u][i] = -INFINITY;
-                mx = fmaxf(mx, s[u][i]);
+                for (int c = 0; c < NDC; ++c) s[h][u] = mma_d(s[h][u], kf[u][c], qf[h][c]);   // S^T: [key 4 g + i][query r]
+                const bool there = u == 0 || t + u < nt;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (!there || k0[u] + 4 * g + i >= length) s[h][u][i] = -INFINITY;
+                    mx[h] = fmaxf(mx[h], s[h][u][i]);
+                }
+            }
+            above |= mx[h] * scale_log2 > limit[h];
+        }
+        if (__any(above)) {
+#pragma unroll
+            for (int h = 0; h < NQ; ++h) {
+                const float m_new = fmaxf(m[h], group_max(mx[h]) * scale_log2);
+                const float alpha = exp2f(m[h] - m_new);
+                m[h] = m_new;
+                limit[h] = m_new + kRescaleSlack;
+                lsum[h] *= alpha;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) oacc[h][e] *= alpha;
             }
         }
-        if (__any(mx * scale_log2 > limit)) {
-            const float m_new = fmaxf(m, group_max(mx) * scale_log2);
-            const float alpha = exp2f(m - m_new);
-            m = m_new;
-            limit = m_new + kRescaleSlack;
-            lsum *= alpha;
+        Quad pq[NQ][KT];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) oacc[0][e] *= alpha;
-        }
-        Quad pq[1][KT];
+        for (int h = 0; h < NQ; ++h)
 #pragma unroll
-        for (int u = 0; u < KT; ++u) {
-            f32x4 p;
+            for (int u = 0; u < KT; ++u) {
+                f32x4 p;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                p[i] = exp2f(fmaf(s[u][i], scale_log2, -m));
-                lsum += p[i];
+                for (int i = 0; i < 4; ++i) {
+                    p[i] = exp2f(fmaf(s[h][u][i], scale_log2, -m[h]));
+                    lsum[h] += p[i];
+                }
+                if constexpr (DROP) {
+                    unsigned d[4];
+                    query_draws(draws, row0 + 16 * h + r, k0[u] + 4 * g, d);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p[i] = d[i] < x.threshold ? 0.f : p[i];
+                }
+                pq[h][u] = to_quad<T>(p);
             }
-            if constexpr (DROP) {
-                unsigned d[4];
-                query_draws(draws, query, k0[u] + 4 * g, d);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) p[i] = d[i] < x.threshold ? 0.f : p[i];
-            }
-            pq[0][u] = to_quad<T>(p);
-        }
         mma_cols(oacc, vc, pq);   // O^T += V^T P^T
+    };
+    {
+        Frag ka[KT][NDC], kb[KT][NDC];
+        unsigned ba[NQ][KT], bb[NQ][KT];
+        int t = wave * KT;
+        if (t < nt) load_k(ka, ba, t);
+        for (; t < nt; t += 2 * STRIDE) {
+            step(ka, ba, kb, bb, t);
+            if (t + STRIDE < nt) step(kb, bb, ka, ba, t + STRIDE);
+        }
     }
 
     // the waves' shares of each row: rescaled to the row's largest m and added up in wave order
-    put_patch<1>(&o_s[wave][0], oacc, r, g);
-    const float l = group_sum(lsum);
-    if (g == 0) {
-        m_s[wave][r] = m;
-        l_s[wave][r] = l;
+    put_patch<NQ>(&o_s[wave][0], oacc, r, g);
+#pragma unroll
+    for (int h = 0; h < NQ; ++h) {
+        const float l = group_sum(lsum[h]);
+        if (g == 0) {
+            m_s[wave][16 * h + r] = m[h];
+            l_s[wave][16 * h + r] = l;
+        }
     }
     __syncthreads();
-    const int q = tid >> 4, d = (tid & 15) * 4;
-    float mm = m_s[0][q], ll = 0.f;
+    auto merged = [&](int q, int d, float& mm, float& l) {
+        mm = m_s[0][q];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) mm = fmaxf(mm, m_s[w][q]);
-    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int w = 1; w < kWaves; ++w) mm = fmaxf(mm, m_s[w][q]);
+        f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+        l = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        const float a = exp2f(m_s[w][q] - mm);
-        ll += l_s[w][q] * a;
-        o += *reinterpret_cast<const f32x4*>(&o_s[w][q * kPatchLd + d]) * a;
+        for (int w = 0; w < kWaves; ++w) {
+            const float a = exp2f(m_s[w][q] - mm);
+            l += l_s[w][q] * a;
+            o += *reinterpret_cast<const f32x4*>(&o_s[w][q * kPatchLd + d]) * a;
+        }
+        return o;
+    };
+    // [head][slot][part]: the rows' numbers, then their references and sums
+    constexpr int kPart = S::OWN * (kD + 2);
+    const float* parts = nullptr;
+    if (cuts.count > 1) {   // a long row in pieces, as in the plain kernel
+        const size_t slot = ((size_t)bh * cut.slots + cuts.slot) * S::PARTS + part;
+        float* const mine = cut.parts + slot * kPart + (size_t)piece * (S::PARTS * kPart);
+        parts = cut.parts + slot * kPart;
+#pragma unroll
+        for (int h = 0; h < NQ; ++h) {
+            const int q = 16 * h + (tid >> 4), d = (tid & 15) * 4;
+            float mm, l;
+            const f32x4 o = merged(q, d, mm, l);
+            put_shared(mine + q * kD + d, o[0], o[1]);
+            put_shared(mine + q * kD + d + 2, o[2], o[3]);
+            if (d == 0) put_shared(mine + S::OWN * kD + 2 * q, mm, l);
+        }
+        if (!last_to_arrive(cut.counters + slot, cut.tag, cuts.count, &flag)) return;
     }
-    const bool empty = !(ll > 0.f) && ll == ll;
-    o = empty || row0 + q >= length ? f32x4{0.f, 0.f, 0.f, 0.f} : o * ((DROP ? x.keep_scale : 1.f) / ll);
-    store_quad<T>(O + head + (size_t)(row0 + q) * kD + d, o);
-    if (d == 0) LSE[(size_t)bh * L + row0 + q] = empty || row0 + q >= length ? -INFINITY : (mm + log2f(ll)) * kLn2;
+#pragma unroll
+    for (int h = 0; h < NQ; ++h) {
+        const int q = 16 * h + (tid >> 4), d = (tid & 15) * 4;
+        float mm, l;
+        f32x4 o;
+        if (parts) {   // (a reference is kLowest at least)
+            mm = -INFINITY;
+            l = 0.f;
+            o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+            for (int c = 0; c < cuts.count; ++c) {
+                const float* const p = parts + (size_t)c * (S::PARTS * kPart);
+                const float2 lo = get_shared(p + q * kD + d), hi = get_shared(p + q * kD + d + 2);
+                const float2 ml = get_shared(p + S::OWN * kD + 2 * q);
+                const float m_new = fmaxf(mm, ml.x), a = exp2f(mm - m_new), b = exp2f(ml.x - m_new);
+                mm = m_new;
+                l = l * a + ml.y * b;
+                o = o * a + f32x4{lo.x, lo.y, hi.x, hi.y} * b;
+            }
+        } else {
+            o = merged(q, d, mm, l);
+        }
+        const bool empty = (!(l > 0.f) && l == l) || row0 + q >= length;
+        o = empty ? f32x4{0.f, 0.f, 0.f, 0.f} : o * ((DROP ? x.keep_scale : 1.f) / l);
+        store_quad<T>(O + head + (size_t)(row0 + q) * kD + d, o);
+        if (d == 0) LSE[(size_t)bh * L + row0 + q] = empty ? -INFINITY : (mm + log2f(l)) * kLn2;
+    }
 }
 
+// The key side's work items, see attn_key_items.h.
+struct ColumnCut {
+    int chunk, n_first, n_items, n_slots, by_length;   // items per head that come before the rows, and all
+    unsigned long long tag;
+    unsigned long long* counters;   // one per slot and 16 rows
+    float* parts;
+};
+
 // ------------------------------------------------------------------------------------------------
-// backward: workgroup = (head, 16 rows of a block row) on the query side, (head, 16 keys of a block column) on the key side.
+// backward: workgroup = (head, Tiles::OWN rows of a block row) on the query side, (head, as many keys of a block column) on the key side.
 // The sides share no data; all sums in fixed order.  The query side leaves, for the table's gradient, the sums over the 31 diagonals of each
 // 16 x 16 tile of dS in slices[head][kept block][query tile][key tile][32].
 // ------------------------------------------------------------------------------------------------
-template <typename T, int BS, bool DROP>
-__global__ __launch_bounds__(kWaves * 64, 2) void attn_bwd_with_kernel(
-    const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, const T* __restrict__ O, const T* __restrict__ dO,
-    const float* __restrict__ LSE, T* __restrict__ dQ, T* __restrict__ dK, T* __restrict__ dV, const int* __restrict__ row_ptr,
-    const int* __restrict__ col_idx, const int* __restrict__ col_ptr, const int* __restrict__ row_idx, Extras x, int L, int nb, int nnzb,
-    int total, float scale, float scale_log2) {
+template <typename T>
+struct BwdOfRows {
+    const T *Q, *K, *V, *O, *dO;
+    const float* LSE;
+    T *dQ, *dK, *dV;
+    const int *row_ptr, *col_idx, *col_ptr, *row_idx;
+    Extras x;
+    RowCut cut;
+    ColumnCut columns;
+    int BH, L, nb, nnzb, sort_rows;
+    float scale, scale_log2;
+};
+
+template <typename T, int BS, int NQ, int W, bool DROP>
+__global__ __launch_bounds__(W * 64, 2) void attn_bwd_with_kernel(const BwdOfRows<T> a) {
+    const T *__restrict__ const Q = a.Q, *__restrict__ const K = a.K, *__restrict__ const V = a.V, *__restrict__ const O = a.O, *__restrict__ const dO = a.dO;
+    const float* __restrict__ const LSE = a.LSE;
+    const Extras& x = a.x;
+    const int L = a.L;
+    const float scale_log2 = a.scale_log2;
     typedef typename Elem<T>::Frag Frag;
     typedef typename Elem<T>::Quad Quad;
     typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-    constexpr int KT = Tiles<T>::KT, NDC = Tiles<T>::NDC, TPB = BS / 16, STRIDE = kWaves * KT;
+    typedef Tiles<T, BS, NQ> S;
+    constexpr int KT = S::KT, NDC = S::NDC, TPB = S::TPB, STRIDE = W * KT;
     constexpr int kDiag = 48;   // floats per lane group and wave: places of distance 16 kt + 4 g - p, behind each other
-    __shared__ __attribute__((aligned(16))) float acc_s[kWaves][16 * kPatchLd];
-    __shared__ float tab[Extras::kMaxBuckets], diag_s[kWaves][4][kDiag];
+    __shared__ __attribute__((aligned(16))) float acc_s[W][S::OWN * kPatchLd];
+    __shared__ float tab[Extras::kMaxBuckets], diag_s[W][4][kDiag];
+    __shared__ int flag;
 
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     if (blockIdx.x == 0 && x.counters)
-        for (int h = tid; h < x.H; h += kWaves * 64) x.counters[h * Extras::kCounterStride] = 0u;
-    const int half = (total + 7) / 8 * 8;   // workgroups of a side
-    const bool key_side = (int)blockIdx.x >= half;
-    const int item = item_of_group(key_side ? blockIdx.x - half : blockIdx.x, total);
-    if (item < 0) return;
-    const int bh = item / (nb * TPB), block = item % (nb * TPB) / TPB, sub = item % TPB, row0 = block * BS + sub * 16;
+        for (int h = tid; h < x.H; h += W * 64) x.counters[h * Extras::kCounterStride] = 0u;
+    const RowCut& cut = a.cut;
+    const ColumnCut& columns = a.columns;
+    const int BH = a.BH, nb = a.nb, sort_rows = a.sort_rows;
+    const int *__restrict__ const row_ptr = a.row_ptr, *__restrict__ const col_ptr = a.col_ptr;
+    // helpers, chunks of columns and long columns, rows, the other columns
+    const int first = BH * columns.n_first * S::PARTS, first_groups = (first + 7) & ~7;
+    const int row_groups = sort_rows ? S::PARTS * ((BH * nb + 7) & ~7) : (BH * nb * S::PARTS + 7) & ~7;
+    int id = (int)blockIdx.x, bh, block, part, piece = 0;
+    RowPieces cuts = {0, 1, 0, 0};
+    KeyItem it = {0, 0, 0, -1, 0, 1};
+    const bool key_side = id >= cut.groups && (id < cut.groups + first_groups || id >= cut.groups + first_groups + row_groups);
+    if (key_side) {   // the items of all heads together, longest first; heads keep to an XCD where that shares them out evenly
+        id -= cut.groups;
+        int from = 0;
+        if (id >= first_groups) {
+            id -= first_groups + row_groups;
+            from = columns.n_first;
+        }
+        int xcd = 0, heads = BH;
+        if ((BH & 7) == 0) {
+            xcd = id & 7;
+            heads = BH >> 3;
+            id >>= 3;
+        }
+        bh = xcd * heads + id % heads;
+        part = id / heads % S::PARTS;
+        const int idx = from + id / heads / S::PARTS;
+        if (idx >= (from ? columns.n_items : columns.n_first)) return;
+        it = key_item_lookup(col_ptr, nb, columns.chunk, columns.by_length, idx, lane);
+        if (it.J < 0) return;
+        block = it.J;
+    } else {
+        if (id >= cut.groups) id -= first_groups;
+        if (!row_of_group<S::PARTS>(row_ptr, nb, BH, cut, sort_rows, id, lane, bh, block, part, cuts, piece)) return;
+    }
+    const int sub = part * NQ, row0 = block * BS + sub * 16;
     const size_t head = (size_t)bh * L * kD, vec = (size_t)bh * L;
     const int length = length_of(x, bh, L);
-    if (x.table) load_bias_table(tab, x, bh % x.H, tid, kWaves * 64);
+    if (x.table) load_bias_table(tab, x, bh % x.H, tid, W * 64);
     if (!key_side && x.slices)
-        for (int i = tid; i < kWaves * 4 * kDiag; i += kWaves * 64) (&diag_s[0][0][0])[i] = 0.f;
+        for (int i = tid; i < W * 4 * kDiag; i += W * 64) (&diag_s[0][0][0])[i] = 0.f;
     __syncthreads();
     [[maybe_unused]] ScoreDraws draws(x.rng, x.stream, bh);
     const float keep = DROP ? x.keep_scale : 1.f;
-    const int own = row0 + r;
 
-    auto merged = [&]() {
-        const int o = (tid >> 4) * kPatchLd + (tid & 15) * 4;
+    constexpr int kAtOnce = 4 * W;   // rows that all threads have together, 4 columns each
+    auto merged = [&](int p) {       // rows p + tid / 16
+        const int q = p + (tid >> 4), o = q * kPatchLd + (tid & 15) * 4;
         f32x4 v = *reinterpret_cast<const f32x4*>(&acc_s[0][o]);
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) v += *reinterpret_cast<const f32x4*>(&acc_s[w][o]);
-        return row0 + (tid >> 4) < length ? v : f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int w = 1; w < W; ++w) v += *reinterpret_cast<const f32x4*>(&acc_s[w][o]);
+        return row0 + q < length ? v : f32x4{0.f, 0.f, 0.f, 0.f};
     };
-    const size_t out = head + (size_t)(row0 + (tid >> 4)) * kD + (tid & 15) * 4;
-    const int* list = (key_side ? row_idx : col_idx) + (key_side ? col_ptr : row_ptr)[block];
-    const int n_list = (key_side ? col_ptr : row_ptr)[block + 1] - (key_side ? col_ptr : row_ptr)[block];
+    const int out = (sub * 16 + (tid >> 4)) * kD + (tid & 15) * 4;   // in the block
+    int entry0 = key_side ? it.kb : row_ptr[block], n_list = key_side ? it.ke - it.kb : row_ptr[block + 1] - entry0;
+    if (!key_side && n_list > cut.longest) piece_of_row(row_ptr, nb, cut, block, lane, cuts, piece, entry0, n_list);
+    const int* list = (key_side ? a.row_idx : a.col_idx) + entry0;
     const int n = row0 < length ? blocks_below<BS>(list, n_list, length, lane) : 0;
     const int nt = n * TPB;
     const int list64 = n > 0 ? list[lane < n ? lane : n - 1] : 0;
     auto tile0 = [&](int t) { return list_at(list, list64, t / TPB) * BS + t % TPB * 16; };
 
     if (!key_side) {
-        Frag qf[NDC], dof[NDC];
-        float delta = 0.f, lse2 = INFINITY;
-        if (own < length) {
-            Frag of[NDC];
-            const size_t at = head + (size_t)row0 * kD;
-            load_rows<T>(qf, Q + at, r, g);
-            load_rows<T>(dof, dO + at, r, g);
-            load_rows<T>(of, O + at, r, g);
-            lse2 = LSE[vec + own] * kLog2e;
-            if (lse2 == -INFINITY) lse2 = INFINITY;   // a row that keeps nothing
+        Frag qf[NQ][NDC], dof[NQ][NDC];
+        float delta[NQ], lse2[NQ];
 #pragma unroll
-            for (int c = 0; c < NDC; ++c)
+        for (int h = 0; h < NQ; ++h) {
+            delta[h] = 0.f;
+            lse2[h] = INFINITY;
+            if (row0 + 16 * h + r < length) {
+                Frag of[NDC];
+                const size_t at = head + (size_t)(row0 + 16 * h) * kD;
+                load_rows<T>(qf[h], Q + at, r, g);
+                load_rows<T>(dof[h], dO + at, r, g);
+                load_rows<T>(of, O + at, r, g);
+                lse2[h] = LSE[vec + row0 + 16 * h + r] * kLog2e;
+                if (lse2[h] == -INFINITY) lse2[h] = INFINITY;   // a row that keeps nothing
 #pragma unroll
-                for (int e = 0; e < Elem<T>::EPL; ++e) delta = fmaf((float)dof[c][e], (float)of[c][e], delta);
-        } else {
-            clear(qf);
-            clear(dof);
+                for (int c = 0; c < NDC; ++c)
+#pragma unroll
+                    for (int e = 0; e < Elem<T>::EPL; ++e) delta[h] = fmaf((float)dof[h][c][e], (float)of[c][e], delta[h]);
+            } else {
+                clear(qf[h]);
+                clear(dof[h]);
+            }
+            delta[h] = group_sum(delta[h]);
         }
-        delta = group_sum(delta);
+        auto slice = [&](int entry, int h, int key_tile) {
+            return a.x.slices + ((((size_t)bh * a.nnzb + entry0 + entry) * TPB + sub + h) * TPB + key_tile) * 32;
+        };
         if (x.slices)   // what is not computed
-            for (int e = n * TPB + tid; e < n_list * TPB; e += kWaves * 64)
-                x.slices[((((size_t)bh * nnzb + row_ptr[block] + e / TPB) * TPB + sub) * TPB + e % TPB) * 32 + 31] = __builtin_bit_cast(float, kNoSlice);
-        f32x4 dq[1][4];
-        clear_acc<1>(dq);
+            for (int e = n * TPB + tid; e < n_list * TPB; e += W * 64)
+#pragma unroll
+                for (int h = 0; h < NQ; ++h) slice(e / TPB, h, e % TPB)[31] = __builtin_bit_cast(float, kNoSlice);
+        f32x4 dq[NQ][4];
+        clear_acc<NQ>(dq);
         for (int t = wave * KT; t < nt; t += STRIDE) {
-            Quad kc[KT][4], dsq[1][KT];
+            Quad kc[KT][4], dsq[NQ][KT];
+            Frag kf[KT][NDC], vf[KT][NDC];
+            unsigned buckets[NQ][KT];
+            int k0[KT];
+#pragma unroll
+            for (int u = 0; u < KT; ++u) {   // past the end: tile t once more, which counts nothing
+                k0[u] = tile0(u == 0 || t + u < nt ? t + u : t);
+                const size_t at = head + (size_t)k0[u] * kD;
+                load_rows<T>(kf[u], K + at, r, g);
+                load_rows<T>(vf[u], V + at, r, g);
+                load_cols<T>(kc[u], K + at, r, g);
+#pragma unroll
+                for (int h = 0; h < NQ; ++h) buckets[h][u] = buckets_of<false>(x, row0 + 16 * h + r, k0[u] + 4 * g, L);
+            }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int u = 0; u < KT; ++u) {
                 const bool there = u == 0 || t + u < nt;
-                const int k0 = tile0(there ? t + u : t);
-                const size_t at = head + (size_t)k0 * kD;
-                Frag kf[NDC], vf[NDC];
-                load_rows<T>(kf, K + at, r, g);
-                load_rows<T>(vf, V + at, r, g);
-                load_cols<T>(kc[u], K + at, r, g);
-                f32x4 s = bias_of<false>(x, tab, own, k0 + 4 * g, L), dp = f32x4{0.f, 0.f, 0.f, 0.f};
-                if (k0 + 16 > length) {
-                    zero_rows_from<T>(kf, k0 + r >= length);
-                    zero_rows_from<T>(vf, k0 + r >= length);
-                    zero_cols_from<T>(kc[u], k0 + 4 * g, length);
+                if (k0[u] + 16 > length) {
+                    zero_rows_from<T>(kf[u], k0[u] + r >= length);
+                    zero_rows_from<T>(vf[u], k0[u] + r >= length);
+                    zero_cols_from<T>(kc[u], k0[u] + 4 * g, length);
                 }
                 if (!there) clear(kc[u]);
 #pragma unroll
-                for (int c = 0; c < NDC; ++c) {
-                    s = mma_d(s, kf[c], qf[c]);      // S^T = K Q^T
-                    dp = mma_d(dp, vf[c], dof[c]);   // dP^T = V dO^T
-                }
-                unsigned d[4] = {};
-                if constexpr (DROP) query_draws(draws, own, k0 + 4 * g, d);
-                f32x4 ds;
+                for (int h = 0; h < NQ; ++h) {
+                    f32x4 s = bias_of<false>(x, tab, buckets[h][u]), dp = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const bool masked = !there || k0 + 4 * g + i >= length;
-                    const float p = masked ? 0.f : exp2f(fmaf(s[i], scale_log2, -lse2));
-                    const float dpi = DROP && d[i] < x.threshold ? 0.f : dp[i] * keep;
-                    ds[i] = p * (dpi - delta);
-                }
-                dsq[0][u] = to_quad<T>(ds);
-                if (x.slices && there) {
-                    const f32x4 one[1] = {ds};
-                    float du[2];
-                    diagonal_sums<1>(one, du);
-                    diag_s[wave][g][4 * g - r + 15] = du[0];
-                    diag_s[wave][g][4 * g - r + 31] = du[1];
-                    __builtin_amdgcn_wave_barrier();
-                    if (lane < 32) {
-                        const float v = diag_s[wave][0][lane] + diag_s[wave][1][lane] + diag_s[wave][2][lane] + diag_s[wave][3][lane];
-                        const size_t entry = (size_t)bh * nnzb + row_ptr[block] + (t + u) / TPB;
-                        x.slices[((entry * TPB + sub) * TPB + (t + u) % TPB) * 32 + lane] = lane < 31 ? v : __builtin_bit_cast(float, k0 - row0);
+                    for (int c = 0; c < NDC; ++c) {
+                        s = mma_d(s, kf[u][c], qf[h][c]);      // S^T = K Q^T
+                        dp = mma_d(dp, vf[u][c], dof[h][c]);   // dP^T = V dO^T
                     }
-                    __builtin_amdgcn_wave_barrier();
+                    unsigned d[4] = {};
+                    if constexpr (DROP) query_draws(draws, row0 + 16 * h + r, k0[u] + 4 * g, d);
+                    f32x4 ds;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const bool masked = !there || k0[u] + 4 * g + i >= length;
+                        const float p = masked ? 0.f : exp2f(fmaf(s[i], scale_log2, -lse2[h]));
+                        const float dpi = DROP && d[i] < x.threshold ? 0.f : dp[i] * keep;
+                        ds[i] = p * (dpi - delta[h]);
+                    }
+                    dsq[h][u] = to_quad<T>(ds);
+                    if (x.slices && there) {
+                        const f32x4 one[1] = {ds};
+                        float du[2];
+                        diagonal_sums<1>(one, du);
+                        diag_s[wave][g][4 * g - r + 15] = du[0];
+                        diag_s[wave][g][4 * g - r + 31] = du[1];
+                        __builtin_amdgcn_wave_barrier();
+                        if (lane < 32) {
+                            const float v = diag_s[wave][0][lane] + diag_s[wave][1][lane] + diag_s[wave][2][lane] + diag_s[wave][3][lane];
+                            slice((t + u) / TPB, h, (t + u) % TPB)[lane] = lane < 31 ? v : __builtin_bit_cast(float, k0[u] - row0 - 16 * h);
+                        }
+                        __builtin_amdgcn_wave_barrier();
+                    }
                 }
             }
             mma_cols(dq, kc, dsq);   // dQ^T += K^T dS^T
         }
-        put_patch<1>(&acc_s[wave][0], dq, r, g);
+        put_patch<NQ>(&acc_s[wave][0], dq, r, g);
         __syncthreads();
-        store_quad<T>(dQ + out, merged() * scale);
+        const auto& z = args_again<BwdOfRows<T>>();
+        const float scale = z.scale;
+        T* const rows = z.dQ + head + (size_t)block * BS * kD + out;
+        if (cuts.count > 1) {   // a long row in pieces
+            const size_t slot = ((size_t)bh * z.cut.slots + cuts.slot) * S::PARTS + part;
+            float* const parts = z.cut.parts + slot * (S::OWN * kD) + tid * 4;
+            constexpr int kPiece = S::PARTS * S::OWN * kD;
+#pragma unroll
+            for (int p = 0; p < S::OWN; p += kAtOnce) {
+                const f32x4 v = merged(p);
+                float* const mine = parts + (size_t)piece * kPiece + p * kD;
+                put_shared(mine, v[0], v[1]);
+                put_shared(mine + 2, v[2], v[3]);
+            }
+            if (!last_to_arrive(z.cut.counters + slot, z.cut.tag, cuts.count, &flag)) return;
+#pragma unroll
+            for (int p = 0; p < S::OWN; p += kAtOnce) {
+                f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+                for (int c = 0; c < cuts.count; ++c) {
+                    const float* const from = parts + (size_t)c * kPiece + p * kD;
+                    const float2 lo = get_shared(from), hi = get_shared(from + 2);
+                    v += f32x4{lo.x, lo.y, hi.x, hi.y};
+                }
+                store_quad<T>(rows + p * kD, v * scale);
+            }
+            return;
+        }
+#pragma unroll
+        for (int p = 0; p < S::OWN; p += kAtOnce) store_quad<T>(rows + p * kD, merged(p) * scale);
         return;
     }
 
-    Frag kf[NDC], vf[NDC];
-    if (own < length) {
-        load_rows<T>(kf, K + head + (size_t)row0 * kD, r, g);
-        load_rows<T>(vf, V + head + (size_t)row0 * kD, r, g);
-    } else {
-        clear(kf);
-        clear(vf);
+    Frag kf[NQ][NDC], vf[NQ][NDC];
+#pragma unroll
+    for (int h = 0; h < NQ; ++h) {
+        if (row0 + 16 * h + r < length) {
+            load_rows<T>(kf[h], K + head + (size_t)(row0 + 16 * h) * kD, r, g);
+            load_rows<T>(vf[h], V + head + (size_t)(row0 + 16 * h) * kD, r, g);
+        } else {
+            clear(kf[h]);
+            clear(vf[h]);
+        }
     }
-    f32x4 dk[1][4], dv[1][4];
-    clear_acc<1>(dk);
-    clear_acc<1>(dv);
+    f32x4 dk[NQ][4], dv[NQ][4];
+    clear_acc<NQ>(dk);
+    clear_acc<NQ>(dv);
     for (int t = wave * KT; t < nt; t += STRIDE) {
-        Quad qc[KT][4], dc[KT][4], pq[1][KT], dsq[1][KT];
+        Quad qc[KT][4], dc[KT][4], pq[NQ][KT], dsq[NQ][KT];
 #pragma unroll
         for (int u = 0; u < KT; ++u) {
-            const bool there = u == 0 || t + u < nt;
-            const int q0 = tile0(there ? t + u : t);
+            if (u > 0 && t + u >= nt) {
+                clear(dc[u]);
+                clear(qc[u]);
+#pragma unroll
+                for (int h = 0; h < NQ; ++h) pq[h][u] = dsq[h][u] = Quad{};
+                continue;
+            }
+            const int q0 = tile0(t + u);
             const size_t at = head + (size_t)q0 * kD;
             Frag qf[NDC], df[NDC], of[NDC];
+            unsigned buckets[NQ];
             load_rows<T>(df, dO + at, r, g);
             load_rows<T>(of, O + at, r, g);
             load_rows<T>(qf, Q + at, r, g);
             const f32x4_any lse = *reinterpret_cast<const f32x4_any*>(LSE + vec + q0 + 4 * g);
             load_cols<T>(dc[u], dO + at, r, g);
             load_cols<T>(qc[u], Q + at, r, g);
+#pragma unroll
+            for (int h = 0; h < NQ; ++h) buckets[h] = buckets_of<true>(x, q0 + 4 * g, row0 + 16 * h + r, L);
+            __builtin_amdgcn_sched_barrier(0);
             if (q0 + 16 > length) {
                 zero_rows_from<T>(df, q0 + r >= length);
                 zero_rows_from<T>(of, q0 + r >= length);
                 zero_rows_from<T>(qf, q0 + r >= length);
                 zero_cols_from<T>(dc[u], q0 + 4 * g, length);
                 zero_cols_from<T>(qc[u], q0 + 4 * g, length);
-            }
-            if (!there) {
-                clear(dc[u]);
-                clear(qc[u]);
             }
             float part = 0.f;
 #pragma unroll
@@ -369,37 +624,73 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_bwd_with_kernel(
                 for (int e = 0; e < Elem<T>::EPL; ++e) part = fmaf((float)df[c][e], (float)of[c][e], part);
             // delta of rows 4 g + i in every lane: the lanes' shares of row r times a tile of ones
             const f32x4 delta = __builtin_amdgcn_mfma_f32_16x16x4f32(part, 1.f, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-            f32x4 s = bias_of<true>(x, tab, q0 + 4 * g, own, L), dp = f32x4{0.f, 0.f, 0.f, 0.f};
+            f32x4 lse2;
 #pragma unroll
-            for (int c = 0; c < NDC; ++c) {
-                s = mma_d(s, qf[c], kf[c]);     // S = Q K^T
-                dp = mma_d(dp, df[c], vf[c]);   // dP = dO V^T
-            }
-            unsigned d[4] = {};
-            if constexpr (DROP) key_draws(draws, q0 + 4 * g, own, d);
-            f32x4 p, ds;
+            for (int i = 0; i < 4; ++i) lse2[i] = lse[i] == -INFINITY || q0 + 4 * g + i >= length ? INFINITY : lse[i] * kLog2e;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float lse2 = lse[i] == -INFINITY || q0 + 4 * g + i >= length ? INFINITY : lse[i] * kLog2e;
-                const float pi = there ? exp2f(fmaf(s[i], scale_log2, -lse2)) : 0.f;
-                const bool drop = DROP && d[i] < x.threshold;
-                p[i] = drop ? 0.f : pi * keep;
-                ds[i] = there ? pi * ((drop ? 0.f : dp[i] * keep) - delta[i]) : 0.f;
+            for (int h = 0; h < NQ; ++h) {
+                f32x4 s = bias_of<true>(x, tab, buckets[h]), dp = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < NDC; ++c) {
+                    s = mma_d(s, qf[c], kf[h][c]);     // S = Q K^T
+                    dp = mma_d(dp, df[c], vf[h][c]);   // dP = dO V^T
+                }
+                unsigned d[4] = {};
+                if constexpr (DROP) key_draws(draws, q0 + 4 * g, row0 + 16 * h + r, d);
+                f32x4 p, ds;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float pi = exp2f(fmaf(s[i], scale_log2, -lse2[i]));
+                    const bool drop = DROP && d[i] < x.threshold;
+                    p[i] = drop ? 0.f : pi * keep;
+                    ds[i] = pi * ((drop ? 0.f : dp[i] * keep) - delta[i]);
+                }
+                pq[h][u] = to_quad<T>(p);
+                dsq[h][u] = to_quad<T>(ds);
             }
-            pq[0][u] = to_quad<T>(p);
-            dsq[0][u] = to_quad<T>(ds);
         }
         mma_cols(dv, dc, pq);    // dV^T += dO^T P
         mma_cols(dk, qc, dsq);   // dK^T += Q^T dS
     }
+    const auto& z = args_again<BwdOfRows<T>>();
+    const float scale = z.scale;
+    // The rows, or a chunk's sums, unscaled: [head][slot][dK | dV][block][64], which the last of a column's chunks with these rows adds up in their order.
+    constexpr int kPart = 2 * BS * kD;
+    float* const parts = z.columns.parts + ((size_t)bh * z.columns.n_slots + it.first) * kPart + out;
+    float* const mine = parts + (size_t)(it.slot - it.first) * kPart;   // where slot >= 0
+    const size_t column = head + (size_t)block * BS * kD + out;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         if (which) __syncthreads();
-        put_patch<1>(&acc_s[wave][0], which ? dv : dk, r, g);
+        put_patch<NQ>(&acc_s[wave][0], which ? dv : dk, r, g);
         __syncthreads();
-        const f32x4 v = merged();
-        store_quad<T>((which ? dV : dK) + out, which ? v : v * scale);
+#pragma unroll
+        for (int p = 0; p < S::OWN; p += kAtOnce) {
+            const f32x4 v = merged(p);
+            if (it.slot >= 0) {
+                float* const to = mine + which * BS * kD + p * kD;
+                put_shared(to, v[0], v[1]);
+                put_shared(to + 2, v[2], v[3]);
+            } else {
+                store_quad<T>((which ? z.dV : z.dK) + column + p * kD, which ? v : v * scale);
+            }
+        }
     }
+    if (it.slot < 0) return;
+    if (!last_to_arrive(z.columns.counters + ((size_t)bh * z.columns.n_slots + it.first) * TPB + part, z.columns.tag, it.count, &flag)) return;
+#pragma unroll
+    for (int which = 0; which < 2; ++which)
+#pragma unroll
+        for (int p = 0; p < S::OWN; p += kAtOnce) {
+            f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+            for (int c = 0; c < it.count; ++c) {
+                const float* const from = parts + (size_t)c * kPart + which * BS * kD + p * kD;
+                const float2 lo = get_shared(from), hi = get_shared(from + 2);
+                v += f32x4{lo.x, lo.y, hi.x, hi.y};
+            }
+            store_quad<T>((which ? z.dV : z.dK) + column + p * kD, which ? v : v * scale);
+        }
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -458,7 +749,31 @@ __global__ __launch_bounds__(256) void table_grad_kernel(const float* __restrict
 // ------------------------------------------------------------------------------------------------
 namespace {
 
-// The backward's: of the bf16 kernels of block 32 and 64 first, then what the table's gradient takes.
+// The backward plan of fp32 and block 16: rows and waves of a workgroup, pieces of rows and columns as in the plain kernel.
+struct GenericBwd {
+    bool wide;          // 32 rows
+    int waves, parts;   // workgroups a block row
+    long long resident;
+    RowCut cut;
+    BwdWorkspace ws;
+    GenericBwd(const AttnShape& s, int nnzb)
+        : wide(s.bs > 16), waves(s.bs == 16 && generic_bwd_many_short_rows(s, nnzb) ? 2 : 4), parts(s.bs / (wide ? 32 : 16)),
+          resident(generic_bwd_resident(s.is_bf16, waves)), cut(decide(s, nnzb, parts, resident)), ws(s.BH, s.bs, s.nb, nnzb, kChunk, 0, cut.slots) {}
+    static RowCut decide(const AttnShape& s, int nnzb, int parts, long long resident) {
+        RowCut cut;
+        generic_bwd_decide(cut, s, nnzb, parts, resident);
+        if (cut.slots == 0) {
+            cut = RowCut{};
+            cut.longest = INT_MAX;
+            return cut;
+        }
+        cut.helpers = cut.slots - 1;
+        cut.groups = parts * ((s.BH * cut.helpers + 7) & ~7);
+        return cut;
+    }
+};
+
+// The backward's: of pieces of rows and columns first, then what the table's gradient takes.
 struct WithWorkspace {
     int tile, parts;                           // rows of a tile that has its own slice; workgroups per head
     size_t slices, partial, counters, total;   // offsets, and the end
@@ -466,7 +781,7 @@ struct WithWorkspace {
         auto up = [](size_t n) { return (n + 255) / 256 * 256; };
         const bool tiled = s.is_bf16 && s.bs > 16;
         tile = tiled ? s.bs : 16;
-        slices = tiled ? up(attn_bwd_workspace(s, nnzb).with_rows) : 0;
+        slices = up(tiled ? attn_bwd_workspace(s, nnzb).with_rows : GenericBwd(s, nnzb).ws.with_rows);
         if (n_buckets == 0) {
             total = slices;
             return;
@@ -486,15 +801,32 @@ hipError_t fwd_with(const AttnShape& s, const Extras& x, const void* Q, const vo
     if constexpr (sizeof(T) == 2 && BS > 16) {
         return fwd_with_bf16<BS>(s, x, Q, K, V, O, LSE, row_ptr, col_idx, nnzb, st);
     } else {
-        const long long total = (long long)s.BH * s.nb * (BS / 16), grid = group_grid(total);
+        const int rows = generic_fwd_rows(s, nnzb) == 32 ? 32 : 16, parts = BS / rows;
+        const long long all = (long long)s.BH * s.nb;
+        // (rows of fewer than 6 tiles gain nothing by their order and pay the search; see launch_fwd)
+        const int sort_rows = s.nb > 32 && (long long)nnzb * (BS / 16) >= 6ll * s.nb && 2 * all * parts > 3 * 256 * (rows == 16 ? 4 : 3);
+        RowCut cut;
+        if (s.fwd_room) cut = RowCut(s, nnzb);
+        if (cut.slots == 0) {
+            cut = RowCut{};
+            cut.longest = INT_MAX;
+        }
+        const long long grid = cut.groups + (sort_rows ? parts * group_grid(all) : group_grid(all * parts));
         if (grid > 0x7fffffffll) return hipErrorInvalidValue;
         auto launch = [&](auto kernel) {
             kernel<<<dim3((unsigned)grid), dim3(kWaves * 64), 0, st>>>(
                 static_cast<const T*>(Q), static_cast<const T*>(K), static_cast<const T*>(V), static_cast<T*>(O), LSE, row_ptr, col_idx, x,
-                s.L, s.nb, (int)total, s.scale * kLog2e);
+                cut, s.BH, s.L, s.nb, sort_rows, s.scale * kLog2e);
         };
-        if (x.threshold) launch(attn_fwd_with_kernel<T, BS, true>);
-        else launch(attn_fwd_with_kernel<T, BS, false>);
+        if constexpr (BS > 16) {
+            if (rows == 32) {
+                if (x.threshold) launch(attn_fwd_with_kernel<T, BS, 2, true>);
+                else launch(attn_fwd_with_kernel<T, BS, 2, false>);
+                return hipGetLastError();
+            }
+        }
+        if (x.threshold) launch(attn_fwd_with_kernel<T, BS, 1, true>);
+        else launch(attn_fwd_with_kernel<T, BS, 1, false>);
         return hipGetLastError();
     }
 }
@@ -506,16 +838,33 @@ hipError_t bwd_with(const AttnShape& s, const Extras& x, const void* Q, const vo
     if constexpr (sizeof(T) == 2 && BS > 16) {
         return bwd_with_bf16<BS>(s, x, Q, K, V, O, dO, LSE, dQ, dK, dV, row_ptr, col_idx, col_ptr, row_idx, nnzb, workspace, st);
     } else {
-        const long long total = (long long)s.BH * s.nb * (BS / 16), grid = 2 * group_grid(total);
+        GenericBwd plan(s, nnzb);
+        const long long all = (long long)s.BH * s.nb, items = (long long)s.BH * plan.parts * (plan.ws.w_max + s.nb);
+        const int sort_rows = (long long)nnzb * (BS / 16) >= 6ll * s.nb && s.nb >= 32 && 4 * items > 5 * plan.resident;   // see launch_bwd
+        plan.cut.counters = reinterpret_cast<unsigned long long*>(static_cast<char*>(workspace) + plan.ws.total);
+        plan.cut.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.ws.row_parts);
+        const ColumnCut columns = {plan.ws.chunk, plan.ws.w_first, plan.ws.w_max, plan.ws.n_slots, 2 * items > 3 * plan.resident, s.tag,
+                                   static_cast<unsigned long long*>(workspace),
+                                   reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.ws.counter_bytes)};
+        const long long grid = plan.cut.groups + group_grid((long long)s.BH * plan.parts * columns.n_first) + (sort_rows ? plan.parts * group_grid(all) : group_grid(all * plan.parts)) +
+                               group_grid((long long)s.BH * plan.parts * (columns.n_items - columns.n_first));
         if (grid > 0x7fffffffll) return hipErrorInvalidValue;
+        const BwdOfRows<T> args = {static_cast<const T*>(Q), static_cast<const T*>(K), static_cast<const T*>(V), static_cast<const T*>(O),
+                                   static_cast<const T*>(dO), LSE, static_cast<T*>(dQ), static_cast<T*>(dK), static_cast<T*>(dV), row_ptr, col_idx,
+                                   col_ptr, row_idx, x, plan.cut, columns, s.BH, s.L, s.nb, nnzb, sort_rows, s.scale, s.scale * kLog2e};
         auto launch = [&](auto kernel) {
-            kernel<<<dim3((unsigned)grid), dim3(kWaves * 64), 0, st>>>(
-                static_cast<const T*>(Q), static_cast<const T*>(K), static_cast<const T*>(V), static_cast<const T*>(O),
-                static_cast<const T*>(dO), LSE, static_cast<T*>(dQ), static_cast<T*>(dK), static_cast<T*>(dV), row_ptr, col_idx, col_ptr,
-                row_idx, x, s.L, s.nb, nnzb, (int)total, s.scale, s.scale * kLog2e);
+            kernel<<<dim3((unsigned)grid), dim3(plan.waves * 64), 0, st>>>(args);
         };
-        if (x.threshold) launch(attn_bwd_with_kernel<T, BS, true>);
-        else launch(attn_bwd_with_kernel<T, BS, false>);
+        if constexpr (BS > 16) {
+            if (x.threshold) launch(attn_bwd_with_kernel<T, BS, 2, 4, true>);
+            else launch(attn_bwd_with_kernel<T, BS, 2, 4, false>);
+        } else if (plan.waves == 2) {
+            if (x.threshold) launch(attn_bwd_with_kernel<T, BS, 1, 2, true>);
+            else launch(attn_bwd_with_kernel<T, BS, 1, 2, false>);
+        } else {
+            if (x.threshold) launch(attn_bwd_with_kernel<T, BS, 1, 4, true>);
+            else launch(attn_bwd_with_kernel<T, BS, 1, 4, false>);
+        }
         return hipGetLastError();
     }
 }
@@ -523,7 +872,7 @@ hipError_t bwd_with(const AttnShape& s, const Extras& x, const void* Q, const vo
 }  // namespace
 
 size_t attn_with_workspace_bytes(const AttnShape& s, int n_buckets, int H, int nnzb, bool is_bwd) {
-    if (!is_bwd) return s.is_bf16 && s.bs > 16 ? RowCut(s, nnzb).room_bytes(s.BH, s.bs) : 0;
+    if (!is_bwd) return RowCut(s, nnzb).room_bytes(s.BH, s.bs);
     return WithWorkspace(s, n_buckets, H, nnzb).total;
 }
 

@@ -71,70 +71,6 @@ template <typename T> struct SplitMany<T, 64> {
     typedef Split<T, 64, 2, 1, 2> bwd_single;
 };
 
-// The block row that workgroup number l (all of a row's beside each other) takes when there are more than run at once.
-// Heads that do not divide over the XCDs: the rows with more than twice the mean number of kept blocks first, of all the heads (a
-// row of 80 blocks that starts last runs alone for as long as everything before it took), then head by
-// head the others, so that neighbours in time share K and V in an L2; each of the two lists is shared out over the XCDs head by head.
-// Patterns without a long row skip the second search, and the counts are loaded four groups at a time.  By length, on the XCDs
-// as deal_heads() has them, which the bf16 kernels gain by, took as long: 96 shapes, forward 0.95 to 1.04 of the time, backward 0.95 to 1.11.
-// All lanes of the calling wave must be active.
-__device__ __forceinline__ ItemOfHead long_rows_first(const int* __restrict__ row_ptr, int nb, int heads, int l, int lane) {
-    const int limit = 2 * row_ptr[nb] / nb;
-    int n_long = 0, cnt_first = 0;   // rows 0 .. 63 are kept for the second search
-    int base0 = 0;
-    for (; base0 + 256 <= nb; base0 += 256) {   // four groups whose loads are in flight together
-        int from[4], to[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            from[k] = row_ptr[base0 + 64 * k + lane];
-            to[k] = row_ptr[base0 + 64 * k + lane + 1];
-        }
-        if (base0 == 0) cnt_first = to[0] - from[0];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) n_long += __popcll(__ballot(to[k] - from[k] > limit));
-    }
-    for (int base = base0; base < nb; base += 64) {
-        const int r = base + lane;
-        const int cnt = r < nb ? row_ptr[r + 1] - row_ptr[r] : 0;
-        if (base == 0) cnt_first = cnt;
-        n_long += __popcll(__ballot(r < nb && cnt > limit));
-    }
-    const int longs = heads * n_long;
-    const bool want_long = l < longs;
-    int head, rank;
-    if (want_long) {
-        l = xcd_deal(l, 0, longs);
-        head = l / n_long;
-        rank = l % n_long;
-    } else {
-        l = xcd_deal(l, longs, heads * nb);
-        head = l / (nb - n_long);
-        rank = l % (nb - n_long);
-    }
-    if (n_long == 0) return {head, rank};
-    for (int base = 0; base < nb; base += 64) {   // the counts are in the cache by now
-        const int r = base + lane;
-        int cnt = cnt_first;
-        if (base != 0) cnt = r < nb ? row_ptr[r + 1] - row_ptr[r] : 0;
-        const unsigned long long mine = __ballot(r < nb && (cnt > limit) == want_long);
-        const int members = __popcll(mine);
-        if (rank < members) {
-            const unsigned long long hit = __ballot(((mine >> lane) & 1ull) && lanes_below(mine) == rank);
-            return {head, base + __ffsll((long long)hit) - 1};
-        }
-        rank -= members;
-    }
-    return {head, 0};
-}
-
-// By length, all heads of an XCD together, where each XCD has whole heads: what starts last is short then.  Forward, long rows
-// first and so: fp32, block 16, 16 x 2048 23.5 -> 22.5.
-__device__ __forceinline__ ItemOfHead rows_in_order(const int* __restrict__ row_ptr, int nb, int heads, int l, int lane) {
-    if (heads & 7) return long_rows_first(row_ptr, nb, heads, l, lane);
-    const ItemOfHead mine = deal_heads(l, heads, false);
-    return {mine.head, row_by_length(row_ptr, nb, mine.item, lane)};
-}
-
 }  // namespace
 
 // ------------------------------------------------------------------------------------------------
@@ -811,7 +747,7 @@ static bool many_short_rows(const AttnShape& s, int nnzb) { return short_rows(s,
 // hardly more workgroups than run at once: up to 13 block rows 1.13 to 1.17 at 101 to 141 (30 x 352, block 32, 18.8 / 21.3 us), with over 2000 workgroups (of 32
 // rows, both sides) 1.05 to 1.18 (16 x 2080, block 32, 62 / 74), the others 0.87 to 0.88 at 105 to 144 (42 x 544, block 32, 51 / 44) and
 // 0.63 to 1.06 at 157 to 198.
-static bool many_short_rows_bwd(const AttnShape& s, int nnzb) {
+bool generic_bwd_many_short_rows(const AttnShape& s, int nnzb) {
     if (s.bs == 16) return many_short_rows(s, nnzb);
     const bool can_be_long = s.nb >= 16 && 2ll * s.BH * s.nb * (s.bs / 32) <= 2000;
     return short_rows(s, nnzb) >= (10ll * nnzb < 11ll * s.nb ? 60 : single_block_rows(s, nnzb) ? 120 : can_be_long ? 150 : 100);
@@ -822,16 +758,16 @@ struct GenericBwdSplit {
     int waves, waves_a_row, parts;   // of a workgroup, of them for the same rows; workgroups a block row
 };
 static GenericBwdSplit generic_bwd_split(const AttnShape& s, int nnzb) {
-    if (!many_short_rows_bwd(s, nnzb)) return {4, 4, s.bs == 64 ? 2 : 1};
+    if (!generic_bwd_many_short_rows(s, nnzb)) return {4, 4, s.bs == 64 ? 2 : 1};
     const int wide = s.bs == 64 ? 2 : 1;
     return single_block_rows(s, nnzb) ? GenericBwdSplit{s.bs == 16 ? 2 : wide, s.bs == 16 ? 2 : 1, 1} : GenericBwdSplit{2 * wide, 2, 1};
 }
 
 // Workgroups of the generic backward that run at once: two (fp32) or three waves a SIMD.
-static long long generic_bwd_resident(bool is_bf16, int waves) { return 256 * 4 * (is_bf16 ? 3 : 2) / waves; }
+long long generic_bwd_resident(bool is_bf16, int waves) { return 256 * 4 * (is_bf16 ? 3 : 2) / waves; }
 
 // Which of its query side's rows are cut, with the steps of both sides and as many helpers as the forward.
-static void generic_bwd_decide(RowCut& cut, const AttnShape& s, int nnzb, int parts, long long resident) {
+void generic_bwd_decide(RowCut& cut, const AttnShape& s, int nnzb, int parts, long long resident) {
     cut.decide(s, nnzb, 2ll * s.BH * ((long long)nnzb + s.nb) * parts / resident);
     const long long most = 512 / ((long long)s.BH * parts);
     if (cut.slots > most) cut.slots = (int)most;
@@ -861,7 +797,7 @@ bool attn_bwd_grids_fit(int BH, int bs, int nb, int nnzb) {
 // 32, 3 %, 87 -> 54 us; 8 x 2048, 10 %, 24.3 -> 18.7; 4 x 1024, block 64, 20 %, 11.7 -> 7.8; 8 x 2048, 30 %, 37.5 -> 35.0;
 // 32 x 2048, block 64 (2048 workgroups of 32 rows) 45.9 -> 47.3; 64 x 2048, block 32 (4096) 96.4 both.
 // 0: many short rows, which waves do not share.
-static int fwd_rows(const AttnShape& s, int nnzb) {
+int generic_fwd_rows(const AttnShape& s, int nnzb) {
     if (s.bs == 16) return 16;
     if (many_short_rows(s, nnzb)) return 0;
     return s.bs > 16 && (long long)s.BH * s.L / 32 >= 2048 ? 32 : 16;
@@ -884,7 +820,7 @@ static bool fwd_many(const AttnShape& s, int rows) { return 2ll * s.BH * s.L / r
 RowCut generic_fwd_cut(const AttnShape& s, int nnzb) {
     RowCut cut;
     if (s.nb <= 32) return cut;   // decide() cuts none
-    const int rows = fwd_rows(s, nnzb);
+    const int rows = generic_fwd_rows(s, nnzb);
     if (rows == 0) return cut;
     const bool many = fwd_many(s, rows);
     // block 16: rows that can be long enough for what the pieces cost, 2 us
@@ -994,7 +930,7 @@ static hipError_t fwd_t(const AttnShape& s, const void* Q, const void* K, const 
     if constexpr (sizeof(T) == 2 && BS >= 32) {
         return fwd_bf16<BS>(s, Q, K, V, O, LSE, row_ptr, col_idx, nnzb, st);
     } else {
-        const int rows = fwd_rows(s, nnzb);
+        const int rows = generic_fwd_rows(s, nnzb);
         if constexpr (BS > 16) {
             if (rows == 0) return launch_fwd<T, BS, typename SplitMany<T, BS>::fwd>(s, Q, K, V, O, LSE, row_ptr, col_idx, nnzb, st);
             if (rows == 32) return launch_fwd<T, BS, SplitFew<T, BS>>(s, Q, K, V, O, LSE, row_ptr, col_idx, nnzb, st);
@@ -1023,7 +959,7 @@ static hipError_t bwd_t(const AttnShape& s, const void* Q, const void* K, const 
         // (0.95).  With few block rows there is no long chain to shorten: 18 x 384, block 64, 20.4 -> 21.7, 8 x 512 15.4 -> 17.2.
         if constexpr (BS > 16)
             if (s.nb >= 16 && (long long)s.BH * (ws.w_max + s.nb) * (BS / 32) <= (nnzb > 6ll * s.nb ? 760 : 800)) launch = launch_bwd<T, BS, Split<T, BS, 1, 4, 1>>;
-        if (many_short_rows_bwd(s, nnzb))
+        if (generic_bwd_many_short_rows(s, nnzb))
             launch = single_block_rows(s, nnzb) ? launch_bwd<T, BS, typename SplitMany<T, BS>::bwd_single>
                                                                : launch_bwd<T, BS, typename SplitMany<T, BS>::bwd>;
         return launch(s, Q, K, V, O, dO, LSE, dQ, dK, dV, row_ptr, col_idx, col_ptr, row_idx, ws, workspace, st);

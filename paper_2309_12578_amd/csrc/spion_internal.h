@@ -93,6 +93,10 @@ struct RowCut {
 
 // attn_kernels.hip: the plan for fp32 and block 16, without its memory
 RowCut generic_fwd_cut(const AttnShape& s, int nnzb);
+int generic_fwd_rows(const AttnShape& s, int nnzb);   // of a workgroup: 16 or 32; 0: many short rows
+void generic_bwd_decide(RowCut& cut, const AttnShape& s, int nnzb, int parts, long long resident);
+long long generic_bwd_resident(bool is_bf16, int waves);
+bool generic_bwd_many_short_rows(const AttnShape& s, int nnzb);
 
 hipError_t launch_attn_fwd(const AttnShape& s, const void* Q, const void* K, const void* V, void* O,
                            float* LSE, const int* row_ptr, const int* col_idx, int nnzb, hipStream_t st);
