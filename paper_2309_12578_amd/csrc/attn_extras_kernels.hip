@@ -701,12 +701,13 @@ __global__ __launch_bounds__(W * 64, 2) void attn_bwd_with_kernel(const BwdOfRow
 // kInFlight tiles a wave and share of it at a time, whose numbers are requested together, then their buckets: 4 x 8 heads x 4096, 851 blocks
 // of 64, 10.5 us; 2 x 8 heads x 16320, 13.5 us.
 // ------------------------------------------------------------------------------------------------
+constexpr int kTilesInFlight = 4;   // of a share of a wave
 template <int TS>
 __global__ __launch_bounds__(256) void table_grad_kernel(const float* __restrict__ slices, Extras x, int L, unsigned tiles_of_head,
                                                          unsigned tiles_a_sequence, int parts, float* partial, unsigned long long* __restrict__ counters,
                                                          void* __restrict__ dtable) {
     extern __shared__ float hist[];   // [n_buckets][threads]
-    constexpr int F = 2 * TS, LANES = F / 4, GROUP = 64 / LANES, kInFlight = 4;   // lanes of a tile, four numbers each; tiles of a wave
+    constexpr int F = 2 * TS, LANES = F / 4, GROUP = 64 / LANES, kInFlight = kTilesInFlight;   // lanes of a tile, four numbers each; tiles of a wave
     const int h = blockIdx.x % x.H, part = blockIdx.x / x.H, tid = threadIdx.x, threads = blockDim.x, lane = tid & 63;
     for (int b = 0; b < x.n_buckets; ++b) hist[b * threads + tid] = 0.f;
     const int t = lane % LANES * 4;
@@ -786,9 +787,10 @@ struct WithWorkspace {
             total = slices;
             return;
         }
-        // sixteen slices a workgroup or more, and about two workgroups a compute unit
+        // as many slices as a workgroup requests together, or more, and up to four workgroups a compute unit
+        const long long together = (long long)table_grad_threads(n_buckets) / (tile / 2) * kTilesInFlight;
         const long long tiles = (long long)s.BH / H * nnzb * (s.bs / tile) * (s.bs / tile);
-        parts = (int)std::max<long long>(1, std::min<long long>(tiles / 16, 1024 / H));
+        parts = (int)std::max<long long>(1, std::min<long long>((tiles + together - 1) / together, 1024 / H));
         partial = up(slices + (size_t)s.BH * nnzb * (s.bs / tile) * (s.bs / tile) * 2 * tile * sizeof(float));
         counters = up(partial + (size_t)H * parts * n_buckets * sizeof(float));
         total = up(counters + (size_t)H * Extras::kCounterStride * 8);
