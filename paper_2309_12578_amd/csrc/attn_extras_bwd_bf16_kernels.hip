@@ -7,6 +7,12 @@
 // The table's gradient needs dS by distance.  The query side adds up its diagonals: within a wave's 16 queries by lane
 // shifts (diagonal_sums) and through LDS, over the waves of the workgroup one step later, behind the barrier that is there anyway.  What leaves
 // is one number for each distance of a block, slices[head][kept block][2 BS], 1/32 of what the block's tiles bring in.
+//
+// Three waves a SIMD at 168 registers, which the arguments read again where they are used (args_again) and addresses made anew for each block (once)
+// leave room for; at two the backward with bias and dropout took 253 instead of 220 us (4 x 8 heads x 4096, 20.8 %).  Neither the matrix nor the vector
+// pipes are busy half of the time: a step is one chain of products, exponentials and products, longer than the plain one by
+// the draws and the biases.  Kernel time, us, of the plain one, with lengths, bias, dropout, bias and dropout: 4 x 4 heads x 4096, block 64, 8 %, 45.5 / 52 / 66 /
+// 72 / 86; 4 x 8 heads, 20.8 %, 149 / 155 / 175 / 200 / 220; 2 x 8 x 16320, 5 %, 302 / 292 / 325 / 363 / 392; 16 x 4 x 1024, block 32, 15 %, 28.5 / 33.5 / 44 / 42.5 / 54.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <stdint.h>

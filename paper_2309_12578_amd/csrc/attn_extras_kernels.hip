@@ -6,7 +6,10 @@
 // Queries and keys from the length on: O = 0, LSE = -inf, gradients 0; nothing of theirs is added up.
 //
 // The kernels of this file are for fp32 and block 16: a workgroup of four waves has 16 or 32 rows, whose 16-row tiles of the other
-// side the waves take in turn, straight from memory into registers (layouts, order and pieces as in attn_kernels.hip).
+// side the waves take in turn, straight from memory into registers (layouts, order and pieces as in attn_kernels.hip).  Bound, as there, by the
+// latency of those loads, and in fp32 by its MFMA rate.  Kernel time, us, of the plain ones, with lengths, bias, dropout, bias and dropout, forward and
+// backward: fp32, 8 heads x 2048, block 32, 10 %, 20.2 / 21 / 22.3 / 22.5 / 23.7, 54 / 55.6 / 59 / 60 / 65; 16 x 4096, block 64, 10 %, 79 / 82 / 83 / 87 / 91,
+// 280 / 286 / 296 / 293 / 319; bf16, block 16, 9 x 1936, 8 %, 12.7 / 14.5 / 15.3 / 15.2 / 16.3, 27.4 / 30 / 32 / 31 / 33.5; 32 x 4096 78 / 80 / 88 / 85 / 91, 296 / 294 / 315 / 300 / 321.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -699,7 +702,7 @@ __global__ __launch_bounds__(W * 64, 2) void attn_bwd_with_kernel(const BwdOfRow
 // computed.  Every thread adds into its own copy of the buckets in LDS, the copies are added up in a fixed order, and so
 // are the parts of a head, by the last of its workgroups to arrive; the counters of arrivals, a line each, are 0 from the backward kernel on.
 // kInFlight tiles a wave and share of it at a time, whose numbers are requested together, then their buckets: 4 x 8 heads x 4096, 851 blocks
-// of 64, 10.5 us; 2 x 8 heads x 16320, 13.5 us.
+// of 64, 11.3 us; 2 x 8 heads x 16320, 13.5; 16 x 4 heads x 1024, 157 blocks of 32, 8.3.
 // ------------------------------------------------------------------------------------------------
 constexpr int kTilesInFlight = 4;   // of a share of a wave
 template <int TS>
