@@ -214,6 +214,8 @@ typedef struct {
     int32_t table_dtype;       /* spion_dtype of table and dtable */
     uint32_t stream;           /* tells apart the dropouts that share an rng */
     uint32_t reserved;         /* must be 0 */
+    void *o_rest;              /* bf16: as O, what its rounding left; written by spion_attn_fwd_with, read by spion_attn_bwd_with, whose delta is
+                                  then exact; or NULL (delta from the rounded O, and the gradients less exact).  fp32: not used */
 } spion_attn_extras;
 
 /* Bytes of device scratch of the two calls below; (size_t)-1 if the parameters are unsupported. */

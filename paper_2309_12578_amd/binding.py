@@ -48,7 +48,7 @@ class _AttnExtras(ctypes.Structure):
     _fields_ = [("table", ctypes.c_void_p), ("bucket_of", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
                 ("rng", ctypes.c_void_p), ("rng_used", ctypes.c_void_p), ("dropout", ctypes.c_double),
                 ("n_buckets", ctypes.c_int32), ("table_dtype", ctypes.c_int32), ("stream", ctypes.c_uint32),
-                ("reserved", ctypes.c_uint32)]
+                ("reserved", ctypes.c_uint32), ("o_rest", ctypes.c_void_p)]
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -256,7 +256,7 @@ def _bytes(workspace: Optional[torch.Tensor]) -> int:
     return 0 if workspace is None else workspace.numel() * workspace.element_size()
 
 
-def _attn_extras(H, L, table, bucket_of, lengths, rng, rng_used, dropout, dropout_stream) -> _AttnExtras:
+def _attn_extras(H, L, table, bucket_of, lengths, rng, rng_used, dropout, dropout_stream, o_rest=None) -> _AttnExtras:
     n_buckets = 0 if table is None else int(table.shape[0])
     if table is not None and (table.shape != (n_buckets, H) or bucket_of is None or bucket_of.numel() != 2 * L - 1 or
                               bucket_of.dtype != torch.uint8):
@@ -267,7 +267,7 @@ def _attn_extras(H, L, table, bucket_of, lengths, rng, rng_used, dropout, dropou
         if t is not None and (t.dtype != torch.int64 or t.numel() != 2):
             raise ValueError("rng must be int64 {seed, offset}")
     return _AttnExtras(_ptr(table), _ptr(bucket_of), _ptr(lengths), _ptr(rng), _ptr(rng_used), float(dropout), n_buckets,
-                       SPION_F32 if table is None else _dtype_code(table.dtype), dropout_stream, 0)
+                       SPION_F32 if table is None else _dtype_code(table.dtype), dropout_stream, 0, _ptr(o_rest))
 
 
 def spion_attn_with_workspace_bytes(B, H, L, d, block, dtype, nnzb, is_bwd, scale=0.0, table=None, bucket_of=None, lengths=None,
@@ -281,9 +281,10 @@ def spion_attn_with_workspace_bytes(B, H, L, d, block, dtype, nnzb, is_bwd, scal
 
 
 def spion_attn_fwd_with(Q, K, V, O, LSE, row_ptr, col_idx, nnzb, B, H, L, d, block, dtype, scale=0.0, table=None, bucket_of=None,
-                        lengths=None, rng=None, rng_used=None, dropout=0.0, dropout_stream=0, workspace=None, stream=None) -> None:
+                        lengths=None, rng=None, rng_used=None, dropout=0.0, dropout_stream=0, workspace=None, stream=None,
+                        o_rest=None) -> None:
     p = _attn_params(B, H, L, d, block, dtype, scale, 0)
-    x = _attn_extras(H, L, table, bucket_of, lengths, rng, rng_used, dropout, dropout_stream)
+    x = _attn_extras(H, L, table, bucket_of, lengths, rng, rng_used, dropout, dropout_stream, o_rest)
     rc = load().spion_attn_fwd_with(_ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(LSE), _ptr(row_ptr), _ptr(col_idx), int(nnzb),
                                     ctypes.byref(p), ctypes.byref(x), _ptr(workspace), _bytes(workspace), _stream(stream))
     if rc != 0:
@@ -292,9 +293,9 @@ def spion_attn_fwd_with(Q, K, V, O, LSE, row_ptr, col_idx, nnzb, B, H, L, d, blo
 
 def spion_attn_bwd_with(Q, K, V, O, dO, LSE, dQ, dK, dV, dtable, row_ptr, col_idx, col_ptr, row_idx, bsr_pos, nnzb, B, H, L, d,
                         block, dtype, scale=0.0, table=None, bucket_of=None, lengths=None, rng=None, dropout=0.0,
-                        dropout_stream=0, workspace=None, stream=None) -> None:
+                        dropout_stream=0, workspace=None, stream=None, o_rest=None) -> None:
     p = _attn_params(B, H, L, d, block, dtype, scale, 0)
-    x = _attn_extras(H, L, table, bucket_of, lengths, rng, None, dropout, dropout_stream)
+    x = _attn_extras(H, L, table, bucket_of, lengths, rng, None, dropout, dropout_stream, o_rest)
     rc = load().spion_attn_bwd_with(_ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(dO), _ptr(LSE), _ptr(dQ), _ptr(dK), _ptr(dV),
                                     _ptr(dtable), _ptr(row_ptr), _ptr(col_idx), _ptr(col_ptr), _ptr(row_idx), _ptr(bsr_pos),
                                     int(nnzb), ctypes.byref(p), ctypes.byref(x), _ptr(workspace), _bytes(workspace),

@@ -31,6 +31,23 @@ __device__ __forceinline__ int length_of(const Extras& x, int bh, int L) {
     return n < 0 ? 0 : n > L ? L : n;
 }
 
+// Where rows of head bh are, see HeadRows.
+struct Rows {
+    int H, beside;
+    __device__ __forceinline__ int in_row() const { return beside ? 3 * H * kD : kD; }
+    __device__ __forceinline__ int out_row() const { return beside ? H * kD : kD; }
+    __device__ __forceinline__ size_t in_head(int bh, int L) const {
+        return beside ? ((size_t)(bh / H) * L * 3 * H + bh % H) * kD : (size_t)bh * L * kD;
+    }
+    __device__ __forceinline__ size_t out_head(int bh, int L) const {
+        return beside ? ((size_t)(bh / H) * L * H + bh % H) * kD : (size_t)bh * L * kD;
+    }
+};
+
+// What is lost of v when it is stored as T.
+template <typename T>
+__device__ __forceinline__ float rounded_off(float v) { return v - (float)(T)v; }
+
 // The head's column of the table into LDS, as what the accumulators start from; all threads of the workgroup, which has to
 // meet before it is read.  Entries of the map beyond the table read its last bucket (the table is never read past its end).
 __device__ __forceinline__ void load_bias_table(float* tab, const Extras& x, int h, int tid, int threads) {

@@ -120,19 +120,6 @@ struct TableColumn {
     }
 };
 
-// Where rows of head bh are, see HeadRows.
-struct Rows {
-    int H, beside;
-    __device__ __forceinline__ int in_row() const { return beside ? 3 * H * kD : kD; }
-    __device__ __forceinline__ int out_row() const { return beside ? H * kD : kD; }
-    __device__ __forceinline__ size_t in_head(int bh, int L) const {
-        return beside ? ((size_t)(bh / H) * L * 3 * H + bh % H) * kD : (size_t)bh * L * kD;
-    }
-    __device__ __forceinline__ size_t out_head(int bh, int L) const {
-        return beside ? ((size_t)(bh / H) * L * H + bh % H) * kD : (size_t)bh * L * kD;
-    }
-};
-
 // What the end of a row's piece needs of its cut, in one register: at most RowCut::kSlots each.
 struct CutRow {
     int count, slot, piece;

@@ -318,7 +318,15 @@ __global__ __launch_bounds__(BS * 4, BS == 32 && DROP ? 5 : 4) void attn_fwd_wit
     // the stage that the last block did not use is free, see the plain kernel
     bf16_t* patch = ((n & 1) ? sm1.k : sm0.k) + wave * (16 * kD);
     const Rows at = {z.at.H, z.at.beside};
-    store_rows_coalesced(patch, z.O + at.out_head(bh, z.L) + (size_t)(I * BS + wave * 16) * at.out_row(), at.out_row(), oacc, inv, l);
+    const size_t row0 = at.out_head(bh, z.L) + (size_t)(I * BS + wave * 16) * at.out_row();
+    store_rows_coalesced(patch, z.O + row0, at.out_row(), oacc, inv, l);
+    if (z.x.rest) {
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) oacc[dt][i] = rounded_off<bf16_t>(oacc[dt][i] * inv);
+        store_rows_coalesced(patch, static_cast<bf16_t*>(z.x.rest) + row0, at.out_row(), oacc, 1.f, l);
+    }
     if (l < 16) z.LSE[(size_t)bh * z.L + qrow_l] = none ? -INFINITY : (m + log2f(lsum)) * kLn2;
 }
 

@@ -2,17 +2,20 @@
 // grid, the work items and the cuts of the plain bf16 kernel (attn_bwd_bf16_kernels.hip).
 //
 // With c = 1 / (1 - p) the exponentials are taken against LSE - log c, so that they are c P; delta is divided by c to match:
-// dS = c P (M dP - delta / c), dV = (M c P)^T dO.  Both sides make the factors M anew.
+// dS = c P (M dP - delta / c), dV = (M c P)^T dO.  Both sides make the factors M anew.  Both numbers of every row come from a
+// kernel before this one (row_terms_kernel): made by the key side from its tiles of O, each step had a third tile, a product and a
+// barrier more.
 //
 // The table's gradient needs dS by distance.  The query side adds up its diagonals: within a wave's 16 queries by lane
 // shifts (diagonal_sums) and through LDS, over the waves of the workgroup one step later, behind the barrier that is there anyway.  What leaves
 // is one number for each distance of a block, slices[head][kept block][2 BS], 1/32 of what the block's tiles bring in.
 //
-// Three waves a SIMD at 168 registers, which the arguments read again where they are used (args_again) and addresses made anew for each block (once)
-// leave room for; at two the backward with bias and dropout took 253 instead of 220 us (4 x 8 heads x 4096, 20.8 %).  Neither the matrix nor the vector
-// pipes are busy half of the time: a step is one chain of products, exponentials and products, longer than the plain one by
-// the draws and the biases.  Kernel time, us, of the plain one, with lengths, bias, dropout, bias and dropout: 4 x 4 heads x 4096, block 64, 8 %, 45.5 / 52 / 66 /
-// 72 / 86; 4 x 8 heads, 20.8 %, 149 / 155 / 175 / 200 / 220; 2 x 8 x 16320, 5 %, 302 / 292 / 325 / 363 / 392; 16 x 4 x 1024, block 32, 15 %, 28.5 / 33.5 / 44 / 42.5 / 54.
+// Three waves a SIMD at up to 168 registers (block 32: four at 128), which the arguments read again where they are used (args_again) and addresses made
+// anew for each block (once) leave room for; at two the backward with bias and dropout took 253 instead of 220 us (4 x 8 heads x 4096, 20.8 %).  Neither
+// the matrix nor the vector pipes are busy half of the time: a step is one chain of products, exponentials and products, longer than the plain one by
+// the draws and the biases.  Kernel time, us, of the plain one, with lengths, bias, dropout, bias and dropout (row_terms_kernel not counted): 4 x 4 heads x 4096,
+// block 64, 8 %, 45.5 / 48.5 / 62 / 67 / 83; 4 x 8 heads, 20.8 %, 151 / 145 / 160 / 185 / 208; 2 x 8 x 16320, 5 %, 303 / 263 / 306 / 344 / 387; 16 x 4 x 1024, block 32,
+// 15 %, 28.5 / 28.7 / 38.6 / 37.9 / 50.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <stdint.h>
@@ -27,8 +30,7 @@
 namespace spion {
 
 struct BwdWith {
-    const bf16_t *Q, *K, *V, *O, *dO;
-    const float* LSE;
+    const bf16_t *Q, *K, *V, *dO;
     bf16_t *dQ, *dK, *dV;
     const int *row_ptr, *col_idx, *col_ptr, *row_idx;
     float* partial;
@@ -51,12 +53,14 @@ __device__ __forceinline__ float where_kept(float v, const unsigned (&f)[2], int
 }  // namespace
 
 template <int BS, bool BIAS, bool DROP>
-__global__ __launch_bounds__(BS * 4, 3) void attn_bwd_with_bf16_kernel(BwdWith a) {
+__global__ __launch_bounds__(BS * 4, BS == 32 ? 4 : 3) void attn_bwd_with_bf16_kernel(BwdWith a) {
     constexpr int NT = BS / 16;   // 16-row tiles per block = waves per workgroup
-    // Query side: {ta, tb} hold {K, V} of a block, two stages; tc0 and tc1 what adds up diagonals.  Key side: {ta, tb, tc} hold
-    // {Q, dO, O} of a block row, two stages.
-    __shared__ __attribute__((aligned(16))) bf16_t ta0[BS * kD], tb0[BS * kD], tc0[BS * kD];
-    __shared__ __attribute__((aligned(16))) bf16_t ta1[BS * kD], tb1[BS * kD], tc1[BS * kD];
+    // {ta, tb} hold {K, V} of a block (query side) or {Q, dO} of a block row (key side), two stages
+    __shared__ __attribute__((aligned(16))) bf16_t ta0[BS * kD], tb0[BS * kD], ta1[BS * kD], tb1[BS * kD];
+    // Diagonals (query side): each wave's places (lane group, distance), of which those it never writes stay 0, and for two steps each
+    // wave's sums of every distance of the block.
+    constexpr int kPlaces = 16 * NT + 32;
+    __shared__ float all_places[BIAS ? NT * 4 * kPlaces : 1], sums[BIAS ? 2 * NT * 2 * BS : 1];   // sums [step % 2][wave][2 BS]
     __shared__ __attribute__((aligned(16))) float lse0[BS], del0[BS], lse1[BS], del1[BS];
     __shared__ __attribute__((aligned(16))) float bias0[kSlice<BS>], bias1[kSlice<BS>];
     __shared__ float tab[BIAS ? Extras::kMaxBuckets : 1];
@@ -64,8 +68,6 @@ __global__ __launch_bounds__(BS * 4, 3) void attn_bwd_with_bf16_kernel(BwdWith a
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int L = a.L, nb = a.nb;
-    if (BIAS && blockIdx.x == 0)
-        for (int h = tid; h < a.x.H; h += BS * 4) a.x.counters[h * Extras::kCounterStride] = 0u;
 
     // which workgroup am I
     const ItemOfHead dealt_to = deal_heads(blockIdx.x, a.BH, a.few != 0);
@@ -103,8 +105,6 @@ __global__ __launch_bounds__(BS * 4, 3) void attn_bwd_with_bf16_kernel(BwdWith a
     const BlockBias<BS, BIAS> biases(a.x, tab, L, wave);
     const SwzLane sl(r, g);
     const int length = length_of(a.x, bh, L);
-    // what a row's exponentials are taken against; a row that keeps nothing, or past the sequence's end, has no probabilities
-    auto reference = [](float lse, float log2_keep) { return lse == -INFINITY ? INFINITY : fmaf(lse, kLog2e, -log2_keep); };
 
     if (!key_side) {
         // ========================================================================================
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(BS * 4, 3) void attn_bwd_with_bf16_kernel(BwdWith a
         const size_t head = at.in_head(bh, L), out_head = at.out_head(bh, L), vec = (size_t)bh * L;
         [[maybe_unused]] const ScoreDraws draws(b.x.rng, b.x.stream, bh);
         [[maybe_unused]] const unsigned below = both_halves(b.x.threshold - 1u);
-        const float scale_log2 = b.scale_log2, log2_keep = DROP ? log2f(b.x.keep_scale) : 0.f;
+        const float scale_log2 = b.scale_log2;
         const int I = idx;
         const int qrow = I * BS + wave * 16 + r;
         unsigned bucket = biases.request(0, tid);
@@ -129,23 +129,12 @@ __global__ __launch_bounds__(BS * 4, 3) void attn_bwd_with_bf16_kernel(BwdWith a
         };
         if (!helper) issue(ta0, tb0, I);   // the diagonal block, before any index is known
         bf16x8 qf[2], dof[2];
-        float delta = 0.f, lse2 = INFINITY;
-        {
-            bf16x8 of[2];
+        const float lse2 = b.x.row_lse[vec + qrow], ndelta = b.x.row_delta[vec + qrow];
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const size_t out = out_head + (size_t)qrow * out_row + c * 32 + g * 8;
-                qf[c] = *reinterpret_cast<const bf16x8*>(b.Q + head + (size_t)qrow * in_row + c * 32 + g * 8);
-                dof[c] = *reinterpret_cast<const bf16x8*>(b.dO + out);
-                of[c] = *reinterpret_cast<const bf16x8*>(b.O + out);
-                if (qrow >= length) qf[c] = dof[c] = of[c] = bf16x8{};
-            }
-            if (qrow < length) lse2 = reference(b.LSE[vec + qrow], log2_keep);
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) delta = fmaf((float)dof[c][e], (float)of[c][e], delta);
-            delta = group_sum(delta) * (DROP ? 1.f / b.x.keep_scale : 1.f);
+        for (int c = 0; c < 2; ++c) {
+            qf[c] = *reinterpret_cast<const bf16x8*>(b.Q + head + (size_t)qrow * in_row + c * 32 + g * 8);
+            dof[c] = *reinterpret_cast<const bf16x8*>(b.dO + out_head + (size_t)qrow * out_row + c * 32 + g * 8);
+            if (qrow >= length) qf[c] = dof[c] = bf16x8{};
         }
         int jb = b.row_ptr[I], n = b.row_ptr[I + 1] - jb;
         if (n > a.cut.longest) {
@@ -187,14 +176,10 @@ __global__ __launch_bounds__(BS * 4, 3) void attn_bwd_with_bf16_kernel(BwdWith a
             }
             issue(ta0, tb0, jcur);
         }
-        // Diagonals: this wave's places (lane group, distance), of which those it never writes stay 0, and for two steps each
-        // wave's sums of every distance of the block.
-        constexpr int kPlaces = 16 * NT + 32;
-        float* const places = reinterpret_cast<float*>(tc0) + wave * (4 * kPlaces);
-        float* const sums = reinterpret_cast<float*>(tc1);   // [step % 2][wave][2 BS]
+        float* const places = all_places + wave * (4 * kPlaces);
         float* const my_slices = BIAS ? b.x.slices + ((size_t)bh * b.nnzb + jb) * (2 * BS) + tid : nullptr;   // of this row (piece)
         if constexpr (BIAS) {
-            for (int i = tid; i < NT * 4 * kPlaces; i += BS * 4) reinterpret_cast<float*>(tc0)[i] = 0.f;
+            for (int i = tid; i < NT * 4 * kPlaces; i += BS * 4) all_places[i] = 0.f;
             for (int e = n + tid; e < n_all; e += BS * 4)   // what is not computed
                 (my_slices - tid)[(size_t)e * (2 * BS) + 2 * BS - 1] = __builtin_bit_cast(float, kNoSlice);
         }
@@ -254,7 +239,7 @@ __global__ __launch_bounds__(BS * 4, 3) void attn_bwd_with_bf16_kernel(BwdWith a
 #pragma unroll
             for (int kt16 = 0; kt16 < NT; ++kt16) {
                 // without dropout dP - delta comes out of the MFMA: the accumulator starts at -delta
-                dp[kt16] = DROP ? f32x4{0.f, 0.f, 0.f, 0.f} : f32x4{-delta, -delta, -delta, -delta};
+                dp[kt16] = DROP ? f32x4{0.f, 0.f, 0.f, 0.f} : f32x4{ndelta, ndelta, ndelta, ndelta};
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     s[kt16] = mma_d(s[kt16], kfr[kt16][c], qf[c]);      // S^T = K Q^T
@@ -293,7 +278,7 @@ __global__ __launch_bounds__(BS * 4, 3) void attn_bwd_with_bf16_kernel(BwdWith a
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float p = fast_exp2(fmaf(s[kt16][i], scale_log2, -lse2));
-                    s[kt16][i] = p * (DROP ? where_kept(dp[kt16][i], factors[kt16], i) - delta : dp[kt16][i]);
+                    s[kt16][i] = p * (DROP ? where_kept(dp[kt16][i], factors[kt16], i) + ndelta : dp[kt16][i]);
                 }
                 dsq[kt16] = to_quad<bf16_t>(s[kt16]);
             }
@@ -389,7 +374,7 @@ __global__ __launch_bounds__(BS * 4, 3) void attn_bwd_with_bf16_kernel(BwdWith a
     }
 
     // ============================================================================================
-    // key side: work item idx of head bh.  {Q, dO, O} tiles and LSE of a block row in two stages.
+    // key side: work item idx of head bh.  {Q, dO} tiles and the rows' numbers of a block row in two stages.
     // ============================================================================================
     const auto& b = args_again<BwdWith>();   // this side's
     const Rows at = {b.at.H, b.at.beside};
@@ -397,7 +382,7 @@ __global__ __launch_bounds__(BS * 4, 3) void attn_bwd_with_bf16_kernel(BwdWith a
     const size_t head = at.in_head(bh, L), out_head = at.out_head(bh, L), vec = (size_t)bh * L;
     [[maybe_unused]] const ScoreDraws draws(b.x.rng, b.x.stream, bh);
     [[maybe_unused]] const unsigned below = both_halves(b.x.threshold - 1u);
-    const float scale_log2 = b.scale_log2, log2_keep = DROP ? log2f(b.x.keep_scale) : 0.f;
+    const float scale_log2 = b.scale_log2;
     const KeyItem item = key_item_lookup(b.col_ptr, nb, b.chunk, b.finest, idx, lane);
     if (item.J < 0) return;
     const int J = item.J, slot = item.slot;
@@ -410,9 +395,9 @@ __global__ __launch_bounds__(BS * 4, 3) void attn_bwd_with_bf16_kernel(BwdWith a
     const int last = n > 0 ? n - 1 : 0;
     auto row_at = [&](int t) { return __builtin_amdgcn_readlane(rows_v, t < last ? t : last); };
 
-    const bf16_t *const Qh = b.Q + head, *const dOh = b.dO + out_head, *const Oh = b.O + out_head;
-    const float* const LSEh = b.LSE + vec;
-    // six tile loads per wave, plus one 4-byte-per-lane load of LSE in wave 0
+    const bf16_t *const Qh = b.Q + head, *const dOh = b.dO + out_head;
+    const float *const lse_h = b.x.row_lse + vec, *const delta_h = b.x.row_delta + vec;
+    // four tile loads per wave, plus one 4-byte-per-lane load in waves 0 and 1
     auto load_q = [&](bf16_t* qt, int I) {   // (offsets of the lane made here each time: registers are short)
         const TileLoadLane tli(wave, once(lane), in_row);
         tile_load_async(Qh + (size_t)I * BS * in_row, qt, wave, tli, tile_range<BS>(I * BS, length, in_row));
@@ -421,10 +406,9 @@ __global__ __launch_bounds__(BS * 4, 3) void attn_bwd_with_bf16_kernel(BwdWith a
         const TileLoadLane tlo(wave, once(lane), out_row);
         tile_load_async(dOh + (size_t)I * BS * out_row, dt_, wave, tlo, tile_range<BS>(I * BS, length, out_row));
     };
-    auto load_o = [&](bf16_t* ot, float* lse_s, int I) {
-        const TileLoadLane tlo(wave, once(lane), out_row);
-        tile_load_async(Oh + (size_t)I * BS * out_row, ot, wave, tlo, tile_range<BS>(I * BS, length, out_row));
-        if (wave == 0 && lane < BS) __builtin_amdgcn_global_load_lds(LSEh + (size_t)I * BS + once(lane), (lds_void_ptr)lse_s, 4, 0, 0);
+    auto load_rows = [&](float* lse_s, float* del_s, int I) {
+        if (wave < 2 && lane < BS)
+            __builtin_amdgcn_global_load_lds((wave ? delta_h : lse_h) + (size_t)I * BS + once(lane), (lds_void_ptr)(wave ? del_s : lse_s), 4, 0, 0);
     };
     unsigned bucket = 0;
     int icur = 0, inext = 0;   // block row of steps it, it + 1
@@ -436,7 +420,7 @@ __global__ __launch_bounds__(BS * 4, 3) void attn_bwd_with_bf16_kernel(BwdWith a
         bucket = biases.request(J - inext, tid);
         load_q(ta0, icur);
         load_do(tb0, icur);
-        load_o(tc0, lse0, icur);
+        load_rows(lse0, del0, icur);
         if constexpr (BIAS) {
             lds_meet();   // the table is there
             biases.put(bias0, first, tid);
@@ -457,39 +441,20 @@ __global__ __launch_bounds__(BS * 4, 3) void attn_bwd_with_bf16_kernel(BwdWith a
         dv[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     const int slice_at = wave * 16 + r - 4 * g + BS - 1;   // of query 4 g of the block
-    const float delta_scale = DROP ? -1.f / b.x.keep_scale : -1.f;
 
-    auto step = [&](const bf16_t* qt, const bf16_t* dt_, const bf16_t* ot, float* lse_s, float* del_s, const float* bias_c, bf16_t* nq, bf16_t* nd,
-                    bf16_t* no, float* nlse, float* bias_n, int it) {
+    auto step = [&](const bf16_t* qt, const bf16_t* dt_, const float* lse_s, const float* del_s, const float* bias_c, bf16_t* nq, bf16_t* nd,
+                    float* nlse, float* ndel, float* bias_n, int it) {
         // everyone's part of block `it` has landed and the other stage is no longer read
         meet(false);
-        constexpr bool kSpread = BS == 64;   // the next tiles are requested in three places, see the plain kernel
+        constexpr bool kSpread = BS == 64;   // the next tiles are requested in two places, see the plain kernel
         const bool more = it + 1 < n;
         if (more) {
             if constexpr (BIAS) biases.put(bias_n, bucket, tid);
             load_q(nq, inext);
-            if (!kSpread) {
-                load_do(nd, inext);
-                load_o(no, nlse, inext);
-            }
+            load_rows(nlse, ndel, inext);
+            if (!kSpread) load_do(nd, inext);
         }
         if constexpr (BIAS) bucket = biases.request(J - row_at(it + 2), tid);
-        // delta of the 16 query rows 16 wave .. + 15: the diagonal of dO O^T; stored negated (and divided by c)
-        {
-            f32x4 dd = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const int off = wave * 16 * kD + sl.frag[c];
-                dd = mma_d(dd, *reinterpret_cast<const bf16x8*>(dt_ + off), *reinterpret_cast<const bf16x8*>(ot + off));
-            }
-            // lane (r, g) holds (dO O^T)[4 g + i][r]: the diagonal entry of row r sits in lane group r / 4
-            const int l = once(lane), row = l & 15;
-            const float d0 = (row & 1) ? dd[1] : dd[0], d1 = (row & 1) ? dd[3] : dd[2];
-            if ((l >> 4) == (row >> 2)) del_s[wave * 16 + row] = ((row & 2) ? d1 : d0) * delta_scale;
-            if (wave == 0 && l < BS) lse_s[l] = reference(lse_s[l], log2_keep);
-        }
-        lds_meet();
-        if (kSpread && more) load_do(nd, inext);
         // 32 query rows at a time: S and dP of two 16-row tiles, then their share of dV and dK
         bf16x8 fq[2], fd[2];
         auto frags = [&](int qt16) {
@@ -550,7 +515,7 @@ __global__ __launch_bounds__(BS * 4, 3) void attn_bwd_with_bf16_kernel(BwdWith a
                 if constexpr (DROP) pq[h] = drop(pq[h], factors[h]);
                 dsq[h] = to_quad<bf16_t>(ds);
             }
-            if (kSpread && pc == 0 && more) load_o(no, nlse, inext);
+            if (kSpread && pc == 0 && more) load_do(nd, inext);
             // dV^T[d][key] += dO^T P and dK^T[d][key] += Q^T dS for these 32 rows, interleaved
             const bf16x8 pf = join(pq[0], pq[1]), dsf = join(dsq[0], dsq[1]);
             bf16x8 ring[2];
@@ -568,8 +533,8 @@ __global__ __launch_bounds__(BS * 4, 3) void attn_bwd_with_bf16_kernel(BwdWith a
     };
 
     for (int it = 0; it < n; it += 2) {
-        step(ta0, tb0, tc0, lse0, del0, bias0, ta1, tb1, tc1, lse1, bias1, it);
-        if (it + 1 < n) step(ta1, tb1, tc1, lse1, del1, bias1, ta0, tb0, tc0, lse0, bias0, it + 1);
+        step(ta0, tb0, lse0, del0, bias0, ta1, tb1, lse1, del1, bias1, it);
+        if (it + 1 < n) step(ta1, tb1, lse1, del1, bias1, ta0, tb0, lse0, del0, bias0, it + 1);
     }
     __builtin_amdgcn_s_waitcnt(kWaitVm0);   // the owned fragments of a column without kept rows
 
@@ -619,8 +584,7 @@ __global__ __launch_bounds__(BS * 4, 3) void attn_bwd_with_bf16_kernel(BwdWith a
 
 // The plan of the plain kernel: cuts, order and lengths of work items as there.
 template <int BS>
-hipError_t bwd_with_bf16(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, const void* O, const void* dO,
-                         const float* LSE, void* dQ, void* dK, void* dV, const int* row_ptr, const int* col_idx, const int* col_ptr,
+hipError_t bwd_with_bf16(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, const void* dO, void* dQ, void* dK, void* dV, const int* row_ptr, const int* col_idx, const int* col_ptr,
                          const int* row_idx, int nnzb, void* workspace, hipStream_t st) {
     const BwdWorkspace ws(s.BH, s.bs, s.nb, nnzb, key_chunk(s.BH, BS, s.nb, nnzb), s.nb / 4, bwd_bf16_row_slots(s, nnzb));
     const int n_key_a = ws.w_first, n_key_c = ws.w_max - ws.w_first;
@@ -641,8 +605,8 @@ hipError_t bwd_with_bf16(const AttnShape& s, const Extras& x, const void* Q, con
     const int sort_rows = total > bwd_resident(BS) && (nnzb >= 6 * s.nb || s.nb >= 8 * bwd_steps_per_slot(s.BH, BS, s.nb, nnzb));
     const long long at_once = bwd_resident(BS);
     const int finest = 3 * total <= at_once ? 0 : total <= at_once ? 1 : total <= 4 * at_once ? 2 : 4;
-    const BwdWith args = {static_cast<const bf16_t*>(Q), static_cast<const bf16_t*>(K), static_cast<const bf16_t*>(V), static_cast<const bf16_t*>(O),
-                          static_cast<const bf16_t*>(dO), LSE, static_cast<bf16_t*>(dQ), static_cast<bf16_t*>(dK), static_cast<bf16_t*>(dV),
+    const BwdWith args = {static_cast<const bf16_t*>(Q), static_cast<const bf16_t*>(K), static_cast<const bf16_t*>(V),
+                          static_cast<const bf16_t*>(dO), static_cast<bf16_t*>(dQ), static_cast<bf16_t*>(dK), static_cast<bf16_t*>(dV),
                           row_ptr, col_idx, col_ptr, row_idx, reinterpret_cast<float*>(static_cast<char*>(workspace) + ws.counter_bytes),
                           static_cast<unsigned long long*>(workspace), s.tag, Rows{x.H, s.heads_beside != 0}, x, cut, ws.n_slots, s.BH, s.L, s.nb,
                           nnzb, n_key_a, n_key_c, ws.w_first, ws.chunk, sort_rows, finest, few, s.scale, s.scale * kLog2e};
@@ -656,9 +620,9 @@ hipError_t bwd_with_bf16(const AttnShape& s, const Extras& x, const void* Q, con
     }
     return hipGetLastError();
 }
-template hipError_t bwd_with_bf16<32>(const AttnShape&, const Extras&, const void*, const void*, const void*, const void*, const void*, const float*,
+template hipError_t bwd_with_bf16<32>(const AttnShape&, const Extras&, const void*, const void*, const void*, const void*,
                                       void*, void*, void*, const int*, const int*, const int*, const int*, int, void*, hipStream_t);
-template hipError_t bwd_with_bf16<64>(const AttnShape&, const Extras&, const void*, const void*, const void*, const void*, const void*, const float*,
+template hipError_t bwd_with_bf16<64>(const AttnShape&, const Extras&, const void*, const void*, const void*, const void*,
                                       void*, void*, void*, const int*, const int*, const int*, const int*, int, void*, hipStream_t);
 
 }  // namespace spion

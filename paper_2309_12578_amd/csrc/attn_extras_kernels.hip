@@ -332,6 +332,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_fwd_with_kernel(
         const bool empty = (!(l > 0.f) && l == l) || row0 + q >= length;
         o = empty ? f32x4{0.f, 0.f, 0.f, 0.f} : o * ((DROP ? x.keep_scale : 1.f) / l);
         store_quad<T>(O + head + (size_t)(row0 + q) * kD + d, o);
+        if constexpr (sizeof(T) == 2) {
+            if (x.rest)
+                store_quad<T>(static_cast<T*>(x.rest) + head + (size_t)(row0 + q) * kD + d,
+                              f32x4{rounded_off<T>(o[0]), rounded_off<T>(o[1]), rounded_off<T>(o[2]), rounded_off<T>(o[3])});
+        }
         if (d == 0) LSE[(size_t)bh * L + row0 + q] = empty ? -INFINITY : (mm + log2f(l)) * kLn2;
     }
 }
@@ -345,14 +350,51 @@ struct ColumnCut {
 };
 
 // ------------------------------------------------------------------------------------------------
+// Before the backward: the two numbers of a row that both of its sides need.  Exponentials are taken against log2(e) LSE - log2(c), so that they are
+// c P, and delta = rowsum(dO . O) is left as -delta / c; a row that keeps nothing, or past the sequence's end, has no probabilities.  O is
+// what the forward stored plus what its rounding left (x.rest): with bf16's rounding alone dQ and dK are off by a twentieth more and the table's
+// gradient, over whose far buckets a row's error adds up, by up to the double.  Bound by memory, 8 lanes a row.
+// ------------------------------------------------------------------------------------------------
+template <typename T>
+__global__ __launch_bounds__(256) void row_terms_kernel(const T* __restrict__ O, const T* __restrict__ dO, const float* __restrict__ LSE, Extras x, int beside,
+                                                        int L, long long rows) {
+    constexpr int VEC = 16 / sizeof(T), LANES = 8, PER = kD / LANES;
+    typedef T Vec __attribute__((ext_vector_type(VEC)));
+    if (blockIdx.x == 0 && x.counters)
+        for (int h = threadIdx.x; h < x.H; h += 256) x.counters[h * Extras::kCounterStride] = 0ull;
+    const long long row = (long long)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    if (row >= rows) return;   // (all lanes of a row together)
+    const int bh = (int)(row / L), i = (int)(row % L), part = threadIdx.x % LANES;
+    const Rows at = {x.H, beside};
+    float delta = 0.f, lse = -INFINITY;
+    if (i < length_of(x, bh, L)) {
+        const size_t from = at.out_head(bh, L) + (size_t)i * at.out_row() + part * PER;
+        lse = LSE[row];
+#pragma unroll
+        for (int c = 0; c < PER; c += VEC) {
+            const Vec o = *reinterpret_cast<const Vec*>(O + from + c), g = *reinterpret_cast<const Vec*>(dO + from + c);
+            Vec rest = {};
+            if (sizeof(T) == 2 && x.rest) rest = *reinterpret_cast<const Vec*>(static_cast<const T*>(x.rest) + from + c);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) delta = fmaf((float)g[e], (float)o[e] + (float)rest[e], delta);
+        }
+    }
+#pragma unroll
+    for (int o = 1; o < LANES; o <<= 1) delta += __shfl_xor(delta, o);
+    if (part == 0) {
+        x.row_lse[row] = lse == -INFINITY ? INFINITY : fmaf(lse, kLog2e, -log2f(x.keep_scale));
+        x.row_delta[row] = lse == -INFINITY ? 0.f : -delta / x.keep_scale;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
 // backward: workgroup = (head, Tiles::OWN rows of a block row) on the query side, (head, as many keys of a block column) on the key side.
-// The sides share no data; all sums in fixed order.  The query side leaves, for the table's gradient, the sums over the 31 diagonals of each
+// The exponentials are c P, delta is divided by c to match (see row_terms_kernel).  The sides share no data; all sums in fixed order.  The query side leaves, for the table's gradient, the sums over the 31 diagonals of each
 // 16 x 16 tile of dS in slices[head][kept block][query tile][key tile][32].
 // ------------------------------------------------------------------------------------------------
 template <typename T>
 struct BwdOfRows {
-    const T *Q, *K, *V, *O, *dO;
-    const float* LSE;
+    const T *Q, *K, *V, *dO;
     T *dQ, *dK, *dV;
     const int *row_ptr, *col_idx, *col_ptr, *row_idx;
     Extras x;
@@ -364,14 +406,12 @@ struct BwdOfRows {
 
 template <typename T, int BS, int NQ, int W, bool DROP>
 __global__ __launch_bounds__(W * 64, 2) void attn_bwd_with_kernel(const BwdOfRows<T> a) {
-    const T *__restrict__ const Q = a.Q, *__restrict__ const K = a.K, *__restrict__ const V = a.V, *__restrict__ const O = a.O, *__restrict__ const dO = a.dO;
-    const float* __restrict__ const LSE = a.LSE;
+    const T *__restrict__ const Q = a.Q, *__restrict__ const K = a.K, *__restrict__ const V = a.V, *__restrict__ const dO = a.dO;
     const Extras& x = a.x;
     const int L = a.L;
     const float scale_log2 = a.scale_log2;
     typedef typename Elem<T>::Frag Frag;
     typedef typename Elem<T>::Quad Quad;
-    typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
     typedef Tiles<T, BS, NQ> S;
     constexpr int KT = S::KT, NDC = S::NDC, TPB = S::TPB, STRIDE = W * KT;
     constexpr int kDiag = 48;   // floats per lane group and wave: places of distance 16 kt + 4 g - p, behind each other
@@ -381,8 +421,6 @@ __global__ __launch_bounds__(W * 64, 2) void attn_bwd_with_kernel(const BwdOfRow
 
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    if (blockIdx.x == 0 && x.counters)
-        for (int h = tid; h < x.H; h += W * 64) x.counters[h * Extras::kCounterStride] = 0u;
     const RowCut& cut = a.cut;
     const ColumnCut& columns = a.columns;
     const int BH = a.BH, nb = a.nb, sort_rows = a.sort_rows;
@@ -426,7 +464,6 @@ __global__ __launch_bounds__(W * 64, 2) void attn_bwd_with_kernel(const BwdOfRow
         for (int i = tid; i < W * 4 * kDiag; i += W * 64) (&diag_s[0][0][0])[i] = 0.f;
     __syncthreads();
     [[maybe_unused]] ScoreDraws draws(x.rng, x.stream, bh);
-    const float keep = DROP ? x.keep_scale : 1.f;
 
     constexpr int kAtOnce = 4 * W;   // rows that all threads have together, 4 columns each
     auto merged = [&](int p) {       // rows p + tid / 16
@@ -447,28 +484,20 @@ __global__ __launch_bounds__(W * 64, 2) void attn_bwd_with_kernel(const BwdOfRow
 
     if (!key_side) {
         Frag qf[NQ][NDC], dof[NQ][NDC];
-        float delta[NQ], lse2[NQ];
+        float ndelta[NQ], lse2[NQ];
 #pragma unroll
         for (int h = 0; h < NQ; ++h) {
-            delta[h] = 0.f;
-            lse2[h] = INFINITY;
-            if (row0 + 16 * h + r < length) {
-                Frag of[NDC];
-                const size_t at = head + (size_t)(row0 + 16 * h) * kD;
+            const int row = row0 + 16 * h + r;
+            const size_t at = head + (size_t)(row0 + 16 * h) * kD;
+            if (row < length) {
                 load_rows<T>(qf[h], Q + at, r, g);
                 load_rows<T>(dof[h], dO + at, r, g);
-                load_rows<T>(of, O + at, r, g);
-                lse2[h] = LSE[vec + row0 + 16 * h + r] * kLog2e;
-                if (lse2[h] == -INFINITY) lse2[h] = INFINITY;   // a row that keeps nothing
-#pragma unroll
-                for (int c = 0; c < NDC; ++c)
-#pragma unroll
-                    for (int e = 0; e < Elem<T>::EPL; ++e) delta[h] = fmaf((float)dof[h][c][e], (float)of[c][e], delta[h]);
             } else {
                 clear(qf[h]);
                 clear(dof[h]);
             }
-            delta[h] = group_sum(delta[h]);
+            lse2[h] = x.row_lse[vec + row];
+            ndelta[h] = x.row_delta[vec + row];
         }
         auto slice = [&](int entry, int h, int key_tile) {
             return a.x.slices + ((((size_t)bh * a.nnzb + entry0 + entry) * TPB + sub + h) * TPB + key_tile) * 32;
@@ -519,8 +548,7 @@ __global__ __launch_bounds__(W * 64, 2) void attn_bwd_with_kernel(const BwdOfRow
                     for (int i = 0; i < 4; ++i) {
                         const bool masked = !there || k0[u] + 4 * g + i >= length;
                         const float p = masked ? 0.f : exp2f(fmaf(s[i], scale_log2, -lse2[h]));
-                        const float dpi = DROP && d[i] < x.threshold ? 0.f : dp[i] * keep;
-                        ds[i] = p * (dpi - delta[h]);
+                        ds[i] = p * ((DROP && d[i] < x.threshold ? 0.f : dp[i]) + ndelta[h]);
                     }
                     dsq[h][u] = to_quad<T>(ds);
                     if (x.slices && there) {
@@ -602,12 +630,12 @@ __global__ __launch_bounds__(W * 64, 2) void attn_bwd_with_kernel(const BwdOfRow
             }
             const int q0 = tile0(t + u);
             const size_t at = head + (size_t)q0 * kD;
-            Frag qf[NDC], df[NDC], of[NDC];
+            Frag qf[NDC], df[NDC];
             unsigned buckets[NQ];
             load_rows<T>(df, dO + at, r, g);
-            load_rows<T>(of, O + at, r, g);
             load_rows<T>(qf, Q + at, r, g);
-            const f32x4_any lse = *reinterpret_cast<const f32x4_any*>(LSE + vec + q0 + 4 * g);
+            const f32x4 lse2 = *reinterpret_cast<const f32x4*>(x.row_lse + vec + q0 + 4 * g);
+            const f32x4 ndelta = *reinterpret_cast<const f32x4*>(x.row_delta + vec + q0 + 4 * g);
             load_cols<T>(dc[u], dO + at, r, g);
             load_cols<T>(qc[u], Q + at, r, g);
 #pragma unroll
@@ -615,21 +643,10 @@ __global__ __launch_bounds__(W * 64, 2) void attn_bwd_with_kernel(const BwdOfRow
             __builtin_amdgcn_sched_barrier(0);
             if (q0 + 16 > length) {
                 zero_rows_from<T>(df, q0 + r >= length);
-                zero_rows_from<T>(of, q0 + r >= length);
                 zero_rows_from<T>(qf, q0 + r >= length);
                 zero_cols_from<T>(dc[u], q0 + 4 * g, length);
                 zero_cols_from<T>(qc[u], q0 + 4 * g, length);
             }
-            float part = 0.f;
-#pragma unroll
-            for (int c = 0; c < NDC; ++c)
-#pragma unroll
-                for (int e = 0; e < Elem<T>::EPL; ++e) part = fmaf((float)df[c][e], (float)of[c][e], part);
-            // delta of rows 4 g + i in every lane: the lanes' shares of row r times a tile of ones
-            const f32x4 delta = __builtin_amdgcn_mfma_f32_16x16x4f32(part, 1.f, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-            f32x4 lse2;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) lse2[i] = lse[i] == -INFINITY || q0 + 4 * g + i >= length ? INFINITY : lse[i] * kLog2e;
 #pragma unroll
             for (int h = 0; h < NQ; ++h) {
                 f32x4 s = bias_of<true>(x, tab, buckets[h]), dp = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -645,8 +662,8 @@ __global__ __launch_bounds__(W * 64, 2) void attn_bwd_with_kernel(const BwdOfRow
                 for (int i = 0; i < 4; ++i) {
                     const float pi = exp2f(fmaf(s[i], scale_log2, -lse2[i]));
                     const bool drop = DROP && d[i] < x.threshold;
-                    p[i] = drop ? 0.f : pi * keep;
-                    ds[i] = pi * ((drop ? 0.f : dp[i] * keep) - delta[i]);
+                    p[i] = drop ? 0.f : pi;
+                    ds[i] = pi * ((drop ? 0.f : dp[i]) + ndelta[i]);
                 }
                 pq[h][u] = to_quad<T>(p);
                 dsq[h][u] = to_quad<T>(ds);
@@ -777,15 +794,16 @@ struct GenericBwd {
     }
 };
 
-// The backward's: of pieces of rows and columns first, then what the table's gradient takes.
+// The backward's: of pieces of rows and columns first, then the rows' numbers and what the table's gradient takes.
 struct WithWorkspace {
-    int tile, parts;                           // rows of a tile that has its own slice; workgroups per head
-    size_t slices, partial, counters, total;   // offsets, and the end
+    int tile, parts;                                 // rows of a tile that has its own slice; workgroups per head
+    size_t rows, slices, partial, counters, total;   // offsets, and the end
     WithWorkspace(const AttnShape& s, int n_buckets, int H, int nnzb) {   // n_buckets 0: no table
         auto up = [](size_t n) { return (n + 255) / 256 * 256; };
         const bool tiled = s.is_bf16 && s.bs > 16;
         tile = tiled ? s.bs : 16;
-        slices = up(tiled ? attn_bwd_workspace(s, nnzb).with_rows : GenericBwd(s, nnzb).ws.with_rows);
+        rows = up(tiled ? attn_bwd_workspace(s, nnzb).with_rows : GenericBwd(s, nnzb).ws.with_rows);
+        slices = up(rows + 2 * (size_t)s.BH * s.L * sizeof(float));
         if (n_buckets == 0) {
             total = slices;
             return;
@@ -837,11 +855,10 @@ hipError_t fwd_with(const AttnShape& s, const Extras& x, const void* Q, const vo
 }
 
 template <typename T, int BS>
-hipError_t bwd_with(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, const void* O, const void* dO,
-                    const float* LSE, void* dQ, void* dK, void* dV, const int* row_ptr, const int* col_idx, const int* col_ptr,
-                    const int* row_idx, int nnzb, void* workspace, hipStream_t st) {
+hipError_t bwd_with(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, const void* dO, void* dQ, void* dK, void* dV,
+                    const int* row_ptr, const int* col_idx, const int* col_ptr, const int* row_idx, int nnzb, void* workspace, hipStream_t st) {
     if constexpr (sizeof(T) == 2 && BS > 16) {
-        return bwd_with_bf16<BS>(s, x, Q, K, V, O, dO, LSE, dQ, dK, dV, row_ptr, col_idx, col_ptr, row_idx, nnzb, workspace, st);
+        return bwd_with_bf16<BS>(s, x, Q, K, V, dO, dQ, dK, dV, row_ptr, col_idx, col_ptr, row_idx, nnzb, workspace, st);
     } else {
         GenericBwd plan(s, nnzb);
         const long long all = (long long)s.BH * s.nb, items = (long long)s.BH * plan.parts * (plan.ws.w_max + s.nb);
@@ -854,8 +871,8 @@ hipError_t bwd_with(const AttnShape& s, const Extras& x, const void* Q, const vo
         const long long grid = plan.cut.groups + group_grid((long long)s.BH * plan.parts * columns.n_first) + (sort_rows ? plan.parts * group_grid(all) : group_grid(all * plan.parts)) +
                                group_grid((long long)s.BH * plan.parts * (columns.n_items - columns.n_first));
         if (grid > 0x7fffffffll) return hipErrorInvalidValue;
-        const BwdOfRows<T> args = {static_cast<const T*>(Q), static_cast<const T*>(K), static_cast<const T*>(V), static_cast<const T*>(O),
-                                   static_cast<const T*>(dO), LSE, static_cast<T*>(dQ), static_cast<T*>(dK), static_cast<T*>(dV), row_ptr, col_idx,
+        const BwdOfRows<T> args = {static_cast<const T*>(Q), static_cast<const T*>(K), static_cast<const T*>(V),
+                                   static_cast<const T*>(dO), static_cast<T*>(dQ), static_cast<T*>(dK), static_cast<T*>(dV), row_ptr, col_idx,
                                    col_ptr, row_idx, x, plan.cut, columns, s.BH, s.L, s.nb, nnzb, sort_rows, s.scale, s.scale * kLog2e};
         auto launch = [&](auto kernel) {
             kernel<<<dim3((unsigned)grid), dim3(plan.waves * 64), 0, st>>>(args);
@@ -898,10 +915,10 @@ hipError_t launch_attn_fwd_with(const AttnShape& s, const Extras& x, const void*
     SPION_DISPATCH(fwd_with, s, x, Q, K, V, O, LSE, row_ptr, col_idx, nnzb, st);
 }
 
-static hipError_t launch_bwd(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, const void* O,
-                             const void* dO, const float* LSE, void* dQ, void* dK, void* dV, const int* row_ptr, const int* col_idx,
-                             const int* col_ptr, const int* row_idx, int nnzb, void* workspace, hipStream_t st) {
-    SPION_DISPATCH(bwd_with, s, x, Q, K, V, O, dO, LSE, dQ, dK, dV, row_ptr, col_idx, col_ptr, row_idx, nnzb, workspace, st);
+static hipError_t launch_bwd(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, const void* dO, void* dQ, void* dK,
+                             void* dV, const int* row_ptr, const int* col_idx, const int* col_ptr, const int* row_idx, int nnzb, void* workspace,
+                             hipStream_t st) {
+    SPION_DISPATCH(bwd_with, s, x, Q, K, V, dO, dQ, dK, dV, row_ptr, col_idx, col_ptr, row_idx, nnzb, workspace, st);
 }
 
 hipError_t launch_attn_bwd_with(const AttnShape& s, const Extras& extras, const void* Q, const void* K, const void* V, const void* O,
@@ -912,7 +929,18 @@ hipError_t launch_attn_bwd_with(const AttnShape& s, const Extras& extras, const 
     char* const base = static_cast<char*>(workspace);
     x.slices = x.table ? reinterpret_cast<float*>(base + ws.slices) : nullptr;
     x.counters = x.table ? reinterpret_cast<unsigned long long*>(base + ws.counters) : nullptr;
-    hipError_t e = launch_bwd(s, x, Q, K, V, O, dO, LSE, dQ, dK, dV, row_ptr, col_idx, col_ptr, row_idx, nnzb, workspace, st);
+    const long long rows = (long long)s.BH * s.L;
+    x.row_lse = reinterpret_cast<float*>(base + ws.rows);
+    x.row_delta = x.row_lse + rows;
+    auto row_terms = [&](auto kernel, auto type) {
+        typedef decltype(type) T;
+        kernel<<<dim3((unsigned)((rows + 31) / 32)), dim3(256), 0, st>>>(static_cast<const T*>(O), static_cast<const T*>(dO), LSE, x, s.heads_beside != 0, s.L, rows);
+    };
+    if ((rows + 31) / 32 > 0x7fffffffll) return hipErrorInvalidValue;
+    if (s.is_bf16) row_terms(row_terms_kernel<bf16_t>, bf16_t{});
+    else row_terms(row_terms_kernel<float>, float{});
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess) e = launch_bwd(s, x, Q, K, V, dO, dQ, dK, dV, row_ptr, col_idx, col_ptr, row_idx, nnzb, workspace, st);
     if (e != hipSuccess || !dtable) return e;
     const long long tiles = (long long)nnzb * (s.bs / ws.tile) * (s.bs / ws.tile);
     if (s.BH / x.H * tiles > 0x7fffffffll) return hipErrorInvalidValue;   // (256 GB of slices and more)

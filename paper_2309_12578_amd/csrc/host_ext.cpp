@@ -794,7 +794,7 @@ at::Tensor with_workspace(const spion_attn_params& p, const spion_attn_extras& x
 
 // The gradient of sparse_attention_with, and of heads_attention_with (q = qkv, no k and v).
 struct AttentionWithBackward : public torch::autograd::Node {
-    torch::autograd::SavedVariable q, k, v, o, lse, table, lengths, rng;
+    torch::autograd::SavedVariable q, k, v, o, rest, lse, table, lengths, rng;
     Index ix;
     AttentionExtras extras;
     int64_t H = 0;   // of qkv's heads; 0: Q, K and V
@@ -802,7 +802,7 @@ struct AttentionWithBackward : public torch::autograd::Node {
     std::string name() const override { return "SparseAttentionWithBackward"; }
 
     void release_variables() override {
-        for (torch::autograd::SavedVariable* s : {&q, &k, &v, &o, &lse, &table, &lengths, &rng}) s->reset_data();
+        for (torch::autograd::SavedVariable* s : {&q, &k, &v, &o, &rest, &lse, &table, &lengths, &rng}) s->reset_data();
     }
 
     torch::autograd::variable_list apply(torch::autograd::variable_list&& grads) override {
@@ -811,7 +811,7 @@ struct AttentionWithBackward : public torch::autograd::Node {
         if (!grads[0].defined()) return out;
         return differentiate("sparse_attention cannot be differentiated twice", [&] {
             const at::Tensor Q = q.unpack(), O = o.unpack(shared_from_this()), stat = lse.unpack(), T = table.unpack(), R = rng.unpack();
-            const at::Tensor K = H ? Q : k.unpack(), V = H ? Q : v.unpack();
+            const at::Tensor K = H ? Q : k.unpack(), V = H ? Q : v.unpack(), O_rest = rest.unpack();
             AttentionExtras with = extras;
             with.lengths = lengths.unpack();
             const c10::DeviceGuard guard(Q.device());
@@ -825,11 +825,13 @@ struct AttentionWithBackward : public torch::autograd::Node {
             const spion_attn_params p = H ? heads_params(Q, H, ix) : params_of(Q, ix);
             for (const at::Tensor* t : {&K, &V}) same(t->numel() == Q.numel() && t->scalar_type() == Q.scalar_type() && t->is_contiguous());
             for (const at::Tensor* t : {&O, &g}) same(t->numel() == Q.numel() / (H ? 3 : 1) && t->scalar_type() == Q.scalar_type() && t->is_contiguous());
+            same(!O_rest.defined() || (O_rest.numel() == O.numel() && O_rest.scalar_type() == O.scalar_type() && O_rest.is_contiguous()));
             same(stat.numel() == (int64_t)p.B * p.H * p.L && stat.scalar_type() == at::kFloat && stat.is_contiguous());
             same(!extras.n_buckets || (T.numel() == (int64_t)extras.n_buckets * p.H && T.is_contiguous() && T.device() == Q.device()));
             same(!with.lengths.defined() || (with.lengths.numel() == p.B && with.lengths.scalar_type() == at::kInt && with.lengths.is_contiguous()));
             same(!R.defined() || (R.numel() == 2 && R.scalar_type() == at::kLong && R.is_contiguous()));
-            const spion_attn_extras x = with.params(T, R);
+            spion_attn_extras x = with.params(T, R);
+            x.o_rest = O_rest.defined() ? O_rest.data_ptr() : nullptr;
             const bool table_grad = extras.n_buckets && task_should_compute_output(inputs);
             for (int i = 0; i < inputs; ++i) out[i] = new_like(Q);
             if (table_grad) out[inputs] = new_like(T);
@@ -884,9 +886,11 @@ struct ExtrasArgs {
 };
 
 // The node of a call, but for q, k, v and o.
-std::shared_ptr<AttentionWithBackward> with_node(AttentionExtras&& extras, Index&& ix, const at::Tensor& lse, const at::Tensor& table, const at::Tensor& used) {
+std::shared_ptr<AttentionWithBackward> with_node(AttentionExtras&& extras, Index&& ix, const at::Tensor& lse, const at::Tensor& rest, const at::Tensor& table,
+                                                 const at::Tensor& used) {
     auto node = std::shared_ptr<AttentionWithBackward>(new AttentionWithBackward(), torch::autograd::deleteNode);
     node->lse = torch::autograd::SavedVariable(lse, false);
+    node->rest = torch::autograd::SavedVariable(rest, false);
     node->table = torch::autograd::SavedVariable(table, false);
     node->lengths = torch::autograd::SavedVariable(extras.lengths, false);
     node->rng = torch::autograd::SavedVariable(used, false);
@@ -921,7 +925,7 @@ PyObject* py_sparse_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) 
         const at::Tensor& table = with.table;
         const c10::DeviceGuard guard(device);
         const bool grad = table.defined() ? torch::autograd::compute_requires_grad(q, k, v, table) : torch::autograd::compute_requires_grad(q, k, v);
-        at::Tensor o, lse, qc, kc, vc, tc, used;
+        at::Tensor o, rest, lse, qc, kc, vc, tc, used;
         {
             at::NoGradGuard no_grad;
             qc = dense(q);
@@ -934,6 +938,10 @@ PyObject* py_sparse_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) 
             if (with.rng.defined() && grad) used = new_longs(2, qc);
             spion_attn_extras x = with.extras.params(tc, with.rng);
             if (used.defined()) x.rng_used = (int64_t*)used.data_ptr();
+            if (grad && o.scalar_type() == at::kBFloat16) {
+                rest = new_like(o);
+                x.o_rest = rest.data_ptr();
+            }
             const at::Tensor ws = with_workspace(p, x, ix, false, qc);
             const int rc = spion_attn_fwd_with(device_ptr(qc), device_ptr(kc), device_ptr(vc), device_ptr(o), (float*)device_ptr(lse),
                                                (const int32_t*)device_ptr(ix.row_ptr), (const int32_t*)device_ptr(ix.col_idx), ix.nnzb, &p, &x,
@@ -945,7 +953,7 @@ PyObject* py_sparse_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) 
             ix.row_idx = tensor_arg(a[6]);
             ix.bsr_pos = tensor_arg(a[7]);
             for (const at::Tensor* t : {&ix.col_ptr, &ix.row_idx, &ix.bsr_pos}) check_operand(*t, device);
-            auto node = with_node(std::move(with.extras), std::move(ix), lse, tc, used);
+            auto node = with_node(std::move(with.extras), std::move(ix), lse, rest, tc, used);
             node->set_next_edges(table.defined() ? torch::autograd::collect_next_edges(q, k, v, table) : torch::autograd::collect_next_edges(q, k, v));
             node->q = torch::autograd::SavedVariable(qc, false);
             node->k = torch::autograd::SavedVariable(kc, false);
@@ -981,7 +989,7 @@ PyObject* py_heads_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::Tensor& table = with.table;
         const c10::DeviceGuard guard(device);
         const bool grad = table.defined() ? torch::autograd::compute_requires_grad(qkv, table) : torch::autograd::compute_requires_grad(qkv);
-        at::Tensor tc, used;
+        at::Tensor tc, used, rest;
         at::Tensor s(at::detail::empty_cuda({B, L, H * 64}, qkv.scalar_type(), device, std::nullopt));
         at::Tensor lse(at::detail::empty_cuda({B, H, L}, at::kFloat, device, std::nullopt));
         {
@@ -991,6 +999,10 @@ PyObject* py_heads_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) {
             if (with.rng.defined() && grad) used = new_longs(2, qkv);
             spion_attn_extras x = with.extras.params(tc, with.rng);
             if (used.defined()) x.rng_used = (int64_t*)used.data_ptr();
+            if (grad) {
+                rest = new_like(s);
+                x.o_rest = rest.data_ptr();
+            }
             const at::Tensor ws = with_workspace(p, x, ix, false, qkv);
             const int rc = spion_heads_attn_fwd_with(device_ptr(qkv), device_ptr(s), (float*)device_ptr(lse), (const int32_t*)device_ptr(ix.row_ptr),
                                                      (const int32_t*)device_ptr(ix.col_idx), ix.nnzb, &p, &x, device_ptr(ws), (size_t)ws.nbytes(),
@@ -1002,7 +1014,7 @@ PyObject* py_heads_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) {
             ix.row_idx = tensor_arg(a[5]);
             ix.bsr_pos = tensor_arg(a[6]);
             for (const at::Tensor* t : {&ix.col_ptr, &ix.row_idx}) check_operand(*t, device);
-            auto node = with_node(std::move(with.extras), std::move(ix), lse, tc, used);
+            auto node = with_node(std::move(with.extras), std::move(ix), lse, rest, tc, used);
             node->H = H;
             node->set_next_edges(table.defined() ? torch::autograd::collect_next_edges(qkv, table) : torch::autograd::collect_next_edges(qkv));
             node->q = torch::autograd::SavedVariable(qkv, false);

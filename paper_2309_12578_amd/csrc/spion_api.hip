@@ -508,6 +508,7 @@ static int take_extras(const spion_attn_params* p, const spion_attn_extras* x, i
         if (!x->bucket_of) return SPION_ERR_NULL;
     }
     if (threshold && !x->rng) return SPION_ERR_NULL;
+    if ((uintptr_t)x->o_rest % 16 != 0) return SPION_ERR_PARAM;
     const spion::AttnShape s = make_shape(p);
     out.table = x->table;
     out.bucket_of = x->bucket_of;
@@ -521,7 +522,8 @@ static int take_extras(const spion_attn_params* p, const spion_attn_extras* x, i
     out.threshold = threshold;
     out.stream = x->stream;
     out.keep_scale = keep_scale(threshold);
-    out.slices = nullptr;
+    out.rest = p->dtype == SPION_BF16 ? x->o_rest : nullptr;
+    out.row_lse = out.row_delta = out.slices = nullptr;
     out.counters = nullptr;
     return SPION_OK;
 }

@@ -60,8 +60,11 @@ struct Extras {
     float inv_scale;                  // 1 / score scale
     unsigned threshold, stream;       // draws below are dropped; 0: no dropout
     float keep_scale;                 // 65536 / (65536 - threshold)
-    float* slices;                    // backward, with a table: sums of dS over diagonals
-    // With them: [H], kCounterStride numbers apart, which the backward kernels set to 0 first thing.  (Of a type that nothing of the
+    void* rest;                       // bf16: what rounding left of O, written by the forward kernels and read by the backward's rows; or nullptr
+    // backward, [B, H, L]: what a row's exponentials are taken against, log2(e) LSE - log2(c) (infinity where it keeps nothing), and -delta / c
+    float *row_lse, *row_delta;
+    float* slices;                    // with a table: sums of dS over diagonals
+    // With them: [H], kCounterStride numbers apart, set to 0 before the backward kernels.  (Of a type that nothing of the
     // index has: behind a store that might have changed the index the compiler keeps it, and all that comes from it, in vector registers.)
     unsigned long long* counters;
     static constexpr int kMaxBuckets = 256, kCounterStride = 32;
@@ -136,8 +139,7 @@ template <int BS>
 hipError_t fwd_with_bf16(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, void* O, float* LSE,
                          const int* row_ptr, const int* col_idx, int nnzb, hipStream_t st);
 template <int BS>
-hipError_t bwd_with_bf16(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, const void* O, const void* dO,
-                         const float* LSE, void* dQ, void* dK, void* dV, const int* row_ptr, const int* col_idx, const int* col_ptr,
+hipError_t bwd_with_bf16(const AttnShape& s, const Extras& x, const void* Q, const void* K, const void* V, const void* dO, void* dQ, void* dK, void* dV, const int* row_ptr, const int* col_idx, const int* col_ptr,
                          const int* row_idx, int nnzb, void* workspace, hipStream_t st);
 size_t attn_with_workspace_bytes(const AttnShape& s, int n_buckets, int H, int nnzb, bool is_bwd);
 
