@@ -4,10 +4,14 @@
 //     S^T starts from is read from there (neighbouring lanes read neighbouring words);
 //   - dropout factors made while the tiles are on their way;
 //   - tiles whose rows from the sequence's length on come as zeros, whatever memory holds there: the loads' range ends with the sequence.
+// WHOLE, where the backward pass may have a table's gradient to make: the probabilities' rounding to bf16 goes through the product with V (and the sums) as
+// well.  A row's delta comes from O, and its error is the same for all of the row's dS: over the far buckets, which have many keys of a row, it added
+// up to 0.9e-3 of the table's gradient in the mean (bf16's own rounding of it is 1.7e-3).
+//
 // What it adds is vector work beside the products (seven rounds of Philox for eight draws, a sixteenth of a 64 x 64 block's a wave; 16
 // biases a lane) and, where rows are short, the table's way into LDS before the first scores.  Kernel time, us, of the plain one, with lengths,
-// bias, dropout, bias and dropout: 4 x 4 heads x 4096, block 64, 8 %, 16.8 / 18.9 / 21.5 / 24.5 / 26.5; 4 x 8 heads, 20.8 %, 47 / 50 / 58 / 72 / 76;
-// 2 x 8 x 16320, 5 %, 92 / 107 / 121 / 150 / 157; 16 x 4 x 1024, block 32, 15 %, 13.0 / 15.8 / 20.4 / 20.1 / 25.0.
+// bias, dropout, bias and dropout, and the last as WHOLE: 4 x 4 heads x 4096, block 64, 8 %, 16.9 / 18.9 / 21.5 / 24.5 / 26.5 / 31.5; 4 x 8 heads, 20.8 %,
+// 47 / 50 / 58 / 72 / 76 / 95; 2 x 8 x 16320, 5 %, 92 / 107 / 121 / 150 / 157 / 187; 16 x 4 x 1024, block 32, 15 %, 13.0 / 15.8 / 20.4 / 20.1 / 25.0 / 28.7.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <stdint.h>
@@ -48,8 +52,8 @@ struct FwdWith {
 // In which order block rows start, see the launcher.
 enum WithOrder { kInOrder, kDealtHeads, kLongestFirst };
 
-template <int BS, bool BIAS, bool DROP>
-__global__ __launch_bounds__(BS * 4, BS == 32 && DROP ? 5 : 4) void attn_fwd_with_bf16_kernel(FwdWith a) {
+template <int BS, bool BIAS, bool DROP, bool WHOLE>
+__global__ __launch_bounds__(BS * 4, BS == 32 && DROP && !WHOLE ? 5 : 4) void attn_fwd_with_bf16_kernel(FwdWith a) {
     constexpr int NKT = BS / 16;
     __shared__ __attribute__((aligned(16))) KvTiles<BS> sm0, sm1;
     __shared__ __attribute__((aligned(16))) float bias0[kSlice<BS>], bias1[kSlice<BS>];
@@ -210,11 +214,12 @@ __global__ __launch_bounds__(BS * 4, BS == 32 && DROP ? 5 : 4) void attn_fwd_wit
         }
         // the generator's turn: the matrix cores have the scores to do
         [[maybe_unused]] unsigned factors[NKT][2];
-        if constexpr (DROP) {
+        auto make_factors = [&]() {
             __builtin_amdgcn_sched_barrier(0);
             query_factors<NKT>(draws, qrow, jcur * BS, g, below, factors);
             __builtin_amdgcn_sched_barrier(0);
-        }
+        };
+        if constexpr (DROP && !WHOLE) make_factors();   // (else there is no room for them yet)
         // the transposed V operands of O^T += V^T P^T for 32 keys: requested here, they land while the exponentials are computed
         bf16x8 vop[4];
         auto request_v = [&](int pc) {
@@ -227,6 +232,7 @@ __global__ __launch_bounds__(BS * 4, BS == 32 && DROP ? 5 : 4) void attn_fwd_wit
         request_v(0);
         __builtin_amdgcn_sched_barrier(0);
         bf16x4 pq[NKT];
+        [[maybe_unused]] bf16x4 rest[NKT];
         f32x4 sums;
         auto probabilities = [&]() {   // and their sums, see the plain kernel
 #pragma unroll
@@ -235,10 +241,14 @@ __global__ __launch_bounds__(BS * 4, BS == 32 && DROP ? 5 : 4) void attn_fwd_wit
 #pragma unroll
                 for (int i = 0; i < 4; ++i) p[i] = fast_exp2(fmaf(s[kt][i], scale_log2, -m));
                 pq[kt] = to_quad<bf16_t>(p);
+                if constexpr (WHOLE) rest[kt] = to_quad<bf16_t>(p - f32x4{(float)pq[kt][0], (float)pq[kt][1], (float)pq[kt][2], (float)pq[kt][3]});
             }
             sums = lacc;
 #pragma unroll
-            for (int pc = 0; pc < BS / 32; ++pc) sums = mma_d(sums, ones, join(pq[2 * pc], pq[2 * pc + 1]));
+            for (int pc = 0; pc < BS / 32; ++pc) {
+                sums = mma_d(sums, ones, join(pq[2 * pc], pq[2 * pc + 1]));
+                if constexpr (WHOLE) sums = mma_d(sums, ones, join(rest[2 * pc], rest[2 * pc + 1]));
+            }
         };
         if (it > 0) probabilities();
         if (it == 0 || __any(!(sums[0] <= kSumLimit))) {
@@ -257,15 +267,24 @@ __global__ __launch_bounds__(BS * 4, BS == 32 && DROP ? 5 : 4) void attn_fwd_wit
             probabilities();
         }
         lacc = sums;
+        if constexpr (DROP && WHOLE) make_factors();
         if constexpr (DROP) {   // behind the sums: the softmax is over all of them
 #pragma unroll
-            for (int kt = 0; kt < NKT; ++kt) pq[kt] = drop(pq[kt], factors[kt]);
+            for (int kt = 0; kt < NKT; ++kt) {
+                pq[kt] = drop(pq[kt], factors[kt]);
+                if constexpr (WHOLE) rest[kt] = drop(rest[kt], factors[kt]);
+            }
         }
 #pragma unroll
         for (int pc = 0; pc < BS / 32; ++pc) {
             const bf16x8 p = join(pq[2 * pc], pq[2 * pc + 1]);
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt) oacc[dt] = mma_d(oacc[dt], vop[dt], p);   // O^T[d][query] += V^T P^T
+            if constexpr (WHOLE) {
+                const bf16x8 q = join(rest[2 * pc], rest[2 * pc + 1]);
+#pragma unroll
+                for (int dt = 0; dt < 4; ++dt) oacc[dt] = mma_d(oacc[dt], vop[dt], q);
+            }
             if (pc + 1 < BS / 32) request_v(pc + 1);
         }
         jcur = jnext;
@@ -355,12 +374,15 @@ hipError_t fwd_with_bf16(const AttnShape& s, const Extras& x, const void* Q, con
     const FwdWith args = {static_cast<const bf16_t*>(Q), static_cast<const bf16_t*>(K), static_cast<const bf16_t*>(V), static_cast<bf16_t*>(O), LSE,
                           row_ptr, col_idx, Rows{x.H, s.heads_beside != 0}, x, cut, s.L, s.nb, s.BH, order, s.scale * kLog2e};
     auto launch = [&](auto kernel) { kernel<<<dim3((unsigned)grid), dim3(BS * 4), 0, st>>>(args); };
-    if (x.table) {
-        if (x.threshold) launch(attn_fwd_with_bf16_kernel<BS, true, true>);
-        else launch(attn_fwd_with_bf16_kernel<BS, true, false>);
+    if (x.table && x.rest) {   // a gradient of the table may follow
+        if (x.threshold) launch(attn_fwd_with_bf16_kernel<BS, true, true, true>);
+        else launch(attn_fwd_with_bf16_kernel<BS, true, false, true>);
+    } else if (x.table) {
+        if (x.threshold) launch(attn_fwd_with_bf16_kernel<BS, true, true, false>);
+        else launch(attn_fwd_with_bf16_kernel<BS, true, false, false>);
     } else {
-        if (x.threshold) launch(attn_fwd_with_bf16_kernel<BS, false, true>);
-        else launch(attn_fwd_with_bf16_kernel<BS, false, false>);
+        if (x.threshold) launch(attn_fwd_with_bf16_kernel<BS, false, true, false>);
+        else launch(attn_fwd_with_bf16_kernel<BS, false, false, false>);
     }
     return hipGetLastError();
 }

@@ -233,6 +233,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_fwd_with_kernel(
             }
         }
         Quad pq[NQ][KT];
+        [[maybe_unused]] Quad rest[NQ][KT];   // of bf16: what the rounding leaves, see attn_extras_bf16_kernels.hip
 #pragma unroll
         for (int h = 0; h < NQ; ++h)
 #pragma unroll
@@ -250,8 +251,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_fwd_with_kernel(
                     for (int i = 0; i < 4; ++i) p[i] = d[i] < x.threshold ? 0.f : p[i];
                 }
                 pq[h][u] = to_quad<T>(p);
+                if constexpr (sizeof(T) == 2) rest[h][u] = to_quad<T>(f32x4{rounded_off<T>(p[0]), rounded_off<T>(p[1]), rounded_off<T>(p[2]), rounded_off<T>(p[3])});
             }
         mma_cols(oacc, vc, pq);   // O^T += V^T P^T
+        if constexpr (sizeof(T) == 2) {
+            if (x.table && x.rest) mma_cols(oacc, vc, rest);
+        }
     };
     {
         Frag ka[KT][NDC], kb[KT][NDC];

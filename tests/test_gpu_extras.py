@@ -359,8 +359,12 @@ def test_only_what_is_asked_for(sp):
     kw = dict(buckets=buckets, dropout=0.1, rng=_rng())
     want = _run(sp, q, k, v, do, pat, table, **kw)
     assert want["dtable"].dtype == torch.float32
+    # without gradients the probabilities are rounded to bf16, as summands (u = 2^-8 of each) and in their sum (u), with
+    # gradients not, and either output is rounded (2 u): within 4 u of the magnitudes
     with torch.no_grad():
-        assert torch.equal(sp.sparse_attention(q, k, v, pat, bias=table, **kw), want["o"])
+        o = sp.sparse_attention(q, k, v, pat, bias=table, **kw)
+    exact, _ = _formula(q, k, v, do, torch.ones((L, L), dtype=torch.bool, device="cuda"), table, buckets.map, None, 0.1, RNG, 0)
+    assert ((o.double() - want["o"].double()).abs() <= 4 * 2.0 ** -8 * exact["o"][1]).all()
     a = q.clone().requires_grad_(True)
     o = sp.sparse_attention(a, k, v, pat, bias=table, **kw)
     assert torch.equal(torch.autograd.grad(o, a, do)[0], want["dq"])
