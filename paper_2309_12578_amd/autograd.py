@@ -41,6 +41,7 @@ def sparse_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, pattern:
     softmax; differentiable as well.  A bias of -infinity, or down from -1e30, masks.
     lengths: int32 [B], the tokens of each sequence; keys from there on are masked, rows from there on are 0, gradients too.
     dropout, rng, stream: dropout of the probabilities, see `dropout_add`.
+    In bf16 the graph keeps a second tensor of O's size, what rounding left of O: the gradients are made from both.
     With any of them flags must be 0, and second derivatives, tracing and transforms are refused."""
     if bias is None and lengths is None and dropout == 0.0:
         O = (_b._host or _b._native()).sparse_attention(

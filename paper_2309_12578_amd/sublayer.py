@@ -84,8 +84,8 @@ class SparseMHA(nn.Module):
     def forward(self, E: torch.Tensor, pattern: _b.Pattern, flags: int = 0, *, lengths: Optional[torch.Tensor] = None,
                 rng: Optional[torch.Tensor] = None, stream: int = 0) -> torch.Tensor:
         """E: [B, L, embed_dim] on the GPU (bf16 or fp32); pattern: the layer's sparsity pattern.
-        lengths: int32 [B], the tokens of each sequence, see `sparse_attention`; rows from there on leave as they came, or
-        as w_o's bias leaves them.
+        lengths: int32 [B], the tokens of each sequence, see `sparse_attention`; rows from there on leave as they came, but
+        for w_o's bias, and have to be finite (the projections' gradients add them up, times 0).
         rng, stream: int64 tensor {seed, offset} and a number of the layer's own, from which both dropouts then draw, see
         `dropout_add`; without it the last one is torch's."""
         B, L, D = E.shape
@@ -118,5 +118,5 @@ class SparseMHA(nn.Module):
                                  dropout=attn_dropout, rng=rng, stream=stream)   # lines 4-7, all heads at once
             S = S.transpose(1, 2).reshape(B, L, D)                            # concatenate the heads
         if rng is not None and self.training and self.drop.p > 0.0:
-            return dropout_add(w_o(S), R, self.drop.p, rng, stream)
+            return dropout_add(w_o(S).to(R.dtype), R, self.drop.p, rng, stream)
         return self.drop(w_o(S)) + R

@@ -203,6 +203,44 @@ def test_long_and_short_rows(sp, dtype, block, nb, B, H):
     _near(got, want, TOL[dtype])
 
 
+# More workgroups than run at once: rows and columns in their other orders, 32 rows a workgroup in fp32; heads that divide over the XCDs and not
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("block", [16, 32, 64])
+@pytest.mark.parametrize("B,H", [(8, 8), (9, 7)])
+def test_many_heads(sp, dtype, block, B, H):
+    L = 1088
+    nb = L // block
+    fl = _mask(nb, seed=block + B, density=0.2)
+    fl[:, nb - 1] = 1
+    pat = _pattern_from_mask(sp, fl, block)
+    q, k, v, do = _inputs(B, H, L, dtype, 50)
+    table, buckets = _table(32, H, dtype, 51), sp.relative_buckets(L, device="cuda")
+    lengths = torch.tensor([L - 130 * b for b in range(B)], dtype=torch.int32, device="cuda")
+    got = _run(sp, q, k, v, do, pat, table, buckets=buckets, lengths=lengths, dropout=0.15, rng=_rng())
+    want, _ = _formula(q, k, v, do, _kept(fl, block), table, buckets.map, lengths, 0.15, RNG, 0)
+    _near(got, want, TOL[dtype])
+
+
+def test_calls_on_two_streams_at_once(sp):
+    block, nb = 64, 40
+    L = nb * block
+    pat = _pattern_from_mask(sp, _mask(nb, seed=6, density=0.9), block)   # rows and columns in pieces
+    buckets, rng = sp.relative_buckets(L, device="cuda"), _rng()
+    sets = [(*_inputs(1, 2, L, torch.bfloat16, 60 + i), _table(32, 2, torch.float32, 62 + i)) for i in range(2)]
+    run = lambda s: _run(sp, *s[:4], pat, s[4], buckets=buckets, dropout=0.1, rng=rng)
+    want = [run(s) for s in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[i].append(run(sets[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(g[n], want[i][n]) for g in got[i] for n in want[i])
+
+
 @pytest.mark.parametrize("dtype,block", [(torch.float32, 16), (torch.bfloat16, 16), (torch.bfloat16, 32), (torch.bfloat16, 64)])
 @pytest.mark.parametrize("count", [1, 3, 64, 65, 256])
 def test_any_map_and_any_number_of_buckets(sp, dtype, block, count):
@@ -667,6 +705,19 @@ def test_sub_layer_without_the_state_to_draw_from(sp):
     plain = sp.SparseMHA(128, 2, device="cuda", dtype=torch.bfloat16)
     plain.load_state_dict(mha.state_dict())
     assert torch.equal(mha(E, pat), plain(E, pat))
+
+
+def test_sub_layer_under_autocast(sp):
+    """fp32 weights, products in bf16: the attention's heads in bf16, the residual in fp32."""
+    pat = _pattern_from_mask(sp, np.ones((2, 2), dtype=np.uint8), 32)
+    mha = sp.SparseMHA(128, 2, dropout=0.3, device="cuda", buckets=sp.relative_buckets(64, device="cuda"), attn_dropout=0.1)
+    E = torch.randn(2, 64, 128, device="cuda", requires_grad=True)
+    with torch.autocast("cuda", dtype=torch.bfloat16):
+        out = mha(E, pat, rng=_rng())
+    whole = mha(E, pat, rng=_rng())
+    assert out.dtype == torch.float32
+    assert (out - whole).norm() <= 16 * 2.0 ** -8 * whole.norm()   # X, qkv, P, S, the products and their weights: fewer than 16 roundings
+    assert all(torch.isfinite(g).all() for g in torch.autograd.grad(out.square().sum(), [E, *mha.parameters()]))
 
 
 def test_sub_layer_whose_projection_is_watched(sp):
