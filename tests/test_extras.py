@@ -88,7 +88,7 @@ def _calls(p, x, nnzb=10):
     (dict(B=0), {}, -2), (dict(L=65536 + 64, block=64), {}, -2), ({}, dict(reserved=1), -5),
     ({}, dict(dropout=1.0), -5), ({}, dict(dropout=-0.1), -5), ({}, dict(dropout=math.nan), -5), ({}, dict(dropout=1 - 2.0 ** -18), -5),
     ({}, dict(rng=None), -1), ({}, dict(bucket_of=None), -1), ({}, dict(n_buckets=0), -5), ({}, dict(n_buckets=257), -5),
-    ({}, dict(table_dtype=7), -3)])
+    ({}, dict(table_dtype=7), -3), ({}, dict(o_rest=264), -5)])
 def test_attention_calls_that_are_refused(params, extras, code):
     p, x = _params(**params), _extras(**extras)
     for call, args in _calls(p, x):

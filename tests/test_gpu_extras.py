@@ -579,6 +579,46 @@ def test_dropout_add_past_32_bits(sp):
         assert torch.equal(y[at:at + 200].double(), 1 + f)
 
 
+@pytest.mark.parametrize("dtype,block", [(torch.float32, 32), (torch.bfloat16, 16), (torch.bfloat16, 64)])
+def test_entries_of_the_c_abi(sp, dtype, block):
+    """The calls themselves, with workspaces of their sizes that hold anything: the same bits as the nodes; and without o_rest."""
+    nb, B, H = 34, 1, 2
+    L = nb * block
+    fl = _mask(nb, seed=8, density=0.8)
+    pat = _pattern_from_mask(sp, fl, block)
+    q, k, v, do = _inputs(B, H, L, dtype, 70)
+    table, buckets, rng = _table(32, H, dtype, 71), sp.relative_buckets(L, device="cuda"), _rng()
+    lengths = torch.full((B,), L - 9, dtype=torch.int32, device="cuda")
+    want = _run(sp, q, k, v, do, pat, table, buckets=buckets, lengths=lengths, dropout=0.1, rng=rng, stream=3)
+    formula, _ = _formula(q, k, v, do, _kept(fl, block), table, buckets.map, lengths, 0.1, RNG, 3)
+    code = sp.SPION_F32 if dtype == torch.float32 else sp.SPION_BF16
+    shape = dict(B=B, H=H, L=L, d=64, block=block, dtype=code)
+    room = lambda n: torch.full((max(n, 256),), 0xa5, dtype=torch.uint8, device="cuda")
+    for rest in (torch.empty_like(q), None):
+        kw = dict(table=table, bucket_of=buckets.map, lengths=lengths, dropout=0.1)
+        sizes = [sp.spion_attn_with_workspace_bytes(**shape, nnzb=pat.nnzb, is_bwd=b, rng=rng, **kw) for b in (False, True)]
+        got = {n: torch.full_like(table if n == "dtable" else q, float("nan")) for n in ("o", "dq", "dk", "dv", "dtable")}
+        lse, used = torch.empty((B, H, L), device="cuda"), torch.zeros(2, dtype=torch.int64, device="cuda")
+        sp.spion_attn_fwd_with(q, k, v, got["o"], lse, pat.row_ptr, pat.col_idx, pat.nnzb, **shape, rng=rng, rng_used=used, dropout_stream=3,
+                               workspace=room(sizes[0]), o_rest=rest, **kw)
+        assert torch.equal(used, rng)
+        sp.spion_attn_bwd_with(q, k, v, got["o"], do, lse, got["dq"], got["dk"], got["dv"], got["dtable"], pat.row_ptr, pat.col_idx, pat.col_ptr,
+                               pat.row_idx, pat.bsr_pos, pat.nnzb, **shape, rng=used, dropout_stream=3, workspace=room(sizes[1]), o_rest=rest, **kw)
+        if rest is not None:
+            assert all(torch.equal(got[n], want[n]) for n in want)
+        _near(got, formula, TOL[dtype])
+    bias = torch.empty((H, 70, L), dtype=dtype, device="cuda")
+    sp.spion_relative_bias(table, buckets.map, bias, L, 32, H, 70, L, 5, code)
+    t = table.clone().requires_grad_(True)
+    node = sp.relative_bias(t, buckets, 70, L, 5)
+    g, dtable = torch.randn_like(bias), torch.empty_like(table)
+    sp.spion_relative_bias_grad(g, buckets.map, dtable, L, 32, H, 70, L, 5, code, room(sp.spion_relative_bias_workspace_bytes(32, H, 70, L)))
+    assert torch.equal(bias, node) and torch.equal(dtable, torch.autograd.grad(node, t, g)[0])
+    y, used = torch.empty_like(q), torch.zeros(2, dtype=torch.int64, device="cuda")
+    sp.spion_dropout_add(q, k, y, q.numel(), code, 0.2, rng, used, 7)
+    assert torch.equal(y, sp.dropout_add(q, k, 0.2, rng, 7)) and torch.equal(used, rng)
+
+
 def test_calls_that_are_refused(sp):
     block, nb, H = 32, 2, 2
     L = nb * block
