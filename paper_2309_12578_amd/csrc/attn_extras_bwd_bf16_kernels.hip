@@ -14,8 +14,8 @@
 // anew for each block (once) leave room for; at two the backward with bias and dropout took 253 instead of 220 us (4 x 8 heads x 4096, 20.8 %).  Neither
 // the matrix nor the vector pipes are busy half of the time: a step is one chain of products, exponentials and products, longer than the plain one by
 // the draws and the biases.  Kernel time, us, of the plain one, with lengths, bias, dropout, bias and dropout (row_terms_kernel not counted): 4 x 4 heads x 4096,
-// block 64, 8 %, 45.5 / 48.5 / 62 / 67 / 83; 4 x 8 heads, 20.8 %, 151 / 145 / 160 / 185 / 208; 2 x 8 x 16320, 5 %, 303 / 263 / 306 / 344 / 387; 16 x 4 x 1024, block 32,
-// 15 %, 28.5 / 28.7 / 38.6 / 37.9 / 50.
+// block 64, 8 %, 45.5 / 48.5 / 62 / 64 / 80; 4 x 8 heads, 20.8 %, 151 / 145 / 160 / 186 / 204; 2 x 8 x 16320, 5 %, 303 / 263 / 306 / 335 / 364; 16 x 4 x 1024, block 32,
+// 15 %, 28.5 / 28.7 / 38.6 / 36.6 / 48.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <stdint.h>
@@ -44,10 +44,14 @@ struct BwdWith {
 
 namespace {
 
-// dp of the kept elements, 0 of the dropped ones: element i of four whose factors are f.
-__device__ __forceinline__ float where_kept(float v, const unsigned (&f)[2], int i) {
-    const int mask = __builtin_amdgcn_sbfe((int)f[i >> 1], 16 * (i & 1), 1);
-    return __builtin_bit_cast(float, __builtin_bit_cast(int, v) & mask);
+// With dropout, 2^-24 (M dP - delta / c) in one instruction: the factor, 0 or 1 in 16 bits, is 0 or 2^-24 as a half, what is added comes times
+// 2^-24, and the exponentials (query side) or the result (key side) are taken times 2^24.
+constexpr float kHalfOne = 1.f / 16777216.f;
+__device__ __forceinline__ float where_kept_plus(float v, const unsigned (&f)[2], int i, float add) {   // element i of four whose factors are f
+    float d;
+    if (i & 1) asm("v_fma_mix_f32 %0, %1, %2, %3 op_sel:[0,1,0] op_sel_hi:[0,1,0]" : "=v"(d) : "v"(v), "v"(f[i >> 1]), "v"(add));
+    else asm("v_fma_mix_f32 %0, %1, %2, %3 op_sel_hi:[0,1,0]" : "=v"(d) : "v"(v), "v"(f[i >> 1]), "v"(add));
+    return d;
 }
 
 }  // namespace
@@ -129,7 +133,7 @@ __global__ __launch_bounds__(BS * 4, BS == 32 ? 4 : 3) void attn_bwd_with_bf16_k
         };
         if (!helper) issue(ta0, tb0, I);   // the diagonal block, before any index is known
         bf16x8 qf[2], dof[2];
-        const float lse2 = b.x.row_lse[vec + qrow], ndelta = b.x.row_delta[vec + qrow];
+        const float lse2 = b.x.row_lse[vec + qrow] - (DROP ? 24.f : 0.f), ndelta = b.x.row_delta[vec + qrow];
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             qf[c] = *reinterpret_cast<const bf16x8*>(b.Q + head + (size_t)qrow * in_row + c * 32 + g * 8);
@@ -278,7 +282,7 @@ __global__ __launch_bounds__(BS * 4, BS == 32 ? 4 : 3) void attn_bwd_with_bf16_k
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float p = fast_exp2(fmaf(s[kt16][i], scale_log2, -lse2));
-                    s[kt16][i] = p * (DROP ? where_kept(dp[kt16][i], factors[kt16], i) + ndelta : dp[kt16][i]);
+                    s[kt16][i] = p * (DROP ? where_kept_plus(dp[kt16][i], factors[kt16], i, ndelta) : dp[kt16][i]);
                 }
                 dsq[kt16] = to_quad<bf16_t>(s[kt16]);
             }
@@ -509,7 +513,7 @@ __global__ __launch_bounds__(BS * 4, BS == 32 ? 4 : 3) void attn_bwd_with_bf16_k
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     p[i] = fast_exp2(fmaf(s[i], scale_log2, -lse4[i]));
-                    ds[i] = p[i] * (DROP ? where_kept(dp[i], factors[h], i) + ndelta[i] : dp[i]);
+                    ds[i] = p[i] * (DROP ? where_kept_plus(dp[i], factors[h], i, ndelta[i]) : dp[i]);
                 }
                 pq[h] = to_quad<bf16_t>(p);
                 if constexpr (DROP) pq[h] = drop(pq[h], factors[h]);
@@ -578,7 +582,7 @@ __global__ __launch_bounds__(BS * 4, BS == 32 ? 4 : 3) void attn_bwd_with_bf16_k
     bf16_t* pb = (odd ? tb1 : tb0) + wave * (16 * kD);
     const Rows out = {z.at.H, z.at.beside};
     const size_t row0 = out.in_head(bh, z.L) + (size_t)(J * BS + wave * 16) * out.in_row();
-    store_rows_coalesced(pa, z.dK + row0, out.in_row(), dk, z.scale, l);
+    store_rows_coalesced(pa, z.dK + row0, out.in_row(), dk, DROP ? z.scale / kHalfOne : z.scale, l);
     store_rows_coalesced(pb, z.dV + row0, out.in_row(), dv, 1.f, l);
 }
 

@@ -362,7 +362,7 @@ struct ColumnCut {
 // ------------------------------------------------------------------------------------------------
 template <typename T>
 __global__ __launch_bounds__(256) void row_terms_kernel(const T* __restrict__ O, const T* __restrict__ dO, const float* __restrict__ LSE, Extras x, int beside,
-                                                        int L, long long rows) {
+                                                        int L, long long rows, float delta_scale) {
     constexpr int VEC = 16 / sizeof(T), LANES = 8, PER = kD / LANES;
     typedef T Vec __attribute__((ext_vector_type(VEC)));
     if (blockIdx.x == 0 && x.counters)
@@ -388,7 +388,7 @@ __global__ __launch_bounds__(256) void row_terms_kernel(const T* __restrict__ O,
     for (int o = 1; o < LANES; o <<= 1) delta += __shfl_xor(delta, o);
     if (part == 0) {
         x.row_lse[row] = lse == -INFINITY ? INFINITY : fmaf(lse, kLog2e, -log2f(x.keep_scale));
-        x.row_delta[row] = lse == -INFINITY ? 0.f : -delta / x.keep_scale;
+        x.row_delta[row] = lse == -INFINITY ? 0.f : delta * delta_scale;
     }
 }
 
@@ -937,9 +937,12 @@ hipError_t launch_attn_bwd_with(const AttnShape& s, const Extras& extras, const 
     const long long rows = (long long)s.BH * s.L;
     x.row_lse = reinterpret_cast<float*>(base + ws.rows);
     x.row_delta = x.row_lse + rows;
+    // the kernels of bf16 and block 32 and 64 take it times 2^-24 with dropout
+    const float delta_scale = (x.threshold && s.is_bf16 && s.bs > 16 ? -1.f / 16777216.f : -1.f) / x.keep_scale;
     auto row_terms = [&](auto kernel, auto type) {
         typedef decltype(type) T;
-        kernel<<<dim3((unsigned)((rows + 31) / 32)), dim3(256), 0, st>>>(static_cast<const T*>(O), static_cast<const T*>(dO), LSE, x, s.heads_beside != 0, s.L, rows);
+        kernel<<<dim3((unsigned)((rows + 31) / 32)), dim3(256), 0, st>>>(static_cast<const T*>(O), static_cast<const T*>(dO), LSE, x, s.heads_beside != 0, s.L, rows,
+                                                                           delta_scale);
     };
     if ((rows + 31) / 32 > 0x7fffffffll) return hipErrorInvalidValue;
     if (s.is_bf16) row_terms(row_terms_kernel<bf16_t>, bf16_t{});
