@@ -10,8 +10,8 @@
 //
 // What it adds is vector work beside the products (seven rounds of Philox for eight draws, a sixteenth of a 64 x 64 block's a wave; 16
 // biases a lane) and, where rows are short, the table's way into LDS before the first scores.  Kernel time, us, of the plain one, with lengths,
-// bias, dropout, bias and dropout, and the last as WHOLE: 4 x 4 heads x 4096, block 64, 8 %, 16.9 / 18.9 / 21.5 / 24.5 / 26.5 / 31.5; 4 x 8 heads, 20.8 %,
-// 47 / 50 / 58 / 72 / 76 / 95; 2 x 8 x 16320, 5 %, 92 / 107 / 121 / 150 / 157 / 187; 16 x 4 x 1024, block 32, 15 %, 13.0 / 15.8 / 20.4 / 20.1 / 25.0 / 28.7.
+// bias, dropout, bias and dropout, and the last as WHOLE: 4 x 4 heads x 4096, block 64, 8 %, 16.9 / 18.9 / 21.5 / 24.5 / 26.5 / 30; 4 x 8 heads, 20.8 %,
+// 47 / 50 / 58 / 72 / 76 / 92; 2 x 8 x 16320, 5 %, 92 / 107 / 121 / 150 / 157 / 186; 16 x 4 x 1024, block 32, 15 %, 13.0 / 15.8 / 20.4 / 20.1 / 25.0 / 28.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <stdint.h>
@@ -25,6 +25,20 @@
 namespace spion {
 
 namespace {
+
+// p - q, exact where q is p rounded: a product of two pairs each takes one of q's halves off, in place of two instructions that widen and subtract.
+__device__ __forceinline__ f32x4 without(f32x4 p, bf16x4 q) {
+    typedef __bf16 Pair __attribute__((ext_vector_type(2)));
+    typedef unsigned Words __attribute__((ext_vector_type(2)));
+    const Words w = __builtin_bit_cast(Words, q);
+    unsigned first = 0x0000bf80u, second = 0xbf800000u;   // {-1, 0} and {0, -1}, in registers: as a constant the first comes out as -1.0 in 32 bits
+    asm("" : "+s"(first), "+s"(second));
+    const Pair even = __builtin_bit_cast(Pair, first), odd = __builtin_bit_cast(Pair, second);
+    const unsigned w0 = w[0], w1 = w[1];
+    const Pair lo = __builtin_bit_cast(Pair, w0), hi = __builtin_bit_cast(Pair, w1);
+    return f32x4{__builtin_amdgcn_fdot2_f32_bf16(lo, even, p[0], false), __builtin_amdgcn_fdot2_f32_bf16(lo, odd, p[1], false),
+                 __builtin_amdgcn_fdot2_f32_bf16(hi, even, p[2], false), __builtin_amdgcn_fdot2_f32_bf16(hi, odd, p[3], false)};
+}
 
 template <int BS>
 struct KvTiles {
@@ -241,7 +255,7 @@ __global__ __launch_bounds__(BS * 4, BS == 32 && DROP && !WHOLE ? 5 : 4) void at
 #pragma unroll
                 for (int i = 0; i < 4; ++i) p[i] = fast_exp2(fmaf(s[kt][i], scale_log2, -m));
                 pq[kt] = to_quad<bf16_t>(p);
-                if constexpr (WHOLE) rest[kt] = to_quad<bf16_t>(p - f32x4{(float)pq[kt][0], (float)pq[kt][1], (float)pq[kt][2], (float)pq[kt][3]});
+                if constexpr (WHOLE) rest[kt] = to_quad<bf16_t>(without(p, pq[kt]));
             }
             sums = lacc;
 #pragma unroll
