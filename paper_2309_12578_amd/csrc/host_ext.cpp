@@ -773,12 +773,11 @@ struct AttentionExtras {
     int n_buckets = 0;
     double dropout = 0.0;
     unsigned stream = 0;
-    spion_attn_extras params(const at::Tensor& table, const at::Tensor& rng) const {
+    spion_attn_extras params(const at::Tensor& table) const {
         spion_attn_extras x = {};
         x.table = table.defined() ? table.data_ptr() : nullptr;
         x.bucket_of = table.defined() ? (const uint8_t*)bucket_of.data_ptr() : nullptr;
         x.lengths = lengths.defined() ? (const int32_t*)lengths.data_ptr() : nullptr;
-        x.rng = rng.defined() ? (const int64_t*)rng.data_ptr() : nullptr;
         x.dropout = dropout;
         x.n_buckets = n_buckets;
         x.table_dtype = table.defined() ? dtype_code(table) : SPION_F32;
@@ -787,14 +786,45 @@ struct AttentionExtras {
     }
 };
 
-at::Tensor with_workspace(const spion_attn_params& p, const spion_attn_extras& x, const Index& ix, bool is_bwd, const at::Tensor& like) {
-    const size_t n = spion_attn_with_workspace_bytes(&p, &x, ix.nnzb, is_bwd);
-    return new_bytes(n == (size_t)-1 ? 0 : n, like);   // what is unsupported the call itself tells
-}
+// Of a call; nothing where it needs none.
+struct WithWorkspace {
+    at::Tensor memory;
+    void* ptr = nullptr;
+    size_t bytes = 0;
+    WithWorkspace(const spion_attn_params& p, const spion_attn_extras& x, const Index& ix, bool is_bwd, const at::Tensor& like) {
+        const size_t n = spion_attn_with_workspace_bytes(&p, &x, ix.nnzb, is_bwd);
+        if (n == 0 || n == (size_t)-1) return;   // what is unsupported the call itself tells
+        memory = new_bytes(n, like);
+        ptr = memory.data_ptr();
+        bytes = n;
+    }
+};
+
+// What the forward leaves for its backward besides O, in one tensor of bytes (each costs the host more than a microsecond): LSE, and where there are such,
+// the generator's state and what rounding left of O.
+struct WithState {
+    size_t used = 0, rest = 0, bytes;   // where they are; 0: not there
+    WithState(const spion_attn_params& p, bool draws, bool saved) {
+        auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+        const size_t rows = (size_t)p.B * p.H * p.L;
+        bytes = up(rows * 4);
+        if (!saved) return;
+        if (draws) {
+            used = bytes;
+            bytes += 256;
+        }
+        if (p.dtype == SPION_BF16) {
+            rest = bytes;
+            bytes += up(rows * 64 * 2);
+        }
+    }
+    static void* at(const at::Tensor& state, size_t offset) { return offset ? static_cast<char*>(state.data_ptr()) + offset : nullptr; }
+};
+bool draws(const AttentionExtras& extras) { return std::nearbyint(65536.0 * extras.dropout) > 0.0; }
 
 // The gradient of sparse_attention_with, and of heads_attention_with (q = qkv, no k and v).
 struct AttentionWithBackward : public torch::autograd::Node {
-    torch::autograd::SavedVariable q, k, v, o, rest, lse, table, lengths, rng;
+    torch::autograd::SavedVariable q, k, v, o, state, table, lengths;
     Index ix;
     AttentionExtras extras;
     int64_t H = 0;   // of qkv's heads; 0: Q, K and V
@@ -802,7 +832,7 @@ struct AttentionWithBackward : public torch::autograd::Node {
     std::string name() const override { return "SparseAttentionWithBackward"; }
 
     void release_variables() override {
-        for (torch::autograd::SavedVariable* s : {&q, &k, &v, &o, &rest, &lse, &table, &lengths, &rng}) s->reset_data();
+        for (torch::autograd::SavedVariable* s : {&q, &k, &v, &o, &state, &table, &lengths}) s->reset_data();
     }
 
     torch::autograd::variable_list apply(torch::autograd::variable_list&& grads) override {
@@ -810,8 +840,8 @@ struct AttentionWithBackward : public torch::autograd::Node {
         torch::autograd::variable_list out(inputs + (extras.n_buckets ? 1 : 0));
         if (!grads[0].defined()) return out;
         return differentiate("sparse_attention cannot be differentiated twice", [&] {
-            const at::Tensor Q = q.unpack(), O = o.unpack(shared_from_this()), stat = lse.unpack(), T = table.unpack(), R = rng.unpack();
-            const at::Tensor K = H ? Q : k.unpack(), V = H ? Q : v.unpack(), O_rest = rest.unpack();
+            const at::Tensor Q = q.unpack(), O = o.unpack(shared_from_this()), left = state.unpack(), T = table.unpack();
+            const at::Tensor K = H ? Q : k.unpack(), V = H ? Q : v.unpack();
             AttentionExtras with = extras;
             with.lengths = lengths.unpack();
             const c10::DeviceGuard guard(Q.device());
@@ -825,30 +855,30 @@ struct AttentionWithBackward : public torch::autograd::Node {
             const spion_attn_params p = H ? heads_params(Q, H, ix) : params_of(Q, ix);
             for (const at::Tensor* t : {&K, &V}) same(t->numel() == Q.numel() && t->scalar_type() == Q.scalar_type() && t->is_contiguous());
             for (const at::Tensor* t : {&O, &g}) same(t->numel() == Q.numel() / (H ? 3 : 1) && t->scalar_type() == Q.scalar_type() && t->is_contiguous());
-            same(!O_rest.defined() || (O_rest.numel() == O.numel() && O_rest.scalar_type() == O.scalar_type() && O_rest.is_contiguous()));
-            same(stat.numel() == (int64_t)p.B * p.H * p.L && stat.scalar_type() == at::kFloat && stat.is_contiguous());
+            const WithState at(p, draws(extras), true);
+            same(left.numel() == (int64_t)at.bytes && left.scalar_type() == at::kByte && left.is_contiguous());
             same(!extras.n_buckets || (T.numel() == (int64_t)extras.n_buckets * p.H && T.is_contiguous() && T.device() == Q.device()));
             same(!with.lengths.defined() || (with.lengths.numel() == p.B && with.lengths.scalar_type() == at::kInt && with.lengths.is_contiguous()));
-            same(!R.defined() || (R.numel() == 2 && R.scalar_type() == at::kLong && R.is_contiguous()));
-            spion_attn_extras x = with.params(T, R);
-            x.o_rest = O_rest.defined() ? O_rest.data_ptr() : nullptr;
+            spion_attn_extras x = with.params(T);
+            x.rng = (const int64_t*)WithState::at(left, at.used);
+            x.o_rest = WithState::at(left, at.rest);
+            const float* const stat = (const float*)device_ptr(left);
             const bool table_grad = extras.n_buckets && task_should_compute_output(inputs);
             for (int i = 0; i < inputs; ++i) out[i] = new_like(Q);
             if (table_grad) out[inputs] = new_like(T);
             void* const dtable = table_grad ? device_ptr(out[inputs]) : nullptr;
-            const at::Tensor ws = with_workspace(p, x, ix, true, Q);
+            const WithWorkspace ws(p, x, ix, true, Q);
             auto index = [](const at::Tensor& t) { return (const int32_t*)device_ptr(t); };
             if (H) {
-                const int rc = spion_heads_attn_bwd_with(device_ptr(Q), device_ptr(O), device_ptr(g), (const float*)device_ptr(stat), device_ptr(out[0]),
+                const int rc = spion_heads_attn_bwd_with(device_ptr(Q), device_ptr(O), device_ptr(g), stat, device_ptr(out[0]),
                                                          dtable, index(ix.row_ptr), index(ix.col_idx), index(ix.col_ptr), index(ix.row_idx), ix.nnzb,
-                                                         &p, &x, device_ptr(ws), (size_t)ws.nbytes(), current_stream());
+                                                         &p, &x, ws.ptr, ws.bytes, current_stream());
                 if (rc != SPION_OK) throw SpionFailure{rc, "spion_heads_attn_bwd_with"};
                 return out;
             }
-            const int rc = spion_attn_bwd_with(device_ptr(Q), device_ptr(K), device_ptr(V), device_ptr(O), device_ptr(g), (const float*)device_ptr(stat),
+            const int rc = spion_attn_bwd_with(device_ptr(Q), device_ptr(K), device_ptr(V), device_ptr(O), device_ptr(g), stat,
                                                device_ptr(out[0]), device_ptr(out[1]), device_ptr(out[2]), dtable, index(ix.row_ptr), index(ix.col_idx),
-                                               index(ix.col_ptr), index(ix.row_idx), index(ix.bsr_pos), ix.nnzb, &p, &x, device_ptr(ws),
-                                               (size_t)ws.nbytes(), current_stream());
+                                               index(ix.col_ptr), index(ix.row_idx), index(ix.bsr_pos), ix.nnzb, &p, &x, ws.ptr, ws.bytes, current_stream());
             if (rc != SPION_OK) throw SpionFailure{rc, "spion_attn_bwd_with"};
             return out;
         });
@@ -881,19 +911,16 @@ struct ExtrasArgs {
             if (extras.lengths.scalar_type() != at::kInt || extras.lengths.numel() != B || !extras.lengths.is_contiguous())
                 bad_value("lengths must be a contiguous int32 tensor [B]");
         }
-        if (std::nearbyint(65536.0 * extras.dropout) > 0.0) rng = rng_arg(a[4], device);
+        if (draws(extras)) rng = rng_arg(a[4], device);
     }
 };
 
 // The node of a call, but for q, k, v and o.
-std::shared_ptr<AttentionWithBackward> with_node(AttentionExtras&& extras, Index&& ix, const at::Tensor& lse, const at::Tensor& rest, const at::Tensor& table,
-                                                 const at::Tensor& used) {
+std::shared_ptr<AttentionWithBackward> with_node(AttentionExtras&& extras, Index&& ix, const at::Tensor& state, const at::Tensor& table) {
     auto node = std::shared_ptr<AttentionWithBackward>(new AttentionWithBackward(), torch::autograd::deleteNode);
-    node->lse = torch::autograd::SavedVariable(lse, false);
-    node->rest = torch::autograd::SavedVariable(rest, false);
+    node->state = torch::autograd::SavedVariable(state, false);
     node->table = torch::autograd::SavedVariable(table, false);
     node->lengths = torch::autograd::SavedVariable(extras.lengths, false);
-    node->rng = torch::autograd::SavedVariable(used, false);
     extras.lengths.reset();
     node->extras = std::move(extras);
     node->ix = std::move(ix);
@@ -925,7 +952,7 @@ PyObject* py_sparse_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) 
         const at::Tensor& table = with.table;
         const c10::DeviceGuard guard(device);
         const bool grad = table.defined() ? torch::autograd::compute_requires_grad(q, k, v, table) : torch::autograd::compute_requires_grad(q, k, v);
-        at::Tensor o, rest, lse, qc, kc, vc, tc, used;
+        at::Tensor o, state, qc, kc, vc, tc;
         {
             at::NoGradGuard no_grad;
             qc = dense(q);
@@ -934,18 +961,16 @@ PyObject* py_sparse_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) 
             if (table.defined()) tc = table.contiguous();
             const spion_attn_params p = params_of(qc, ix);
             o = new_like(qc);
-            lse = at::Tensor(at::detail::empty_cuda({q.size(0), q.size(1), q.size(2)}, at::kFloat, device, std::nullopt));
-            if (with.rng.defined() && grad) used = new_longs(2, qc);
-            spion_attn_extras x = with.extras.params(tc, with.rng);
-            if (used.defined()) x.rng_used = (int64_t*)used.data_ptr();
-            if (grad && o.scalar_type() == at::kBFloat16) {
-                rest = new_like(o);
-                x.o_rest = rest.data_ptr();
-            }
-            const at::Tensor ws = with_workspace(p, x, ix, false, qc);
-            const int rc = spion_attn_fwd_with(device_ptr(qc), device_ptr(kc), device_ptr(vc), device_ptr(o), (float*)device_ptr(lse),
+            const WithState at(p, with.rng.defined(), grad);
+            state = new_bytes(at.bytes, qc);
+            spion_attn_extras x = with.extras.params(tc);
+            if (with.rng.defined()) x.rng = (const int64_t*)with.rng.data_ptr();
+            x.rng_used = (int64_t*)WithState::at(state, at.used);
+            x.o_rest = WithState::at(state, at.rest);
+            const WithWorkspace ws(p, x, ix, false, qc);
+            const int rc = spion_attn_fwd_with(device_ptr(qc), device_ptr(kc), device_ptr(vc), device_ptr(o), (float*)device_ptr(state),
                                                (const int32_t*)device_ptr(ix.row_ptr), (const int32_t*)device_ptr(ix.col_idx), ix.nnzb, &p, &x,
-                                               device_ptr(ws), (size_t)ws.nbytes(), current_stream());
+                                               ws.ptr, ws.bytes, current_stream());
             if (rc != SPION_OK) throw SpionFailure{rc, "spion_attn_fwd_with"};
         }
         if (grad) {
@@ -953,7 +978,7 @@ PyObject* py_sparse_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) 
             ix.row_idx = tensor_arg(a[6]);
             ix.bsr_pos = tensor_arg(a[7]);
             for (const at::Tensor* t : {&ix.col_ptr, &ix.row_idx, &ix.bsr_pos}) check_operand(*t, device);
-            auto node = with_node(std::move(with.extras), std::move(ix), lse, rest, tc, used);
+            auto node = with_node(std::move(with.extras), std::move(ix), state, tc);
             node->set_next_edges(table.defined() ? torch::autograd::collect_next_edges(q, k, v, table) : torch::autograd::collect_next_edges(q, k, v));
             node->q = torch::autograd::SavedVariable(qc, false);
             node->k = torch::autograd::SavedVariable(kc, false);
@@ -989,23 +1014,21 @@ PyObject* py_heads_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::Tensor& table = with.table;
         const c10::DeviceGuard guard(device);
         const bool grad = table.defined() ? torch::autograd::compute_requires_grad(qkv, table) : torch::autograd::compute_requires_grad(qkv);
-        at::Tensor tc, used, rest;
+        at::Tensor tc, state;
         at::Tensor s(at::detail::empty_cuda({B, L, H * 64}, qkv.scalar_type(), device, std::nullopt));
-        at::Tensor lse(at::detail::empty_cuda({B, H, L}, at::kFloat, device, std::nullopt));
         {
             at::NoGradGuard no_grad;
             if (table.defined()) tc = table.contiguous();
             const spion_attn_params p = heads_params(qkv, H, ix);
-            if (with.rng.defined() && grad) used = new_longs(2, qkv);
-            spion_attn_extras x = with.extras.params(tc, with.rng);
-            if (used.defined()) x.rng_used = (int64_t*)used.data_ptr();
-            if (grad) {
-                rest = new_like(s);
-                x.o_rest = rest.data_ptr();
-            }
-            const at::Tensor ws = with_workspace(p, x, ix, false, qkv);
-            const int rc = spion_heads_attn_fwd_with(device_ptr(qkv), device_ptr(s), (float*)device_ptr(lse), (const int32_t*)device_ptr(ix.row_ptr),
-                                                     (const int32_t*)device_ptr(ix.col_idx), ix.nnzb, &p, &x, device_ptr(ws), (size_t)ws.nbytes(),
+            const WithState at(p, with.rng.defined(), grad);
+            state = new_bytes(at.bytes, qkv);
+            spion_attn_extras x = with.extras.params(tc);
+            if (with.rng.defined()) x.rng = (const int64_t*)with.rng.data_ptr();
+            x.rng_used = (int64_t*)WithState::at(state, at.used);
+            x.o_rest = WithState::at(state, at.rest);
+            const WithWorkspace ws(p, x, ix, false, qkv);
+            const int rc = spion_heads_attn_fwd_with(device_ptr(qkv), device_ptr(s), (float*)device_ptr(state), (const int32_t*)device_ptr(ix.row_ptr),
+                                                     (const int32_t*)device_ptr(ix.col_idx), ix.nnzb, &p, &x, ws.ptr, ws.bytes,
                                                      current_stream());
             if (rc != SPION_OK) throw SpionFailure{rc, "spion_heads_attn_fwd_with"};
         }
@@ -1014,7 +1037,7 @@ PyObject* py_heads_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) {
             ix.row_idx = tensor_arg(a[5]);
             ix.bsr_pos = tensor_arg(a[6]);
             for (const at::Tensor* t : {&ix.col_ptr, &ix.row_idx}) check_operand(*t, device);
-            auto node = with_node(std::move(with.extras), std::move(ix), lse, rest, tc, used);
+            auto node = with_node(std::move(with.extras), std::move(ix), state, tc);
             node->H = H;
             node->set_next_edges(table.defined() ? torch::autograd::collect_next_edges(qkv, table) : torch::autograd::collect_next_edges(qkv));
             node->q = torch::autograd::SavedVariable(qkv, false);

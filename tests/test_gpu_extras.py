@@ -662,7 +662,10 @@ def test_saved_tensors_are_looked_at(sp):
     q, k, v, do = _inputs(2, H, L, torch.bfloat16, 32)
     table, buckets = _table(32, H, torch.bfloat16, 33), sp.relative_buckets(L, device="cuda")
     kw = dict(buckets=buckets, lengths=torch.full((2,), L, dtype=torch.int32, device="cuda"), dropout=0.1, rng=_rng())
-    shapes = {t.shape for t in (q, table, kw["lengths"], kw["rng"])} | {torch.Size([2, H, L])}
+    shapes = set()
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: shapes.add(t.shape) or t, lambda t: t):
+        sp.sparse_attention(*[t.clone().requires_grad_(True) for t in (q, k, v)], pat, bias=table.clone().requires_grad_(True), **kw)
+    assert {q.shape, table.shape, kw["lengths"].shape} < shapes
     for shape in shapes:   # each kind once: less of it than was saved
         leaves = [t.clone().requires_grad_(True) for t in (q, k, v, table)]
         with torch.autograd.graph.saved_tensors_hooks(lambda t: t, lambda t: t[:1] if t.shape == shape else t):
