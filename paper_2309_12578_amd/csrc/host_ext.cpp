@@ -927,6 +927,15 @@ std::shared_ptr<AttentionWithBackward> with_node(AttentionExtras&& extras, Index
     return node;
 }
 
+// What the kernels read of an index, one of whose directions is (ptr, idx), for sequences of L tokens: a pattern of another length would lead them past it.
+void check_index(const at::Tensor& ptr, const at::Tensor& idx, const Index& ix, int64_t L, const at::Device& device) {
+    check_operand(ptr, device);
+    check_operand(idx, device);
+    if (ix.block < 1 || L % ix.block != 0 || ptr.numel() != L / ix.block + 1 || ix.nnzb < 0 || idx.numel() < ix.nnzb || ptr.scalar_type() != at::kInt ||
+        idx.scalar_type() != at::kInt || !ptr.is_contiguous() || !idx.is_contiguous())
+        bad_value("the pattern is not one of sequences of this length, or its blocks are not counted");
+}
+
 // sparse_attention_with(Q, K, V, row_ptr, col_idx, col_ptr, row_idx, bsr_pos, nnzb, block, scale, table | None, bucket_of | None,
 //                       lengths | None, dropout, rng | None, stream) -> O
 PyObject* py_sparse_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -947,7 +956,7 @@ PyObject* py_sparse_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) 
         ix.nnzb = int_arg(a[8]);
         ix.block = int_arg(a[9]);
         ix.scale = (float)double_arg(a[10]);
-        for (const at::Tensor* t : {&ix.row_ptr, &ix.col_idx}) check_operand(*t, device);
+        check_index(ix.row_ptr, ix.col_idx, ix, q.size(2), device);
         ExtrasArgs with(a + 11, q.size(0), q.size(1), q.size(2), device);
         const at::Tensor& table = with.table;
         const c10::DeviceGuard guard(device);
@@ -977,7 +986,8 @@ PyObject* py_sparse_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) 
             ix.col_ptr = tensor_arg(a[5]);
             ix.row_idx = tensor_arg(a[6]);
             ix.bsr_pos = tensor_arg(a[7]);
-            for (const at::Tensor* t : {&ix.col_ptr, &ix.row_idx, &ix.bsr_pos}) check_operand(*t, device);
+            check_operand(ix.bsr_pos, device);
+            check_index(ix.col_ptr, ix.row_idx, ix, q.size(2), device);
             auto node = with_node(std::move(with.extras), std::move(ix), state, tc);
             node->set_next_edges(table.defined() ? torch::autograd::collect_next_edges(q, k, v, table) : torch::autograd::collect_next_edges(q, k, v));
             node->q = torch::autograd::SavedVariable(qc, false);
@@ -1009,7 +1019,7 @@ PyObject* py_heads_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int64_t B = qkv.size(0), L = qkv.size(1);
         ix.row_ptr = tensor_arg(a[2]);
         ix.col_idx = tensor_arg(a[3]);
-        for (const at::Tensor* t : {&ix.row_ptr, &ix.col_idx}) check_operand(*t, device);
+        check_index(ix.row_ptr, ix.col_idx, ix, L, device);
         ExtrasArgs with(a + 10, B, H, L, device);
         const at::Tensor& table = with.table;
         const c10::DeviceGuard guard(device);
@@ -1036,7 +1046,7 @@ PyObject* py_heads_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) {
             ix.col_ptr = tensor_arg(a[4]);
             ix.row_idx = tensor_arg(a[5]);
             ix.bsr_pos = tensor_arg(a[6]);
-            for (const at::Tensor* t : {&ix.col_ptr, &ix.row_idx}) check_operand(*t, device);
+            check_index(ix.col_ptr, ix.row_idx, ix, L, device);
             auto node = with_node(std::move(with.extras), std::move(ix), state, tc);
             node->H = H;
             node->set_next_edges(table.defined() ? torch::autograd::collect_next_edges(qkv, table) : torch::autograd::collect_next_edges(qkv));

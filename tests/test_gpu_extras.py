@@ -640,6 +640,14 @@ def test_calls_that_are_refused(sp):
               lambda: sp.dropout_add(q, None, 1.0, rng), lambda: sp.dropout_add(q, None, 0.1, None), lambda: sp.dropout_add(q, None, 0.1, rng, 2 ** 32)):
         with pytest.raises(ValueError):
             f()
+    longer = _inputs(2, H, L + block, torch.bfloat16, 40, 3)   # than the pattern
+    uncounted = sp.Pattern(**{**vars(pat), "nnzb": -1})
+    for a, p in ((longer, pat), ((q[:, :, :block], k[:, :, :block], v[:, :, :block]), pat), ((q, k, v), uncounted)):
+        with pytest.raises(ValueError):
+            sp.sparse_attention(*a, p, lengths=lengths)
+    mha = sp.SparseMHA(64 * H, H, device="cuda", dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        mha(torch.zeros(2, L + block, 64 * H, device="cuda", dtype=torch.bfloat16), pat, lengths=lengths)
     with pytest.raises(sp.SpionError):
         sp.sparse_attention(q[..., :32], k[..., :32], v[..., :32], pat, lengths=lengths)
     leaf = q.float().requires_grad_(True)
