@@ -8,8 +8,9 @@
 // The kernels of this file are for fp32 and block 16: a workgroup of four waves has 16 or 32 rows, whose 16-row tiles of the other
 // side the waves take in turn, straight from memory into registers (layouts, order and pieces as in attn_kernels.hip).  Bound, as there, by the
 // latency of those loads, and in fp32 by its MFMA rate.  Kernel time, us, of the plain ones, with lengths, bias, dropout, bias and dropout, forward and
-// backward: fp32, 8 heads x 2048, block 32, 10 %, 20.2 / 21 / 22.3 / 22.5 / 23.7, 54 / 55.6 / 59 / 60 / 65; 16 x 4096, block 64, 10 %, 79 / 82 / 83 / 87 / 91,
-// 280 / 286 / 296 / 293 / 319; bf16, block 16, 9 x 1936, 8 %, 12.7 / 14.5 / 15.3 / 15.2 / 16.3, 27.4 / 30 / 32 / 31 / 33.5; 32 x 4096 78 / 80 / 88 / 85 / 91, 296 / 294 / 315 / 300 / 321.
+// backward (row_terms_kernel takes 4.7, 6.5, 5.2 and 9.3 besides): fp32, 8 heads x 2048, block 32, 10 %, 20.2 / 21 / 22.3 / 22.5 / 23.8, 54 / 52.4 / 55.7 / 56.6 / 60.5; 16 x
+// 4096, block 64, 10 %, 79 / 80 / 83 / 87 / 91, 280 / 265 / 280 / 282 / 298; bf16, block 16, 9 x 1936, 8 %, 12.7 / 15.2 / 16.3 / 15.9 / 17, 27 / 26.7 / 29 / 27.7 / 30.5; 32 x 4096
+// 78 / 80 / 89 / 86 / 95, 296 / 261 / 278 / 271 / 290.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
