@@ -844,21 +844,25 @@ struct AttentionWithBackward : public torch::autograd::Node {
             const at::Tensor K = H ? Q : k.unpack(), V = H ? Q : v.unpack();
             AttentionExtras with = extras;
             with.lengths = lengths.unpack();
-            const c10::DeviceGuard guard(Q.device());
+            const at::Device device = grads[0].device();   // the call's: autograd hands on no gradient of another device or shape
+            const c10::DeviceGuard guard(device);
             const at::Tensor g = dense(grads[0]);
-            // what saved-tensor hooks hand back is looked at as the call's own tensors were
-            auto same = [&](bool ok) {
+            // What saved-tensor hooks hand back is looked at as the call's own tensors were: the kernels take sizes from Q and bare addresses of the rest.
+            auto same = [](bool ok) {
                 if (!ok) bad_value("sparse_attention: a saved tensor is not the one that was saved");
             };
-            if (H) same(Q.dim() == 3 && Q.size(2) == 3 * H * 64 && Q.scalar_type() == at::kBFloat16 && Q.is_contiguous());
-            else same(Q.dim() == 4 && Q.is_contiguous());
+            const at::Tensor& n = with.lengths;
+            for (const at::Tensor* t : {&Q, &K, &V, &O, &left, &T, &n})
+                same(!t->defined() || (t->device() == device && t->layout() == at::kStrided && t->is_contiguous()));
+            if (H) same(Q.dim() == 3 && Q.size(0) == g.size(0) && Q.size(1) == g.size(1) && Q.size(2) == 3 * g.size(2) && Q.scalar_type() == at::kBFloat16);
+            else same(Q.sizes() == g.sizes() && K.sizes() == g.sizes() && V.sizes() == g.sizes());
+            for (const at::Tensor* t : {&Q, &K, &V, &O}) same(t->scalar_type() == g.scalar_type());
+            same(O.sizes() == g.sizes());
             const spion_attn_params p = H ? heads_params(Q, H, ix) : params_of(Q, ix);
-            for (const at::Tensor* t : {&K, &V}) same(t->numel() == Q.numel() && t->scalar_type() == Q.scalar_type() && t->is_contiguous());
-            for (const at::Tensor* t : {&O, &g}) same(t->numel() == Q.numel() / (H ? 3 : 1) && t->scalar_type() == Q.scalar_type() && t->is_contiguous());
             const WithState at(p, draws(extras), true);
-            same(left.numel() == (int64_t)at.bytes && left.scalar_type() == at::kByte && left.is_contiguous());
-            same(!extras.n_buckets || (T.numel() == (int64_t)extras.n_buckets * p.H && T.is_contiguous() && T.device() == Q.device()));
-            same(!with.lengths.defined() || (with.lengths.numel() == p.B && with.lengths.scalar_type() == at::kInt && with.lengths.is_contiguous()));
+            same(left.numel() == (int64_t)at.bytes && left.scalar_type() == at::kByte && (uintptr_t)left.data_ptr() % 16 == 0);
+            same(!extras.n_buckets || (T.dim() == 2 && T.size(0) == extras.n_buckets && T.size(1) == p.H));
+            same(!n.defined() || (n.numel() == p.B && n.scalar_type() == at::kInt));
             spion_attn_extras x = with.params(T);
             x.rng = (const int64_t*)WithState::at(left, at.used);
             x.o_rest = WithState::at(left, at.rest);
