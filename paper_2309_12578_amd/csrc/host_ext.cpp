@@ -1149,9 +1149,12 @@ struct DropoutAddBackward : public torch::autograd::Node {
             const c10::DeviceGuard guard(grads[0].device());
             if (has_residual && task_should_compute_output(1)) out[1] = grads[0];
             if (task_should_compute_output(0)) {
-                const at::Tensor g = grads[0].contiguous();
+                const at::Tensor g = grads[0].contiguous(), used = rng.unpack();
+                // looked at again: a saved-tensor hook may have handed back another one
+                if (used.device() != g.device() || used.layout() != at::kStrided || used.scalar_type() != at::kLong || used.numel() != 2 || !used.is_contiguous())
+                    bad_value("dropout_add: a saved tensor is not the one that was saved");
                 out[0] = new_like(g);
-                dropout_call(g, at::Tensor(), out[0], p, rng.unpack(), at::Tensor(), stream);
+                dropout_call(g, at::Tensor(), out[0], p, used, at::Tensor(), stream);
             }
             return out;
         });

@@ -61,3 +61,9 @@ def test_saved_tensors_of_the_attention(sp, name, change):
     f, leaves, g, _ = _calls(sp)[name]
     shapes = {tuple(s) for _, s in _refused_when_changed(f, leaves, g, CHANGES[change])}
     assert {tuple(leaves[0].shape), tuple(g.shape), (32, H), (B,)} < shapes   # Q, K and V; O; the table; the lengths; and what the forward left
+
+
+@pytest.mark.parametrize("change", CHANGES)
+def test_saved_tensors_of_dropout(sp, change):
+    f, leaves, g, _ = _calls(sp)["dropout"]
+    assert _refused_when_changed(f, leaves, g, CHANGES[change]) == {(torch.int64, (2,))}   # seed and offset
