@@ -750,10 +750,11 @@ double dropout_arg(PyObject* o) {
 at::Tensor new_longs(int64_t n, const at::Tensor& like) {
     return at::Tensor(at::detail::empty_cuda({n}, at::kLong, like.device(), std::nullopt));
 }
-// What a node of this kind does about exceptions and second derivatives.
+// What a node of this kind does about exceptions, second derivatives and a gradient that carries a tangent.
 template <class F>
-torch::autograd::variable_list differentiate(const char* twice, F&& f) {
+torch::autograd::variable_list differentiate(const char* twice, const at::Tensor& grad, F&& f) {
     TORCH_CHECK_NOT_IMPLEMENTED(!at::GradMode::is_enabled(), twice);
+    TORCH_CHECK_NOT_IMPLEMENTED(!grad._fw_grad(0).defined(), "libspion's operators have no forward-mode derivative, nor have their gradients");
     try {
         return f();
     } catch (const SpionFailure& e) {
@@ -839,7 +840,7 @@ struct AttentionWithBackward : public torch::autograd::Node {
         const int inputs = H ? 1 : 3;
         torch::autograd::variable_list out(inputs + (extras.n_buckets ? 1 : 0));
         if (!grads[0].defined()) return out;
-        return differentiate("sparse_attention cannot be differentiated twice", [&] {
+        return differentiate("sparse_attention cannot be differentiated twice", grads[0], [&] {
             const at::Tensor Q = q.unpack(), O = o.unpack(shared_from_this()), left = state.unpack(), T = table.unpack();
             const at::Tensor K = H ? Q : k.unpack(), V = H ? Q : v.unpack();
             AttentionExtras with = extras;
@@ -1072,7 +1073,7 @@ struct RelativeBiasBackward : public torch::autograd::Node {
     torch::autograd::variable_list apply(torch::autograd::variable_list&& grads) override {
         torch::autograd::variable_list out(1);
         if (!grads[0].defined()) return out;
-        return differentiate("relative_bias cannot be differentiated twice", [&] {
+        return differentiate("relative_bias cannot be differentiated twice", grads[0], [&] {
             const c10::DeviceGuard guard(bucket_of.device());
             const at::Tensor g = grads[0].contiguous();
             if (g.scalar_type() != type || g.numel() != (int64_t)H * q_len * k_len) bad_value("relative_bias: a gradient of another shape");
@@ -1145,7 +1146,7 @@ struct DropoutAddBackward : public torch::autograd::Node {
     torch::autograd::variable_list apply(torch::autograd::variable_list&& grads) override {
         torch::autograd::variable_list out(has_residual ? 2 : 1);
         if (!grads[0].defined()) return out;
-        return differentiate("dropout_add cannot be differentiated twice", [&] {
+        return differentiate("dropout_add cannot be differentiated twice", grads[0], [&] {
             const c10::DeviceGuard guard(grads[0].device());
             if (has_residual && task_should_compute_output(1)) out[1] = grads[0];
             if (task_should_compute_output(0)) {

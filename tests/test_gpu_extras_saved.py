@@ -67,3 +67,11 @@ def test_saved_tensors_of_the_attention(sp, name, change):
 def test_saved_tensors_of_dropout(sp, change):
     f, leaves, g, _ = _calls(sp)["dropout"]
     assert _refused_when_changed(f, leaves, g, CHANGES[change]) == {(torch.int64, (2,))}   # seed and offset
+
+
+@pytest.mark.parametrize("name", OPERATORS)
+def test_gradients_with_a_tangent_are_refused(sp, name):
+    f, leaves, g, _ = _calls(sp)[name]
+    out = f(*leaves)
+    with torch.autograd.forward_ad.dual_level(), pytest.raises(NotImplementedError):
+        torch.autograd.grad(out, leaves, torch.autograd.forward_ad.make_dual(g, torch.ones_like(g)))
