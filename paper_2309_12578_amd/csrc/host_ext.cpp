@@ -701,12 +701,18 @@ PyObject* py_projection(PyObject*, PyObject* const* a, Py_ssize_t n) {
     throw python_error();
 }
 
-// A tensor that the kernels may read and an autograd node of this file may differentiate; `device`: the call's, once known.
-void check_operand(const at::Tensor& t, const std::optional<at::Device>& device) {
+// Whether a transform or a lazy view has made the tensor: its values are not those in memory.
+bool transformed(const at::Tensor& t) {
     using c10::DispatchKey;
     for (DispatchKey k : {DispatchKey::Functionalize, DispatchKey::FuncTorchBatched, DispatchKey::Batched, DispatchKey::FuncTorchGradWrapper,
                           DispatchKey::Negative, DispatchKey::ZeroTensor})
-        if (t.key_set().has(k)) not_implemented("libspion's operators take plain tensors, none that a transform or a lazy view has made");
+        if (t.key_set().has(k)) return true;
+    return false;
+}
+constexpr const char* kPlainTensors = "libspion's operators take plain tensors, none that a transform or a lazy view has made";
+// A tensor that the kernels may read and an autograd node of this file may differentiate; `device`: the call's, once known.
+void check_operand(const at::Tensor& t, const std::optional<at::Device>& device) {
+    if (transformed(t)) not_implemented(kPlainTensors);
     if (t._fw_grad(0).defined()) not_implemented("libspion's operators have no forward-mode derivative");
     if (!t.is_cuda() || t.layout() != at::kStrided) bad_value("libspion needs device tensors");
     if (device && t.device() != *device) bad_value("the tensors of a call must be on one device");
@@ -750,11 +756,14 @@ double dropout_arg(PyObject* o) {
 at::Tensor new_longs(int64_t n, const at::Tensor& like) {
     return at::Tensor(at::detail::empty_cuda({n}, at::kLong, like.device(), std::nullopt));
 }
-// What a node of this kind does about exceptions, second derivatives and a gradient that carries a tangent.
+// What a node of this kind does about exceptions, second derivatives and a gradient that is more or less than its numbers: one with a tangent or
+// from a transform is refused, one that stands for its negative (autograd makes such from conjugates) is written out.
 template <class F>
-torch::autograd::variable_list differentiate(const char* twice, const at::Tensor& grad, F&& f) {
+torch::autograd::variable_list differentiate(const char* twice, at::Tensor& grad, F&& f) {
     TORCH_CHECK_NOT_IMPLEMENTED(!at::GradMode::is_enabled(), twice);
     TORCH_CHECK_NOT_IMPLEMENTED(!grad._fw_grad(0).defined(), "libspion's operators have no forward-mode derivative, nor have their gradients");
+    if (grad.is_neg()) grad = grad.resolve_neg();
+    TORCH_CHECK_NOT_IMPLEMENTED(!transformed(grad), kPlainTensors);
     try {
         return f();
     } catch (const SpionFailure& e) {
@@ -854,7 +863,7 @@ struct AttentionWithBackward : public torch::autograd::Node {
             };
             const at::Tensor& n = with.lengths;
             for (const at::Tensor* t : {&Q, &K, &V, &O, &left, &T, &n})
-                same(!t->defined() || (t->device() == device && t->layout() == at::kStrided && t->is_contiguous()));
+                same(!t->defined() || (t->device() == device && t->layout() == at::kStrided && t->is_contiguous() && !transformed(*t)));
             if (H) same(Q.dim() == 3 && Q.size(0) == g.size(0) && Q.size(1) == g.size(1) && Q.size(2) == 3 * g.size(2) && Q.scalar_type() == at::kBFloat16);
             else same(Q.sizes() == g.sizes() && K.sizes() == g.sizes() && V.sizes() == g.sizes());
             for (const at::Tensor* t : {&Q, &K, &V, &O}) same(t->scalar_type() == g.scalar_type());
@@ -1152,7 +1161,8 @@ struct DropoutAddBackward : public torch::autograd::Node {
             if (task_should_compute_output(0)) {
                 const at::Tensor g = grads[0].contiguous(), used = rng.unpack();
                 // looked at again: a saved-tensor hook may have handed back another one
-                if (used.device() != g.device() || used.layout() != at::kStrided || used.scalar_type() != at::kLong || used.numel() != 2 || !used.is_contiguous())
+                if (used.device() != g.device() || used.layout() != at::kStrided || used.scalar_type() != at::kLong || used.numel() != 2 || !used.is_contiguous() ||
+                    transformed(used))
                     bad_value("dropout_add: a saved tensor is not the one that was saved");
                 out[0] = new_like(g);
                 dropout_call(g, at::Tensor(), out[0], p, used, at::Tensor(), stream);

@@ -36,9 +36,9 @@ def _calls(sp):
 OPERATORS = ["attention", "heads", "sub-layer", "dense bias", "dropout"]
 
 
-# On the host, of another type, of another shape and, where it has several dimensions, as many elements.
+# On the host, of another type, a lazy negative, of another shape and, where it has several dimensions, as many elements.
 CHANGES = {"host": lambda t: t.cpu(), "type": lambda t: t.to(torch.float64 if t.is_floating_point() else torch.int16),
-           "shape": lambda t: t.transpose(t.dim() // 2 - 1, t.dim() // 2).contiguous() if t.dim() > 1 else t[:-1].clone()}
+           "lazy": torch._neg_view, "shape": lambda t: t.transpose(t.dim() // 2 - 1, t.dim() // 2).contiguous() if t.dim() > 1 else t[:-1].clone()}
 
 
 def _refused_when_changed(f, leaves, g, change, error=ValueError):
@@ -75,3 +75,19 @@ def test_gradients_with_a_tangent_are_refused(sp, name):
     out = f(*leaves)
     with torch.autograd.forward_ad.dual_level(), pytest.raises(NotImplementedError):
         torch.autograd.grad(out, leaves, torch.autograd.forward_ad.make_dual(g, torch.ones_like(g)))
+
+
+@pytest.mark.parametrize("name", ["attention", "heads", "dense bias", "dropout"])   # (the sub-layer's projection writes them out)
+def test_gradients_that_are_lazy_negatives(sp, name):
+    f, leaves, g, _ = _calls(sp)[name]
+    out = f(*leaves)
+    want = torch.autograd.grad(out, leaves, -g, retain_graph=True)
+    got = torch.autograd.grad(out, leaves, torch._neg_view(g))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("name", OPERATORS)
+def test_gradients_in_a_batch_are_refused(sp, name):
+    f, leaves, g, _ = _calls(sp)[name]
+    with pytest.raises(NotImplementedError):
+        torch.autograd.grad(f(*leaves), leaves, torch.stack([g, g]), is_grads_batched=True)
