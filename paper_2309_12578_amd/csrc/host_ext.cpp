@@ -778,6 +778,20 @@ torch::autograd::variable_list differentiate(const char* twice, at::Tensor& grad
     }
 }
 
+// A bucket map as a backward pass keeps it: it must have been left as the forward pass read it.  By its version counter, without a saved variable, since a
+// program keeps the map for good (no hook has anything to move away) and may have made it in inference mode, where nothing is counted.
+struct BucketMap {
+    at::Tensor map;
+    int64_t version = 0;
+    BucketMap() = default;
+    explicit BucketMap(const at::Tensor& t) : map(t), version(t.defined() && !t.is_inference() ? t._version() : 0) {}
+    const at::Tensor& unchanged() const {
+        TORCH_CHECK(!map.defined() || map.is_inference() || map._version() == version,
+                    "a bucket map needed for gradient computation has been modified by an inplace operation");
+        return map;
+    }
+};
+
 struct AttentionExtras {
     at::Tensor bucket_of, lengths;
     int n_buckets = 0;
@@ -836,13 +850,15 @@ bool draws(const AttentionExtras& extras) { return std::nearbyint(65536.0 * extr
 struct AttentionWithBackward : public torch::autograd::Node {
     torch::autograd::SavedVariable q, k, v, o, state, table, lengths;
     Index ix;
-    AttentionExtras extras;
+    AttentionExtras extras;   // without the tensors
+    BucketMap buckets;
     int64_t H = 0;   // of qkv's heads; 0: Q, K and V
 
     std::string name() const override { return "SparseAttentionWithBackward"; }
 
     void release_variables() override {
         for (torch::autograd::SavedVariable* s : {&q, &k, &v, &o, &state, &table, &lengths}) s->reset_data();
+        buckets.map.reset();
     }
 
     torch::autograd::variable_list apply(torch::autograd::variable_list&& grads) override {
@@ -854,6 +870,7 @@ struct AttentionWithBackward : public torch::autograd::Node {
             const at::Tensor K = H ? Q : k.unpack(), V = H ? Q : v.unpack();
             AttentionExtras with = extras;
             with.lengths = lengths.unpack();
+            with.bucket_of = buckets.unchanged();
             const at::Device device = grads[0].device();   // the call's: autograd hands on no gradient of another device or shape
             const c10::DeviceGuard guard(device);
             const at::Tensor g = dense(grads[0]);
@@ -935,7 +952,9 @@ std::shared_ptr<AttentionWithBackward> with_node(AttentionExtras&& extras, Index
     node->state = torch::autograd::SavedVariable(state, false);
     node->table = torch::autograd::SavedVariable(table, false);
     node->lengths = torch::autograd::SavedVariable(extras.lengths, false);
+    node->buckets = BucketMap(extras.bucket_of);
     extras.lengths.reset();
+    extras.bucket_of.reset();
     node->extras = std::move(extras);
     node->ix = std::move(ix);
     return node;
@@ -1073,7 +1092,7 @@ PyObject* py_heads_attention_with(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 struct RelativeBiasBackward : public torch::autograd::Node {
-    at::Tensor bucket_of;
+    BucketMap buckets;   // kept after a pass: without saved tensors a second one needs no retain_graph
     at::ScalarType type = at::kFloat;
     int reach = 0, n_buckets = 0, H = 0, q_len = 0, k_len = 0, q_start = 0;
 
@@ -1083,6 +1102,7 @@ struct RelativeBiasBackward : public torch::autograd::Node {
         torch::autograd::variable_list out(1);
         if (!grads[0].defined()) return out;
         return differentiate("relative_bias cannot be differentiated twice", grads[0], [&] {
+            const at::Tensor& bucket_of = buckets.unchanged();
             const c10::DeviceGuard guard(bucket_of.device());
             const at::Tensor g = grads[0].contiguous();
             if (g.scalar_type() != type || g.numel() != (int64_t)H * q_len * k_len) bad_value("relative_bias: a gradient of another shape");
@@ -1121,7 +1141,7 @@ PyObject* py_relative_bias(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (torch::autograd::compute_requires_grad(table)) {
             auto node = std::shared_ptr<RelativeBiasBackward>(new RelativeBiasBackward(), torch::autograd::deleteNode);
             node->set_next_edges(torch::autograd::collect_next_edges(table));
-            node->bucket_of = bucket_of;
+            node->buckets = BucketMap(bucket_of);
             node->type = tc.scalar_type();
             node->reach = (int)reach;
             node->n_buckets = (int)table.size(0);

@@ -79,7 +79,8 @@ class SparseMHA(nn.Module):
         """Of the bias table, on the module's device."""
         if self.bias_table is None:
             return None
-        return RelativeBuckets((self.bucket_map.numel() + 1) // 2, self.bias_table.shape[0], self.bucket_map)
+        # .data: with a version counter of its own, since DistributedDataParallel writes buffers, with what they hold, at every forward pass
+        return RelativeBuckets((self.bucket_map.numel() + 1) // 2, self.bias_table.shape[0], self.bucket_map.data)
 
     def forward(self, E: torch.Tensor, pattern: _b.Pattern, flags: int = 0, *, lengths: Optional[torch.Tensor] = None,
                 rng: Optional[torch.Tensor] = None, stream: int = 0) -> torch.Tensor:

@@ -91,3 +91,39 @@ def test_gradients_in_a_batch_are_refused(sp, name):
     f, leaves, g, _ = _calls(sp)[name]
     with pytest.raises(NotImplementedError):
         torch.autograd.grad(f(*leaves), leaves, torch.stack([g, g]), is_grads_batched=True)
+
+
+@pytest.mark.parametrize("name", ["attention", "heads", "dense bias"])
+def test_a_map_changed_in_place_is_seen(sp, name):
+    f, leaves, g, bucket_map = _calls(sp)[name]
+    out = f(*leaves)
+    torch.autograd.grad(out, leaves, g, retain_graph=True)
+    bucket_map[0] = 1   # of a distance that these sequences do not have: the counter is the whole map's
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        torch.autograd.grad(out, leaves, g)
+    torch.autograd.grad(f(*leaves), leaves, g)
+
+
+def test_a_map_made_in_inference_mode(sp):
+    pat = _pattern_from_mask(sp, np.ones((NB, NB), dtype=np.uint8), BLOCK)
+    q, k, v, do = _inputs(B, H, L, torch.bfloat16, 1)
+    table = _table(32, H, torch.bfloat16, 2).requires_grad_(True)
+    with torch.inference_mode():
+        made_there = sp.relative_buckets(L, device="cuda")
+    maps = made_there, sp.relative_buckets(L, device="cuda")
+    a, b = [torch.autograd.grad(sp.sparse_attention(q, k, v, pat, bias=table, buckets=m), table, do)[0] for m in maps]
+    assert torch.equal(a, b)
+    dbias = torch.randn(H, L, L, device="cuda").to(torch.bfloat16)
+    a, b = [torch.autograd.grad(sp.relative_bias(table, m, L, L), table, dbias)[0] for m in maps]
+    assert torch.equal(a, b)
+
+
+def test_a_sub_layers_map_written_between_two_passes(sp):
+    """As DistributedDataParallel does with a module's buffers, before a backward pass through both."""
+    f, leaves, g, bucket_map = _calls(sp)["sub-layer"]
+    want = torch.autograd.grad(f(*leaves), leaves, g)
+    first = f(*leaves)
+    bucket_map.copy_(bucket_map.clone())
+    second = f(*leaves)
+    got = torch.autograd.grad([first, second], leaves, [g, torch.zeros_like(g)])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
