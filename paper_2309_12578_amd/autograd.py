@@ -43,6 +43,8 @@ def sparse_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, pattern:
     dropout, rng, stream: dropout of the probabilities, see `dropout_add`.
     In bf16 the graph keeps a second tensor of O's size, what rounding left of O: the gradients are made from both.
     With any of them flags must be 0, and second derivatives, tracing and transforms are refused."""
+    if bias is None and buckets is not None:
+        raise ValueError("buckets are those of a bias table, which is missing")
     if bias is None and lengths is None and dropout == 0.0:
         O = (_b._host or _b._native()).sparse_attention(
             Q, K, V, pattern.row_ptr, pattern.col_idx, pattern.col_ptr, pattern.row_idx, pattern.bsr_pos, pattern.nnzb,

@@ -179,3 +179,12 @@ def test_sub_layer_arguments():
     assert set(sp.SparseMHA(128, 2).state_dict()) == {"norm.weight", "norm.bias", "w_qkv.weight", "w_o.weight"}
     with pytest.raises(ValueError):
         mha(torch.zeros(1, 64, 128), None, sp.SPION_ATTN_PAPER_DENOM)
+
+
+@pytest.mark.parametrize("more", [{}, dict(lengths=torch.ones(1, dtype=torch.int32)), dict(dropout=0.1)])
+def test_buckets_without_their_table_are_refused(more):
+    q = torch.zeros(1, 1, 32, 64)
+    index = torch.zeros(2, dtype=torch.int32)
+    pattern = sp.Pattern(32, 32, None, index, index, index, index, index, None, None, 1)
+    with pytest.raises(ValueError, match="table"):
+        sp.sparse_attention(q, q, q, pattern, buckets=sp.relative_buckets(32), **more)
