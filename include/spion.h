@@ -202,6 +202,7 @@ int spion_attn_bwd(const void *Q, const void *K, const void *V, const void *O, c
  * A row that keeps nothing (no key below the length, biases that mask) gives O = 0, LSE = -inf and no gradient.  Rows and keys from
  * the length on: O = 0, LSE = -inf, gradients 0; what Q, K, V and dO hold there, NaN included, does not enter any other result.
  * A bias of -infinity, or down from -1e30, masks.  Scores are fp32: a bias of magnitude b leaves probabilities exact to b * 2^-24 or so.
+ * With a table, a scale other than 0 must be 2^-100 or more: the kernels divide the biases by it.
  */
 typedef struct {
     const void *table;         /* [n_buckets, H], or NULL: no bias */

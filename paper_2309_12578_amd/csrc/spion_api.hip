@@ -506,6 +506,7 @@ static int take_extras(const spion_attn_params* p, const spion_attn_extras* x, i
         if (x->table_dtype != SPION_F32 && x->table_dtype != SPION_BF16) return SPION_ERR_DTYPE;
         if (x->n_buckets < 1 || x->n_buckets > spion::Extras::kMaxBuckets) return SPION_ERR_PARAM;
         if (!x->bucket_of) return SPION_ERR_NULL;
+        if (p->scale > 0.f && p->scale < 0x1p-100f) return SPION_ERR_PARAM;   // the kernels divide the biases by it
     }
     if (threshold && !x->rng) return SPION_ERR_NULL;
     if ((uintptr_t)x->o_rest % 16 != 0) return SPION_ERR_PARAM;

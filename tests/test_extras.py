@@ -188,3 +188,13 @@ def test_buckets_without_their_table_are_refused(more):
     pattern = sp.Pattern(32, 32, None, index, index, index, index, index, None, None, 1)
     with pytest.raises(ValueError, match="table"):
         sp.sparse_attention(q, q, q, pattern, buckets=sp.relative_buckets(32), **more)
+
+
+@pytest.mark.parametrize("scale,table,refused", [(2.0 ** -101, 256, True), (1e-39, 256, True), (2.0 ** -100, 256, False), (0.0, 256, False), (1e-39, None, False)])
+def test_scales_that_biases_cannot_be_divided_by(scale, table, refused):
+    """A bias of 2^27 over 2^-100 is a number of fp32, one of 1 over 1e-39 is not."""
+    p, x = _params(scale=scale), _extras(table=table)
+    sizes = [sp.load().spion_attn_with_workspace_bytes(ctypes.byref(p), ctypes.byref(x), 10, is_bwd) for is_bwd in (0, 1)]
+    assert [n == ctypes.c_size_t(-1).value for n in sizes] == [refused] * 2
+    if refused:
+        assert all(call(*args) == -5 for call, args in _calls(p, x))
