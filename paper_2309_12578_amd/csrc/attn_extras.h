@@ -62,7 +62,9 @@ __device__ __forceinline__ int bucket_index(const Extras& x, unsigned b) { retur
 struct ScoreDraws {
     PhiloxKey key;
     unsigned bh;
-    __device__ __forceinline__ ScoreDraws(const long long* rng, unsigned stream, int bh_) : key(rng, stream), bh((unsigned)bh_ | 0x80000000u) {}
+    // `any`: whether there is dropout; without it rng may be a null pointer
+    __device__ __forceinline__ ScoreDraws(bool any, const long long* rng, unsigned stream, int bh_)
+        : key(any ? PhiloxKey(rng, stream) : PhiloxKey()), bh((unsigned)bh_ | 0x80000000u) {}
     // queries q, q ^ 1 and keys k .. k + 3 (k a multiple of 4)
     __device__ __forceinline__ uint4 call(int q, int k) const { return key.words((unsigned)(q >> 1) << 14 | (unsigned)k >> 2, bh); }
 };

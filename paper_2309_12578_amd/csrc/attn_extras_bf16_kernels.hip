@@ -176,7 +176,7 @@ __global__ __launch_bounds__(BS * 4, BS == 32 && DROP && !WHOLE ? 5 : 4) void at
             biases.put(bias0, first, tid);
         }
     }
-    [[maybe_unused]] const ScoreDraws draws(a.x.rng, a.x.stream, bh);
+    [[maybe_unused]] const ScoreDraws draws(DROP, a.x.rng, a.x.stream, bh);
     [[maybe_unused]] const unsigned below = both_halves(a.x.threshold - 1u);
     const float scale_log2 = a.scale_log2;
 

@@ -118,7 +118,7 @@ __global__ __launch_bounds__(BS * 4, BS == 32 ? 4 : 3) void attn_bwd_with_bf16_k
         const Rows at = {b.at.H, b.at.beside};
         const int in_row = at.in_row(), out_row = at.out_row();   // elements between rows of Q, K, V and of O, dO
         const size_t head = at.in_head(bh, L), out_head = at.out_head(bh, L), vec = (size_t)bh * L;
-        [[maybe_unused]] const ScoreDraws draws(b.x.rng, b.x.stream, bh);
+        [[maybe_unused]] const ScoreDraws draws(DROP, b.x.rng, b.x.stream, bh);
         [[maybe_unused]] const unsigned below = both_halves(b.x.threshold - 1u);
         const float scale_log2 = b.scale_log2;
         const int I = idx;
@@ -384,7 +384,7 @@ __global__ __launch_bounds__(BS * 4, BS == 32 ? 4 : 3) void attn_bwd_with_bf16_k
     const Rows at = {b.at.H, b.at.beside};
     const int in_row = at.in_row(), out_row = at.out_row();   // elements between rows of Q, K, V and of O, dO
     const size_t head = at.in_head(bh, L), out_head = at.out_head(bh, L), vec = (size_t)bh * L;
-    [[maybe_unused]] const ScoreDraws draws(b.x.rng, b.x.stream, bh);
+    [[maybe_unused]] const ScoreDraws draws(DROP, b.x.rng, b.x.stream, bh);
     [[maybe_unused]] const unsigned below = both_halves(b.x.threshold - 1u);
     const float scale_log2 = b.scale_log2;
     const KeyItem item = key_item_lookup(b.col_ptr, nb, b.chunk, b.finest, idx, lane);

@@ -162,7 +162,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_fwd_with_kernel(
         if (row0 + 16 * h + r < length) load_rows<T>(qf[h], Q + head + (size_t)(row0 + 16 * h) * kD, r, g);
         else clear(qf[h]);
     }
-    [[maybe_unused]] ScoreDraws draws(x.rng, x.stream, bh);
+    [[maybe_unused]] ScoreDraws draws(DROP, x.rng, x.stream, bh);
     // K of tiles t, t + 1, .. and the buckets (past the end: tile t once more, which counts nothing)
     auto load_k = [&](Frag (&k)[KT][NDC], unsigned (&buckets)[NQ][KT], int t) {
 #pragma unroll
@@ -469,7 +469,7 @@ __global__ __launch_bounds__(W * 64, 2) void attn_bwd_with_kernel(const BwdOfRow
     if (!key_side && x.slices)
         for (int i = tid; i < W * 4 * kDiag; i += W * 64) (&diag_s[0][0][0])[i] = 0.f;
     __syncthreads();
-    [[maybe_unused]] ScoreDraws draws(x.rng, x.stream, bh);
+    [[maybe_unused]] ScoreDraws draws(DROP, x.rng, x.stream, bh);
 
     constexpr int kAtOnce = 4 * W;   // rows that all threads have together, 4 columns each
     auto merged = [&](int p) {       // rows p + tid / 16

@@ -13,6 +13,7 @@ __device__ __forceinline__ unsigned xor3(unsigned a, unsigned b, unsigned c) { r
 
 struct PhiloxKey {
     unsigned k0, k1, c2, c3;   // the same for a whole launch: kept in scalar registers
+    __device__ __forceinline__ PhiloxKey() : k0(0), k1(0), c2(0), c3(0) {}
     __device__ __forceinline__ PhiloxKey(const long long* __restrict__ rng, unsigned stream)
         : k0(uniform((unsigned)rng[0])), k1(uniform((unsigned)((unsigned long long)rng[0] >> 32))), c2(uniform((unsigned)rng[1])), c3(stream) {}
     static __device__ __forceinline__ unsigned uniform(unsigned v) { return (unsigned)__builtin_amdgcn_readfirstlane((int)v); }
