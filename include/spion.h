@@ -216,7 +216,9 @@ typedef struct {
     uint32_t stream;           /* tells apart the dropouts that share an rng */
     uint32_t reserved;         /* must be 0 */
     void *o_rest;              /* bf16: as O, what its rounding left; written by spion_attn_fwd_with, read by spion_attn_bwd_with, whose delta is
-                                  then exact; or NULL (delta from the rounded O, and the gradients less exact).  fp32: not used */
+                                  then free of O's rounding (to 2^-16 of O) and, with a table, of that of P, which the forward then takes
+                                  apart as well (without a table P is rounded to bf16); or NULL: delta from the rounded O, and the gradients
+                                  less exact.  fp32: not used */
 } spion_attn_extras;
 
 /* Bytes of device scratch of the two calls below; (size_t)-1 if the parameters are unsupported. */
@@ -227,7 +229,8 @@ int spion_attn_fwd_with(const void *Q, const void *K, const void *V, void *O, fl
                         void *workspace, size_t workspace_bytes, void *hip_stream);
 /* Gradient of spion_attn_fwd_with (same rng): dQ, dK, dV as spion_attn_bwd, and
  *   dtable[b][head] = sum of dS_qk over all (batch, q, k) of bucket b, dS = P .* (c M .* (dO V^T) - delta);
- * fp32 sums in a fixed order.  dtable [n_buckets, H] in table_dtype, or NULL.  flags must be 0. */
+ * fp32 sums in a fixed order.  dtable [n_buckets, H] in table_dtype, or NULL, which saves the last kernel alone: what it adds up is made for any table.
+ * flags must be 0. */
 int spion_attn_bwd_with(const void *Q, const void *K, const void *V, const void *O, const void *dO, const float *LSE,
                         void *dQ, void *dK, void *dV, void *dtable, const int32_t *row_ptr, const int32_t *col_idx,
                         const int32_t *col_ptr, const int32_t *row_idx, const int32_t *bsr_pos, int32_t nnzb,

@@ -38,7 +38,7 @@ def sparse_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, pattern:
     differentiable with respect to Q, K and V.
 
     bias, buckets: a table [buckets, H] (bf16 or fp32) of biases by the distance key - query, added to the scores inside the
-    softmax; differentiable as well.  A bias of -infinity, or down from -1e30, masks.
+    softmax; differentiable as well (one that needs no gradient costs nearly the same).  A bias of -infinity, or down from -1e30, masks.
     lengths: int32 [B], the tokens of each sequence; keys from there on are masked, rows from there on are 0, gradients too.
     dropout, rng, stream: dropout of the probabilities, see `dropout_add`.
     In bf16 the graph keeps a second tensor of O's size, what rounding left of O: the gradients are made from both.

@@ -4,7 +4,7 @@
 //     S^T starts from is read from there (neighbouring lanes read neighbouring words);
 //   - dropout factors made while the tiles are on their way;
 //   - tiles whose rows from the sequence's length on come as zeros, whatever memory holds there: the loads' range ends with the sequence.
-// WHOLE, where the backward pass may have a table's gradient to make: the probabilities' rounding to bf16 goes through the product with V (and the sums) as
+// WHOLE, where the backward pass may have a table's gradient to make (there is a table and o_rest; the call does not say whether the table is learned): the probabilities' rounding to bf16 goes through the product with V (and the sums) as
 // well.  A row's delta comes from O, and its error is the same for all of the row's dS: over the far buckets, which have many keys of a row, it added
 // up to 0.9e-3 of the table's gradient in the mean (bf16's own rounding of it is 1.7e-3).
 //

@@ -10,7 +10,7 @@
 // shifts (diagonal_sums) and through LDS, over the waves of the workgroup one step later, behind the barrier that is there anyway.  What leaves
 // is one number for each distance of a block, slices[head][kept block][2 BS], 1/32 of what the block's tiles bring in.
 //
-// Three waves a SIMD at up to 168 registers (block 32: four at 128), which the arguments read again where they are used (args_again) and addresses made
+// Three waves a SIMD at up to 168 registers (block 32: four at 128; with a bias LDS has room for seven workgroups of two, 3.5), which the arguments read again where they are used (args_again) and addresses made
 // anew for each block (once) leave room for; at two the backward with bias and dropout took 253 instead of 220 us (4 x 8 heads x 4096, 20.8 %).  Neither
 // the matrix nor the vector pipes are busy half of the time: a step is one chain of products, exponentials and products, longer than the plain one by
 // the draws and the biases.  Kernel time, us, of the plain one, with lengths, bias, dropout, bias and dropout (row_terms_kernel not counted): 4 x 4 heads x 4096,
