@@ -259,6 +259,72 @@ int spion_dropout_add(const void *x, const void *residual, void *y, int64_t n, i
                       int64_t *rng_used, uint32_t stream, void *hip_stream);
 
 /*
+ * Positions as rotations (of queries and keys, before the attention), with one axis or several (height and width of an image, time besides).
+ *   x, y [B, H, L, d] by their strides, elements of d beside each other (any address); y must not overlap x.  Of the first `rotated` heads, pair i (of
+ *   d / 2) of token l turns by t = position[axis_of[i]][b][l] * frequency of i:  a' = a cos t - b sin t,  b' = b cos t + a sin t.  The other heads are copied.
+ *   A pair is elements i and i + d / 2, with SPION_ROTARY_NEIGHBOURS 2 i and 2 i + 1.  SPION_ROTARY_BACK: by -t, which is the gradient.
+ *   turns     [d / 2] frequencies in turns, as integers in 2^-64 modulo 2^64 (rint(2^64 * frequency / (2 pi))): an angle is exact to position * 2^-65 turns.
+ *   axis_of   [d / 2]; an entry from `axes` on counts as the last axis.
+ *   positions int32 or int64, any sign, at position_stride[0] * axis + [1] * b + [2] * l.
+ * Supported: d a multiple of 16 up to 256, H up to 65535, up to 255 axes, fewer than 2^31 tokens.
+ */
+#define SPION_ROTARY_NEIGHBOURS 1u
+#define SPION_ROTARY_BACK 2u
+typedef struct {
+    int32_t B, H, L, d;
+    int32_t rotated;             /* 0 .. H */
+    int32_t axes;
+    int32_t dtype;               /* spion_dtype of x and y */
+    int32_t position_bytes;      /* 4 or 8 */
+    int64_t x_stride[3];         /* of B, H, L, in elements */
+    int64_t y_stride[3];
+    int64_t position_stride[3];  /* of axes, B, L, in positions */
+    uint32_t flags;              /* SPION_ROTARY_* bits, otherwise 0 */
+    uint32_t reserved;           /* must be 0 */
+} spion_rotary_params;
+int spion_rotary(const void *x, void *y, const int64_t *turns, const uint8_t *axis_of, const void *positions,
+                 const spion_rotary_params *p /* HOST */, void *hip_stream);
+
+/*
+ * Rows held in 8 bits.  A row of D elements goes in groups of 64, the last one filled up with zeros: codes [rows, P] with P the next multiple of 64,
+ * 8-byte aligned, exponents [rows, P / 64].  A group's scale is the smallest power of two 2^k >= 2^-126 with max |x| <= 127 * 2^k, its exponent byte k + 127; a code is
+ * rint(x / 2^k), ties to even.  A group with an infinity or NaN has exponent byte 255, codes 0, and stands for NaN.  (Numbers from 127 * 2^121 on are rounded
+ * to 2^128, an infinity in both types.)
+ *   spion_pack_eight    x [rows, D] of `dtype`.
+ *   spion_unpack_eight  y [rows, D] of `dtype` = code * 2^k * weight[column]; weight [D] of weight_dtype, or NULL: 1 (bf16 then holds every value exactly).
+ * 1 <= D <= 2^20, rows * P < 2^60.
+ */
+int spion_pack_eight(const void *x, int8_t *codes, uint8_t *exponents, int64_t rows, int32_t D, int32_t dtype, void *hip_stream);
+int spion_unpack_eight(const int8_t *codes, const uint8_t *exponents, const void *weight, int32_t weight_dtype, void *y, int64_t rows, int32_t D,
+                       int32_t dtype, void *hip_stream);
+
+/*
+ * Root-mean-square norm over rows of D elements (1 <= D <= 16384; x, residual, weight, y, h, dy, dh, dx, dw of `dtype`; rstd fp32 [rows]):
+ *   s = x + residual (residual may be NULL),  rstd = 1 / sqrt(mean s^2 + eps),  z = s rstd,  y = z weight,  h = s rounded.
+ *   y, h, rstd, codes may be NULL: not wanted.  codes, exponents: z in 8 bits (as above), with SPION_NORM_CODES_OF_Y y.  Sums of squares, and what
+ *   decides a code, are in 64 bits.
+ * Gradient:  dx = dh + rstd (weight dy - z mean(weight dy z)),  dw = sum of dy z.  It is the residual's too.  z from the codes (of z), or codes NULL and z = h rstd.
+ *   dh may be NULL (none), dw may be NULL (not wanted).  fp32 sums in a fixed order.
+ */
+#define SPION_NORM_CODES_OF_Y 1u
+int spion_rms_norm(const void *x, const void *residual, const void *weight, void *y, void *h, float *rstd, int8_t *codes, uint8_t *exponents,
+                   int64_t rows, int32_t D, double eps, int32_t dtype, uint32_t flags, void *hip_stream);
+size_t spion_rms_norm_workspace_bytes(int64_t rows, int32_t D);
+int spion_rms_norm_grad(const void *dy, const void *dh, const void *h, const int8_t *codes, const uint8_t *exponents, const void *weight,
+                        const float *rstd, void *dx, void *dw, int64_t rows, int32_t D, int32_t dtype, void *workspace, size_t workspace_bytes,
+                        void *hip_stream);
+
+/*
+ * Gradients of a projection Y = X W^T + b whose input was kept in 8 bits:
+ *   dW [N, M] = dY^T X,  X = code * 2^k * weight[column] (weight [M] or NULL: 1),  db [N] (or NULL) = column sums of dY.
+ *   dY [rows, N], weight, dW, db of `dtype`; codes [rows, P], 16-byte aligned, exponents [rows, P / 64], as above with D = M.
+ * The codes enter the product exactly, an fp32 dY as well; fp32 sums in a fixed order.  1 <= N, M <= 2^20, N * P <= 2^36, 1 <= rows < 2^31 - 4096.
+ */
+size_t spion_weight_grad_eight_workspace_bytes(int32_t rows, int32_t N, int32_t M);
+int spion_weight_grad_eight(const void *dY, const int8_t *codes, const uint8_t *exponents, const void *weight, void *dW, void *db, int32_t rows,
+                            int32_t N, int32_t M, int32_t dtype, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
  * Producers of the pattern input.
  *
  * spion_score_mean: the score maps of the heads (and batch items) of a layer are averaged into the

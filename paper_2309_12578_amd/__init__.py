@@ -15,7 +15,11 @@ from .binding import (  # noqa: F401
     frobenius_distance, spion_index_check, index_is_well_formed, spion_copy_yardstick,
     spion_attn_with_workspace_bytes, spion_attn_fwd_with, spion_attn_bwd_with, spion_relative_bias,
     spion_relative_bias_workspace_bytes, spion_relative_bias_grad, spion_dropout_add,
+    SPION_ROTARY_NEIGHBOURS, SPION_ROTARY_BACK, SPION_NORM_CODES_OF_Y, spion_rotary, spion_pack_eight, spion_unpack_eight, spion_rms_norm,
+    spion_rms_norm_workspace_bytes, spion_rms_norm_grad, spion_weight_grad_eight_workspace_bytes, spion_weight_grad_eight,
 )
 from .autograd import sparse_attention  # noqa: E402,F401
 from .extras import RelativeBuckets, dropout_add, relative_bias, relative_buckets  # noqa: E402,F401
+from .rotary import RotaryAxes, rotary, rotary_axes  # noqa: E402,F401
+from .eight import Packed8, linear8, pack8, rms_norm, rms_norm8, unpack8  # noqa: E402,F401
 from .sublayer import SparseMHA  # noqa: E402,F401

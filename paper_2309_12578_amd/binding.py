@@ -24,6 +24,9 @@ SPION_PATTERN_FROM_POOL = 4
 SPION_ATTN_PAPER_DENOM = 1
 SPION_ATTN_BWD_QUERY_SIDE_ONLY = 2
 SPION_ATTN_BWD_KEY_SIDE_ONLY = 4
+SPION_ROTARY_NEIGHBOURS = 1
+SPION_ROTARY_BACK = 2
+SPION_NORM_CODES_OF_Y = 1
 
 
 class SpionError(RuntimeError):
@@ -42,6 +45,12 @@ class _AttnParams(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("L", ctypes.c_int32),
                 ("d", ctypes.c_int32), ("block", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("scale", ctypes.c_float), ("flags", ctypes.c_uint32)]
+
+
+class _RotaryParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "H", "L", "d", "rotated", "axes", "dtype", "position_bytes")] + [
+        ("x_stride", ctypes.c_int64 * 3), ("y_stride", ctypes.c_int64 * 3), ("position_stride", ctypes.c_int64 * 3),
+        ("flags", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
 
 
 class _AttnExtras(ctypes.Structure):
@@ -109,6 +118,23 @@ def load() -> ctypes.CDLL:
     lib.spion_relative_bias_grad.argtypes = [vp] * 3 + [i32] * 7 + [vp, sz, vp]
     lib.spion_dropout_add.restype = ctypes.c_int
     lib.spion_dropout_add.argtypes = [vp] * 3 + [ctypes.c_int64, i32, ctypes.c_double, vp, vp, ctypes.c_uint32, vp]
+    i64, f64, u32 = ctypes.c_int64, ctypes.c_double, ctypes.c_uint32
+    lib.spion_rotary.restype = ctypes.c_int
+    lib.spion_rotary.argtypes = [vp] * 5 + [ctypes.POINTER(_RotaryParams), vp]
+    lib.spion_pack_eight.restype = ctypes.c_int
+    lib.spion_pack_eight.argtypes = [vp] * 3 + [i64, i32, i32, vp]
+    lib.spion_unpack_eight.restype = ctypes.c_int
+    lib.spion_unpack_eight.argtypes = [vp] * 3 + [i32, vp, i64, i32, i32, vp]
+    lib.spion_rms_norm.restype = ctypes.c_int
+    lib.spion_rms_norm.argtypes = [vp] * 8 + [i64, i32, f64, i32, u32, vp]
+    lib.spion_rms_norm_workspace_bytes.restype = sz
+    lib.spion_rms_norm_workspace_bytes.argtypes = [i64, i32]
+    lib.spion_rms_norm_grad.restype = ctypes.c_int
+    lib.spion_rms_norm_grad.argtypes = [vp] * 9 + [i64, i32, i32, vp, sz, vp]
+    lib.spion_weight_grad_eight_workspace_bytes.restype = sz
+    lib.spion_weight_grad_eight_workspace_bytes.argtypes = [i32] * 3
+    lib.spion_weight_grad_eight.restype = ctypes.c_int
+    lib.spion_weight_grad_eight.argtypes = [vp] * 6 + [i32] * 4 + [vp, sz, vp]
     _lib = lib
     return lib
 
@@ -333,6 +359,65 @@ def spion_dropout_add(x, residual, y, n: int, dtype: int, dropout: float, rng, r
                                   dropout_stream, _stream(stream))
     if rc != 0:
         raise SpionError(rc, "spion_dropout_add")
+
+
+def spion_rotary(x, y, turns, axis_of, positions, B: int, H: int, L: int, d: int, rotated: int, axes: int, dtype: int, x_stride, y_stride, position_stride,
+                 flags: int = 0, stream=None) -> None:
+    """Strides as spion_rotary_params has them; x, y and positions may be views (of the memory that their strides reach)."""
+    address = lambda t: None if t is None else t.data_ptr()
+    i64x3 = ctypes.c_int64 * 3
+    p = _RotaryParams(B, H, L, d, rotated, axes, dtype, positions.element_size(), i64x3(*x_stride), i64x3(*y_stride), i64x3(*position_stride), flags, 0)
+    rc = load().spion_rotary(address(x), address(y), _ptr(turns), _ptr(axis_of), address(positions), ctypes.byref(p), _stream(stream))
+    if rc != 0:
+        raise SpionError(rc, "spion_rotary")
+
+
+def spion_pack_eight(x, codes, exponents, rows: int, D: int, dtype: int, stream=None) -> None:
+    rc = load().spion_pack_eight(_ptr(x), _ptr(codes), _ptr(exponents), rows, D, dtype, _stream(stream))
+    if rc != 0:
+        raise SpionError(rc, "spion_pack_eight")
+
+
+def spion_unpack_eight(codes, exponents, weight, y, rows: int, D: int, dtype: int, stream=None) -> None:
+    rc = load().spion_unpack_eight(_ptr(codes), _ptr(exponents), _ptr(weight), SPION_F32 if weight is None else _dtype_code(weight.dtype), _ptr(y), rows, D,
+                                   dtype, _stream(stream))
+    if rc != 0:
+        raise SpionError(rc, "spion_unpack_eight")
+
+
+def spion_rms_norm(x, residual, weight, y, h, rstd, codes, exponents, rows: int, D: int, eps: float, dtype: int, flags: int = 0, stream=None) -> None:
+    rc = load().spion_rms_norm(_ptr(x), _ptr(residual), _ptr(weight), _ptr(y), _ptr(h), _ptr(rstd), _ptr(codes), _ptr(exponents), rows, D, float(eps), dtype,
+                               flags, _stream(stream))
+    if rc != 0:
+        raise SpionError(rc, "spion_rms_norm")
+
+
+def spion_rms_norm_workspace_bytes(rows: int, D: int) -> int:
+    n = int(load().spion_rms_norm_workspace_bytes(rows, D))
+    if n == ctypes.c_size_t(-1).value:
+        raise SpionError(-2, "spion_rms_norm_workspace_bytes")
+    return n
+
+
+def spion_rms_norm_grad(dy, dh, h, codes, exponents, weight, rstd, dx, dw, rows: int, D: int, dtype: int, workspace=None, stream=None) -> None:
+    rc = load().spion_rms_norm_grad(_ptr(dy), _ptr(dh), _ptr(h), _ptr(codes), _ptr(exponents), _ptr(weight), _ptr(rstd), _ptr(dx), _ptr(dw), rows, D, dtype,
+                                    _ptr(workspace), _bytes(workspace), _stream(stream))
+    if rc != 0:
+        raise SpionError(rc, "spion_rms_norm_grad")
+
+
+def spion_weight_grad_eight_workspace_bytes(rows: int, N: int, M: int) -> int:
+    n = int(load().spion_weight_grad_eight_workspace_bytes(rows, N, M))
+    if n == ctypes.c_size_t(-1).value:
+        raise SpionError(-2, "spion_weight_grad_eight_workspace_bytes")
+    return n
+
+
+def spion_weight_grad_eight(dY, codes, exponents, weight, dW, db, rows: int, N: int, M: int, dtype: int, workspace, stream=None) -> None:
+    rc = load().spion_weight_grad_eight(_ptr(dY), _ptr(codes), _ptr(exponents), _ptr(weight), _ptr(dW), _ptr(db), rows, N, M, dtype, _ptr(workspace),
+                                        _bytes(workspace), _stream(stream))
+    if rc != 0:
+        raise SpionError(rc, "spion_weight_grad_eight")
 
 
 # ------------------------------------------------------------------------------------------------

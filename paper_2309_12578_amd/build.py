@@ -37,6 +37,9 @@ SOURCES = [
     ("attn_extras_bwd_bf16_kernels.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form"]),
     ("dropout_kernels.hip", []),
     ("norm_kernels.hip", []),
+    ("rms_norm_kernels.hip", []),
+    ("rotary_kernels.hip", []),
+    ("weight_grad_eight_kernels.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form"]),
     ("projection_kernels.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form"]),
 ]
 

@@ -552,9 +552,12 @@ PyObject* py_heads_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// A norm's node, which can take the gradient of a residual from its input as its second (see residual).
+struct TakesResidual : public torch::autograd::Node {};
+
 // The gradient of layer_norm, all three in one pass over X and dY; torch's operator where more than numbers is wanted.  A
 // second incoming gradient is that of a residual from X (see residual), whose sum with dX the same pass writes.
-struct NormBackward : public torch::autograd::Node {
+struct NormBackward : public TakesResidual {
     torch::autograd::SavedVariable x, w, b, mean, rstd;
 
     std::string name() const override { return "NormBackward"; }
@@ -635,7 +638,7 @@ PyObject* py_layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// residual(X, Y) -> X for a residual around Y = layer_norm(X): an alias whose gradient goes to Y's node, which adds it to
+// residual(X, Y) -> X for a residual around Y = layer_norm(X) or rms_norm(X): an alias whose gradient goes to Y's node, which adds it to
 // its own, instead of an addition after it; X itself where Y did not come from that node alone.
 PyObject* py_residual(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!arg_count(n, 2, "residual")) return nullptr;
@@ -647,7 +650,7 @@ PyObject* py_residual(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (!nothing_between() || !plain(a[0]) || !plain(a[1]) || !at::GradMode::is_enabled()) return as_it_is();
         const at::Tensor &x = THPVariable_Unpack(a[0]), &y = THPVariable_Unpack(a[1]);
         if (!x.requires_grad() || !y.grad_fn()) return as_it_is();
-        const auto node = std::dynamic_pointer_cast<NormBackward>(y.grad_fn());
+        const auto node = std::dynamic_pointer_cast<TakesResidual>(y.grad_fn());
         if (!node || node->num_inputs() != 1 || node->next_edge(0) != torch::autograd::impl::gradient_edge(x)) return as_it_is();
         at::Tensor r;
         {
@@ -1231,6 +1234,538 @@ PyObject* py_dropout_add(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ------------------------------------------------------------------------------------------------
+// Rotary positions, root-mean-square norm, rows in 8 bits.
+// ------------------------------------------------------------------------------------------------
+// A second gradient is looked at as the first (see differentiate).
+void check_gradient(at::Tensor& grad) {
+    if (!grad.defined()) return;
+    TORCH_CHECK_NOT_IMPLEMENTED(!grad._fw_grad(0).defined(), "libspion's operators have no forward-mode derivative, nor have their gradients");
+    if (grad.is_neg()) grad = grad.resolve_neg();
+    TORCH_CHECK_NOT_IMPLEMENTED(!transformed(grad), kPlainTensors);
+}
+at::Tensor new_tensor(at::IntArrayRef sizes, at::ScalarType type, const at::Device& device) {
+    return at::Tensor(at::detail::empty_cuda(sizes, type, device, std::nullopt));
+}
+// A saved tensor as the kernels may read it: where and what it was.
+bool as_saved(const at::Tensor& t, const at::Device& device, at::ScalarType type) {
+    return t.defined() && t.device() == device && t.layout() == at::kStrided && t.is_contiguous() && !transformed(t) && t.scalar_type() == type;
+}
+void saved(bool ok, const char* message) {
+    if (!ok) bad_value(message);
+}
+
+struct RotaryArgs {
+    at::Tensor turns, axis_of;
+    int64_t axes = 0, rotated = 0;
+    bool neighbours = false;
+};
+
+// y as x lies, if that is without gaps.
+at::Tensor turn(const at::Tensor& x, const RotaryArgs& a, const at::Tensor& positions, bool back) {
+    const at::Tensor y = x.is_non_overlapping_and_dense()
+                             ? at::Tensor(at::detail::empty_strided_cuda(x.sizes(), x.strides(), x.scalar_type(), x.device()))
+                             : new_like(x);
+    if (x.numel() == 0) return y;
+    spion_rotary_params p = {};
+    p.B = (int32_t)x.size(0);
+    p.H = (int32_t)x.size(1);
+    p.L = (int32_t)x.size(2);
+    p.d = (int32_t)x.size(3);
+    p.rotated = (int32_t)a.rotated;
+    p.axes = (int32_t)a.axes;
+    p.dtype = dtype_code(x);
+    p.position_bytes = positions.scalar_type() == at::kLong ? 8 : 4;
+    for (int i = 0; i < 3; ++i) {
+        p.x_stride[i] = x.stride(i);
+        p.y_stride[i] = y.stride(i);
+    }
+    p.position_stride[0] = positions.stride(0);
+    p.position_stride[1] = positions.dim() == 3 ? positions.stride(1) : 0;
+    p.position_stride[2] = positions.stride(-1);
+    p.flags = (a.neighbours ? SPION_ROTARY_NEIGHBOURS : 0u) | (back ? SPION_ROTARY_BACK : 0u);
+    const int rc = spion_rotary(x.data_ptr(), y.data_ptr(), (const int64_t*)device_ptr(a.turns), (const uint8_t*)device_ptr(a.axis_of), positions.data_ptr(), &p,
+                                current_stream());
+    if (rc != SPION_OK) throw SpionFailure{rc, "spion_rotary"};
+    return y;
+}
+
+struct RotaryBackward : public torch::autograd::Node {
+    torch::autograd::SavedVariable positions;
+    RotaryArgs args;
+    BucketMap turns, axis_of;   // kept for good by the program, as a bucket map is
+    std::vector<int64_t> position_sizes;
+    at::ScalarType position_type = at::kLong;
+
+    std::string name() const override { return "RotaryBackward"; }
+
+    void release_variables() override { positions.reset_data(); }
+
+    torch::autograd::variable_list apply(torch::autograd::variable_list&& grads) override {
+        torch::autograd::variable_list out(1);
+        if (!grads[0].defined()) return out;
+        return differentiate("rotary cannot be differentiated twice", grads[0], [&] {
+            const at::Device device = grads[0].device();
+            const c10::DeviceGuard guard(device);
+            const at::Tensor g = grads[0].stride(3) == 1 ? grads[0] : grads[0].contiguous(), pos = positions.unpack();
+            saved(pos.defined() && pos.device() == device && pos.layout() == at::kStrided && !transformed(pos) && pos.sizes() == at::IntArrayRef(position_sizes) &&
+                      pos.scalar_type() == position_type, "rotary: a saved tensor is not the one that was saved");
+            RotaryArgs a = args;
+            a.turns = turns.unchanged();
+            a.axis_of = axis_of.unchanged();
+            out[0] = turn(g, a, pos, true);
+            return out;
+        });
+    }
+};
+
+// rotary(x, turns, axis_of, positions, axes, rotated, neighbours) -> y
+PyObject* py_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!arg_count(n, 7, "rotary")) return nullptr;
+    return guarded([&]() -> PyObject* {
+        not_traced();
+        const at::Tensor &x = tensor_arg(a[0]), &positions = tensor_arg(a[3]);
+        check_operand(x, std::nullopt);
+        const at::Device device = x.device();
+        RotaryArgs args;
+        args.turns = tensor_arg(a[1]);
+        args.axis_of = tensor_arg(a[2]);
+        args.axes = long_arg(a[4]);
+        args.rotated = long_arg(a[5]);
+        args.neighbours = a[6] == Py_True;
+        check_operand(positions, device);
+        check_operand(args.turns, device);
+        check_operand(args.axis_of, device);
+        dtype_code(x);
+        if (x.dim() != 4) bad_value("rotary takes tensors of shape [B, H, L, head_dim]");
+        const int64_t d = x.size(3);
+        if (args.turns.dim() != 1 || 2 * args.turns.size(0) != d || args.turns.scalar_type() != at::kLong || !args.turns.is_contiguous() ||
+            args.axis_of.dim() != 1 || 2 * args.axis_of.size(0) != d || args.axis_of.scalar_type() != at::kByte || !args.axis_of.is_contiguous())
+            bad_value("the axes are not those of heads of this dimension");
+        if (args.rotated < 0 || args.rotated > x.size(1)) bad_value("heads must be a number of x's heads");
+        if ((positions.scalar_type() != at::kLong && positions.scalar_type() != at::kInt) || positions.dim() < 2 || positions.dim() > 3 ||
+            positions.size(0) != args.axes || positions.size(-1) != x.size(2) || (positions.dim() == 3 && positions.size(1) != x.size(0)))
+            bad_value("positions must be int32 or int64 [axes, L] or [axes, B, L]");
+        if (x.size(0) > 0x7fffffff || x.size(1) > 65535 || x.size(2) > 0x7fffffff) bad_value("rotary: too many heads or tokens");
+        const c10::DeviceGuard guard(device);
+        const bool grad = torch::autograd::compute_requires_grad(x);
+        at::Tensor y;
+        {
+            at::NoGradGuard no_grad;
+            y = turn(x.stride(3) == 1 ? x : x.contiguous(), args, positions, false);
+        }
+        if (grad) {
+            auto node = std::shared_ptr<RotaryBackward>(new RotaryBackward(), torch::autograd::deleteNode);
+            node->set_next_edges(torch::autograd::collect_next_edges(x));
+            node->positions = torch::autograd::SavedVariable(positions, false);
+            node->position_sizes = positions.sizes().vec();
+            node->position_type = positions.scalar_type();
+            node->turns = BucketMap(args.turns);
+            node->axis_of = BucketMap(args.axis_of);
+            node->args = std::move(args);
+            node->args.turns.reset();
+            node->args.axis_of.reset();
+            torch::autograd::set_history(y, node);
+        }
+        return wrap(y);
+    });
+}
+
+// Codes and exponents of rows, as Packed8 has them.
+struct Eight {
+    at::Tensor codes, exponents;
+    Eight() = default;
+    // of rows like x's
+    explicit Eight(const at::Tensor& x) {
+        std::vector<int64_t> sizes = x.sizes().vec();
+        sizes.back() = (sizes.back() + 63) / 64 * 64;
+        codes = new_tensor(sizes, at::kChar, x.device());
+        sizes.back() /= 64;
+        exponents = new_tensor(sizes, at::kByte, x.device());
+    }
+    // those that a caller hands over, for x's rows
+    Eight(const at::Tensor& c, const at::Tensor& e, at::IntArrayRef lead, int64_t D, const at::Device& device) : codes(c), exponents(e) {
+        check_operand(codes, device);
+        check_operand(exponents, device);
+        std::vector<int64_t> sizes(lead.begin(), lead.end());
+        sizes.push_back((D + 63) / 64 * 64);
+        const bool fits = codes.sizes() == at::IntArrayRef(sizes) && codes.scalar_type() == at::kChar && codes.is_contiguous();
+        sizes.back() /= 64;
+        if (!fits || exponents.sizes() != at::IntArrayRef(sizes) || exponents.scalar_type() != at::kByte || !exponents.is_contiguous() ||
+            (uintptr_t)codes.data_ptr() % 16 != 0)
+            bad_value("codes must be contiguous int8 [..., P], exponents uint8 [..., P / 64], P the multiple of 64 from the rows' size on");
+    }
+    int8_t* c() const { return (int8_t*)codes.data_ptr(); }
+    uint8_t* e() const { return (uint8_t*)exponents.data_ptr(); }
+};
+
+// Rows of a tensor [..., D].
+int64_t rows_of(const at::Tensor& x) {
+    if (x.dim() < 1 || x.size(-1) < 1) bad_value("expected rows of at least one element");
+    return x.numel() / x.size(-1);
+}
+
+void pack(const at::Tensor& x, const Eight& to) {
+    const int64_t rows = rows_of(x);
+    if (rows == 0) return;
+    const int rc = spion_pack_eight(device_ptr(x), to.c(), to.e(), rows, (int32_t)x.size(-1), dtype_code(x), current_stream());
+    if (rc != SPION_OK) throw SpionFailure{rc, "spion_pack_eight"};
+}
+
+void check_width(int64_t D) {
+    if (D > 1 << 20) bad_value("rows of more than 2^20 elements are not supported");
+}
+
+// pack8(x) -> (codes, exponents)
+PyObject* py_pack8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!arg_count(n, 1, "pack8")) return nullptr;
+    return guarded([&]() -> PyObject* {
+        not_traced();
+        const at::Tensor& x = tensor_arg(a[0]);
+        check_operand(x, std::nullopt);
+        dtype_code(x);
+        rows_of(x);
+        check_width(x.size(-1));
+        const c10::DeviceGuard guard(x.device());
+        at::NoGradGuard no_grad;
+        const Eight to(x);
+        pack(x.contiguous(), to);
+        PyObject* r = PyTuple_New(2);
+        if (!r) return nullptr;
+        PyTuple_SET_ITEM(r, 0, wrap(to.codes));
+        PyTuple_SET_ITEM(r, 1, wrap(to.exponents));
+        return r;
+    });
+}
+
+// unpack8(codes, exponents, weight | None, D, dtype code) -> values
+PyObject* py_unpack8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!arg_count(n, 5, "unpack8")) return nullptr;
+    return guarded([&]() -> PyObject* {
+        not_traced();
+        const at::Tensor& codes = tensor_arg(a[0]);
+        check_operand(codes, std::nullopt);
+        const at::Device device = codes.device();
+        const int64_t D = long_arg(a[3]);
+        if (D < 1 || codes.dim() < 1) bad_value("expected rows of at least one element");
+        check_width(D);
+        const Eight from(codes, tensor_arg(a[1]), codes.sizes().slice(0, codes.dim() - 1), D, device);
+        at::Tensor weight = optional_arg(a[2]);
+        if (weight.defined()) {
+            check_operand(weight, device);
+            dtype_code(weight);
+            if (weight.dim() != 1 || weight.size(0) != D) bad_value("weight must be [size]");
+        }
+        const c10::DeviceGuard guard(device);
+        at::NoGradGuard no_grad;
+        if (weight.defined()) weight = weight.contiguous();
+        std::vector<int64_t> sizes = codes.sizes().vec();
+        sizes.back() = D;
+        const int type = int_arg(a[4]);
+        const at::Tensor y = new_tensor(sizes, type == SPION_F32 ? at::kFloat : at::kBFloat16, device);
+        if (y.numel() > 0) {
+            const int rc = spion_unpack_eight(from.c(), from.e(), weight.defined() ? device_ptr(weight) : nullptr, weight.defined() ? dtype_code(weight) : SPION_F32,
+                                              device_ptr(y), rows_of(y), (int32_t)D, type, current_stream());
+            if (rc != SPION_OK) throw SpionFailure{rc, "spion_unpack_eight"};
+        }
+        return wrap(y);
+    });
+}
+
+// x, weight, residual | None of a norm; contiguous.
+struct NormArgs {
+    at::Tensor x, w, residual;
+    int64_t rows, D;
+    double eps;
+    NormArgs(const at::Tensor& x_in, const at::Tensor& w_in, const at::Tensor& r_in, PyObject* e) {
+        const at::Device device = x_in.device();
+        check_operand(x_in, std::nullopt);
+        check_operand(w_in, device);
+        dtype_code(x_in);
+        rows = rows_of(x_in);
+        D = x_in.size(-1);
+        if (D > 16384) bad_value("rows of more than 16384 elements are not supported");
+        if (w_in.dim() != 1 || w_in.size(0) != D || w_in.scalar_type() != x_in.scalar_type()) bad_value("weight must be [D], of x's dtype");
+        if (r_in.defined()) {
+            check_operand(r_in, device);
+            if (r_in.sizes() != x_in.sizes() || r_in.scalar_type() != x_in.scalar_type()) bad_value("residual must have x's shape and dtype");
+        }
+        eps = double_arg(e);
+        if (!(eps >= 0.0) || std::isinf(eps)) bad_value("eps must be a number from 0 on");
+        at::NoGradGuard no_grad;
+        x = x_in.contiguous();
+        w = w_in.contiguous();
+        if (r_in.defined()) residual = r_in.contiguous();
+    }
+    void run(const at::Tensor& y, const at::Tensor& h, const at::Tensor& rstd, const Eight& eight, unsigned flags) const {
+        if (rows == 0) return;
+        auto ptr = [](const at::Tensor& t) { return t.defined() ? device_ptr(t) : nullptr; };
+        const bool codes = eight.codes.defined();
+        const int rc = spion_rms_norm(device_ptr(x), ptr(residual), device_ptr(w), ptr(y), ptr(h), (float*)ptr(rstd), codes ? eight.c() : nullptr,
+                                      codes ? eight.e() : nullptr, rows, (int32_t)D, eps, dtype_code(x), flags, current_stream());
+        if (rc != SPION_OK) throw SpionFailure{rc, "spion_rms_norm"};
+    }
+};
+
+// The gradient of rms_norm: of x, weight and, if there was one, the residual, whose is x's.  The second incoming one is that of the stream h, or of a
+// residual from x (see residual).
+struct RmsNormBackward : public TakesResidual {
+    torch::autograd::SavedVariable h, codes, exponents, w, rstd;   // h, which may be x, or codes and exponents
+    std::vector<int64_t> sizes;
+    bool has_residual = false, eight = false, h_is_output = false;
+    at::ScalarType type = at::kFloat;
+
+    std::string name() const override { return "RmsNormBackward"; }
+
+    void release_variables() override {
+        for (torch::autograd::SavedVariable* s : {&h, &codes, &exponents, &w, &rstd}) s->reset_data();
+    }
+
+    torch::autograd::variable_list apply(torch::autograd::variable_list&& grads) override {
+        torch::autograd::variable_list out(has_residual ? 3 : 2);
+        at::Tensor dh = grads.size() > 1 ? grads[1] : at::Tensor();
+        auto give = [&](const at::Tensor& dx) {
+            if (task_should_compute_output(0)) out[0] = dx;
+            if (has_residual && task_should_compute_output(2)) out[2] = dx;
+        };
+        if (!grads[0].defined()) {
+            give(dh);
+            return out;
+        }
+        return differentiate("rms_norm cannot be differentiated twice", grads[0], [&] {
+            check_gradient(dh);
+            const char* const other = "rms_norm: a saved tensor is not the one that was saved";
+            const at::Device device = grads[0].device();
+            const c10::DeviceGuard guard(device);
+            const at::Tensor g = grads[0].contiguous(), W = w.unpack(), rs = rstd.unpack();
+            if (dh.defined()) dh = dh.contiguous();
+            const int64_t D = sizes.back(), rows = rows_of(g);
+            saved(as_saved(W, device, type) && W.dim() == 1 && W.size(0) == D && as_saved(rs, device, at::kFloat) && rs.numel() == rows, other);
+            Eight from;
+            at::Tensor H;
+            if (eight) {
+                from.codes = codes.unpack();
+                from.exponents = exponents.unpack();
+                const int64_t pitch = (D + 63) / 64 * 64;
+                saved(as_saved(from.codes, device, at::kChar) && from.codes.numel() == rows * pitch && as_saved(from.exponents, device, at::kByte) &&
+                          from.exponents.numel() == rows * (pitch / 64) && (uintptr_t)from.codes.data_ptr() % 8 == 0, other);
+            } else {
+                H = h_is_output ? h.unpack(shared_from_this()) : h.unpack();
+                saved(as_saved(H, device, type) && H.numel() == g.numel(), other);
+            }
+            at::Tensor dx = new_like(g), dw;
+            if (task_should_compute_output(1)) dw = rows == 0 ? at::zeros({D}, W.options()) : new_like(W);
+            if (rows > 0) {
+                at::Tensor ws;
+                if (dw.defined()) ws = new_bytes(spion_rms_norm_workspace_bytes(rows, (int32_t)D), g);
+                const int rc = spion_rms_norm_grad(device_ptr(g), dh.defined() ? device_ptr(dh) : nullptr, eight ? nullptr : device_ptr(H), eight ? from.c() : nullptr,
+                                                   eight ? from.e() : nullptr, device_ptr(W), (const float*)device_ptr(rs), device_ptr(dx),
+                                                   dw.defined() ? device_ptr(dw) : nullptr, rows, (int32_t)D, dtype_code(g), ws.defined() ? ws.data_ptr() : nullptr,
+                                                   ws.defined() ? (size_t)ws.nbytes() : 0, current_stream());
+                if (rc != SPION_OK) throw SpionFailure{rc, "spion_rms_norm_grad"};
+            }
+            give(dx);
+            out[1] = dw;
+            return out;
+        });
+    }
+};
+
+PyObject* optional(const at::Tensor& t) {
+    if (t.defined()) return wrap(t);
+    Py_RETURN_NONE;
+}
+
+// rms_norm(x, weight, residual | None, eps, checkpoint) -> (y, h | None, codes | None, exponents | None)
+PyObject* py_rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!arg_count(n, 5, "rms_norm")) return nullptr;
+    return guarded([&]() -> PyObject* {
+        not_traced();
+        const at::Tensor &x = tensor_arg(a[0]), &w = tensor_arg(a[1]);
+        const at::Tensor residual = optional_arg(a[2]);
+        const NormArgs args(x, w, residual, a[3]);
+        const bool checkpoint = PyObject_IsTrue(a[4]) == 1;
+        const c10::DeviceGuard guard(x.device());
+        const bool grad = residual.defined() ? torch::autograd::compute_requires_grad(x, w, residual) : torch::autograd::compute_requires_grad(x, w);
+        at::Tensor y = new_like(args.x), h, rstd;
+        if (residual.defined()) h = new_like(args.x);
+        if (grad) rstd = new_tensor({args.rows}, at::kFloat, x.device());
+        const Eight eight = checkpoint ? Eight(args.x) : Eight();
+        args.run(y, h, rstd, eight, 0);
+        if (grad) {
+            auto node = std::shared_ptr<RmsNormBackward>(new RmsNormBackward(), torch::autograd::deleteNode);
+            node->set_next_edges(residual.defined() ? torch::autograd::collect_next_edges(x, w, residual) : torch::autograd::collect_next_edges(x, w));
+            node->sizes = args.x.sizes().vec();
+            node->type = args.x.scalar_type();
+            node->has_residual = residual.defined();
+            node->eight = checkpoint;
+            node->w = torch::autograd::SavedVariable(args.w, false);
+            node->rstd = torch::autograd::SavedVariable(rstd, false);
+            torch::autograd::set_history(y, node);
+            if (h.defined()) torch::autograd::set_history(h, node);
+            if (checkpoint) {
+                node->codes = torch::autograd::SavedVariable(eight.codes, false);
+                node->exponents = torch::autograd::SavedVariable(eight.exponents, false);
+            } else {
+                node->h_is_output = h.defined();
+                node->h = h.defined() ? torch::autograd::SavedVariable(h, true) : torch::autograd::SavedVariable(args.x, false);
+            }
+        }
+        PyObject* r = PyTuple_New(4);
+        if (!r) return nullptr;
+        PyTuple_SET_ITEM(r, 0, wrap(y));
+        PyTuple_SET_ITEM(r, 1, optional(h));
+        PyTuple_SET_ITEM(r, 2, optional(eight.codes));
+        PyTuple_SET_ITEM(r, 3, optional(eight.exponents));
+        return r;
+    });
+}
+
+// rms_norm8(x, weight, residual | None, eps) -> (codes, exponents, h | None)
+PyObject* py_rms_norm8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!arg_count(n, 4, "rms_norm8")) return nullptr;
+    return guarded([&]() -> PyObject* {
+        not_traced();
+        const at::Tensor &x = tensor_arg(a[0]), &w = tensor_arg(a[1]);
+        const at::Tensor residual = optional_arg(a[2]);
+        if (residual.defined() ? torch::autograd::compute_requires_grad(x, w, residual) : torch::autograd::compute_requires_grad(x, w))
+            bad_value("rms_norm8 has no gradient: call it under torch.no_grad()");
+        const NormArgs args(x, w, residual, a[3]);
+        const c10::DeviceGuard guard(x.device());
+        at::Tensor h;
+        if (residual.defined()) h = new_like(args.x);
+        const Eight eight(args.x);
+        args.run(at::Tensor(), h, at::Tensor(), eight, SPION_NORM_CODES_OF_Y);
+        PyObject* r = PyTuple_New(3);
+        if (!r) return nullptr;
+        PyTuple_SET_ITEM(r, 0, wrap(eight.codes));
+        PyTuple_SET_ITEM(r, 1, wrap(eight.exponents));
+        PyTuple_SET_ITEM(r, 2, optional(h));
+        return r;
+    });
+}
+
+// The gradient of linear8: x's as a library product, the weight's and the bias' from the codes.
+struct Linear8Backward : public torch::autograd::Node {
+    torch::autograd::SavedVariable codes, exponents, column, w;   // column: the weight of the codes, if they have one
+    std::vector<int64_t> sizes;   // of x
+    bool has_bias = false, has_column = false;
+    at::ScalarType type = at::kFloat;
+
+    std::string name() const override { return "Linear8Backward"; }
+
+    void release_variables() override {
+        for (torch::autograd::SavedVariable* s : {&codes, &exponents, &column, &w}) s->reset_data();
+    }
+
+    torch::autograd::variable_list apply(torch::autograd::variable_list&& grads) override {
+        torch::autograd::variable_list out(has_bias ? 3 : 2);
+        if (!grads[0].defined()) return out;
+        return differentiate("linear8 cannot be differentiated twice", grads[0], [&] {
+            const char* const other = "linear8: a saved tensor is not the one that was saved";
+            const at::Device device = grads[0].device();
+            const c10::DeviceGuard guard(device);
+            const c10::impl::ExcludeDispatchKeyGuard no_autocast(c10::autocast_dispatch_keyset);
+            const int64_t M = sizes.back(), N = grads[0].size(-1);
+            const at::Tensor g = grads[0].reshape({-1, N}).contiguous();
+            const int64_t rows = g.size(0);
+            const bool needs_w = task_should_compute_output(1), needs_b = has_bias && task_should_compute_output(2);
+            if (task_should_compute_output(0)) {
+                const at::Tensor W = w.unpack();
+                saved(W.defined() && W.device() == device && W.dim() == 2 && W.size(0) == N && W.size(1) == M && W.scalar_type() == type, other);
+                out[0] = at::mm(g, W).view(sizes);
+            }
+            if (needs_w && rows > 0) {
+                Eight from;
+                from.codes = codes.unpack();
+                from.exponents = exponents.unpack();
+                const at::Tensor col = has_column ? column.unpack() : at::Tensor();
+                const int64_t pitch = (M + 63) / 64 * 64;
+                saved(as_saved(from.codes, device, at::kChar) && from.codes.numel() == rows * pitch && as_saved(from.exponents, device, at::kByte) &&
+                          from.exponents.numel() == rows * (pitch / 64) && (uintptr_t)from.codes.data_ptr() % 16 == 0 &&
+                          (!has_column || (as_saved(col, device, type) && col.numel() == M)), other);
+                out[1] = new_tensor({N, M}, type, device);
+                if (needs_b) out[2] = new_tensor({N}, type, device);
+                const size_t bytes = spion_weight_grad_eight_workspace_bytes((int32_t)rows, (int32_t)N, (int32_t)M);
+                if (bytes == (size_t)-1) throw SpionFailure{SPION_ERR_SHAPE, "spion_weight_grad_eight_workspace_bytes"};
+                const at::Tensor ws = new_bytes(bytes, g);
+                const int rc = spion_weight_grad_eight(device_ptr(g), from.c(), from.e(), has_column ? device_ptr(col) : nullptr, device_ptr(out[1]),
+                                                       needs_b ? device_ptr(out[2]) : nullptr, (int32_t)rows, (int32_t)N, (int32_t)M, dtype_code(g), ws.data_ptr(),
+                                                       (size_t)ws.nbytes(), current_stream());
+                if (rc != SPION_OK) throw SpionFailure{rc, "spion_weight_grad_eight"};
+            } else {
+                if (needs_w) out[1] = at::zeros({N, M}, g.options());
+                if (needs_b) out[2] = g.sum(0);
+            }
+            return out;
+        });
+    }
+};
+
+// linear8(x, weight, bias | None, codes | None, exponents | None, column weight | None) -> y
+PyObject* py_linear8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!arg_count(n, 6, "linear8")) return nullptr;
+    return guarded([&]() -> PyObject* {
+        not_traced();
+        const at::Tensor &x = tensor_arg(a[0]), &w = tensor_arg(a[1]);
+        const at::Tensor b = optional_arg(a[2]), c = optional_arg(a[3]);
+        check_operand(x, std::nullopt);
+        const at::Device device = x.device();
+        check_operand(w, device);
+        dtype_code(x);
+        const int64_t rows = rows_of(x), M = x.size(-1);
+        if (w.dim() != 2 || w.size(1) != M || w.size(0) < 1 || w.scalar_type() != x.scalar_type()) bad_value("weight must be [N, M] for x [..., M], of x's dtype");
+        const int64_t N = w.size(0);
+        if (b.defined()) {
+            check_operand(b, device);
+            if (b.dim() != 1 || b.size(0) != N || b.scalar_type() != x.scalar_type()) bad_value("bias must be [N], of x's dtype");
+        }
+        if (M > 1 << 20 || N > 1 << 20 || rows >= 0x7fffffff - 4096 || (rows > 0 && spion_weight_grad_eight_workspace_bytes((int32_t)rows, (int32_t)N, (int32_t)M) == (size_t)-1))
+            bad_value("linear8: too many rows or too large a weight");
+        const c10::DeviceGuard guard(device);
+        Eight eight;
+        at::Tensor column;
+        if (c.defined()) {
+            eight = Eight(c, tensor_arg(a[4]), x.sizes().slice(0, x.dim() - 1), M, device);
+            column = optional_arg(a[5]);
+            if (column.defined()) {
+                check_operand(column, device);
+                if (column.dim() != 1 || column.size(0) != M || column.scalar_type() != x.scalar_type()) bad_value("the checkpoint's weight must be [M], of x's dtype");
+            }
+        }
+        const bool grad = b.defined() ? torch::autograd::compute_requires_grad(x, w, b) : torch::autograd::compute_requires_grad(x, w);
+        const bool keeps = grad && w.requires_grad();
+        at::Tensor y;
+        {
+            at::NoGradGuard no_grad;
+            const c10::impl::ExcludeDispatchKeyGuard no_autocast(c10::autocast_dispatch_keyset);
+            y = at::linear(x, w, b.defined() ? std::optional<at::Tensor>(b) : std::nullopt);
+            if (keeps && !c.defined()) {
+                const at::Tensor xc = x.contiguous();
+                eight = Eight(xc);
+                pack(xc, eight);
+            }
+            if (column.defined()) column = column.contiguous();
+        }
+        if (grad) {
+            auto node = std::shared_ptr<Linear8Backward>(new Linear8Backward(), torch::autograd::deleteNode);
+            node->set_next_edges(b.defined() ? torch::autograd::collect_next_edges(x, w, b) : torch::autograd::collect_next_edges(x, w));
+            node->sizes = x.sizes().vec();
+            node->type = x.scalar_type();
+            node->has_bias = b.defined();
+            node->w = torch::autograd::SavedVariable(w, false);
+            if (keeps) {
+                node->codes = torch::autograd::SavedVariable(eight.codes, false);
+                node->exponents = torch::autograd::SavedVariable(eight.exponents, false);
+                node->has_column = column.defined();
+                if (column.defined()) node->column = torch::autograd::SavedVariable(column, false);
+            }
+            torch::autograd::set_history(y, node);
+        }
+        return wrap(y);
+    });
+}
+
 // generate_pattern(A_s, L, block, filter, mode, value, flags, fl_out, row_ptr, col_idx, col_ptr, row_idx, bsr_pos,
 //                  nnzb, pool_sum, workspace | None) -> nnzb, after the pattern is complete
 PyObject* py_generate_pattern(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -1282,6 +1817,12 @@ PyMethodDef kMethods[] = {
     {"sparse_attention_with", (PyCFunction)(void*)py_sparse_attention_with, METH_FASTCALL, nullptr},
     {"relative_bias", (PyCFunction)(void*)py_relative_bias, METH_FASTCALL, nullptr},
     {"dropout_add", (PyCFunction)(void*)py_dropout_add, METH_FASTCALL, nullptr},
+    {"rotary", (PyCFunction)(void*)py_rotary, METH_FASTCALL, nullptr},
+    {"pack8", (PyCFunction)(void*)py_pack8, METH_FASTCALL, nullptr},
+    {"unpack8", (PyCFunction)(void*)py_unpack8, METH_FASTCALL, nullptr},
+    {"rms_norm", (PyCFunction)(void*)py_rms_norm, METH_FASTCALL, nullptr},
+    {"rms_norm8", (PyCFunction)(void*)py_rms_norm8, METH_FASTCALL, nullptr},
+    {"linear8", (PyCFunction)(void*)py_linear8, METH_FASTCALL, nullptr},
     {"generate_pattern", (PyCFunction)(void*)py_generate_pattern, METH_FASTCALL, nullptr},
     {"set_error_class", py_set_error_class, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},

@@ -618,6 +618,111 @@ int spion_dropout_add(const void* x, const void* residual, void* y, int64_t n, i
                ? SPION_OK : SPION_ERR_HIP;
 }
 
+int spion_rotary(const void* x, void* y, const int64_t* turns, const uint8_t* axis_of, const void* positions, const spion_rotary_params* p,
+                 void* hip_stream) {
+    if (!x || !y || !turns || !axis_of || !positions || !p) return SPION_ERR_NULL;
+    if (p->dtype != SPION_F32 && p->dtype != SPION_BF16) return SPION_ERR_DTYPE;
+    if (p->B < 1 || p->H < 1 || p->H > 65535 || p->L < 1 || p->d < 16 || p->d > 256 || p->d % 16 != 0 || (int64_t)p->B * p->L > 0x7fffffff)
+        return SPION_ERR_SHAPE;
+    if (p->rotated < 0 || p->rotated > p->H || p->axes < 1 || p->axes > 255 || (p->position_bytes != 4 && p->position_bytes != 8) ||
+        (p->flags & ~(SPION_ROTARY_NEIGHBOURS | SPION_ROTARY_BACK)) || p->reserved)
+        return SPION_ERR_PARAM;
+    const uintptr_t element = p->dtype == SPION_BF16 ? 2 : 4;
+    if (((uintptr_t)x | (uintptr_t)y) % element != 0 || (uintptr_t)positions % p->position_bytes != 0 || (uintptr_t)turns % 8 != 0) return SPION_ERR_PARAM;
+    spion::RotaryShape s;
+    s.B = p->B;
+    s.N = p->H;
+    s.rotated = p->rotated;
+    s.L = p->L;
+    s.d = p->d;
+    s.axes = p->axes;
+    for (int i = 0; i < 3; ++i) {
+        s.x_stride[i] = p->x_stride[i];
+        s.y_stride[i] = p->y_stride[i];
+    }
+    s.pos_axis = p->position_stride[0];
+    s.pos_batch = p->position_stride[1];
+    s.pos_token = p->position_stride[2];
+    s.pos_bytes = p->position_bytes;
+    s.neighbours = p->flags & SPION_ROTARY_NEIGHBOURS;
+    s.back = p->flags & SPION_ROTARY_BACK;
+    s.tokens_first = p->y_stride[1] < p->y_stride[2];
+    return spion::launch_rotary(x, y, s, reinterpret_cast<const long long*>(turns), axis_of, positions, p->dtype == SPION_BF16,
+                                static_cast<hipStream_t>(hip_stream)) == hipSuccess ? SPION_OK : SPION_ERR_HIP;
+}
+
+static int rows_ok(int64_t rows, int32_t D, int32_t most, int32_t dtype) {
+    if (dtype != SPION_F32 && dtype != SPION_BF16) return SPION_ERR_DTYPE;
+    return rows < 1 || D < 1 || D > most || rows > (1ll << 60) / spion::eight_pitch(D) ? SPION_ERR_SHAPE : SPION_OK;
+}
+constexpr int32_t kEightMaxWidth = 1 << 20;
+
+int spion_pack_eight(const void* x, int8_t* codes, uint8_t* exponents, int64_t rows, int32_t D, int32_t dtype, void* hip_stream) {
+    if (!x || !codes || !exponents) return SPION_ERR_NULL;
+    const int rc = rows_ok(rows, D, kEightMaxWidth, dtype);
+    if (rc != SPION_OK) return rc;
+    if ((uintptr_t)codes % 8 != 0) return SPION_ERR_PARAM;
+    return spion::launch_pack_eight(x, reinterpret_cast<signed char*>(codes), exponents, rows, D, dtype == SPION_BF16,
+                                    static_cast<hipStream_t>(hip_stream)) == hipSuccess ? SPION_OK : SPION_ERR_HIP;
+}
+
+int spion_unpack_eight(const int8_t* codes, const uint8_t* exponents, const void* weight, int32_t weight_dtype, void* y, int64_t rows, int32_t D,
+                       int32_t dtype, void* hip_stream) {
+    if (!codes || !exponents || !y) return SPION_ERR_NULL;
+    if (weight && weight_dtype != SPION_F32 && weight_dtype != SPION_BF16) return SPION_ERR_DTYPE;
+    const int rc = rows_ok(rows, D, kEightMaxWidth, dtype);
+    if (rc != SPION_OK) return rc;
+    if ((uintptr_t)codes % 8 != 0) return SPION_ERR_PARAM;
+    return spion::launch_unpack_eight(reinterpret_cast<const signed char*>(codes), exponents, weight, weight_dtype == SPION_BF16, y, rows, D,
+                                      dtype == SPION_BF16, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? SPION_OK : SPION_ERR_HIP;
+}
+
+int spion_rms_norm(const void* x, const void* residual, const void* weight, void* y, void* h, float* rstd, int8_t* codes, uint8_t* exponents,
+                   int64_t rows, int32_t D, double eps, int32_t dtype, uint32_t flags, void* hip_stream) {
+    if (!x || !weight || (!codes != !exponents) || (!y && !h && !rstd && !codes)) return SPION_ERR_NULL;
+    const int rc = rows_ok(rows, D, spion::kRmsNormMaxWidth, dtype);
+    if (rc != SPION_OK) return rc;
+    if (!(eps >= 0.0) || isinf(eps) || (flags & ~SPION_NORM_CODES_OF_Y) || (uintptr_t)codes % 8 != 0) return SPION_ERR_PARAM;
+    spion::RmsNorm a = {x, residual, weight, y, h, rstd, reinterpret_cast<signed char*>(codes), exponents, (flags & SPION_NORM_CODES_OF_Y) != 0, rows, D, eps};
+    return spion::launch_rms_norm(a, dtype == SPION_BF16, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? SPION_OK : SPION_ERR_HIP;
+}
+
+size_t spion_rms_norm_workspace_bytes(int64_t rows, int32_t D) {
+    if (rows_ok(rows, D, spion::kRmsNormMaxWidth, SPION_F32) != SPION_OK) return (size_t)-1;
+    return spion::rms_norm_workspace_bytes(rows, D);
+}
+
+int spion_rms_norm_grad(const void* dy, const void* dh, const void* h, const int8_t* codes, const uint8_t* exponents, const void* weight,
+                        const float* rstd, void* dx, void* dw, int64_t rows, int32_t D, int32_t dtype, void* workspace, size_t workspace_bytes,
+                        void* hip_stream) {
+    if (!dy || !weight || !rstd || !dx || (!codes != !exponents) || (!codes && !h)) return SPION_ERR_NULL;
+    const int rc = rows_ok(rows, D, spion::kRmsNormMaxWidth, dtype);
+    if (rc != SPION_OK) return rc;
+    if ((uintptr_t)codes % 8 != 0) return SPION_ERR_PARAM;
+    if (dw && (!workspace || (uintptr_t)workspace % kAlign != 0 || workspace_bytes < spion::rms_norm_workspace_bytes(rows, D))) return SPION_ERR_WORKSPACE;
+    spion::RmsNormGrad a = {dy, dh, h, reinterpret_cast<const signed char*>(codes), exponents, weight, rstd, dx, dw, static_cast<float*>(workspace), rows, D};
+    return spion::launch_rms_norm_grad(a, dtype == SPION_BF16, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? SPION_OK : SPION_ERR_HIP;
+}
+
+static bool weight_grad_eight_ok(int32_t rows, int32_t N, int32_t M) {
+    return rows >= 1 && rows < 0x7fffffff - 4096 && N >= 1 && N <= kEightMaxWidth && M >= 1 && M <= kEightMaxWidth && N * spion::eight_pitch(M) <= 1ll << 36;
+}
+
+size_t spion_weight_grad_eight_workspace_bytes(int32_t rows, int32_t N, int32_t M) {
+    return weight_grad_eight_ok(rows, N, M) ? spion::weight_grad_eight_workspace_bytes(rows, N, M) : (size_t)-1;
+}
+
+int spion_weight_grad_eight(const void* dY, const int8_t* codes, const uint8_t* exponents, const void* weight, void* dW, void* db, int32_t rows,
+                            int32_t N, int32_t M, int32_t dtype, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    if (!dY || !codes || !exponents || !dW) return SPION_ERR_NULL;
+    if (dtype != SPION_F32 && dtype != SPION_BF16) return SPION_ERR_DTYPE;
+    if (!weight_grad_eight_ok(rows, N, M)) return SPION_ERR_SHAPE;
+    if ((uintptr_t)codes % 16 != 0) return SPION_ERR_PARAM;
+    if (!workspace || (uintptr_t)workspace % kAlign != 0 || workspace_bytes < spion::weight_grad_eight_workspace_bytes(rows, N, M)) return SPION_ERR_WORKSPACE;
+    spion::WeightGradEight a = {dY, reinterpret_cast<const signed char*>(codes), exponents, weight, dW, db, rows, N, M, workspace};
+    return spion::launch_weight_grad_eight(a, dtype == SPION_BF16, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? SPION_OK : SPION_ERR_HIP;
+}
+
 int spion_heads_attn_fwd(const void* qkv, void* S, float* LSE, const int32_t* row_ptr, const int32_t* col_idx, int32_t nnzb,
                          const spion_attn_params* p, void* room, size_t room_bytes, void* hip_stream) {
     if (!qkv || !S || !LSE || !row_ptr || !col_idx || !p) return SPION_ERR_NULL;

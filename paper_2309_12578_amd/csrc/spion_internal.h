@@ -159,6 +159,64 @@ hipError_t launch_layer_norm(const void* x, const void* w, const void* b, void* 
 hipError_t launch_layer_norm_grad(const void* dy, const void* dr, const void* x, const void* w, const float* mean,
                                   const float* rstd, void* dx, void* dw, void* db, float* partial, int rows, int D, bool is_bf16, hipStream_t st);
 
+// rotary_kernels.hip
+struct RotaryShape {
+    int B, N, rotated, L, d, axes;
+    int64_t x_stride[3], y_stride[3];               // of batch items, heads, tokens, in elements
+    int64_t pos_axis, pos_batch, pos_token;         // strides of the positions, in elements of pos_bytes
+    int pos_bytes;                                  // 4 or 8
+    bool neighbours, back, tokens_first;            // tokens_first: heads of a token lie together
+};
+hipError_t launch_rotary(const void* x, void* y, const RotaryShape& s, const long long* turns, const uint8_t* axis, const void* positions, bool is_bf16,
+                         hipStream_t st);
+
+// eight_bit.h: bytes of a row of D elements in 8 bits
+__host__ __device__ inline long long eight_pitch(long long D) { return (D + 63) / 64 * 64; }
+
+// rms_norm_kernels.hip: rows of D elements, 1 .. kRmsNormMaxWidth
+constexpr int kRmsNormMaxWidth = 16384;
+struct RmsNorm {
+    const void *x, *residual, *w;   // residual may be nullptr
+    void *y, *h;                    // either may be nullptr
+    float* rstd;                    // [rows] or nullptr
+    signed char* codes;             // [rows, eight_pitch(D)] or nullptr: no codes
+    uint8_t* exponents;
+    bool codes_of_y;                // else of z
+    long long rows;
+    int D;
+    double eps;
+};
+hipError_t launch_rms_norm(const RmsNorm& a, bool is_bf16, hipStream_t st);
+struct RmsNormGrad {
+    const void *dy, *dh, *h;        // dh may be nullptr; h: not read where there are codes
+    const signed char* codes;
+    const uint8_t* exponents;
+    const void* w;
+    const float* rstd;
+    void *dx, *dw;                  // dw may be nullptr
+    float* partial;
+    long long rows;
+    int D;
+};
+size_t rms_norm_workspace_bytes(long long rows, int D);
+hipError_t launch_rms_norm_grad(const RmsNormGrad& a, bool is_bf16, hipStream_t st);
+hipError_t launch_pack_eight(const void* x, signed char* codes, uint8_t* exponents, long long rows, int D, bool is_bf16, hipStream_t st);
+hipError_t launch_unpack_eight(const signed char* codes, const uint8_t* exponents, const void* weight, bool weight_bf16, void* y, long long rows, int D,
+                               bool is_bf16, hipStream_t st);
+
+// weight_grad_eight_kernels.hip
+struct WeightGradEight {
+    const void* dY;                 // [rows, N]
+    const signed char* codes;       // [rows, eight_pitch(M)]
+    const uint8_t* exponents;
+    const void* weight;             // [M] or nullptr: what the codes' columns are to be multiplied with
+    void *dW, *db;                  // db may be nullptr
+    int rows, N, M;
+    void* workspace;
+};
+size_t weight_grad_eight_workspace_bytes(int rows, int N, int M);
+hipError_t launch_weight_grad_eight(const WeightGradEight& a, bool is_bf16, hipStream_t st);
+
 // projection_kernels.hip: dW [N, M] = dY^T X over `rows` rows, bf16, N and M multiples of 8
 size_t weight_grad_workspace_bytes(int rows, int N, int M);
 hipError_t launch_weight_grad(const void* dY, const void* X, void* dW, int rows, int N, int M, void* workspace,

@@ -14,7 +14,9 @@ from torch.nn.modules import module as _module
 
 from . import binding as _b
 from .autograd import sparse_attention
+from .eight import Packed8, linear8, rms_norm
 from .extras import RelativeBuckets, _map_for, dropout_add
+from .rotary import RotaryAxes, rotary
 
 HEAD_DIM = 64   # the only head dimension the kernels are built for
 
@@ -29,11 +31,27 @@ class _Norm(nn.LayerNorm):
         return super().forward(x) if y is None else y
 
 
+class _RmsNorm(nn.Module):
+    """rms_norm with its weight."""
+
+    def __init__(self, dim: int, eps: float = 1e-6, device=None, dtype=None):
+        super().__init__()
+        self.eps = eps
+        self.weight = nn.Parameter(torch.ones(dim, device=device, dtype=dtype))
+
+    def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None, checkpoint: bool = False):
+        return rms_norm(x, self.weight, residual, self.eps, checkpoint)
+
+
 class _Projection(nn.Linear):
     """nn.Linear whose bf16 weight gradient, few outputs and a sum over every token, is a kernel of the
-    library (csrc/projection_kernels.hip)."""
+    library (csrc/projection_kernels.hip); with `eight_bit`, linear8."""
 
-    def forward(self, x: torch.Tensor) -> torch.Tensor:
+    eight_bit = False
+
+    def forward(self, x: torch.Tensor, checkpoint: Optional[Packed8] = None) -> torch.Tensor:
+        if self.eight_bit:
+            return linear8(x, self.weight, self.bias, checkpoint)
         y = None
         if x.is_cuda and not torch.compiler.is_compiling():
             y = (_b._host or _b._native()).projection(x, self.weight, self.bias)
@@ -55,24 +73,36 @@ class SparseMHA(nn.Module):
     Q, K, V = LayerNorm(E) W^{Q,K,V} (Algorithm 5).  `embed_dim` must be 64 * heads.
 
     buckets: adds a learned relative position bias, `bias_table` [buckets.count, heads], to the scores; it starts at 0.
-    attn_dropout: dropout of the probabilities while training; it draws from the `rng` of the call."""
+    attn_dropout: dropout of the probabilities while training; it draws from the `rng` of the call.
+    norm: "layer", or "rms" for the root-mean-square norm (`rms_norm`), which also takes the residual of the sub-layer before.
+    rotary: turns queries and keys by their positions (`rotary`), heads of 64.
+    eight_bit: the graph keeps the input of the joint projection, and with the "rms" norm that of the norm by the same codes, in 8 bits (`linear8`)."""
 
     def __init__(self, embed_dim: int, heads: int, dropout: float = 0.0, bias: bool = False,
-                 device=None, dtype=None, *, buckets: Optional[RelativeBuckets] = None, attn_dropout: float = 0.0):
+                 device=None, dtype=None, *, buckets: Optional[RelativeBuckets] = None, attn_dropout: float = 0.0, norm: str = "layer",
+                 rotary: Optional[RotaryAxes] = None, eight_bit: bool = False):
         super().__init__()
+        if norm not in ("layer", "rms"):
+            raise ValueError("norm must be 'layer' or 'rms'")
+        if rotary is not None and rotary.head_dim != HEAD_DIM:
+            raise ValueError("rotary axes must be of heads of %d" % HEAD_DIM)
         if embed_dim != heads * HEAD_DIM:
             raise ValueError("embed_dim must be %d * heads" % HEAD_DIM)
         if not 0.0 <= attn_dropout < 1.0:
             raise ValueError("attn_dropout must be a probability below 1")
         kw = dict(device=device, dtype=dtype)
         self.heads = heads
-        self.norm = _Norm(embed_dim, **kw)
+        self.norm = _Norm(embed_dim, **kw) if norm == "layer" else _RmsNorm(embed_dim, **kw)
         self.w_qkv = _Projection(embed_dim, 3 * embed_dim, bias=bias, **kw)   # W^Q | W^K | W^V
-        self.w_o = _Projection(embed_dim, embed_dim, bias=bias, **kw)
+        self.w_qkv.eight_bit = eight_bit
+        self.w_o = _Projection(embed_dim, embed_dim, bias=bias, **kw)   # (its input the attention keeps as well)
         self.drop = nn.Dropout(dropout)
         self.attn_dropout = attn_dropout
         self.bias_table = None if buckets is None else nn.Parameter(torch.zeros(buckets.count, heads, **kw))
         self.register_buffer("bucket_map", None if buckets is None else buckets.map.to(device), persistent=False)
+        self._axes = (0, False) if rotary is None else (rotary.count, rotary.neighbours)
+        self.register_buffer("turns", None if rotary is None else rotary.turns.to(device), persistent=False)
+        self.register_buffer("axis_of", None if rotary is None else rotary.axis_of.to(device), persistent=False)
 
     @property
     def buckets(self) -> Optional[RelativeBuckets]:
@@ -82,8 +112,16 @@ class SparseMHA(nn.Module):
         # .data: with a version counter of its own, since DistributedDataParallel writes buffers, with what they hold, at every forward pass
         return RelativeBuckets((self.bucket_map.numel() + 1) // 2, self.bias_table.shape[0], self.bucket_map.data)
 
+    @property
+    def rotary(self) -> Optional[RotaryAxes]:
+        """On the module's device."""
+        if self.turns is None:
+            return None
+        return RotaryAxes(HEAD_DIM, self._axes[0], self.turns.data, self.axis_of.data, self._axes[1])
+
     def forward(self, E: torch.Tensor, pattern: _b.Pattern, flags: int = 0, *, lengths: Optional[torch.Tensor] = None,
-                rng: Optional[torch.Tensor] = None, stream: int = 0) -> torch.Tensor:
+                rng: Optional[torch.Tensor] = None, stream: int = 0, positions: Optional[torch.Tensor] = None,
+                residual: Optional[torch.Tensor] = None):
         """E: [B, L, embed_dim] on the GPU (bf16 or fp32); pattern: the layer's sparsity pattern.
         lengths: int32 [B], the tokens of each sequence, see `sparse_attention`; rows from there on leave as they came, but
         for w_o's bias, and have to be finite (the projections' gradients add them up, times 0).
@@ -95,12 +133,23 @@ class SparseMHA(nn.Module):
         plain = self.bias_table is None and lengths is None and attn_dropout == 0.0
         if not plain and flags:
             raise ValueError("flags are not supported together with a bias, lengths or dropout")
-        X = self.norm(E)
-        qkv = w_qkv(X)
-        S, R = None, E
+        S, R, checkpoint = None, E, None
+        if isinstance(self.norm, _RmsNorm):
+            # a hook, or another forward, may change what the norm's codes stand for before the projection has it
+            shares = w_qkv.eight_bit and torch.is_grad_enabled() and not _hands_on(w_qkv) and not self.norm._forward_hooks
+            X, h, checkpoint = self.norm(E, residual, shares)
+            R = E if residual is None else h
+        elif residual is not None:
+            raise ValueError("a residual goes into the 'rms' norm only")
+        else:
+            X = self.norm(E)
+        qkv = w_qkv(X) if checkpoint is None else w_qkv(X, checkpoint)
         if qkv.is_cuda and not torch.compiler.is_compiling():
             host = _b._host or _b._native()
-            R = host.residual(E, X)   # E, its gradient added up in LayerNorm's pass
+            if residual is None:
+                R = host.residual(E, X)   # E, its gradient added up in the norm's pass
+            if self.turns is not None:
+                qkv = self._turned(qkv, positions)
             # lines 4-7 for every head, on the heads as they lie in qkv
             index = (qkv, self.heads, pattern.row_ptr, pattern.col_idx, pattern.col_ptr, pattern.row_idx, pattern.bsr_pos,
                      pattern.nnzb, pattern.block)
@@ -111,6 +160,8 @@ class SparseMHA(nn.Module):
                 S = host.heads_attention_with(
                     *index, apart, self.bias_table, None if self.bias_table is None else _map_for(self.bias_table, self.buckets, L),
                     lengths, attn_dropout, rng, stream)
+        elif self.turns is not None:
+            qkv = self._turned(qkv, positions)
         if S is None:
             qkv = qkv.view(B, L, 3, self.heads, HEAD_DIM)
             # [B, H, L, 64] contiguous per tensor: the layout the kernels take
@@ -118,6 +169,21 @@ class SparseMHA(nn.Module):
             S = sparse_attention(Q, K, V, pattern, flags=flags, bias=self.bias_table, buckets=self.buckets, lengths=lengths,
                                  dropout=attn_dropout, rng=rng, stream=stream)   # lines 4-7, all heads at once
             S = S.transpose(1, 2).reshape(B, L, D)                            # concatenate the heads
-        if rng is not None and self.training and self.drop.p > 0.0:
-            return dropout_add(w_o(S).to(R.dtype), R, self.drop.p, rng, stream)
-        return self.drop(w_o(S)) + R
+        branch = w_o(S)
+        draws = rng is not None and self.training and self.drop.p > 0.0
+        if residual is not None:
+            return (dropout_add(branch, None, self.drop.p, rng, stream) if draws else self.drop(branch)), R
+        if draws:
+            return dropout_add(branch.to(R.dtype), R, self.drop.p, rng, stream)
+        return self.drop(branch) + R
+
+    def _turned(self, qkv: torch.Tensor, positions: Optional[torch.Tensor]) -> torch.Tensor:
+        """Queries and keys, the first two thirds of the heads beside each other in qkv, turned by their positions."""
+        B, L, D = qkv.shape
+        axes = self.rotary
+        if positions is None:
+            if axes.count != 1:
+                raise ValueError("positions of %d axes are missing" % axes.count)
+            positions = torch.arange(L, device=qkv.device)[None]
+        heads = qkv.view(B, L, 3 * self.heads, HEAD_DIM).transpose(1, 2)
+        return rotary(heads, axes, positions, 2 * self.heads).transpose(1, 2).reshape(B, L, D)

@@ -1,0 +1,899 @@
+"""Rotary positions, root-mean-square norm, rows in 8 bits and the projection that keeps them, against their formulas in 64 bits.
+
+Tolerances count roundings: `half(t)` = eps / 2 of a type, once for a rounded result, and u = 2^-24 for each fp32 operation on the way, relative to the
+magnitudes that the operation has."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.float32, torch.bfloat16]
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def sp():
+    import paper_2309_12578_amd as m
+    return m
+
+
+def half(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+def _near(got, want, tol):
+    assert got.shape == want.shape
+    off = (got.double() - want).abs() - tol
+    assert not torch.isnan(off).any() and off.max() <= 0, "off by %.3g more than allowed" % off.max()
+
+
+def _randn(shape, dtype, seed, scale=1.0):
+    return (torch.randn(shape, generator=torch.Generator("cuda").manual_seed(seed), device="cuda") * scale).to(dtype)
+
+
+# ------------------------------------------------------------------------------------------------
+# rotary positions
+# ------------------------------------------------------------------------------------------------
+def _angles(axes, positions):
+    """[.., L, pairs]: of whole turns and 2^-64ths in integers, then in 64 bits."""
+    turns = [int(t) % 2 ** 64 for t in axes.turns.tolist()]
+    which = [min(a, axes.count - 1) for a in axes.axis_of.tolist()]
+    pos = positions.cpu().numpy().astype(object)
+    rows = [np.vectorize(lambda p, t=t: ((int(p) * t + 2 ** 63) % 2 ** 64 - 2 ** 63) / 2.0 ** 64, otypes=[float])(pos[a]) for t, a in zip(turns, which)]
+    return torch.from_numpy(np.stack(rows, axis=-1) * (2 * math.pi)).cuda()
+
+
+def _rotary(x, axes, positions, rotated, back=False):
+    """(result, sum of the magnitudes that each element was made of)"""
+    B, H, L, d = x.shape
+    angle = _angles(axes, positions)
+    angle = (angle[:, None] if positions.dim() == 3 else angle[None, None]) * (-1 if back else 1)
+    c, s = torch.cos(angle), torch.sin(angle)
+    y, m = x.double().clone(), x.double().abs()
+    one, two = (slice(0, None, 2), slice(1, None, 2)) if axes.neighbours else (slice(0, d // 2), slice(d // 2, None))
+    a, b = y[:, :rotated, :, one].clone(), y[:, :rotated, :, two].clone()
+    y[:, :rotated, :, one] = a * c - b * s
+    y[:, :rotated, :, two] = b * c + a * s
+    m[:, :rotated, :, one] = m[:, :rotated, :, two] = a.abs() + b.abs()
+    return y, m
+
+
+def _rotary_tolerance(want, made_of, dtype):
+    # sine and cosine: 3 u for the functions, 2 u for the rounded angle (at most pi / 4); two products and a sum: 3 u
+    return half(dtype) * want.abs() + 8 * U * made_of
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("neighbours", [False, True])
+@pytest.mark.parametrize("B,H,L,d,sections,rotated", [
+    (1, 1, 1, 64, (32,), 1), (64, 16, 1, 64, (8, 12, 12), 16), (2, 6, 33, 64, (16, 16), 4), (3, 5, 70, 16, (1, 2, 3), 0), (2, 3, 100, 256, (128,), 2),
+    (1, 2, 257, 48, (5, 7), 1), (2, 12, 300, 128, (10, 20, 30), 8), (1, 40, 5, 96, (48,), 39), (1, 1, 5000, 32, (16,), 1)])
+def test_rotary_against_the_formula(sp, dtype, neighbours, B, H, L, d, sections, rotated):
+    axes = sp.rotary_axes(d, sections, ladder="own", neighbours=neighbours, device="cuda")
+    x, dy = _randn((B, H, L, d), dtype, 1), _randn((B, H, L, d), dtype, 2)
+    positions = torch.randint(-5000, 5000, (len(sections), B, L), generator=torch.Generator("cuda").manual_seed(3), device="cuda")
+    for pos in (positions, positions[:, 0], positions.int(), positions.transpose(1, 2).contiguous().transpose(1, 2)):
+        leaf = x.clone().requires_grad_()
+        y = sp.rotary(leaf, axes, pos, rotated)
+        assert y.is_contiguous() and y.dtype == dtype
+        want, made_of = _rotary(x, axes, pos, rotated)
+        _near(y, want, _rotary_tolerance(want, made_of, dtype))
+        assert torch.equal(y[:, rotated:], x[:, rotated:])
+        dx, = torch.autograd.grad(y, leaf, dy)
+        want, made_of = _rotary(dy, axes, pos, rotated, back=True)
+        _near(dx, want, _rotary_tolerance(want, made_of, dtype))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rotary_of_far_positions(sp, dtype):
+    """However far, an angle is exact to position * 2^-65 turns; against frequencies as they are, in integers."""
+    axes = sp.rotary_axes(64, (10, 22), device="cuda")
+    pos = torch.tensor([[0, 1, -1, 2 ** 31 - 1, -2 ** 31, 2 ** 40, -2 ** 52, 7], [3, 2 ** 20, 2 ** 30, -2 ** 30, 2 ** 33 + 1, 0, 5, -2 ** 45]], device="cuda")
+    x = _randn((2, 3, 8, 64), dtype, 1)
+    want, made_of = _rotary(x, axes, pos, 3)
+    _near(sp.rotary(x, axes, pos), want, _rotary_tolerance(want, made_of, dtype))
+    from fractions import Fraction
+    pi = Fraction("3.14159265358979323846264338327950288419716939937510582")
+    near = pos.clamp(-2 ** 31, 2 ** 31)
+    f = [Fraction(10000.0 ** -(i / 32)) for i in range(32)]
+    turns = [[float((Fraction(int(near[int(a), t])) * f[i] / (2 * pi)) % 1) for i, a in enumerate(axes.axis_of.tolist())] for t in range(8)]
+    angle = 2 * math.pi * torch.tensor(turns, dtype=torch.float64, device="cuda")
+    a, b = x.double()[..., :32], x.double()[..., 32:]
+    want = torch.cat([a * angle.cos() - b * angle.sin(), b * angle.cos() + a * angle.sin()], -1)
+    made_of = (a.abs() + b.abs()).repeat(1, 1, 1, 2)
+    _near(sp.rotary(x, axes, near), want, _rotary_tolerance(want, made_of, dtype) + 2 * math.pi * 2.0 ** -34 * made_of)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rotary_of_any_strides(sp, dtype):
+    """Heads inside a joint projection, tokens first, odd addresses, shared batch items, a last dimension that is not dense."""
+    axes = sp.rotary_axes(64, (32,), device="cuda")
+    B, H, L, d = 2, 3, 37, 64
+    pos = torch.arange(100, 100 + L, device="cuda")[None]
+    room = _randn((B * L * 3 * H * d + 1,), dtype, 1)
+    qkv = room[1:].view(B, L, 3 * H, d)
+    assert sp.rotary(qkv.transpose(1, 2), axes, pos).stride() == qkv.transpose(1, 2).stride()   # lies as x does
+    views = [qkv.transpose(1, 2), qkv[:, :, H:2 * H].transpose(1, 2), qkv[:1, :, :H].transpose(1, 2).expand(4, -1, -1, -1),
+             _randn((B, H, d, L), dtype, 2).transpose(2, 3), _randn((B, L, H, 2 * d), dtype, 3)[..., ::2].transpose(1, 2),
+             _randn((B, L, H, 2 * d), dtype, 3)[..., 3:3 + d].transpose(1, 2), _randn((L, B, H, d), dtype, 4).permute(1, 2, 0, 3)]
+    for x in views:
+        y = sp.rotary(x, axes, pos)
+        want, made_of = _rotary(x, axes, pos, x.shape[1])
+        _near(y, want, _rotary_tolerance(want, made_of, dtype))
+        leaf = x.detach().requires_grad_()
+        g = torch.ones((), dtype=dtype, device="cuda").expand(x.shape)   # all strides 0
+        dx, = torch.autograd.grad(sp.rotary(leaf, axes, pos), leaf, g)
+        want, made_of = _rotary(g, axes, pos, x.shape[1], back=True)
+        _near(dx, want, _rotary_tolerance(want, made_of, dtype))
+
+
+def test_rotary_of_any_axes(sp):
+    """Axes beyond the last count as the last, any turns will do, and nothing is read that is not there."""
+    g = torch.Generator().manual_seed(5)
+    turns = torch.randint(-2 ** 63, 2 ** 63 - 1, (32,), generator=g).cuda()
+    axis = torch.randint(0, 256, (32,), generator=g).to(torch.uint8).cuda()
+    axes = sp.RotaryAxes(64, 3, turns, axis)
+    x, pos = _randn((2, 2, 50, 64), torch.float32, 1), torch.randint(-2 ** 40, 2 ** 40, (3, 2, 50), generator=g).cuda()
+    want, made_of = _rotary(x, axes, pos, 2)
+    _near(sp.rotary(x, axes, pos), want, _rotary_tolerance(want, made_of, torch.float32))
+
+
+def test_rotary_gradient_against_differences(sp):
+    """The operator is linear: the gradient in one element's direction is the difference that the element makes, exactly but for roundings."""
+    axes = sp.rotary_axes(32, (4, 12), neighbours=True, device="cuda")
+    x, w = _randn((1, 2, 5, 32), torch.float32, 1).requires_grad_(), _randn((1, 2, 5, 32), torch.float32, 2)
+    pos = torch.randint(0, 1000, (2, 5), device="cuda")
+    dx, = torch.autograd.grad((sp.rotary(x, axes, pos) * w).sum(), x)
+    for at in ((0, 0, 0, 0), (0, 1, 3, 17), (0, 0, 4, 31), (0, 1, 2, 8)):
+        e = torch.zeros_like(x)
+        e[at] = 1.0
+        with torch.no_grad():
+            d = ((sp.rotary(x + e, axes, pos).double() - sp.rotary(x - e, axes, pos).double()) * w.double()).sum() / 2
+        # sums of two terms of at most |x| + 1 beside |w|, three operations each
+        assert abs(d - dx[at].double()) <= 16 * U * 2 * (x.abs().max() + 1) * w.abs().max()
+
+
+def test_rotary_past_32_bits(sp):
+    axes = sp.rotary_axes(64, (32,), device="cuda")
+    room = torch.zeros(2 ** 31 + 2 ** 20, dtype=torch.bfloat16, device="cuda")
+    x = room.as_strided((2, 2, 3, 64), (2 ** 31, 2 ** 19, 64, 1))
+    x.copy_(_randn((2, 2, 3, 64), torch.bfloat16, 1))
+    pos = torch.arange(3, device="cuda")[None]
+    want, made_of = _rotary(x, axes, pos, 2)
+    _near(sp.rotary(x, axes, pos), want, _rotary_tolerance(want, made_of, torch.bfloat16))
+    big = torch.zeros((3, 2 ** 13, 2 ** 11, 64), dtype=torch.bfloat16, device="cuda")   # 3 * 2^30 elements, and as many of the result
+    big[2, -1] = 1.0
+    y = sp.rotary(big, axes, torch.arange(2 ** 11, device="cuda")[None])
+    want, made_of = _rotary(big[2:, -1:], axes, torch.arange(2 ** 11, device="cuda")[None], 1)
+    _near(y[2:, -1:], want, _rotary_tolerance(want, made_of, torch.bfloat16))
+    assert not y[2, -2].any() and not y[0].any()
+
+
+# ------------------------------------------------------------------------------------------------
+# rows in 8 bits
+# ------------------------------------------------------------------------------------------------
+def _eight(x):
+    """(codes [.., P], exponents [.., P / 64], values) of x in 64 bits."""
+    *lead, D = x.shape
+    pitch = (D + 63) // 64 * 64
+    g = torch.zeros((*lead, pitch), dtype=torch.float64, device=x.device)
+    g[..., :D] = x
+    g = g.unflatten(-1, (-1, 64))
+    top = g.abs().amax(-1, keepdim=True)
+    finite = torch.isfinite(g).all(-1, keepdim=True) & (top <= torch.finfo(torch.float32).max)
+    k = torch.full_like(top, -126.0)
+    for at in range(-125, 130):
+        k = torch.where(top > 127 * 2.0 ** (at - 1), torch.full_like(k, at), k)
+    codes = torch.where(finite, torch.round(g / torch.exp2(k)), torch.zeros_like(g))
+    values = torch.where(finite, codes * torch.exp2(k), torch.full_like(g, math.nan))
+    exponents = torch.where(finite, k + 127, torch.full_like(k, 255.0)).squeeze(-1)
+    return codes.flatten(-2).to(torch.int8), exponents.to(torch.uint8), values.flatten(-2)[..., :D]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", [(1,), (64,), (65,), (3, 1), (5, 63), (1, 200), (7, 3, 128), (1000, 256), (33, 1000), (2, 100003), (4096, 64)])
+def test_eight_bits_against_their_definition(sp, dtype, shape):
+    x = _randn(shape, dtype, 1) * torch.exp(3 * _randn(shape[:-1] + (1,), torch.float32, 2)).to(dtype)
+    p = sp.pack8(x)
+    codes, exponents, values = _eight(x.double())
+    assert torch.equal(p.codes, codes) and torch.equal(p.exponents, exponents) and p.shape == x.shape and p.weight is None
+    for out in TYPES:
+        y = sp.unpack8(p, out)
+        assert y.dtype == out and torch.equal(y.double(), values)   # exact in both types
+    again = sp.pack8(sp.unpack8(p, dtype))
+    assert torch.equal(again.codes, p.codes)   # (a group's largest code is 64 or more, unless its scale is the smallest)
+    weight = _randn(shape[-1:], dtype, 3)
+    _near(sp.unpack8(sp.Packed8(p.codes, p.exponents, p.size, weight), dtype), values * weight.double(), (half(dtype) + U) * (values * weight.double()).abs())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_eight_bits_at_the_borders(sp, dtype):
+    tiny, most = torch.finfo(dtype).tiny, torch.finfo(dtype).max
+    sub = tiny * torch.finfo(dtype).eps
+    step = torch.finfo(dtype).eps
+    tops = [0.0, sub, 3 * sub, tiny, tiny * 63, tiny * 64, tiny * 127, tiny * 128, 1.0, 127.0, 127.0 * (1 + step), 128.0, 126.0, 63.5, 63.5 * (1 + step), most, most / 2,
+            -127.0, -most, 254.0, 255.0, 253.0]
+    x = torch.zeros((len(tops), 64), dtype=dtype, device="cuda")
+    x[:, 5] = torch.tensor(tops, dtype=dtype)
+    x[:, 1:4] = x[:, 5:6] * torch.tensor([0.5, -0.25, 0.0039215], dtype=dtype, device="cuda")
+    x[8:13, 8:40] = torch.arange(32, device="cuda").to(dtype) * 0.5   # ties
+    x[8, 8:40] /= 64
+    p = sp.pack8(x)
+    codes, exponents, values = _eight(x.double())
+    assert torch.equal(p.exponents, exponents) and torch.equal(p.codes, codes)
+    # the largest numbers are rounded to 64 * 2^122 = 2^128, which neither type has: infinity
+    assert torch.equal(sp.unpack8(p, torch.float32).double(), values.float().double())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_eight_bits_of_what_is_not_finite(sp, dtype, bad):
+    x = _randn((5, 200), dtype, 1)
+    x[1, 70], x[3, 199], x[4, 0] = bad, bad, bad
+    p = sp.pack8(x)
+    codes, exponents, values = _eight(x.double())
+    assert torch.equal(p.codes, codes) and torch.equal(p.exponents, exponents)
+    y = sp.unpack8(p, torch.float32).double()
+    assert torch.equal(torch.isnan(y), torch.isnan(values)) and torch.equal(torch.nan_to_num(y), torch.nan_to_num(values))
+    assert torch.isnan(y[1, 64:128]).all() and torch.isfinite(y[1, :64]).all() and torch.isfinite(y[0]).all()
+
+
+def test_eight_bits_of_nothing_and_of_views(sp):
+    p = sp.pack8(torch.zeros((0, 70), device="cuda"))
+    assert p.codes.shape == (0, 128) and sp.unpack8(p).shape == (0, 70)
+    x = _randn((6, 9, 100), torch.bfloat16, 1)
+    for v in (x.transpose(0, 1), x[::2, :, 3:], x[:, :, :1], x.flatten()[1:701].view(7, 100), x[0].expand(3, 9, 100)):
+        p = sp.pack8(v)
+        codes, exponents, values = _eight(v.double())
+        assert torch.equal(p.codes, codes) and torch.equal(p.exponents, exponents) and torch.equal(sp.unpack8(p).double(), values)
+
+
+def test_eight_bits_past_32_bits(sp):
+    x = torch.zeros((2 ** 21 + 3, 1024), dtype=torch.bfloat16, device="cuda")   # 2^31 elements and more
+    x[-1], x[-2, ::2] = 3.0, -1.0
+    p = sp.pack8(x)
+    y = sp.unpack8(p)
+    assert torch.equal(y[-5:], x[-5:]) and not y[:5].any() and not p.codes[2 ** 20].any()
+
+
+# ------------------------------------------------------------------------------------------------
+# root-mean-square norm
+# ------------------------------------------------------------------------------------------------
+EPS = 1e-6
+
+
+def _norm(x, w, residual=None, eps=EPS):
+    s = x.double() if residual is None else x.double() + residual.double()
+    rstd = 1 / torch.sqrt(s.square().mean(-1, keepdim=True) + eps)
+    return s, rstd, s * rstd, s * rstd * w.double()
+
+
+def _norm_grad(dy, dh, w, rstd, z, dtype):
+    """(dx, its tolerance, dw, its tolerance) with z as the backward pass has it."""
+    D, dy, w = z.shape[-1], dy.double(), w.double()
+    g = dy * w
+    mean, sums = (g * z).mean(-1, keepdim=True), (g * z).abs().mean(-1, keepdim=True)
+    dx = rstd * (g - z * mean) + (0 if dh is None else dh.double())
+    # g 1 u, z 2 u, rstd 1 u; the sum: 8 elements a lane, twice at most, 6 steps in a wave and 16 waves: 40 u with the products; 4 more operations
+    tol = half(dtype) * dx.abs() + U * rstd * (6 * g.abs() + z.abs() * (8 * mean.abs() + 44 * sums)) + (0 if dh is None else U * dh.double().abs())
+    z2, dy2 = z.reshape(-1, D), dy.reshape(-1, D)
+    dw, made_of = (dy2 * z2).sum(0), (dy2 * z2).abs().sum(0)
+    # a lane adds its rows, rows / 1024 at most if there are so many workgroups, one row of each at once; then 32 and 64 + 16 partial sums
+    return dx, tol, dw, half(dtype) * dw.abs() + U * (z2.shape[0] / 1024 + 1 + 32 + 64 + 16 + 4) * made_of
+
+
+WIDTHS = [1, 7, 64, 65, 100, 128, 200, 256, 300, 512, 777, 1024, 2000, 2048, 2056, 4096, 5000, 8192, 16383, 16384]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("with_residual", [False, True])
+@pytest.mark.parametrize("D", WIDTHS)
+def test_norm_against_the_formula(sp, dtype, with_residual, D):
+    for rows in (1, 3, 40) + ((5000,) if D <= 256 else ()):
+        x, w, dy, dh = _randn((rows, D), dtype, 1, 3.0), _randn((D,), dtype, 2), _randn((rows, D), dtype, 3), _randn((rows, D), dtype, 4)
+        residual = _randn((rows, D), dtype, 5) if with_residual else None
+        if not with_residual:
+            dh = None
+        s, rstd, z, y_want = _norm(x, w, residual)
+        for checkpoint in (False, True):
+            leaves = [t.clone().requires_grad_() for t in (x, w) + ((residual,) if with_residual else ())]
+            y, h, p = sp.rms_norm(*leaves, eps=EPS, checkpoint=checkpoint) if with_residual else sp.rms_norm(*leaves, None, EPS, checkpoint)
+            # s 1 u, z 2 u, the product 1 u
+            _near(y, y_want, half(dtype) * y_want.abs() + U * (4 * y_want.abs() + (2 * w.double().abs() * rstd * (x.double().abs() + residual.double().abs()) if with_residual else 0)))
+            assert (h is not None) == with_residual and (p is not None) == checkpoint
+            kept = z
+            if with_residual:
+                _near(h, s, half(dtype) * s.abs() + U * s.abs())
+                kept = h.double() * rstd
+            if checkpoint:
+                codes, exponents, kept = _eight(z)
+                assert torch.equal(p.codes, codes) and torch.equal(p.exponents, exponents) and torch.equal(p.weight, w)
+            grads = torch.autograd.grad([y, h] if with_residual else [y], leaves, [dy, dh] if with_residual else [dy])
+            dx, dx_tol, dw, dw_tol = _norm_grad(dy, dh, w, rstd, kept, dtype)
+            _near(grads[0], dx, dx_tol)
+            _near(grads[1], dw, dw_tol)
+            if with_residual:
+                assert torch.equal(grads[2], grads[0])
+        with torch.no_grad():
+            p, h = sp.rms_norm8(x, w, residual, EPS)
+            codes, exponents, _ = _eight(y_want)
+            assert torch.equal(p.codes, codes) and torch.equal(p.exponents, exponents) and p.weight is None
+            assert (h is None) != with_residual and (h is None or torch.equal(h.double(), s.to(dtype).double()))
+
+
+def test_norm_gradients_against_differences(sp):
+    x, w, r = [_randn(s, torch.float32, i).requires_grad_() for i, s in enumerate([(3, 70), (70,), (3, 70)])]
+    a, b = _randn((3, 70), torch.float32, 8), _randn((3, 70), torch.float32, 9)
+
+    def f(x, w, r):
+        y, h, _ = sp.rms_norm(x, w, r)
+        return (y.double() * a).sum() + (h.double() * b).sum()
+    grads = torch.autograd.grad(f(x, w, r), [x, w, r])
+    step = 2.0 ** -6
+    for i, at in ((0, (1, 3)), (0, (2, 69)), (1, (5,)), (2, (0, 64)), (2, (1, 3))):
+        t = [v.detach().clone() for v in (x, w, r)]
+        values = []
+        for k in (-2, -1, 1, 2):
+            t[i][at] += k * step
+            values.append(f(*t))
+            t[i][at] -= k * step
+        d = (values[0] - 8 * values[1] + 8 * values[2] - values[3]) / (12 * step)
+        # fourth-order differences: h^4 / 30 of a fifth derivative of about 1e2 |a|; values off by 8 u of 420 terms of about 3, times 18 / 12 / step
+        bound = step ** 4 * 100 * 4 + 8 * U * 420 * 3 * 1.5 / step
+        assert abs(d - grads[i][at]) <= bound
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("checkpoint", [False, True])
+def test_norm_through_one_output_only(sp, dtype, checkpoint):
+    x, w, r, g = [_randn(s, dtype, i) for i, s in enumerate([(9, 100), (100,), (9, 100), (9, 100)])]
+    leaves = [t.requires_grad_() for t in (x, w, r)]
+    y, h, _ = sp.rms_norm(*leaves, checkpoint=checkpoint)
+    dx, dw, dr = torch.autograd.grad(h, leaves, g, allow_unused=True, retain_graph=True)
+    assert torch.equal(dx, g) and torch.equal(dr, g) and dw is None
+    dx, dw, dr = torch.autograd.grad(y, leaves, g, retain_graph=True)
+    s, rstd, z, _ = _norm(x, w, r)
+    kept = _eight(z)[2] if checkpoint else h.double() * rstd
+    want, tol, want_w, tol_w = _norm_grad(g, None, w, rstd, kept, dtype)
+    _near(dx, want, tol)
+    _near(dw, want_w, tol_w)
+    assert torch.equal(dx, dr)
+    assert torch.equal(torch.autograd.grad(y, [r], g, retain_graph=True)[0], dr) and torch.equal(torch.autograd.grad(y, [w], g, retain_graph=True)[0], dw)
+    same = x.detach().requires_grad_()   # x as its own residual: both shares
+    y, h, _ = sp.rms_norm(same, w, same, checkpoint=checkpoint)
+    d, = torch.autograd.grad([y, h], [same], [g, g])
+    s, rstd, z, _ = _norm(x, w, x)
+    want, tol, _, _ = _norm_grad(g, g, w, rstd, _eight(z)[2] if checkpoint else h.double() * rstd, dtype)
+    _near(d, 2 * want, 2 * tol + half(dtype) * 2 * want.abs())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_norm_of_rows_that_are_extreme(sp, dtype):
+    """Zeros, squares beyond fp32, numbers whose squares vanish, infinities and NaN: each row by itself."""
+    x = _randn((9, 192), dtype, 1)
+    x[0] = 0
+    x[1] *= 1e30
+    x[2] *= 1e-30
+    x[3, 5], x[4, 7], x[5, 190] = math.inf, math.nan, -math.inf
+    w = _randn((192,), dtype, 2)
+    for eps in (0.0, 1e-6, 1.0):
+        s, rstd, z, want = _norm(x, w, eps=eps)
+        y, _, p = sp.rms_norm(x, w, None, eps, checkpoint=True)
+        codes, exponents, values = _eight(z)
+        assert torch.equal(p.codes, codes) and torch.equal(p.exponents, exponents)
+        assert torch.equal(torch.isnan(y), torch.isnan(want))
+        ok = ~torch.isnan(want)
+        _near(y.double()[ok], want[ok], (half(dtype) + 4 * U) * want[ok].abs() + torch.finfo(dtype).tiny)
+    g = _randn((9, 192), dtype, 3)
+    for checkpoint in (False, True):
+        leaf = x.clone().requires_grad_()
+        y, _, _ = sp.rms_norm(leaf, w, None, EPS, checkpoint=checkpoint)
+        dx, = torch.autograd.grad(y, leaf, g)
+        fine = [0, 1, 2, 6, 7, 8]
+        s, rstd, z, _ = _norm(x[fine], w)
+        want, tol, _, _ = _norm_grad(g[fine], None, w, rstd, _eight(z)[2] if checkpoint else z, dtype)
+        _near(dx[fine], want, tol + torch.finfo(dtype).tiny)
+        assert all(torch.isnan(dx[i]).any() for i in (3, 4, 5))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_norm_of_views_and_of_nothing(sp, dtype):
+    room, w = _randn((6 * 5 * 101 + 1,), dtype, 1), _randn((202,), dtype, 2)
+    for x, wv in ((room[1:].view(6, 5, 101), w[1:102]), (room[1:].view(6, 5, 101).transpose(0, 1), w[::2]), (room[1:].view(6, 5, 101)[:, 2:, ::2], w[:51]),
+                  (room[:101].expand(6, 101), w[:101]), (room[:101], w[:101])):
+        leaf, lw, r = x.detach().requires_grad_(), wv.detach().requires_grad_(), torch.ones((), dtype=dtype, device="cuda").expand(x.shape)
+        y, h, p = sp.rms_norm(leaf, lw, r, checkpoint=True)
+        s, rstd, z, want = _norm(x, wv, r)
+        _near(y, want, half(dtype) * want.abs() + 8 * U * wv.double().abs() * rstd * (x.double().abs() + 1))
+        assert p.shape == x.shape and torch.equal(h, s.to(dtype))
+        g = torch.ones((), dtype=dtype, device="cuda").expand(x.shape)
+        dx, dw = torch.autograd.grad([y, h], [leaf, lw], [g, g])
+        want, tol, want_w, tol_w = _norm_grad(g, g, wv, rstd, _eight(z)[2], dtype)
+        _near(dx, want, tol)
+        _near(dw, want_w, tol_w)
+    x, lw = torch.zeros((0, 64), dtype=dtype, device="cuda", requires_grad=True), w[:64].detach().requires_grad_()
+    for checkpoint in (False, True):
+        y, h, p = sp.rms_norm(x, lw, x, checkpoint=checkpoint)
+        dx, dw = torch.autograd.grad([y, h], [x, lw], [torch.zeros_like(y), torch.zeros_like(y)])
+        assert y.shape == h.shape == dx.shape == (0, 64) and not dw.any()
+    with torch.no_grad():
+        assert sp.rms_norm8(x, lw)[0].codes.shape == (0, 64)
+
+
+def test_norm_past_32_bits(sp):
+    rows, D = 2 ** 18 + 3, 8192   # 2^31 elements and more
+    x = torch.zeros((rows, D), dtype=torch.bfloat16, device="cuda")
+    x[-2:] = _randn((2, D), torch.bfloat16, 1)
+    x.requires_grad_()
+    w = _randn((D,), torch.bfloat16, 2)
+    y, _, p = sp.rms_norm(x, w, checkpoint=True)
+    g = torch.zeros_like(y)
+    g[-2:] = _randn((2, D), torch.bfloat16, 3)
+    dx, = torch.autograd.grad(y, x, g)
+    s, rstd, z, want = _norm(x[-2:].detach(), w)
+    _near(y[-2:].detach(), want, half(torch.bfloat16) * want.abs() + 4 * U * want.abs())
+    codes, exponents, values = _eight(z)
+    assert torch.equal(p.codes[-2:], codes) and torch.equal(p.exponents[-2:], exponents)
+    want, tol, _, _ = _norm_grad(g[-2:], None, w, rstd, values, torch.bfloat16)
+    _near(dx[-2:], want, tol)
+    assert not dx[:3].any()
+
+
+# ------------------------------------------------------------------------------------------------
+# the projection that keeps 8 bits
+# ------------------------------------------------------------------------------------------------
+def _weight_tolerance(dy, x, dw, dtype, rows, products=1):
+    # every sum of `rows` products, in any order, an operation a product: fp32 dY as three
+    made_of = torch.matmul(dy.double().abs().t(), x.double().abs())
+    return half(dtype) * dw.abs() + (products * rows + 400) * U * made_of
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,M,N", [(1, 1, 1), (1, 64, 64), (2, 8, 130), (31, 70, 9), (32, 128, 128), (33, 129, 127), (127, 200, 24), (255, 192, 576), (300, 1, 300),
+                                      (1000, 500, 7), (5000, 64, 64), (4097, 256, 768), (700, 1100, 260), (20000, 40, 72)])
+@pytest.mark.parametrize("column", [False, True])
+def test_linear_against_the_formula(sp, dtype, rows, M, N, column):
+    x, w, b, dy = _randn((rows, M), dtype, 1, 2.0), _randn((N, M), dtype, 2, 0.1), _randn((N,), dtype, 3), _randn((rows, N), dtype, 4)
+    p = None
+    values = _eight(x.double())[2]
+    if column:   # a checkpoint of the caller's, which stands for something else than x
+        other = _randn((rows, M), dtype, 5)
+        packed = sp.pack8(other)
+        p = sp.Packed8(packed.codes, packed.exponents, M, _randn((M,), dtype, 6))
+        values = _eight(other.double())[2] * p.weight.double()
+    leaves = [t.requires_grad_() for t in (x, w, b)]
+    y = sp.linear8(*leaves, checkpoint=p)
+    assert torch.equal(y, torch.nn.functional.linear(x, w, b))
+    dx, dw, db = torch.autograd.grad(y, leaves, dy, retain_graph=True)
+    assert torch.equal(dx, torch.mm(dy, w))
+    want = torch.matmul(dy.double().t(), values)
+    _near(dw, want, _weight_tolerance(dy, values, want, dtype, rows, 3 if dtype == torch.float32 else 1) + U * want.abs())
+    want = dy.double().sum(0)
+    _near(db, want, half(dtype) * want.abs() + (rows + 32) * U * dy.double().abs().sum(0))
+    again = torch.autograd.grad(y, leaves, dy, retain_graph=True)
+    assert all(torch.equal(a, c) for a, c in zip((dx, dw, db), again))   # the same bits every time
+    alone, = torch.autograd.grad(y, [w], dy, retain_graph=True)
+    assert torch.equal(alone, dw)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_linear_is_more_exact_than_its_bound(sp, dtype):
+    """On ordinary data the sums' roundings cancel: a few units beside the 8 bits."""
+    x, w, dy = _randn((8192, 256), dtype, 1), _randn((384, 256), dtype, 2).requires_grad_(), _randn((8192, 384), dtype, 3)
+    dw, = torch.autograd.grad(sp.linear8(x, w), w, dy)
+    want = torch.matmul(dy.double().t(), _eight(x.double())[2])
+    # 8192 roundings of partial sums of standard deviation sqrt(k), in slices: far below 16 u of the whole's
+    assert (dw.double() - want).norm() <= (half(dtype) + 16 * U) * want.norm()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_linear_of_what_is_not_finite(sp, dtype):
+    """A group that is not finite spoils its 64 columns of dW and nothing else; an infinite gradient its row, as infinities where it meets numbers."""
+    x, w, dy = _randn((200, 192), dtype, 1), _randn((64, 192), dtype, 2).requires_grad_(), _randn((200, 64), dtype, 3)
+    clean, = torch.autograd.grad(sp.linear8(x, w), w, dy)
+    y = x.clone()
+    y[77, 70] = math.inf
+    dw, = torch.autograd.grad(sp.linear8(y, w), w, dy)
+    assert torch.isnan(dw[:, 64:128]).all() and torch.equal(dw[:, :64], clean[:, :64]) and torch.equal(dw[:, 128:], clean[:, 128:])
+    g = dy.clone()
+    x[5] = 1.0   # no code is 0 where the infinity meets it
+    clean, = torch.autograd.grad(sp.linear8(x, w), w, dy)
+    g[5, 9] = math.inf
+    dw, = torch.autograd.grad(sp.linear8(x, w), w, g)
+    assert (dw[9] == math.inf).all() and torch.equal(dw[:9], clean[:9]) and torch.equal(dw[10:], clean[10:])
+    g[5, 9] = math.nan
+    dw, = torch.autograd.grad(sp.linear8(x, w), w, g)
+    assert torch.isnan(dw[9]).all() and torch.equal(dw[10:], clean[10:])
+
+
+def test_linear_of_large_and_small_gradients_in_fp32(sp):
+    """The three parts of an fp32 number carry all of it, from subnormal parts up to the largest number."""
+    x = torch.zeros((64, 64), device="cuda")
+    x.fill_diagonal_(1.0)
+    w = torch.zeros((8, 64), device="cuda", requires_grad=True)
+    g = torch.randn((64, 8), generator=torch.Generator("cuda").manual_seed(1), device="cuda")
+    g *= 2.0 ** torch.linspace(-90, 120, 64, device="cuda")[:, None].round()
+    g[0, 0], g[1, 1], g[2, 2] = torch.finfo(torch.float32).max, -torch.finfo(torch.float32).max, 0.0
+    dw, = torch.autograd.grad(sp.linear8(x, w), w, g)
+    assert torch.equal(dw, g.t())   # each sum has one term: exact
+
+
+def test_linear_asked_for_some_gradients_only(sp):
+    x, w, b, dy = [_randn(s, torch.float32, i) for i, s in enumerate([(4, 5, 70), (24, 70), (24,), (4, 5, 24)])]
+    full = [t.clone().requires_grad_() for t in (x, w, b)]
+    dx, dw, db = torch.autograd.grad(sp.linear8(*full), full, dy)
+    assert dx.shape == x.shape
+    for needs in ((0,), (1,), (2,), (0, 2), (1, 2)):
+        leaves = [t.clone().requires_grad_(i in needs) for i, t in enumerate((x, w, b))]
+        got = torch.autograd.grad(sp.linear8(*leaves), [leaves[i] for i in needs], dy)
+        for i, v in zip(needs, got):
+            assert torch.allclose(v, (dx, dw, db)[i], rtol=0, atol=float(20 * 2 * U * dy.abs().sum()))   # (the bias' alone by another sum)
+    with torch.no_grad():
+        assert torch.equal(sp.linear8(*full), torch.nn.functional.linear(x, w, b))
+    empty = torch.zeros((0, 70), device="cuda", requires_grad=True)
+    y = sp.linear8(empty, full[1], full[2])
+    dx, dw, db = torch.autograd.grad(y, [empty, full[1], full[2]], torch.zeros_like(y))
+    assert y.shape == (0, 24) and dx.shape == (0, 70) and not dw.any() and not db.any()
+
+
+def test_linear_past_32_bits(sp):
+    rows, M = 2 ** 20 + 2 ** 10, 2048   # 2^31 codes and more; dY as many elements
+    x = torch.zeros((rows, M), dtype=torch.bfloat16, device="cuda")
+    x[-3:] = _randn((3, M), torch.bfloat16, 1)
+    x[:1000:7] = 1.0
+    w = torch.zeros((40, M), dtype=torch.bfloat16, device="cuda", requires_grad=True)
+    dy = torch.zeros((rows, 40), dtype=torch.bfloat16, device="cuda")
+    dy[-3:], dy[:1000] = _randn((3, 40), torch.bfloat16, 2), _randn((1000, 40), torch.bfloat16, 3)
+    dw, = torch.autograd.grad(sp.linear8(x, w), w, dy)
+    some = torch.cat([torch.arange(1000), torch.arange(rows - 3, rows)]).cuda()
+    values = _eight(x[some].double())[2]
+    want = torch.matmul(dy[some].double().t(), values)
+    _near(dw, want, _weight_tolerance(dy[some], values, want, torch.bfloat16, 1003))
+
+
+# ------------------------------------------------------------------------------------------------
+# all of them
+# ------------------------------------------------------------------------------------------------
+def _mask(nb, seed):
+    g = torch.Generator().manual_seed(seed)
+    m = torch.rand((nb, nb), generator=g) < 0.5
+    return m | torch.eye(nb, dtype=torch.bool)
+
+
+def _pattern(sp, mask, block):
+    nb = mask.shape[0]
+    rows, cols = np.nonzero(mask.numpy())
+    order = np.lexsort((rows, cols))
+    ints = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()
+    ptr = lambda a: ints(np.concatenate([[0], np.cumsum(np.bincount(a, minlength=nb))]))
+    return sp.Pattern(nb * block, block, mask.to(torch.uint8).cuda(), ptr(rows), ints(cols), ptr(cols), ints(rows[order]), ints(order), ints([rows.size]),
+                      torch.zeros((nb, nb), dtype=torch.int64, device="cuda"), int(rows.size))
+
+
+class _Plain(torch.autograd.Function):
+    """x w^T with the weight's gradient from other values than x."""
+
+    @staticmethod
+    def forward(ctx, x, w, kept):
+        ctx.save_for_backward(w, kept)
+        return x @ w.t()
+
+    @staticmethod
+    def backward(ctx, g):
+        w, kept = ctx.saved_tensors
+        return g @ w, g.flatten(0, 1).t() @ kept.flatten(0, 1), None
+
+
+class _PlainNorm(torch.autograd.Function):
+    """The norm of s with its gradient from the normalised row in 8 bits."""
+
+    @staticmethod
+    def forward(ctx, s, w, eps, eight):
+        rstd = 1 / torch.sqrt(s.square().mean(-1, keepdim=True) + eps)
+        ctx.save_for_backward(_eight(s * rstd)[2] if eight else s * rstd, w, rstd)
+        return s * rstd * w
+
+    @staticmethod
+    def backward(ctx, dy):
+        z, w, rstd = ctx.saved_tensors
+        g = dy * w
+        return rstd * (g - z * (g * z).mean(-1, keepdim=True)), (dy * z).flatten(0, 1).sum(0), None, None
+
+
+def _plain_layer(E, residual, parameters, kept, axes, positions, heads, eight):
+    """The sub-layer in 64 bits, on leaves of its own."""
+    wn, wqkv, wo = parameters
+    B, L, D = E.shape
+    s = E + residual
+    X = _PlainNorm.apply(s, wn, 1e-6, eight)
+    z = s.detach() / torch.sqrt(s.detach().square().mean(-1, keepdim=True) + 1e-6)
+    qkv = _Plain.apply(X, wqkv, _eight(z)[2] * wn.detach() if eight else X.detach()).view(B, L, 3, heads, 64).permute(2, 0, 3, 1, 4)
+    angle = _angles(axes, positions)
+    c, n = angle.cos(), angle.sin()
+    turned = [torch.cat([t[..., :32] * c - t[..., 32:] * n, t[..., 32:] * c + t[..., :32] * n], -1) for t in (qkv[0], qkv[1])]
+    P = torch.softmax((turned[0] @ turned[1].transpose(-1, -2).contiguous() / 8).masked_fill(~kept, -math.inf), -1)
+    S = (P @ qkv[2]).transpose(1, 2).reshape(B, L, D)
+    return S @ wo.t(), s
+
+
+@pytest.mark.parametrize("dtype,block", [(torch.float32, 16), (torch.bfloat16, 16), (torch.bfloat16, 32), (torch.bfloat16, 64)])
+@pytest.mark.parametrize("eight", [False, True])
+def test_two_sub_layers_that_hand_on_their_residual(sp, dtype, block, eight):
+    B, L, heads = 2, 192, 2
+    D = 64 * heads
+    axes = sp.rotary_axes(64, (16, 16), ladder="own", device="cuda")
+    i = torch.arange(L, device="cuda")
+    positions = torch.stack([i // 14, i % 14])
+    mask = _mask(L // block, 1)
+    pattern, kept = _pattern(sp, mask, block), mask.repeat_interleave(block, 0).repeat_interleave(block, 1).cuda()
+    torch.manual_seed(3)
+    layers = [sp.SparseMHA(D, heads, norm="rms", rotary=axes, eight_bit=eight, device="cuda", dtype=dtype) for _ in range(2)]
+    E, R, gb, gs = [_randn((B, L, D), dtype, k) for k in range(4)]
+
+    def run(E, R, parameters, layer):
+        for k in range(2):
+            E, R = layer(k, E, R, parameters)
+        return E, R
+    leaves = [E.clone().requires_grad_(), R.clone().requires_grad_()]
+    parameters = [p for m in layers for p in m.parameters()]
+    out = run(*leaves, parameters, lambda k, e, r, _: layers[k](e, pattern, positions=positions, residual=r))
+    got = list(out) + list(torch.autograd.grad(out, leaves + parameters, [gb, gs]))
+    wide = [t.detach().double().requires_grad_() for t in leaves + parameters]
+    out = run(*wide[:2], wide[2:], lambda k, e, r, p: _plain_layer(e, r, p[3 * k:3 * k + 3], kept, axes, positions, heads, eight))
+    want = list(out) + list(torch.autograd.grad(out, wide, [gb.double(), gs.double()]))
+    # fp32: some tens of operations deep, sums of up to 384.  bf16: about ten rounded tensors on the way, 2^-9 each on average.  With 8 bits the second
+    # layer's rows differ a little between the two sides, so that some codes are their neighbours: fp32 then has 2^-7 of a few elements in 10^5.
+    tol = {torch.float32: 2e-4 if eight else 1e-5, torch.bfloat16: 2e-2}[dtype]
+    for a, b in zip(got, want):
+        assert (a.double() - b).norm() <= tol * b.norm()
+
+
+def test_sub_layer_is_the_same_with_its_residual_added_before(sp):
+    """One axis counts from 0; without a residual the stream is added at the end; layer norm takes 8 bits and positions too."""
+    pattern = _pattern(sp, _mask(4, 2), 32)
+    for norm in ("rms", "layer"):
+        m = sp.SparseMHA(128, 2, bias=True, norm=norm, rotary=sp.rotary_axes(64, (32,)), eight_bit=True, device="cuda", dtype=torch.bfloat16)
+        E, g = _randn((2, 128, 128), torch.bfloat16, 1).requires_grad_(), _randn((2, 128, 128), torch.bfloat16, 2)
+        positions = torch.arange(128, device="cuda").expand(1, 2, 128)
+        y = m(E, pattern)
+        assert torch.equal(y, m(E, pattern, positions=positions))
+        grads = torch.autograd.grad(y, [E, *m.parameters()], g)
+        if norm == "layer":
+            with pytest.raises(ValueError):
+                m(E, pattern, residual=E)
+            continue
+        zero = torch.zeros_like(E)
+        branch, stream = m(E, pattern, residual=zero)
+        assert torch.equal(stream, E) and torch.equal(branch + stream, y)
+        other = torch.autograd.grad(branch + stream, [E, *m.parameters()], g)
+        assert all(torch.equal(a, b) for a, b in zip(grads, other))
+        m.w_qkv.register_forward_hook(lambda *a: None)   # a watched projection packs its own input
+        watched = torch.autograd.grad(m(E, pattern), [E, *m.parameters()], g)
+        assert all((a.double() - b.double()).norm() <= 2e-2 * b.double().norm() for a, b in zip(watched, grads))
+    m = sp.SparseMHA(128, 2, norm="rms", rotary=sp.rotary_axes(64, (16, 16)), device="cuda", dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        m(E, pattern)
+
+
+def test_what_the_sub_layer_keeps(sp):
+    """The norm's input and output, 4 bytes an element in bf16, are one byte and a little."""
+    pattern = _pattern(sp, _mask(8, 2), 64)
+    kept = {}
+    for eight in (False, True):
+        m = sp.SparseMHA(512, 8, norm="rms", eight_bit=eight, device="cuda", dtype=torch.bfloat16)
+        E, R = [_randn((8, 512, 512), torch.bfloat16, k).requires_grad_() for k in range(2)]
+        m(E, pattern, residual=R)[0].sum().backward()
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated()
+        out, stream = m(E, pattern, residual=R)
+        del stream
+        kept[eight] = (torch.cuda.memory_allocated() - before) / E.numel()
+        del out
+    assert 4 - 1.1 < kept[False] - kept[True] < 4 - 0.9
+
+
+# ------------------------------------------------------------------------------------------------
+# graphs, streams, devices, what is refused
+# ------------------------------------------------------------------------------------------------
+def _steps(sp, dtype):
+    axes = sp.rotary_axes(64, (8, 24), device="cuda")
+    pos = torch.randint(0, 999, (2, 75), device="cuda")
+
+    def inputs(seed):
+        shapes = [(2, 6, 75, 64), (300, 200), (200,), (300, 200), (72, 200), (72,), (300, 72)]
+        return [_randn(s, dtype, seed + k).requires_grad_(k < 6) for k, s in enumerate(shapes)]
+
+    def step(x, a, w, r, W, b, g):
+        y = sp.rotary(x, axes, pos, 4)
+        n, h, p = sp.rms_norm(a, w, r, checkpoint=True)
+        z = sp.linear8(n, W, b, checkpoint=p)
+        t = sp.linear8(a, W, b)
+        with torch.no_grad():
+            q, _ = sp.rms_norm8(a, w, r)
+            v = sp.unpack8(q)
+        return [y, n, h, z, t, v, *torch.autograd.grad([y, z, h, t], [x, a, w, r, W, b], [y.detach(), g, a.detach(), g])]
+    return inputs, step
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_graphs_and_streams(sp, dtype):
+    """Two captured steps replayed in turn with eager work and new contents between them; another stream, and two at once."""
+    inputs, step = _steps(sp, dtype)
+    sets = [inputs(10), inputs(50)]
+    for s in sets:
+        step(*s)
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for s in sets:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = step(*s)
+        graphs.append(g)
+        outs.append(out)
+    same = lambda a, b: all(torch.equal(x, y) for x, y in zip(a, b))
+    near = lambda a, b: all((x.double() - y.double()).norm() <= 1e-2 * y.double().norm() + 1e-30 for x, y in zip(a, b))
+    for i in range(4):
+        for s, fresh in zip(sets, (inputs(100 + i), inputs(200 + i))):
+            with torch.no_grad():
+                for t, f in zip(s, fresh):
+                    t.copy_(f)
+        wants = [step(*s) for s in sets]
+        for g in graphs:
+            g.replay()
+        for out, want in zip(outs, wants):   # (a library's product may be another one under capture: what has one in it is near, the rest the same)
+            assert near(out, want) and same(out[:3], want[:3]) and torch.equal(out[5], want[5]) and torch.equal(out[6], want[6]), i
+        torch.cuda.synchronize()
+    del outs, graphs
+    wants = [step(*s) for s in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    got = []
+    for stream, s in zip(streams, sets):
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):
+            got.append([step(*s) for _ in range(3)][-1])
+    for stream in streams:
+        torch.cuda.current_stream().wait_stream(stream)
+    assert all(same(a, b) for a, b in zip(got, wants))
+
+
+def test_calls_that_are_refused(sp):
+    x, w, W = _randn((4, 64), torch.float32, 1), _randn((64,), torch.float32, 2), _randn((8, 64), torch.float32, 3)
+    h4, axes = x.view(1, 2, 2, 64), sp.rotary_axes(64, (16, 16), device="cuda")
+    pos = torch.zeros((2, 2), dtype=torch.int64, device="cuda")
+    sp.rotary(h4, axes, pos)
+    host = sp.rotary_axes(64, (16, 16))
+    p = sp.pack8(x)
+    odd = torch.empty(4 * 64 + 8, dtype=torch.int8, device="cuda")[8:].view(4, 64)
+    calls = [
+        lambda: sp.rotary(x, axes, pos), lambda: sp.rotary(h4.half(), axes, pos), lambda: sp.rotary(h4, axes, pos[:1]), lambda: sp.rotary(h4, axes, pos[:, :1]),
+        lambda: sp.rotary(h4, axes, pos[0]), lambda: sp.rotary(h4, axes, pos.float()), lambda: sp.rotary(h4, axes, pos, 3), lambda: sp.rotary(h4, axes, pos, -1),
+        lambda: sp.rotary(h4, axes, pos.cpu()), lambda: sp.rotary(h4, host, pos), lambda: sp.rotary(h4[..., :32], axes, pos),
+        lambda: sp.rotary(h4, axes, pos[:, None].expand(2, 3, 2)),
+        lambda: sp.pack8(x.half()), lambda: sp.pack8(x.cpu()), lambda: sp.pack8(x[0, 0]), lambda: sp.pack8(x[:, :0]), lambda: sp.pack8(x.int()),
+        lambda: sp.pack8(torch.zeros((1, 2 ** 20 + 1), device="cuda")),
+        lambda: sp.unpack8(p, torch.float16), lambda: sp.unpack8(sp.Packed8(p.codes.t().contiguous().t(), p.exponents, 64)),
+        lambda: sp.unpack8(sp.Packed8(p.codes, p.exponents.cpu(), 64)), lambda: sp.unpack8(sp.Packed8(p.codes, p.exponents, 64, w.half())),
+        lambda: sp.unpack8(sp.Packed8(p.codes, p.exponents, 64, w.cpu())),
+        lambda: sp.unpack8(sp.Packed8(odd, p.exponents, 64)) if odd.data_ptr() % 16 else sp.pack8(x.half()),
+        lambda: sp.rms_norm(x, w[:63]), lambda: sp.rms_norm(x, w.bfloat16()), lambda: sp.rms_norm(x, w, x[:3]), lambda: sp.rms_norm(x, w, x.bfloat16()),
+        lambda: sp.rms_norm(x, w, x.cpu()), lambda: sp.rms_norm(x, w, eps=-1.0), lambda: sp.rms_norm(x, w, eps=math.nan), lambda: sp.rms_norm(x.half(), w.half()),
+        lambda: sp.rms_norm(torch.zeros((1, 16385), device="cuda"), torch.zeros(16385, device="cuda")), lambda: sp.rms_norm(x, w[None]),
+        lambda: sp.rms_norm8(x.clone().requires_grad_(), w), lambda: sp.rms_norm8(x, w.clone().requires_grad_()), lambda: sp.rms_norm8(x, w, x.clone().requires_grad_()),
+        lambda: sp.linear8(x, W[:, :63]), lambda: sp.linear8(x, W.bfloat16()), lambda: sp.linear8(x, W, w), lambda: sp.linear8(x.half(), W.half()),
+        lambda: sp.linear8(x, W, W[:, 0].bfloat16()), lambda: sp.linear8(x, W.cpu()), lambda: sp.linear8(x, W, checkpoint=sp.pack8(x[:3])),
+        lambda: sp.linear8(x, W, checkpoint=sp.Packed8(p.codes, p.exponents, 64, w.bfloat16())), lambda: sp.linear8(x, W, checkpoint=sp.pack8(x[:, :63])),
+        lambda: sp.linear8(x, w), lambda: sp.linear8(x, W, checkpoint=sp.Packed8(odd, p.exponents, 64)) if odd.data_ptr() % 16 else sp.pack8(x.half()),
+    ]
+    for i, call in enumerate(calls):
+        with pytest.raises(ValueError):
+            call()
+            print("call %d was taken" % i)
+
+
+def test_gradients_that_are_refused(sp):
+    inputs, _ = _steps(sp, torch.float32)
+    x, a, w, r, W, b, g = inputs(1)
+    axes = sp.rotary_axes(64, (32,), device="cuda")
+    pos = torch.arange(75, device="cuda")[None].clone()
+    for y, leaf in ((sp.rotary(x, axes, pos), x), (sp.rms_norm(a, w, r)[0], a), (sp.linear8(a, W, b), W)):
+        with pytest.raises(NotImplementedError):
+            torch.autograd.grad(y.sum(), leaf, create_graph=True)
+    y = sp.rotary(x, axes, pos)
+    pos += 1
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        torch.autograd.grad(y.sum(), x)
+    y = sp.rotary(x, axes, pos)
+    axes.turns.add_(0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        torch.autograd.grad(y.sum(), x)
+    for checkpoint in (False, True):
+        y, h, p = sp.rms_norm(a, w, r, checkpoint=checkpoint)
+        with torch.no_grad():
+            (p.codes if checkpoint else h).add_(1)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            torch.autograd.grad(y.sum(), a)
+    n, h, p = sp.rms_norm(a, w, r, checkpoint=True)
+    y = sp.linear8(n.detach(), W, b, checkpoint=p)
+    with torch.no_grad():
+        w.mul_(2)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        torch.autograd.grad(y.sum(), W)
+    import torch.autograd.forward_ad as fwd
+    with fwd.dual_level():
+        d = lambda t: fwd.make_dual(t.detach(), torch.ones_like(t))
+        for call in (lambda: sp.rotary(d(x), axes, pos), lambda: sp.rms_norm(d(a), w), lambda: sp.rms_norm(a, d(w)), lambda: sp.linear8(a, d(W)), lambda: sp.pack8(d(a))):
+            with pytest.raises(NotImplementedError):
+                call()
+    with pytest.raises((NotImplementedError, RuntimeError)):
+        torch.func.vmap(sp.pack8)(a)
+
+
+def test_saved_tensors_are_looked_at(sp):
+    """Hooks that hand back a tensor of another size, type or device are refused before a kernel has its address; those that restore what was saved are fine."""
+    inputs, step = _steps(sp, torch.float32)
+    s = inputs(1)
+    want = step(*s)
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t.cpu(), lambda t: t.cuda()):
+        got = step(*s)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    x, a, w, r, W, b, g = s
+    axes = sp.rotary_axes(64, (32,), device="cuda")
+    pos = torch.arange(75, device="cuda")[None]
+    calls = [lambda: (sp.rotary(x, axes, pos), x), lambda: (sp.rms_norm(a, w, r)[0], a), lambda: (sp.rms_norm(a, w, r, checkpoint=True)[0], a),
+             lambda: (sp.linear8(a, W, b), W)]
+    for change in (lambda t: t.cpu(), lambda t: t.flatten()[:1], lambda t: t.double(), lambda t: torch.zeros(2, device="cuda")):
+        for call in calls:
+            with torch.autograd.graph.saved_tensors_hooks(lambda t: t, change):
+                y, leaf = call()
+                with pytest.raises(ValueError):
+                    torch.autograd.grad(y.sum(), leaf)
+
+
+def test_autocast_leaves_types_as_they_are(sp):
+    x, w, W, b = [_randn(s, torch.float32, k).requires_grad_() for k, s in enumerate([(9, 64), (64,), (8, 64), (8,)])]
+    with torch.autocast("cuda", dtype=torch.bfloat16):
+        y, _, p = sp.rms_norm(x, w, checkpoint=True)
+        z = sp.linear8(y, W, b, checkpoint=p)
+        grads = torch.autograd.grad(z.sum(), [x, w, W, b])
+    assert z.dtype == torch.float32 and all(g.dtype == torch.float32 for g in grads)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_entries_of_the_c_abi(sp, dtype):
+    """The ctypes wrappers, against the front end."""
+    code = sp.SPION_F32 if dtype == torch.float32 else sp.SPION_BF16
+    rows, D, N = 70, 130, 20
+    x, r, w, dy, dh = [_randn(s, dtype, k) for k, s in enumerate([(rows, D), (rows, D), (D,), (rows, D), (rows, D)])]
+    new = lambda *s, t=dtype: torch.empty(s, dtype=t, device="cuda")
+    y, h, rstd, codes, exponents = new(rows, D), new(rows, D), new(rows, t=torch.float32), new(rows, 192, t=torch.int8), new(rows, 3, t=torch.uint8)
+    sp.spion_rms_norm(x, r, w, y, h, rstd, codes, exponents, rows, D, EPS, code)
+    leaves = [t.clone().requires_grad_() for t in (x, w, r)]
+    y0, h0, p0 = sp.rms_norm(*leaves, EPS, checkpoint=True)
+    assert torch.equal(y, y0) and torch.equal(h, h0) and torch.equal(codes, p0.codes) and torch.equal(exponents, p0.exponents)
+    dx, dw = new(rows, D), new(D)
+    ws = new(sp.spion_rms_norm_workspace_bytes(rows, D), t=torch.uint8)
+    sp.spion_rms_norm_grad(dy, dh, None, codes, exponents, w, rstd, dx, dw, rows, D, code, ws)
+    dx0, dw0 = torch.autograd.grad([y0, h0], leaves[:2], [dy, dh])
+    assert torch.equal(dx, dx0) and torch.equal(dw, dw0)
+    sp.spion_rms_norm_grad(dy, None, h, None, None, w, rstd, dx, None, rows, D, code)   # from h, dw not wanted
+    sp.spion_rms_norm(x, r, w, None, None, None, codes, exponents, rows, D, EPS, code, sp.SPION_NORM_CODES_OF_Y)
+    p8, _ = sp.rms_norm8(x, w, r, EPS)
+    assert torch.equal(codes, p8.codes) and torch.equal(exponents, p8.exponents)
+    sp.spion_pack_eight(x, codes, exponents, rows, D, code)
+    p = sp.pack8(x)
+    assert torch.equal(codes, p.codes) and torch.equal(exponents, p.exponents)
+    sp.spion_unpack_eight(codes, exponents, w, y, rows, D, code)
+    assert torch.equal(y, sp.unpack8(sp.Packed8(codes, exponents, D, w), dtype))
+    g, dW, db = _randn((rows, N), dtype, 9), new(N, D), new(N)
+    ws = new(sp.spion_weight_grad_eight_workspace_bytes(rows, N, D), t=torch.uint8)
+    sp.spion_weight_grad_eight(g, codes, exponents, w, dW, db, rows, N, D, code, ws)
+    W, b = new(N, D).zero_().requires_grad_(), new(N).zero_().requires_grad_()
+    z = sp.linear8(x, W, b, checkpoint=sp.Packed8(codes, exponents, D, w))
+    dW0, db0 = torch.autograd.grad(z, [W, b], g)
+    assert torch.equal(dW, dW0) and torch.equal(db, db0)
+    axes, q = sp.rotary_axes(64, (16, 16), device="cuda"), _randn((2, 3, 5, 64), dtype, 1)
+    pos, out = torch.randint(0, 100, (2, 5), dtype=torch.int32, device="cuda"), new(2, 3, 5, 64)
+    sp.spion_rotary(q, out, axes.turns, axes.axis_of, pos, 2, 3, 5, 64, 2, 2, code, (960, 320, 64), (960, 320, 64), (5, 0, 1))
+    assert torch.equal(out, sp.rotary(q, axes, pos, 2))
