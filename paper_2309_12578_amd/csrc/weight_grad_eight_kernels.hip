@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "attn_bf16_tiles.h"
 #include "attn_common.h"
@@ -17,11 +18,19 @@ namespace spion {
 
 namespace {
 
-constexpr int kGradGroups = 384;
-constexpr int kGradMinRows = 128;
-constexpr int kTile = 128;       // outputs of a workgroup in each direction; a wave has 64 x 64 of them
-constexpr int kStepRows = 32;    // rows of a step: one bf16 MFMA contracts over 32
-constexpr int kLd = kTile + 16;  // elements between rows in LDS
+constexpr int kStepRows = 32;   // rows of a step
+constexpr int kWaitVm6 = 0x0F76;
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// Outputs of a workgroup, [TN][TM], and how its waves share them.
+template <int TN_, int TM_, int WN_, int WM_>
+struct Tile {
+    static constexpr int TN = TN_, TM = TM_, WN = WN_, WM = WM_, threads = 64 * WN_ * WM_;
+    static constexpr int FN = TN / WN / 32, FM = TM / WM / 32;   // 32 x 32 outputs of a wave
+};
+typedef Tile<128, 128, 2, 2> Small;
+typedef Tile<256, 128, 2, 2> Wide;    // bf16: two workgroups a compute unit
+typedef Tile<256, 256, 4, 2> Large;   // fp32: one
 
 template <typename T>
 struct Planes {
@@ -40,213 +49,458 @@ __device__ __forceinline__ void three_parts(float v, bf16_t& a, bf16_t& b, bf16_
     c = half(rest - top(rest));
 }
 
-template <typename T, bool WHOLE>   // WHOLE: 16-byte loads of dY, whose rows are then aligned
-__global__ __launch_bounds__(256) void weight_grad_eight_kernel(const T* __restrict__ dY, const signed char* __restrict__ codes,
-                                                                const uint8_t* __restrict__ exponents, float* __restrict__ partial,
-                                                                float* __restrict__ bias_partial, int rows, int N, int M, int slices, int slice_rows,
-                                                                int tiles_n, int tiles_m) {
-    constexpr int PLANES = Planes<T>::n;
-    __shared__ __attribute__((aligned(16))) bf16_t ys[2][PLANES][kStepRows * kLd], xs[2][kStepRows * kLd];
-    const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
+// Rows in LDS are 2 TN or 2 TM bytes long without padding; the 16-byte slots of a row are permuted by its number, so that the four rows of 64 bytes that half a
+// wave fetches with a transposing read are on different banks.
+__device__ __forceinline__ int slot_of(int row, int chunk) { return chunk ^ ((row & 3) << 2); }
+
+// Where a lane's part of a transposing read is: rows 8 j + 4 (lane / 32) + .., columns 32 q + 16 (lane / 16 % 2) + .. of a matrix of W columns; lane l receives column
+// 32 q + l % 32 of four rows.
+template <int W>
+__device__ __forceinline__ int read_offset(int lane, int q) {
+    const int r = lane & 15, row = 4 * (lane >> 5) + (r >> 2);
+    return row * W + slot_of(row, 4 * q + 2 * ((lane >> 4) & 1) + ((r & 3) >> 1)) * 8 + 4 * (r & 1);
+}
+
+// Rows `first` to `end` of a matrix with rows of `row` bytes, fewer than 2^31 bytes; what a load asks for beyond them comes as zeros.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_between(const void* p, int first, int end, size_t row) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(p)) + (size_t)first * row, (short)0, (int)((end - first) * row), 0x00027000);
+}
+// Into consecutive LDS: 16 bytes a lane from byte `off` on, or one byte, which becomes a word.
+__device__ __forceinline__ void load_rows(__amdgpu_buffer_rsrc_t from, unsigned off, void* to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void_ptr)to, 16, off, 0, 0, 0);
+}
+__device__ __forceinline__ void load_bytes(__amdgpu_buffer_rsrc_t from, unsigned off, void* to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void_ptr)to, 1, off, 0, 0, 0);
+}
+
+// fp32 sums of products.  A step brings 32 rows of dY and of the codes, and has one barrier.  Codes become bf16 in LDS a step before they are multiplied.
+// bf16 and WHOLE (rows of dY aligned to 16 bytes): dY goes from memory straight into LDS, two steps ahead; codes and exponents too, three steps ahead, each lane's
+// to where it takes them from again.  (All by the same instruction, so that the counts that are waited for do not depend on how the compiler orders loads.)  Rows
+// behind the last come as zeros, codes and scales as well, by the range of the loads.
+// Else through registers, requested two steps ahead.
+template <typename T, typename S, bool WHOLE>
+__global__ __launch_bounds__(S::threads, 2) void weight_grad_eight_kernel(
+    const T* __restrict__ dY, const signed char* __restrict__ codes, const uint8_t* __restrict__ exponents, const T* __restrict__ weight, T* __restrict__ dW,
+    float* __restrict__ partial, float* __restrict__ bias_partial, int rows, int N, int M, int slices, int slice_rows, int tiles_n, int tiles_m) {
+    constexpr int PLANES = Planes<T>::n, TN = S::TN, TM = S::TM, FN = S::FN, FM = S::FM, WAVES = S::threads / 64;
+    constexpr bool ASYNC = WHOLE && PLANES == 1;
+    struct Y {
+        bf16_t v[PLANES][kStepRows * TN];
+    };
+    struct X {
+        bf16_t v[kStepRows * TM];
+    };
+    struct Raw {
+        uint4 codes[S::threads];
+        int exponents[S::threads];
+    };
+    // objects of their own, so that the compiler can tell a read of one stage from a load in flight into another
+    __shared__ __attribute__((aligned(1024))) Y ys0, ys1;
+    __shared__ __attribute__((aligned(1024))) X xs0, xs1;
+    __shared__ __attribute__((aligned(1024))) std::conditional_t<ASYNC, Y, char> ys2;
+    __shared__ __attribute__((aligned(1024))) std::conditional_t<ASYNC, Raw, char> raw0, raw1, raw2;
+    const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int pitch = (int)eight_pitch(M);
-    // the tiles of a slice on one XCD: they read the same rows
-    const int tiles = tiles_n * tiles_m, l = blockIdx.x >> 3;
-    const int slice = l / tiles * 8 + (blockIdx.x & 7), tile = l % tiles;
-    if (slice >= slices) return;
-    const int n0 = tile / tiles_m * kTile, m0 = tile % tiles_m * kTile;
+    // an XCD has slices, or a part of one, whose tiles read the same rows
+    const int tiles = tiles_n * tiles_m, item = xcd_deal(blockIdx.x, 0, gridDim.x);
+    const int slice = item / tiles, tile = item % tiles, tile_n = tile / tiles_m, tile_m = tile % tiles_m;
+    const int n0 = tile_n * TN, m0 = tile_m * TM;
     const int first = slice * slice_rows, end = min(rows, first + slice_rows);
-    const bool sums_bias = bias_partial && m0 == 0;
+    const int wave_n = wave / S::WM, wave_m = wave % S::WM;
 
-    // a thread brings 8 columns of rows row, row + 16 of dY, 16 columns of row x_row of the codes
-    const int row = tid >> 4, col = (tid & 15) * 8, x_row = tid >> 3, x_col = (tid & 7) * 16;
-    const bool has_n = n0 + col < N, has_m = m0 + x_col < pitch;
+    // dY into LDS in pieces of 1 KB
+    constexpr int Y_SLOTS = TN / 8, Y_PIECE = 64 / Y_SLOTS, Y_PIECES = kStepRows / Y_PIECE / WAVES;   // rows of a piece, pieces of a wave
+    unsigned y_off[Y_PIECES];
+#pragma unroll
+    for (int k = 0; k < Y_PIECES; ++k) {
+        const int row = (Y_PIECES * wave + k) * Y_PIECE + lane / Y_SLOTS;
+        y_off[k] = (unsigned)(row * N + n0 + slot_of(row, lane % Y_SLOTS) * 8) * (unsigned)sizeof(bf16_t);
+    }
+    // the next 32 rows, each time
+    const auto y_rows = rows_between(dY, first, end, (size_t)N * sizeof(T)), x_rows = rows_between(codes, first, end, (size_t)pitch),
+               e_rows = rows_between(exponents, first, end, (size_t)(pitch / kGroup));
+    auto own = [&]() {   // the wave's number; computed from it anew each time: kept for every stage, the addresses would not fit the scalar registers
+        int w = wave;
+        asm volatile("" : "+s"(w));
+        return w;
+    };
+    auto request_y = [&](auto& to) {
+        bf16_t* const p = to.v[0] + own() * (Y_PIECES * 512);
+#pragma unroll
+        for (int k = 0; k < Y_PIECES; ++k) {
+            load_rows(y_rows, y_off[k], p + k * 512);
+            y_off[k] += (unsigned)(kStepRows * N) * (unsigned)sizeof(T);
+        }
+    };
+    // through registers: 8 columns of every Y_ROWS-th row from y_row on; 16 columns of row x_row of the codes
+    constexpr int Y_ROWS = S::threads / Y_SLOTS, Y_TIMES = kStepRows / Y_ROWS;
+    const int y_row = tid / Y_SLOTS, y_chunk = tid % Y_SLOTS, x_row = tid / (TM / 16), x_chunk = tid % (TM / 16);
+    static_assert(Y_ROWS * Y_TIMES == kStepRows && S::threads / (TM / 16) == kStepRows && WAVES * Y_PIECES * Y_PIECE == kStepRows, "a step's pieces");
+    const bool has_m = m0 + 16 * x_chunk < pitch;
+    unsigned x_off = (unsigned)(x_row * pitch + m0 + 16 * x_chunk);
+    auto request_raw = [&](auto& to) {
+        const int w = own();
+        load_rows(x_rows, x_off, to.codes + 64 * w);
+        load_bytes(e_rows, x_off / kGroup, to.exponents + 64 * w);
+        x_off += (unsigned)(kStepRows * pitch);
+    };
+    // Codes 2 i and 2 i + 1 of 16 as bf16.  c + 128 as an unsigned byte; (c + 128) 2^k - 128 2^k is exact.
+    auto convert = [&](uint4 q, float scale, int i) {
+        const unsigned words[4] = {q.x, q.y, q.z, q.w};
+        const unsigned w = words[i / 2] ^ 0x80808080u;
+        const float a = fmaf((float)((w >> (16 * (i & 1))) & 0xffu), scale, -128.f * scale), b = fmaf((float)((w >> (16 * (i & 1) + 8)) & 0xffu), scale, -128.f * scale);
+        return __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, b), __builtin_bit_cast(unsigned, a), 0x07060302u);
+    };
+    auto put_x = [&](const unsigned (&v)[8], X& to) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            *reinterpret_cast<uint4*>(&to.v[x_row * TM + slot_of(x_row, 2 * x_chunk + k) * 8]) = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+    };
     struct Rows {
-        float y[2][8];
+        T y[Y_TIMES][8];
         uint4 x;
         int exponent;
     };
     auto request = [&](Rows& v, int at) {
+        const int n = n0 + 8 * y_chunk;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const T* const p = dY + (size_t)min(at + row + 16 * k, end - 1) * N + n0 + (has_n ? col : 0);
+        for (int k = 0; k < Y_TIMES; ++k) {
+            const T* const p = dY + (size_t)min(at + y_row + Y_ROWS * k, end - 1) * N + (n < N ? n : 0);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v.y[k][i] = WHOLE || n0 + col + i < N ? (float)p[i] : 0.f;
+            for (int i = 0; i < 8; ++i) v.y[k][i] = WHOLE || n + i < N ? p[i] : (T)0.f;
         }
         const size_t i = (size_t)min(at + x_row, end - 1);
-        const int c = m0 + (has_m ? x_col : 0);
+        const int c = has_m ? m0 + 16 * x_chunk : 0;
         v.x = *reinterpret_cast<const uint4*>(codes + i * pitch + c);
         v.exponent = exponents[i * (pitch / kGroup) + c / kGroup];
     };
-    float bias[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    auto put = [&](const Rows& v, int at, int b) {
+    auto put = [&](const Rows& v, int at, Y& to_y, X& to_x) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+        for (int k = 0; k < Y_TIMES; ++k) {
+            const int row = y_row + Y_ROWS * k;
             bf16x8 part[3];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float y = at + row + 16 * k < end ? v.y[k][i] : 0.f;
-                bias[i] += y;
+                const T y = at + row < end ? v.y[k][i] : (T)0.f;
                 if constexpr (PLANES == 3) {
                     bf16_t p, q, s;
                     three_parts(y, p, q, s);
                     part[0][i] = p, part[1][i] = q, part[2][i] = s;
                 } else {
-                    part[0][i] = (bf16_t)y;
+                    part[0][i] = y;
                 }
             }
 #pragma unroll
-            for (int p = 0; p < PLANES; ++p) *reinterpret_cast<bf16x8*>(&ys[b][p][(row + 16 * k) * kLd + col]) = part[p];
+            for (int p = 0; p < PLANES; ++p) *reinterpret_cast<bf16x8*>(&to_y.v[p][row * TN + slot_of(row, y_chunk) * 8]) = part[p];
         }
-        const bool has = at + x_row < end;
-        const float scale = eight_scale(v.exponent);
-        const unsigned words[4] = {v.x.x, v.x.y, v.x.z, v.x.w};
+        const float scale = at + x_row < end ? eight_scale(v.exponent) : 0.f;
+        unsigned x[8];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            float x[8];
-            values_of(x, Codes8{words[2 * k], words[2 * k + 1]}, scale);
-            bf16x8 q;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) q[i] = has ? (bf16_t)x[i] : (bf16_t)0.f;
-            *reinterpret_cast<bf16x8*>(&xs[b][x_row * kLd + x_col + 8 * k]) = q;
-        }
+        for (int i = 0; i < 8; ++i) x[i] = convert(v.x, scale, i);
+        put_x(x, to_x);
     };
-    const int wn = (wave >> 1) * 64, wm = (wave & 1) * 64;
-    const int tr = (4 * g + (r >> 2)) * kLd + 4 * (r & 3);   // transpose read: lane r receives column r of rows 4 g ..
-    f32x4 acc[4][4];   // [n tile][m tile]
+
+    int fy_off[FN], fx_off[FM];
 #pragma unroll
-    for (int a = 0; a < 4; ++a)
+    for (int f = 0; f < FN; ++f) fy_off[f] = read_offset<TN>(lane, wave_n * FN + f);
 #pragma unroll
-        for (int b = 0; b < 4; ++b) acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-    auto multiply = [&](int b) {
-        bf16x8 fx[4];
+    for (int f = 0; f < FM; ++f) fx_off[f] = read_offset<TM>(lane, wave_m * FM + f);
+    f32x16 acc[FN][FM];
+    float bias[FN];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const bf16_t* const x = &xs[b][tr + wm + 16 * t];
-            fx[t] = join(lds_read_tr(x), lds_read_tr(x + 16 * kLd));
-        }
+    for (int a = 0; a < FN; ++a) {
+        bias[a] = 0.f;
 #pragma unroll
-        for (int p = 0; p < PLANES; ++p) {
-            bf16x8 fy[4];
+        for (int b = 0; b < FM; ++b)
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const bf16_t* const y = &ys[b][p][tr + wn + 16 * t];
-                fy[t] = join(lds_read_tr(y), lds_read_tr(y + 16 * kLd));
-            }
+            for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
+    }
+    // operands of 16 rows
+    struct Operands {
+        bf16x8 y[FN], x[FM];
+    };
+    auto read_y = [&](Operands& o, const Y& y, int p, int k, int f) {
+        o.y[f] = join(lds_read_tr(y.v[p] + fy_off[f] + 16 * k * TN), lds_read_tr(y.v[p] + fy_off[f] + (16 * k + 8) * TN));
+    };
+    auto read_x = [&](Operands& o, const X& x, int k, int f) {
+        o.x[f] = join(lds_read_tr(x.v + fx_off[f] + 16 * k * TM), lds_read_tr(x.v + fx_off[f] + (16 * k + 8) * TM));
+    };
+    auto multiply = [&](const Operands& o, int i) {
+        const int a = i / FM, b = i % FM;
+        acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(o.y[a], o.x[b], acc[a][b], 0, 0, 0);
+    };
+    auto add_bias = [&](const Operands& o) {
 #pragma unroll
-            for (int a = 0; a < 4; ++a)
+        for (int f = 0; f < FN; ++f)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) acc[a][c] = mma_d(acc[a][c], fx[c], fy[a]);   // [m][n]
-        }
+            for (int i = 0; i < 8; ++i) bias[f] += (float)o.y[f][i];
+    };
+    // the steps' column sums of dY are shared by the workgroups and waves that have the same columns
+    const int shares = tiles_m * S::WM, share = tile_m * S::WM + wave_m;
+    const bool wants_bias = bias_partial != nullptr;
+    int turn = 0;
+    auto meet = [&]() {
+        __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
     };
     const int steps = (end - first + kStepRows - 1) / kStepRows;
-    Rows v;
-    request(v, first);
-    for (int s = 0, at = first; s < steps; ++s, at += kStepRows) {
-        put(v, at, s & 1);
-        request(v, at + kStepRows);
-        __syncthreads();   // (the stage written two steps on has been read by then)
-        multiply(s & 1);
-    }
-    float* const out = partial + (size_t)slice * N * pitch;
+    if constexpr (ASYNC) {
+        // Step s reads ys[s % 3] and xs[s % 2], makes xs[(s + 1) % 2] from raw[(s + 1) % 3], and requests what two and three steps on takes into the stages
+        // that step s - 1 has read.  Of what is in flight at its start, the loads of step s - 1 may stay there: codes and exponents of s + 2, rows of s + 1.
+        static_assert(Y_PIECES == 2 || Y_PIECES == 4, "loads of a step");
+        auto step = [&](Y& y, Y& y_free, X& x, X& x_free, Raw& raw, Raw& raw_free) {
+            __builtin_amdgcn_s_waitcnt(Y_PIECES == 2 ? kWaitVm4 : kWaitVm6);
+            meet();
+            Operands o[2];
+            const uint4 q = raw.codes[tid];
+            const int e = raw.exponents[tid];
 #pragma unroll
-    for (int a = 0; a < 4; ++a) {
-        const int n = n0 + wn + 16 * a + r;
+            for (int f = 0; f < FM; ++f) read_x(o[0], x, 0, f);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const int m = m0 + wm + 16 * c + 4 * g;
-            if (n < N && m < pitch) *reinterpret_cast<f32x4*>(out + (size_t)n * pitch + m) = acc[a][c];
+            for (int f = 0; f < FN; ++f) read_y(o[0], y, 0, 0, f);
+            request_raw(raw_free);
+            request_y(y_free);
+            const float scale = eight_scale(e);
+            unsigned next[8];
+            __builtin_amdgcn_sched_barrier(0);
+            // each of the first products with some of the second's operands and of the next step's codes beside it
+#pragma unroll
+            for (int i = 0; i < FN * FM; ++i) {
+                multiply(o[0], i);
+                if (i < FM) read_x(o[1], x, 1, i);
+                else if (i < FM + FN) read_y(o[1], y, 0, 1, i - FM);
+#pragma unroll
+                for (int k = 0; k < 8 / (FN * FM); ++k) next[i * (8 / (FN * FM)) + k] = convert(q, scale, i * (8 / (FN * FM)) + k);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            put_x(next, x_free);
+#pragma unroll
+            for (int i = 0; i < FN * FM; ++i) multiply(o[1], i);
+            if (wants_bias && turn == share) {
+                add_bias(o[0]);
+                add_bias(o[1]);
+            }
+            turn = turn + 1 == shares ? 0 : turn + 1;
+        };
+        request_raw(raw0);
+        request_raw(raw1);
+        request_y(ys0);
+        request_raw(raw2);
+        request_y(ys1);
+        __builtin_amdgcn_s_waitcnt(kWaitVm0);
+        unsigned x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = convert(raw0.codes[tid], eight_scale(raw0.exponents[tid]), i);
+        put_x(x, xs0);
+        for (int s = 0; s < steps; s += 6) {
+            step(ys0, ys2, xs0, xs1, raw1, raw0);
+            if (s + 1 >= steps) break;
+            step(ys1, ys0, xs1, xs0, raw2, raw1);
+            if (s + 2 >= steps) break;
+            step(ys2, ys1, xs0, xs1, raw0, raw2);
+            if (s + 3 >= steps) break;
+            step(ys0, ys2, xs1, xs0, raw1, raw0);
+            if (s + 4 >= steps) break;
+            step(ys1, ys0, xs0, xs1, raw2, raw1);
+            if (s + 5 >= steps) break;
+            step(ys2, ys1, xs1, xs0, raw0, raw2);
+        }
+        __builtin_amdgcn_s_waitcnt(kWaitVm0);   // what was requested for steps that are not there
+    } else {
+        Rows v;
+        auto step = [&](int s, Y& y, Y& y_free, X& x, X& x_free) {
+            const int at = first + s * kStepRows;
+            meet();
+            put(v, at + kStepRows, y_free, x_free);
+            request(v, at + 2 * kStepRows);
+            const bool sums = wants_bias && turn == share;
+#pragma unroll
+            for (int k = 0; k < kStepRows / 16; ++k) {
+                Operands o;
+#pragma unroll
+                for (int f = 0; f < FM; ++f) read_x(o, x, k, f);
+#pragma unroll
+                for (int p = 0; p < PLANES; ++p) {
+#pragma unroll
+                    for (int f = 0; f < FN; ++f) read_y(o, y, p, k, f);
+#pragma unroll
+                    for (int i = 0; i < FN * FM; ++i) multiply(o, i);
+                    if (sums) add_bias(o);
+                }
+            }
+            turn = turn + 1 == shares ? 0 : turn + 1;
+        };
+        request(v, first);
+        put(v, first, ys0, xs0);
+        request(v, first + kStepRows);
+        for (int s = 0; s < steps; s += 2) {
+            step(s, ys0, ys1, xs0, xs1);
+            if (s + 1 >= steps) break;
+            step(s + 1, ys1, ys0, xs1, xs0);
         }
     }
-    if (!sums_bias) return;
-    float(*const part)[kTile] = reinterpret_cast<float(*)[kTile]>(&xs[0][0]);   // [16][kTile]
-    __syncthreads();
+
+    // lane l has m = .. + l % 32 of rows n = .. + 8 (i / 4) + 4 (l / 32) + i % 4: whole lines
 #pragma unroll
-    for (int i = 0; i < 8; ++i) part[row][col + i] = bias[i];
-    __syncthreads();
-    if (tid < kTile && n0 + tid < N) {
-        float s = part[0][tid];
+    for (int b = 0; b < FM; ++b) {
+        const int m = m0 + (wave_m * FM + b) * 32 + (lane & 31);
+        const float column = weight && m < M ? (float)weight[m] : 1.f;
 #pragma unroll
-        for (int k = 1; k < 16; ++k) s += part[k][tid];
-        bias_partial[(size_t)slice * N + n0 + tid] = s;
+        for (int a = 0; a < FN; ++a)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int n = n0 + (wave_n * FN + a) * 32 + 8 * (i / 4) + 4 * (lane >> 5) + i % 4;
+                if (n >= N) continue;
+                if (partial) {
+                    if (m < pitch) partial[((size_t)slice * N + n) * pitch + m] = acc[a][b][i];
+                } else if (m < M) {
+                    dW[(size_t)n * M + m] = (T)(acc[a][b][i] * column);
+                }
+            }
+    }
+    if (!wants_bias) return;
+#pragma unroll
+    for (int a = 0; a < FN; ++a) {
+        const float v = bias[a] + __shfl_xor(bias[a], 32);
+        const int n = n0 + (wave_n * FN + a) * 32 + (lane & 31);
+        if (lane < 32 && n < N) bias_partial[((size_t)slice * shares + share) * N + n] = v;
     }
 }
 
-// A workgroup has 64 vectors of 4 outputs of dW (the last workgroups: of db), a wave a quarter of their slices; the quarters are added in order.
-template <typename T>
+// COLUMNS vectors of 4 outputs of dW a workgroup, each by 256 / COLUMNS threads that have a run of slices; their sums are added in order.
+// The last workgroups have 16 outputs of db each.
+template <typename T, int COLUMNS>
 __global__ __launch_bounds__(256) void weight_grad_eight_sum_kernel(const float* __restrict__ partial, const float* __restrict__ bias_partial, int slices,
-                                                                    int N, int M, const T* __restrict__ weight, T* __restrict__ dW, T* __restrict__ db,
-                                                                    unsigned groups) {
-    __shared__ float part[4][64][4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, pitch = (int)eight_pitch(M);
-    const bool bias = blockIdx.x >= groups;
-    const size_t n4 = (size_t)N * (pitch / 4), i = (size_t)(bias ? blockIdx.x - groups : blockIdx.x) * 64 + lane;
-    const int begin = wave * slices / 4, end = (wave + 1) * slices / 4;
-    float acc[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s = begin; s < end; ++s) {
-        if (bias) {
+                                                                    int bias_slices, int N, int M, const T* __restrict__ weight, T* __restrict__ dW,
+                                                                    T* __restrict__ db, unsigned groups) {
+    constexpr int RUNS = 256 / COLUMNS, BIAS_COLUMNS = 16, BIAS_RUNS = 256 / BIAS_COLUMNS, kInFlight = 8;
+    __shared__ union {
+        f32x4 part[RUNS][COLUMNS];
+        float bias[BIAS_RUNS][BIAS_COLUMNS];
+    } shared;
+    if (blockIdx.x >= groups) {
+        const int column = threadIdx.x % BIAS_COLUMNS, run = threadIdx.x / BIAS_COLUMNS, n = (int)(blockIdx.x - groups) * BIAS_COLUMNS + column;
+        const int begin = (int)((long long)run * bias_slices / BIAS_RUNS), end = (int)((long long)(run + 1) * bias_slices / BIAS_RUNS);
+        float sum = 0.f;
+        for (int s = begin; s < end; s += kInFlight) {
+            float v[kInFlight];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (4 * i + k < (size_t)N) acc[k] += bias_partial[(size_t)s * N + 4 * i + k];
-        } else if (i < n4) {
-            const f32x4 v = reinterpret_cast<const f32x4*>(partial)[s * n4 + i];
+            for (int u = 0; u < kInFlight; ++u) v[u] = bias_partial[(size_t)min(s + u, end - 1) * N + min(n, N - 1)];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) acc[k] += v[k];
+            for (int u = 0; u < kInFlight; ++u) sum += s + u < end ? v[u] : 0.f;
         }
+        shared.bias[run][column] = sum;
+        __syncthreads();
+        if (run != 0 || n >= N) return;
+#pragma unroll
+        for (int k = 1; k < BIAS_RUNS; ++k) sum += shared.bias[k][column];
+        db[n] = (T)sum;
+        return;
     }
+    const int column = threadIdx.x % COLUMNS, run = threadIdx.x / COLUMNS, pitch = (int)eight_pitch(M);
+    const size_t n4 = (size_t)N * (pitch / 4), i = (size_t)blockIdx.x * COLUMNS + column;
+    const int begin = (int)((long long)run * slices / RUNS), end = (int)((long long)(run + 1) * slices / RUNS);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    const f32x4* const p = reinterpret_cast<const f32x4*>(partial) + (i < n4 ? i : n4 - 1);
+    for (int s = begin; s < end; s += kInFlight) {
+        f32x4 v[kInFlight];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) part[wave][lane][k] = acc[k];
-    __syncthreads();
-    if (wave != 0) return;
+        for (int u = 0; u < kInFlight; ++u) v[u] = p[(size_t)min(s + u, end - 1) * n4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const float v = ((part[0][lane][k] + part[1][lane][k]) + part[2][lane][k]) + part[3][lane][k];
-        if (bias) {
-            if (4 * i + k < (size_t)N) db[4 * i + k] = (T)v;
-        } else if (i < n4) {
-            const size_t n = i / (pitch / 4);
-            const int m = (int)(i - n * (pitch / 4)) * 4 + k;
-            if (m < M) dW[n * M + m] = (T)(weight ? v * (float)weight[m] : v);
-        }
+        for (int u = 0; u < kInFlight; ++u)
+            if (s + u < end) acc += v[u];
+    }
+    if constexpr (RUNS > 1) {
+        shared.part[run][column] = acc;
+        __syncthreads();
+        if (run != 0) return;
+#pragma unroll
+        for (int k = 1; k < RUNS; ++k) acc += shared.part[k][column];
+    }
+    if (i >= n4) return;
+    const size_t n = i / (pitch / 4);
+    const int m = (int)(i - n * (pitch / 4)) * 4;
+    if (weight) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[k] *= (float)weight[min(m + k, M - 1)];
+    }
+    T* const out = dW + n * M + m;
+    if (m + 4 <= M && M % 4 == 0 && (uintptr_t)dW % (4 * sizeof(T)) == 0) {
+        store_quad<T>(out, acc);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (m + k < M) out[k] = (T)acc[k];
     }
 }
+
+constexpr int kMinRows = 128;   // of a slice
+constexpr long long kBig = 1 << 20;
+constexpr int kWant = 512;
 
 struct Plan {
-    int tiles_n, tiles_m, slices, slice_rows;
+    int side_n = 128, side_m = 128;   // of a tile
+    int tiles_n, tiles_m, slices, slice_rows, shares;
     size_t bias_at, total;   // bytes
-    Plan(int rows, int N, int M) {
-        tiles_n = (N + kTile - 1) / kTile;
-        tiles_m = (int)((eight_pitch(M) + kTile - 1) / kTile);
-        const long long most = ((long long)rows + kGradMinRows - 1) / kGradMinRows, want = kGradGroups / ((long long)tiles_n * tiles_m);
+    Plan(int rows, int N, int M, bool is_bf16, bool whole) {
+        const long long pitch = eight_pitch(M);
+        const long long outputs = (long long)N * pitch;
+        if (outputs >= kBig && rows >= 2048 && (whole || !is_bf16)) {
+            side_n = 256;
+            side_m = is_bf16 ? 128 : 256;
+        }
+        tiles_n = (N + side_n - 1) / side_n;
+        tiles_m = (int)((pitch + side_m - 1) / side_m);
+        const long long most = ((long long)rows + kMinRows - 1) / kMinRows, want = (side_m == 256 ? 256 : kWant) / ((long long)tiles_n * tiles_m);
         slices = (int)std::max<long long>(1, std::min(want, most));
         slice_rows = (int)((((long long)rows + slices - 1) / slices + kStepRows - 1) / kStepRows * kStepRows);
+        slice_rows = (int)std::min<long long>(slice_rows, (0x7fffffffll / std::max<long long>(2 * N, pitch) - 4 * kStepRows) / kStepRows * kStepRows);   // 31 bits of offset
         slices = (int)(((long long)rows + slice_rows - 1) / slice_rows);
-        bias_at = (size_t)slices * N * eight_pitch(M) * sizeof(float);
-        total = bias_at + (size_t)slices * N * sizeof(float);
+        shares = tiles_m * 2;
+        bias_at = slices > 1 ? (size_t)slices * outputs * sizeof(float) : 0;
+        total = bias_at + (size_t)slices * shares * N * sizeof(float);
     }
 };
 
 }  // namespace
 
-size_t weight_grad_eight_workspace_bytes(int rows, int N, int M) { return Plan(rows, N, M).total; }
+size_t weight_grad_eight_workspace_bytes(int rows, int N, int M) { 
+    return std::max({Plan(rows, N, M, false, true).total, Plan(rows, N, M, true, true).total, Plan(rows, N, M, true, false).total});
+}
 
 template <typename T>
 static hipError_t launch_t(const WeightGradEight& a, hipStream_t st) {
-    const Plan p(a.rows, a.N, a.M);
-    float *const partial = static_cast<float*>(a.workspace),
-                 *const bias_partial = a.db ? reinterpret_cast<float*>(static_cast<char*>(a.workspace) + p.bias_at) : nullptr;
-    const unsigned groups = (unsigned)((p.slices + 7) / 8 * 8) * (unsigned)(p.tiles_n * p.tiles_m);
-    auto launch = [&](auto kernel) {
-        kernel<<<dim3(groups), dim3(256), 0, st>>>(static_cast<const T*>(a.dY), a.codes, a.exponents, partial, bias_partial, a.rows, a.N, a.M, p.slices,
-                                                   p.slice_rows, p.tiles_n, p.tiles_m);
-    };
+    constexpr bool is_bf16 = sizeof(T) == 2;
     const bool whole = a.N % 8 == 0 && (uintptr_t)a.dY % 16 == 0;
-    whole ? launch(weight_grad_eight_kernel<T, true>) : launch(weight_grad_eight_kernel<T, false>);
+    const Plan p(a.rows, a.N, a.M, is_bf16, whole);
+    float *const partial = p.slices > 1 ? static_cast<float*>(a.workspace) : nullptr,
+                 *const bias_partial = a.db ? reinterpret_cast<float*>(static_cast<char*>(a.workspace) + p.bias_at) : nullptr;
+    T *const dW = static_cast<T*>(a.dW), *const db = static_cast<T*>(a.db);
+    const T* const weight = static_cast<const T*>(a.weight);
+    const unsigned groups = (unsigned)p.slices * (unsigned)p.tiles_n * (unsigned)p.tiles_m;
+    auto launch = [&](auto kernel, int threads) {
+        kernel<<<dim3(groups), dim3(threads), 0, st>>>(static_cast<const T*>(a.dY), a.codes, a.exponents, weight, dW, partial, bias_partial, a.rows, a.N,
+                                                       a.M, p.slices, p.slice_rows, p.tiles_n, p.tiles_m);
+    };
+    typedef std::conditional_t<is_bf16, Wide, Large> Big;
+    if (p.side_n == 256 && whole) launch(weight_grad_eight_kernel<T, Big, true>, Big::threads);
+    else if (p.side_n == 256) launch(weight_grad_eight_kernel<T, std::conditional_t<is_bf16, Small, Big>, false>, Big::threads);   // (fp32 only)
+    else whole ? launch(weight_grad_eight_kernel<T, Small, true>, Small::threads) : launch(weight_grad_eight_kernel<T, Small, false>, Small::threads);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    const unsigned sums = (unsigned)(((size_t)a.N * (eight_pitch(a.M) / 4) + 63) / 64), more = a.db ? (unsigned)((a.N + 255) / 256) : 0u;
-    weight_grad_eight_sum_kernel<T><<<dim3(sums + more), dim3(256), 0, st>>>(partial, bias_partial, p.slices, a.N, a.M, static_cast<const T*>(a.weight),
-                                                                             static_cast<T*>(a.dW), static_cast<T*>(a.db), sums);
+    if (e != hipSuccess || (!partial && !a.db)) return e;
+    const size_t quads = partial ? (size_t)a.N * (eight_pitch(a.M) / 4) : 0;
+    auto sum = [&](auto columns) {
+        constexpr int C = decltype(columns)::value;
+        const unsigned sums = (unsigned)((quads + C - 1) / C), more = a.db ? (unsigned)((a.N + 15) / 16) : 0u;
+        weight_grad_eight_sum_kernel<T, C><<<dim3(sums + more), dim3(256), 0, st>>>(partial, bias_partial, p.slices, p.slices * p.shares, a.N, a.M, weight, dW, db,
+                                                                                    sums);
+    };
+    if (p.slices >= 64) sum(std::integral_constant<int, 8>{});
+    else if (p.slices >= 16) sum(std::integral_constant<int, 32>{});
+    else sum(std::integral_constant<int, 128>{});
     return hipGetLastError();
 }
 hipError_t launch_weight_grad_eight(const WeightGradEight& a, bool is_bf16, hipStream_t st) { return is_bf16 ? launch_t<bf16_t>(a, st) : launch_t<float>(a, st); }

@@ -681,17 +681,18 @@ def test_what_the_sub_layer_keeps(sp):
     """The norm's input and output, 4 bytes an element in bf16, are one byte and a little."""
     pattern = _pattern(sp, _mask(8, 2), 64)
     kept = {}
+    asked_for = lambda: torch.cuda.memory_stats()["requested_bytes.all.current"]   # (blocks may be larger)
     for eight in (False, True):
         m = sp.SparseMHA(512, 8, norm="rms", eight_bit=eight, device="cuda", dtype=torch.bfloat16)
         E, R = [_randn((8, 512, 512), torch.bfloat16, k).requires_grad_() for k in range(2)]
         m(E, pattern, residual=R)[0].sum().backward()
         torch.cuda.synchronize()
-        before = torch.cuda.memory_allocated()
+        before = asked_for()
         out, stream = m(E, pattern, residual=R)
         del stream
-        kept[eight] = (torch.cuda.memory_allocated() - before) / E.numel()
+        kept[eight] = (asked_for() - before) / E.numel()
         del out
-    assert 4 - 1.1 < kept[False] - kept[True] < 4 - 0.9
+    assert abs(kept[False] - kept[True] - (4 - 65 / 64)) < 0.01
 
 
 # ------------------------------------------------------------------------------------------------
