@@ -15,6 +15,7 @@ namespace spion {
 
 constexpr int kGroup = 64;
 constexpr int kNotFinite = 255;
+constexpr float kMost = 3.4028234663852886e38f;   // fp32's largest number
 
 // The exponent byte that a group whose largest magnitude is `most` has.  It grows with `most`: the largest byte of a group's parts is the group's.
 // 127 * 2^-6 = 1 + 63 / 64: a mantissa beyond that takes the next power of two.
@@ -25,10 +26,14 @@ __device__ __forceinline__ int exponent_byte(float most) {
     return e < 1 ? 1 : e;
 }
 __device__ __forceinline__ int exponent_byte(double most) {
-    if (!(most <= 3.4028234663852886e38)) return kNotFinite;
+    if (!(most <= (double)kMost)) return kNotFinite;
     const unsigned long long u = __builtin_bit_cast(unsigned long long, most);
     const int e = (int)(u >> 52) - 1023 + 127 - 6 + ((u & 0xfffffffffffffull) > 0xfc00000000000ull ? 1 : 0);
     return e < 1 ? 1 : e;
+}
+// Whether a number off by up to 8 units of 2^-24 may have another exponent byte than `most`.
+__device__ __forceinline__ bool near_border(float most) {
+    return (__builtin_bit_cast(unsigned, most) & 0x7fffffu) - (0x7e0000u - 8u) <= 16u;
 }
 // The largest of eight lanes beside each other that have a group's 64 elements.
 __device__ __forceinline__ int group_exponent(int e) {
@@ -54,6 +59,25 @@ __device__ __forceinline__ Codes8 codes_of(const S (&v)[8], int exponent) {
     for (int i = 0; i < 2; ++i)
         r[i] = (c[4 * i] & 0xff) | (c[4 * i + 1] & 0xff) << 8 | (c[4 * i + 2] & 0xff) << 16 | (unsigned)c[4 * i + 3] << 24;
     return r;
+}
+// The same for numbers off by up to 4 units of 2^-24; false if one of them may have another code.  127 * 4 * 2^-24 = 2^-15 less 1/128 of it.
+__device__ __forceinline__ bool codes_of(Codes8& q, const float (&v)[8], int exponent) {
+    constexpr float kRound = 12582912.f;   // 1.5 * 2^23: a sum with it has the nearest whole number (ties to even) in its low bits
+    const float inv = eight_inverse(exponent);
+    float far = 0.f;
+    unsigned t[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float sum = fmaf(v[i], inv, kRound);   // (a product with a power of two is exact)
+        far = fmaxf(far, fabsf(fmaf(v[i], inv, -(sum - kRound))));
+        t[i] = __builtin_bit_cast(unsigned, sum);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const unsigned lo = __builtin_amdgcn_perm(t[4 * i + 1], t[4 * i], 0x0c0c0400u), hi = __builtin_amdgcn_perm(t[4 * i + 3], t[4 * i + 2], 0x0c0c0400u);
+        q[i] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+    }
+    return far < 0.5f - 0x1p-15f;
 }
 __device__ __forceinline__ void values_of(float (&v)[8], Codes8 codes, float scale) {
 #pragma unroll
