@@ -16,40 +16,74 @@ namespace spion {
 
 namespace {
 
-constexpr int kRotaryTable = 2048;   // pairs of cosine and sine a workgroup holds
+constexpr int kRotaryTable = 2048, kRotaryTokens = 128;   // pairs of cosine and sine, and tokens, that a workgroup has room for
+
+// Of an eighth of a turn at most, either way, given in 2^-64 turns: the series, whose next terms are below 2^-29 of the results there.
+__device__ __forceinline__ void sine_cosine(float turns, float& sine, float& cosine) {
+    const float t = turns * 3.4061215800098876e-19f;   // 2 pi / 2^64
+    const float q = t * t;
+    sine = fmaf(t * q, fmaf(q, fmaf(q, fmaf(q, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), t);
+    cosine = fmaf(q, fmaf(q, fmaf(q, fmaf(q, fmaf(q, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
+}
 
 template <typename T, bool NEIGHBOURS>
 __global__ __launch_bounds__(256) void rotary_kernel(const T* __restrict__ x, T* __restrict__ y, const RotaryShape s, const long long* __restrict__ turns,
                                                      const uint8_t* __restrict__ axis, const void* __restrict__ positions, int tokens) {
     __shared__ float2 table[kRotaryTable];
+    __shared__ long long place[kRotaryTokens][2];   // of the tokens in x and y
     const int pairs = s.d / 2, tid = threadIdx.x;
-    const long long first = (long long)blockIdx.x * tokens, total = (long long)s.B * s.L;
-    const int here = (int)min((long long)tokens, total - first);
-    for (int i = tid; i < here * pairs; i += 256) {
-        const int t = i / pairs, p = i - t * pairs;
-        const long long token = first + t, b = token / s.L, l = token - b * s.L;
-        const long long at = min((int)axis[p], s.axes - 1) * s.pos_axis + b * s.pos_batch + l * s.pos_token;
-        const long long pos = s.pos_bytes == 8 ? static_cast<const long long*>(positions)[at] : (long long)static_cast<const int*>(positions)[at];
-        const unsigned long long angle = (unsigned long long)pos * (unsigned long long)turns[p];
-        const unsigned long long quarter = (angle + (1ull << 61)) >> 62;
-        // in half turns, -1/4 .. 1/4
-        const float rest = (float)(long long)(angle - (quarter << 62)) * 1.0842021724855044e-19f;
-        float sine, cosine;
-        sincospif(rest, &sine, &cosine);
-        float c = quarter & 1 ? sine : cosine, n = quarter & 1 ? cosine : sine;
-        if ((quarter + 1) & 2) c = -c;
-        if (quarter & 2) n = -n;
-        table[i] = make_float2(c, s.back ? -n : n);
+    const unsigned first = blockIdx.x * (unsigned)tokens, total = (unsigned)s.B * (unsigned)s.L;   // (below 2^31)
+    const int here = (int)min((unsigned)tokens, total - first);
+    // A thread has every 256th of what follows, by numbers that are carried: no divisions.
+    {
+        const int p_step = 256 % pairs, t_step = 256 / pairs;
+        int p = tid % pairs, t = tid / pairs, known = -1;
+        unsigned b = (first + t) / (unsigned)s.L, l = first + t - b * s.L;
+        unsigned long long frequency = 0;
+        long long of_axis = 0;
+        while (t < here) {
+            if (p != known) {   // the same each time where the pairs divide the threads
+                known = p;
+                of_axis = min((int)axis[p], s.axes - 1) * s.pos_axis;
+                frequency = (unsigned long long)turns[p];
+            }
+            const long long at = of_axis + b * s.pos_batch + l * s.pos_token;
+            const long long pos = s.pos_bytes == 8 ? static_cast<const long long*>(positions)[at] : (long long)static_cast<const int*>(positions)[at];
+            const unsigned long long angle = (unsigned long long)pos * frequency;
+            const unsigned long long quarter = (angle + (1ull << 61)) >> 62;
+            float sine, cosine;
+            sine_cosine((float)(long long)(angle - (quarter << 62)), sine, cosine);
+            float c = quarter & 1 ? sine : cosine, n = quarter & 1 ? cosine : sine;
+            if ((quarter + 1) & 2) c = -c;
+            if (quarter & 2) n = -n;
+            table[t * pairs + p] = make_float2(c, s.back ? -n : n);
+            if (p == 0) {
+                place[t][0] = b * s.x_stride[0] + l * s.x_stride[2];
+                place[t][1] = b * s.y_stride[0] + l * s.y_stride[2];
+            }
+            const int was = t;
+            p += p_step;
+            t += t_step;
+            if (p >= pairs) {
+                p -= pairs;
+                ++t;
+            }
+            l += t - was;
+            if (l >= (unsigned)s.L) {
+                b = (first + t) / (unsigned)s.L;
+                l = first + t - b * s.L;
+            }
+        }
     }
     __syncthreads();
-    const int chunks = s.d / 16;   // of 8 elements, and as many half a head further on
-    const int items = here * s.N * chunks;
-    for (int i = tid; i < items; i += 256) {
-        const int c = i % chunks, rest = i / chunks;
-        const int n = s.tokens_first ? rest % s.N : rest / here, t = s.tokens_first ? rest / s.N : rest % here;
-        const long long token = first + t, b = token / s.L, l = token - b * s.L;
-        const T* const from = x + (b * s.x_stride[0] + n * s.x_stride[1] + l * s.x_stride[2]) + 8 * c;
-        T* const to = y + (b * s.y_stride[0] + n * s.y_stride[1] + l * s.y_stride[2]) + 8 * c;
+    // Items (token, head, 8 elements and as many half a head further on), in the order of memory: the elements, then heads and tokens, or tokens and heads.
+    const int chunks = s.d / 16, inner_size = s.tokens_first ? s.N : here, outer_size = s.tokens_first ? here : s.N;
+    const int c_step = 256 % chunks, inner_step = 256 / chunks % inner_size, outer_step = 256 / chunks / inner_size;
+    int c = tid % chunks, inner = tid / chunks % inner_size, outer = tid / chunks / inner_size;
+    while (outer < outer_size) {
+        const int n = s.tokens_first ? inner : outer, t = s.tokens_first ? outer : inner;
+        const T* const from = x + (place[t][0] + n * s.x_stride[1]) + 8 * c;
+        T* const to = y + (place[t][1] + n * s.y_stride[1]) + 8 * c;
         float lo[8], hi[8];
         load8<T, true>(lo, from, 8);
         load8<T, true>(hi, from + pairs, 8);
@@ -77,6 +111,17 @@ __global__ __launch_bounds__(256) void rotary_kernel(const T* __restrict__ x, T*
         }
         store8<T, true>(to, lo, 8);
         store8<T, true>(to + pairs, hi, 8);
+        c += c_step;
+        inner += inner_step;
+        outer += outer_step;
+        if (c >= chunks) {
+            c -= chunks;
+            ++inner;
+        }
+        if (inner >= inner_size) {
+            inner -= inner_size;
+            ++outer;
+        }
     }
 }
 
@@ -85,8 +130,11 @@ __global__ __launch_bounds__(256) void rotary_kernel(const T* __restrict__ x, T*
 hipError_t launch_rotary(const void* x, void* y, const RotaryShape& s, const long long* turns, const uint8_t* axis, const void* positions, bool is_bf16,
                          hipStream_t st) {
     const long long total = (long long)s.B * s.L;
-    int tokens = std::max(1, kRotaryTable / (s.d / 2));
-    while (tokens > 1 && (total / tokens < 1024 || (long long)tokens * s.N * (s.d / 16) > 2048)) tokens /= 2;
+    // Tokens of a workgroup: two items a thread where the heads of a token lie together, eight where a head's tokens do, whose lines then are longer (4 x 24 x 16384 x 64,
+    // bf16, 512, 1024, 2048 and 4096 items: 75, 79, 83 and 88 us, 91, 85, 82 and 83), but 1024 workgroups first.
+    const long long most = s.tokens_first ? 512 : 2048;
+    int tokens = std::min(kRotaryTokens, kRotaryTable / (s.d / 2));
+    while (tokens > 1 && (total / tokens < 1024 || (long long)tokens * s.N * (s.d / 16) > most)) tokens /= 2;
     const long long grid = (total + tokens - 1) / tokens;
     if (grid > 0x7fffffffll) return hipErrorInvalidValue;
     auto launch = [&](auto kernel, auto type) {
