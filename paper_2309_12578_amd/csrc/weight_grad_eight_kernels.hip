@@ -37,13 +37,11 @@ struct Planes {
     static constexpr int n = sizeof(T) == 4 ? 3 : 1;
 };
 
-// v as a sum of three numbers of 8 significant bits; what is not finite stays in the first.
+// v as a sum of three numbers of 8 significant bits.  An infinity stays in the first; of a NaN at least one part is NaN.
 __device__ __forceinline__ void three_parts(float v, bf16_t& a, bf16_t& b, bf16_t& c) {
     auto top = [](float f) { return __builtin_bit_cast(float, __builtin_bit_cast(unsigned, f) & 0xffff0000u); };
     auto half = [](float f) { return __builtin_bit_cast(bf16_t, (unsigned short)(__builtin_bit_cast(unsigned, f) >> 16)); };
-    const bool finite = fabsf(v) <= 3.4028234663852886e38f;
-    const float first = v != v ? __builtin_nanf("") : top(v);
-    const float rest = finite ? v - first : 0.f;
+    const float first = top(v), rest = first == v ? 0.f : v - first;
     a = half(first);
     b = half(rest);
     c = half(rest - top(rest));
@@ -65,6 +63,9 @@ __device__ __forceinline__ int read_offset(int lane, int q) {
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_between(const void* p, int first, int end, size_t row) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(p)) + (size_t)first * row, (short)0, (int)((end - first) * row), 0x00027000);
 }
+typedef unsigned Four __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ Four fetch_four(__amdgpu_buffer_rsrc_t from, unsigned off) { return __builtin_amdgcn_raw_buffer_load_b128(from, off, 0, 0); }
+__device__ __forceinline__ unsigned fetch_byte(__amdgpu_buffer_rsrc_t from, unsigned off) { return __builtin_amdgcn_raw_buffer_load_b8(from, off, 0, 0); }
 // Into consecutive LDS: 16 bytes a lane from byte `off` on, or one byte, which becomes a word.
 __device__ __forceinline__ void load_rows(__amdgpu_buffer_rsrc_t from, unsigned off, void* to) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void_ptr)to, 16, off, 0, 0, 0);
@@ -162,7 +163,28 @@ __global__ __launch_bounds__(S::threads, 2) void weight_grad_eight_kernel(
         uint4 x;
         int exponent;
     };
+    constexpr bool RANGED = WHOLE && !ASYNC;
+    unsigned v_off = (unsigned)(y_row * N + n0 + 8 * y_chunk) * (unsigned)sizeof(T);
     auto request = [&](Rows& v, int at) {
+        if constexpr (RANGED) {   // (fp32) the next 32 rows each time, by their range as above
+#pragma unroll
+            for (int k = 0; k < Y_TIMES; ++k)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const Four f = fetch_four(y_rows, v_off + (unsigned)(Y_ROWS * k * N) * 4u + 16u * i);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const unsigned word = f[u];   // (a cast of the vector's element itself takes the first one)
+                        v.y[k][4 * i + u] = __builtin_bit_cast(float, word);
+                    }
+                }
+            const Four q = fetch_four(x_rows, x_off);
+            v.x = make_uint4(q[0], q[1], q[2], q[3]);
+            v.exponent = (int)fetch_byte(e_rows, x_off / kGroup);
+            v_off += (unsigned)(kStepRows * N) * 4u;
+            x_off += (unsigned)(kStepRows * pitch);
+            return;
+        }
         const int n = n0 + 8 * y_chunk;
 #pragma unroll
         for (int k = 0; k < Y_TIMES; ++k) {
@@ -175,26 +197,34 @@ __global__ __launch_bounds__(S::threads, 2) void weight_grad_eight_kernel(
         v.x = *reinterpret_cast<const uint4*>(codes + i * pitch + c);
         v.exponent = exponents[i * (pitch / kGroup) + c / kGroup];
     };
-    auto put = [&](const Rows& v, int at, Y& to_y, X& to_x) {
+    auto put = [&](Rows& v, int at, Y& to_y, X& to_x) {
+        if (!RANGED && at + kStepRows > end) {   // uniform
+#pragma unroll
+            for (int k = 0; k < Y_TIMES; ++k)
+                if (at + y_row + Y_ROWS * k >= end) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v.y[k][i] = (T)0.f;
+                }
+            if (at + x_row >= end) v.exponent = 0;   // the scale 0
+        }
 #pragma unroll
         for (int k = 0; k < Y_TIMES; ++k) {
             const int row = y_row + Y_ROWS * k;
             bf16x8 part[3];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const T y = at + row < end ? v.y[k][i] : (T)0.f;
                 if constexpr (PLANES == 3) {
                     bf16_t p, q, s;
-                    three_parts(y, p, q, s);
+                    three_parts(v.y[k][i], p, q, s);
                     part[0][i] = p, part[1][i] = q, part[2][i] = s;
                 } else {
-                    part[0][i] = y;
+                    part[0][i] = v.y[k][i];
                 }
             }
 #pragma unroll
             for (int p = 0; p < PLANES; ++p) *reinterpret_cast<bf16x8*>(&to_y.v[p][row * TN + slot_of(row, y_chunk) * 8]) = part[p];
         }
-        const float scale = at + x_row < end ? eight_scale(v.exponent) : 0.f;
+        const float scale = eight_scale(v.exponent);
         unsigned x[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = convert(v.x, scale, i);
@@ -310,12 +340,13 @@ __global__ __launch_bounds__(S::threads, 2) void weight_grad_eight_kernel(
         }
         __builtin_amdgcn_s_waitcnt(kWaitVm0);   // what was requested for steps that are not there
     } else {
-        Rows v;
-        auto step = [&](int s, Y& y, Y& y_free, X& x, X& x_free) {
+        // rows are requested two steps before they are written to LDS, and three before they are multiplied
+        Rows va, vb;
+        auto step = [&](int s, Rows& v, Y& y, Y& y_free, X& x, X& x_free) {
             const int at = first + s * kStepRows;
             meet();
             put(v, at + kStepRows, y_free, x_free);
-            request(v, at + 2 * kStepRows);
+            request(v, at + 3 * kStepRows);
             const bool sums = wants_bias && turn == share;
 #pragma unroll
             for (int k = 0; k < kStepRows / 16; ++k) {
@@ -333,13 +364,14 @@ __global__ __launch_bounds__(S::threads, 2) void weight_grad_eight_kernel(
             }
             turn = turn + 1 == shares ? 0 : turn + 1;
         };
-        request(v, first);
-        put(v, first, ys0, xs0);
-        request(v, first + kStepRows);
+        request(va, first);
+        request(vb, first + kStepRows);
+        put(va, first, ys0, xs0);
+        request(va, first + 2 * kStepRows);
         for (int s = 0; s < steps; s += 2) {
-            step(s, ys0, ys1, xs0, xs1);
+            step(s, vb, ys0, ys1, xs0, xs1);
             if (s + 1 >= steps) break;
-            step(s + 1, ys1, ys0, xs1, xs0);
+            step(s + 1, va, ys1, ys0, xs1, xs0);
         }
     }
 
@@ -457,7 +489,7 @@ struct Plan {
         const long long most = ((long long)rows + kMinRows - 1) / kMinRows, want = (side_m == 256 ? 256 : kWant) / ((long long)tiles_n * tiles_m);
         slices = (int)std::max<long long>(1, std::min(want, most));
         slice_rows = (int)((((long long)rows + slices - 1) / slices + kStepRows - 1) / kStepRows * kStepRows);
-        slice_rows = (int)std::min<long long>(slice_rows, (0x7fffffffll / std::max<long long>(2 * N, pitch) - 4 * kStepRows) / kStepRows * kStepRows);   // 31 bits of offset
+        slice_rows = (int)std::min<long long>(slice_rows, (0x7fffffffll / std::max<long long>(4ll * N, pitch) - 4 * kStepRows) / kStepRows * kStepRows);   // 31 bits of offset
         slices = (int)(((long long)rows + slice_rows - 1) / slice_rows);
         shares = tiles_m * 2;
         bias_at = slices > 1 ? (size_t)slices * outputs * sizeof(float) : 0;
