@@ -469,9 +469,14 @@ __global__ __launch_bounds__(256) void weight_grad_eight_sum_kernel(const float*
     }
 }
 
-constexpr int kMinRows = 128;   // of a slice
-constexpr long long kBig = 1 << 20;
-constexpr int kWant = 512;
+// Slices of at least so many rows, and workgroups to aim at: two on a compute unit, or one where bf16 slices would have fewer than 512 rows, whose partial sums take
+// longer than what more of them save (256 and 512: 4096 x 512 x 512 22.3 and 25.5 us, 65536 x 128 x 128 20 and 24, 65536 x 512 x 512 68 and 61; fp32, 8192 x 1536 x 512,
+// 74 and 60).
+constexpr int kMinRows = 128, kGroups = 512, kFewRows = 512;
+// Outputs from which tiles are 256 wide (at 2^18 and 2^20: 16384 x 768 x 768 47.5 and 42.5 us, 65536 x 512 x 512 72 and 61, 32768 x 1536 x 512 89 and 100; fp32 4096 x 1024 x 512
+// 38 and 33, 16384 x 768 x 768 74 and 77).
+constexpr long long kBigOutputs = 1 << 20;
+constexpr int kBigRows = 2048;
 
 struct Plan {
     int side_n = 128, side_m = 128;   // of a tile
@@ -480,14 +485,16 @@ struct Plan {
     Plan(int rows, int N, int M, bool is_bf16, bool whole) {
         const long long pitch = eight_pitch(M);
         const long long outputs = (long long)N * pitch;
-        if (outputs >= kBig && rows >= 2048 && (whole || !is_bf16)) {
+        if (outputs >= kBigOutputs && rows >= kBigRows && (whole || !is_bf16)) {
             side_n = 256;
             side_m = is_bf16 ? 128 : 256;
         }
         tiles_n = (N + side_n - 1) / side_n;
         tiles_m = (int)((pitch + side_m - 1) / side_m);
-        const long long most = ((long long)rows + kMinRows - 1) / kMinRows, want = (side_m == 256 ? 256 : kWant) / ((long long)tiles_n * tiles_m);
-        slices = (int)std::max<long long>(1, std::min(want, most));
+        const long long tiles = (long long)tiles_n * tiles_m, most = ((long long)rows + kMinRows - 1) / kMinRows;
+        long long groups = side_m == 256 ? kGroups / 2 : kGroups;
+        if (is_bf16 && side_n == 128 && rows * tiles < (long long)kFewRows * kGroups) groups = kGroups / 2;
+        slices = (int)std::max<long long>(1, std::min(groups / tiles, most));
         slice_rows = (int)((((long long)rows + slices - 1) / slices + kStepRows - 1) / kStepRows * kStepRows);
         slice_rows = (int)std::min<long long>(slice_rows, (0x7fffffffll / std::max<long long>(4ll * N, pitch) - 4 * kStepRows) / kStepRows * kStepRows);   // 31 bits of offset
         slices = (int)(((long long)rows + slice_rows - 1) / slice_rows);
