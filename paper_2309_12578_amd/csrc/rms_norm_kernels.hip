@@ -165,13 +165,13 @@ __global__ __launch_bounds__(RowThreads<LANES>::threads) void rms_norm_kernel(co
                 v[i] = z[i] * wv[k].at(i);
                 if constexpr (CODES == kCodesOfY) {
                     z[i] = v[i];
-                    unsure = unsure || !(fabsf(z[i]) <= kMost);
+                    unsure = unsure || !(fabsf(z[i]) < kMost * (1.f - 0x1p-20f));   // (next to infinity as well)
                 }
                 most = fmaxf(most, fabsf(z[i]));
             }
             if constexpr (CODES != kNoCodes) {
-                // a row that is not finite has no finite 1 / rms, or 0
-                unsure = unsure || !(inverse > 0.0 && inverse <= (double)kMost) || near_border(most);
+                // a row that is not finite has no finite 1 / rms, or 0; below 2^-126 fp32 holds it with fewer bits
+                unsure = unsure || !(inverse >= 0x1p-126 && inverse <= (double)kMost) || near_border(most);
                 int exponent = group_exponent(exponent_byte(most));
                 Codes8 q;
                 unsure = !codes_of(q, z, exponent) || unsure;

@@ -26,6 +26,13 @@ __device__ __forceinline__ void sine_cosine(float turns, float& sine, float& cos
     cosine = fmaf(q, fmaf(q, fmaf(q, fmaf(q, fmaf(q, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
 }
 
+// (a, b) by the turn with cosine u.x and sine u.y.  A sine of 0 adds nothing: a pair that does not turn stays as it is beside an infinity or NaN, too.
+__device__ __forceinline__ void turn_pair(float& a, float& b, float2 u) {
+    const float of_a = u.y == 0.f ? 0.f : a * u.y, of_b = u.y == 0.f ? 0.f : b * u.y;
+    a = fmaf(a, u.x, -of_b);
+    b = fmaf(b, u.x, of_a);
+}
+
 template <typename T, bool NEIGHBOURS>
 __global__ __launch_bounds__(256) void rotary_kernel(const T* __restrict__ x, T* __restrict__ y, const RotaryShape s, const long long* __restrict__ turns,
                                                      const uint8_t* __restrict__ axis, const void* __restrict__ positions, int tokens) {
@@ -92,21 +99,12 @@ __global__ __launch_bounds__(256) void rotary_kernel(const T* __restrict__ x, T*
             if constexpr (NEIGHBOURS) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const float2 u = cs[4 * c + k], v = cs[pairs / 2 + 4 * c + k];
-                    const float a = lo[2 * k], e = hi[2 * k];
-                    lo[2 * k] = a * u.x - lo[2 * k + 1] * u.y;
-                    lo[2 * k + 1] = lo[2 * k + 1] * u.x + a * u.y;
-                    hi[2 * k] = e * v.x - hi[2 * k + 1] * v.y;
-                    hi[2 * k + 1] = hi[2 * k + 1] * v.x + e * v.y;
+                    turn_pair(lo[2 * k], lo[2 * k + 1], cs[4 * c + k]);
+                    turn_pair(hi[2 * k], hi[2 * k + 1], cs[pairs / 2 + 4 * c + k]);
                 }
             } else {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const float2 u = cs[8 * c + k];
-                    const float a = lo[k];
-                    lo[k] = a * u.x - hi[k] * u.y;
-                    hi[k] = hi[k] * u.x + a * u.y;
-                }
+                for (int k = 0; k < 8; ++k) turn_pair(lo[k], hi[k], cs[8 * c + k]);
             }
         }
         store8<T, true>(to, lo, 8);

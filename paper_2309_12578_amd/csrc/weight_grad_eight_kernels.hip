@@ -146,11 +146,11 @@ __global__ __launch_bounds__(S::threads, 2) void weight_grad_eight_kernel(
         load_bytes(e_rows, x_off / kGroup, to.exponents + 64 * w);
         x_off += (unsigned)(kStepRows * pitch);
     };
-    // Codes 2 i and 2 i + 1 of 16 as bf16.  c + 128 as an unsigned byte; (c + 128) 2^k - 128 2^k is exact.
+    // Codes 2 i and 2 i + 1 of 16 as bf16: products that are exact, or 2^128.
     auto convert = [&](uint4 q, float scale, int i) {
         const unsigned words[4] = {q.x, q.y, q.z, q.w};
-        const unsigned w = words[i / 2] ^ 0x80808080u;
-        const float a = fmaf((float)((w >> (16 * (i & 1))) & 0xffu), scale, -128.f * scale), b = fmaf((float)((w >> (16 * (i & 1) + 8)) & 0xffu), scale, -128.f * scale);
+        const unsigned w = words[i / 2] >> (16 * (i & 1));
+        const float a = (float)(signed char)w * scale, b = (float)(signed char)(w >> 8) * scale;
         return __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, b), __builtin_bit_cast(unsigned, a), 0x07060302u);
     };
     auto put_x = [&](const unsigned (&v)[8], X& to) {
@@ -506,7 +506,7 @@ struct Plan {
 
 }  // namespace
 
-size_t weight_grad_eight_workspace_bytes(int rows, int N, int M) { 
+size_t weight_grad_eight_workspace_bytes(int rows, int N, int M) {
     return std::max({Plan(rows, N, M, false, true).total, Plan(rows, N, M, true, true).total, Plan(rows, N, M, true, false).total});
 }
 

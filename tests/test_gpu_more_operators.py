@@ -140,6 +140,23 @@ def test_rotary_of_any_axes(sp):
     _near(sp.rotary(x, axes, pos), want, _rotary_tolerance(want, made_of, torch.float32))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("neighbours", [False, True])
+def test_rotary_of_pairs_that_do_not_turn(sp, dtype, neighbours):
+    """They stay as they are, beside infinities and NaN as well; what is not finite stays in its pair."""
+    axes = sp.rotary_axes(64, (3, 5), neighbours=neighbours, device="cuda")
+    x, pos = _randn((2, 3, 20, 64), dtype, 1), torch.randint(1, 900, (2, 20), generator=torch.Generator("cuda").manual_seed(3), device="cuda")
+    clean = sp.rotary(x, axes, pos)
+    one = (lambda i: (2 * i, 2 * i + 1)) if neighbours else (lambda i: (i, i + 32))
+    for i, bad in ((9, math.inf), (17, -math.inf), (31, math.nan), (2, math.nan)):
+        x[:, :, :, one(i)[1]] = bad
+    y = sp.rotary(x, axes, pos)
+    turned = [e for i in range(8) for e in one(i) if i != 2]
+    assert torch.equal(y[..., turned], clean[..., turned]) and torch.isnan(y[..., one(2)]).all()
+    still = [e for i in range(8, 32) for e in one(i)]
+    assert torch.equal(y[..., still].nan_to_num(5.0), x[..., still].nan_to_num(5.0))
+
+
 def test_rotary_gradient_against_differences(sp):
     """The operator is linear: the gradient in one element's direction is the difference that the element makes, exactly but for roundings."""
     axes = sp.rotary_axes(32, (4, 12), neighbours=True, device="cuda")
@@ -321,6 +338,24 @@ def test_norm_against_the_formula(sp, dtype, with_residual, D):
             codes, exponents, _ = _eight(y_want)
             assert torch.equal(p.codes, codes) and torch.equal(p.exponents, exponents) and p.weight is None
             assert (h is None) != with_residual and (h is None or torch.equal(h.double(), s.to(dtype).double()))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("scale,weight", [(2.0 ** 126, 1.0), (2.0 ** -60, 1.0), (2.0 ** -130, 1.0), (1.0, 2.0 ** 125), (1.0, 2.0 ** -125)])
+def test_norm_codes_of_large_and_small_rows(sp, dtype, scale, weight):
+    """The codes of 64 bits wherever a row's 1 / rms, its elements or its results leave fp32's normal numbers."""
+    x = torch.rand((4096, 256), generator=torch.Generator("cuda").manual_seed(1), device="cuda") * 2.0 - 1.0
+    x, w = (x.double() * scale * 1.9).to(dtype), (_randn((256,), torch.float32, 2).clamp(-2.9, 2.9).double() * weight).to(dtype)
+    eps = 0.0 if scale != 1.0 else EPS
+    s, rstd, z, y = _norm(x, w, eps=eps)
+    z, y = (torch.where(rstd < math.inf, t, torch.full_like(t, math.nan)) for t in (z, y))
+    with torch.no_grad():
+        _, _, p = sp.rms_norm(x, w, eps=eps, checkpoint=True)
+        codes, exponents, _ = _eight(z)
+        assert torch.equal(p.codes, codes) and torch.equal(p.exponents, exponents)
+        p, _ = sp.rms_norm8(x, w, eps=eps)
+        codes, exponents, _ = _eight(y)
+        assert torch.equal(p.codes, codes) and torch.equal(p.exponents, exponents)
 
 
 def test_norm_gradients_against_differences(sp):
@@ -518,6 +553,23 @@ def test_linear_of_large_and_small_gradients_in_fp32(sp):
     g[0, 0], g[1, 1], g[2, 2] = torch.finfo(torch.float32).max, -torch.finfo(torch.float32).max, 0.0
     dw, = torch.autograd.grad(sp.linear8(x, w), w, g)
     assert torch.equal(dw, g.t())   # each sum has one term: exact
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,M,N", [(70, 130, 136), (70, 130, 135), (2100, 1024, 1024)])
+def test_linear_of_the_largest_and_smallest_numbers(sp, dtype, rows, M, N):
+    """Scales up to 2^122 and down to 2^-126 come out whole."""
+    of = torch.Generator("cuda").manual_seed(1)
+    x = torch.rand((rows, M), generator=of, device="cuda") * 2.0 - 1.0
+    x[:, :64] *= 3.3e38   # (below 127 * 2^121, from where codes stand for 2^128)
+    x[:, 64:128] *= 2.0 ** -122
+    x, w, dy = x.to(dtype), torch.zeros((N, M), dtype=dtype, device="cuda", requires_grad=True), _randn((rows, N), dtype, 3, 2.0 ** -12)
+    values = _eight(x.double())[2]
+    assert values.abs().max() > 3.2e38
+    dw, = torch.autograd.grad(sp.linear8(x, w), w, dy)
+    want = torch.matmul(dy.double().t(), values)
+    # beside the sums' roundings those of terms below 2^-126, which may go altogether
+    _near(dw, want, _weight_tolerance(dy, values, want, dtype, rows, 3 if dtype == torch.float32 else 1) + U * want.abs() + 3 * rows * 2.0 ** -126)
 
 
 def test_linear_asked_for_some_gradients_only(sp):
