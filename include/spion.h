@@ -266,6 +266,7 @@ int spion_dropout_add(const void *x, const void *residual, void *y, int64_t n, i
  *   turns     [d / 2] frequencies in turns, as integers in 2^-64 modulo 2^64 (rint(2^64 * frequency / (2 pi))): an angle is exact to position * 2^-65 turns.
  *   axis_of   [d / 2]; an entry from `axes` on counts as the last axis.
  *   positions int32 or int64, any sign, at position_stride[0] * axis + [1] * b + [2] * l.
+ *   A pair that does not turn stays as it is, whatever it holds.
  * Supported: d a multiple of 16 up to 256, H up to 65535, up to 255 axes, fewer than 2^31 tokens.
  */
 #define SPION_ROTARY_NEIGHBOURS 1u
@@ -303,6 +304,7 @@ int spion_unpack_eight(const int8_t *codes, const uint8_t *exponents, const void
  *   s = x + residual (residual may be NULL),  rstd = 1 / sqrt(mean s^2 + eps),  z = s rstd,  y = z weight,  h = s rounded.
  *   y, h, rstd, codes may be NULL: not wanted.  codes, exponents: z in 8 bits (as above), with SPION_NORM_CODES_OF_Y y.  Sums of squares, and what
  *   decides a code, are in 64 bits.
+ *   No result may overlap an operand.
  * Gradient:  dx = dh + rstd (weight dy - z mean(weight dy z)),  dw = sum of dy z.  It is the residual's too.  z from the codes (of z), or codes NULL and z = h rstd.
  *   dh may be NULL (none), dw may be NULL (not wanted).  fp32 sums in a fixed order.
  */

@@ -515,6 +515,7 @@ static hipError_t launch_t(const WeightGradEight& a, hipStream_t st) {
     constexpr bool is_bf16 = sizeof(T) == 2;
     const bool whole = a.N % 8 == 0 && (uintptr_t)a.dY % 16 == 0;
     const Plan p(a.rows, a.N, a.M, is_bf16, whole);
+    if ((long long)p.slices * p.tiles_n * p.tiles_m > 0x7fffffffll) return hipErrorInvalidValue;
     float *const partial = p.slices > 1 ? static_cast<float*>(a.workspace) : nullptr,
                  *const bias_partial = a.db ? reinterpret_cast<float*>(static_cast<char*>(a.workspace) + p.bias_at) : nullptr;
     T *const dW = static_cast<T*>(a.dW), *const db = static_cast<T*>(a.db);

@@ -126,8 +126,13 @@ class SparseMHA(nn.Module):
         lengths: int32 [B], the tokens of each sequence, see `sparse_attention`; rows from there on leave as they came, but
         for w_o's bias, and have to be finite (the projections' gradients add them up, times 0).
         rng, stream: int64 tensor {seed, offset} and a number of the layer's own, from which both dropouts then draw, see
-        `dropout_add`; without it the last one is torch's."""
+        `dropout_add`; without it the last one is torch's.
+        positions: int32 or int64 [axes, L] or [axes, B, L], see `rotary`; one axis counts from 0 if they are not given.
+        residual: with the "rms" norm, the stream that E, the branch of the sub-layer before, is to be added to.  The result then is (branch,
+        stream), not their sum: the next sub-layer's E and residual."""
         B, L, D = E.shape
+        if positions is not None and self.turns is None:
+            raise ValueError("positions are for a sub-layer with rotary axes")
         w_qkv, w_o = self.w_qkv, self.w_o
         attn_dropout = self.attn_dropout if self.training else 0.0
         plain = self.bias_table is None and lengths is None and attn_dropout == 0.0
@@ -172,6 +177,7 @@ class SparseMHA(nn.Module):
         branch = w_o(S)
         draws = rng is not None and self.training and self.drop.p > 0.0
         if residual is not None:
+            branch = branch.to(R.dtype)   # (autocast)
             return (dropout_add(branch, None, self.drop.p, rng, stream) if draws else self.drop(branch)), R
         if draws:
             return dropout_add(branch.to(R.dtype), R, self.drop.p, rng, stream)

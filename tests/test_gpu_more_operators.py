@@ -729,6 +729,107 @@ def test_sub_layer_is_the_same_with_its_residual_added_before(sp):
         m(E, pattern)
 
 
+def _everything(sp, dtype, eight):
+    """(module, leaves, contents of the step, step): bias, lengths, both dropouts, positions of several axes and a residual.  What a step returns is detached:
+    a graph that lives, of the same leaves, would be in the way of a capture."""
+    B, L, heads = 3, 128, 2
+    pattern, axes = _pattern(sp, _mask(4, 2), 32), sp.rotary_axes(64, (10, 22), device="cuda")
+    buckets = sp.relative_buckets(L, 8, device="cuda")
+    torch.manual_seed(1)
+    m = sp.SparseMHA(128, heads, dropout=0.25, bias=True, buckets=buckets, attn_dropout=0.25, norm="rms", rotary=axes, eight_bit=eight, device="cuda", dtype=dtype)
+    torch.nn.init.normal_(m.bias_table)
+    E, R, gb, gs = [_randn((B, L, 128), dtype, k) for k in range(4)]
+    leaves = [E.requires_grad_(), R.requires_grad_(), *m.parameters()]
+    given = dict(lengths=torch.tensor([128, 0, 77], dtype=torch.int32, device="cuda"), rng=torch.tensor([5, 6], device="cuda"), stream=4,
+                 positions=torch.randint(0, 500, (2, B, L), generator=torch.Generator("cuda").manual_seed(3), device="cuda"))
+
+    def step(call=lambda e, r: m(e, pattern, residual=r, **given)):
+        out = call(E, R)
+        return [*(t.detach() for t in out), *torch.autograd.grad(out, leaves, [gb, gs])]
+    return m, leaves, (pattern, axes, buckets, given, gb), step
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("eight", [False, True])
+def test_sub_layer_with_everything(sp, dtype, eight):
+    """The operators one after the other give the same; so does the step with checkpointing."""
+    from torch.utils.checkpoint import checkpoint
+    m, (E, R, *_), (pattern, axes, buckets, given, gb), step = _everything(sp, dtype, eight)
+    (B, L, D), heads = E.shape, m.heads
+
+    def by_hand(E, R):
+        X, h, p = sp.rms_norm(E, m.norm.weight, R, m.norm.eps, eight)
+        qkv = sp.linear8(X, m.w_qkv.weight, m.w_qkv.bias, p) if eight else torch.nn.functional.linear(X, m.w_qkv.weight, m.w_qkv.bias)
+        q, k, v = qkv.view(B, L, 3, heads, 64).permute(2, 0, 3, 1, 4)
+        S = sp.sparse_attention(sp.rotary(q, axes, given["positions"]), sp.rotary(k, axes, given["positions"]), v, pattern, bias=m.bias_table, buckets=buckets,
+                                lengths=given["lengths"], dropout=0.25, rng=given["rng"], stream=4)
+        branch = torch.nn.functional.linear(S.transpose(1, 2).reshape(B, L, D), m.w_o.weight, m.w_o.bias)
+        return sp.dropout_add(branch, None, 0.25, given["rng"], 4), h
+    want = step()
+    # the same numbers, in some gradients by other sums (the projections' weights by the library's product): a rounding to the type and some of 24 bits
+    assert all((a.double() - b.double()).norm() <= (2 * half(dtype) + 1e-5) * b.double().norm() for a, b in zip(step(by_hand), want))
+    with_checkpoint = step(lambda e, r: checkpoint(lambda e, r: m(e, pattern, residual=r, **given), e, r, use_reentrant=False))
+    assert all(torch.equal(a, b) for a, b in zip(with_checkpoint, want))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_sub_layer_captured(sp, dtype):
+    m, (E, *_), (_, _, _, given, _), step = _everything(sp, dtype, True)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step()
+    for i in range(3):
+        with torch.no_grad():
+            E.copy_(_randn(E.shape, dtype, 30 + i))
+        given["rng"][1] += 1
+        want = step()
+        graph.replay()
+        assert all((a.double() - b.double()).norm() <= 1e-2 * b.double().norm() for a, b in zip(captured, want))   # (library products may be others)
+        torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("eight", [False, True])
+def test_sub_layer_whose_norm_is_watched(sp, dtype, eight):
+    """A hook that changes the norm's result: the projection keeps what it was handed, not the norm's codes.  As if the norm's weight were twice as large."""
+    m, (E, R, *_), (pattern, _, _, given, gb), _ = _everything(sp, dtype, eight)
+    m.eval()
+    run = lambda: m(E, pattern, lengths=given["lengths"], positions=given["positions"], residual=R)[0]
+    hook = m.norm.register_forward_hook(lambda mod, args, out: (out[0] * 2.0, *out[1:]))
+    twice = run()
+    dw, = torch.autograd.grad(twice, m.w_qkv.weight, gb)
+    hook.remove()
+    with torch.no_grad():
+        m.norm.weight.mul_(2.0)
+    other = run()
+    # fp32 with codes: x + residual is not rounded to 24 bits before it is squared and multiplied, without codes it is, u of each element; two projections and
+    # the attention between them make that some ten times as much of the result
+    near = 1e-5 if eight and dtype == torch.float32 else 0.0
+    assert (twice.double() - other.double()).norm() <= near * other.double().norm()
+    want, = torch.autograd.grad(other, m.w_qkv.weight, gb)
+    # two ways to 8 bits, each with roundings of up to 2^-8 of a group's largest element
+    assert (dw.double() - want.double()).norm() <= (2 ** -6 if eight else 1e-5) * want.double().norm()
+    with pytest.raises(ValueError):   # positions without axes
+        sp.SparseMHA(128, 2, norm="rms", device="cuda", dtype=dtype)(E, pattern, positions=given["positions"])
+
+
+def test_sub_layers_under_autocast(sp):
+    """The stream stays in its type, the branch joins it."""
+    pattern = _pattern(sp, _mask(4, 2), 32)
+    for eight in (False, True):
+        m = sp.SparseMHA(128, 2, norm="rms", rotary=sp.rotary_axes(64, (32,)), eight_bit=eight, device="cuda")
+        E, R = _randn((2, 128, 128), torch.float32, 1).requires_grad_(), _randn((2, 128, 128), torch.float32, 2)
+        want = m(*[m(E, pattern, residual=R)[0], pattern], residual=R)
+        with torch.autocast("cuda", dtype=torch.bfloat16):
+            e, r = m(E, pattern, residual=R)
+            got = m(e, pattern, residual=R)
+            dE, = torch.autograd.grad(got[0].float().sum(), E)
+        assert e.dtype == r.dtype == got[0].dtype == dE.dtype == torch.float32
+        assert all((a - b).norm() <= 5e-2 * b.norm() for a, b in zip(got, want))
+
+
 def test_what_the_sub_layer_keeps(sp):
     """The norm's input and output, 4 bytes an element in bf16, are one byte and a little."""
     pattern = _pattern(sp, _mask(8, 2), 64)
