@@ -3,6 +3,10 @@
 //
 // code * 2^k is exact in bf16, so X enters the product as it was kept, without a rounding.  An fp32 dY enters as the sum of three bf16 numbers, its
 // significand's 24 bits by eights: three bf16 products, exact but for the sums, at 8 times the rate of the fp32 matrix instruction each.
+//
+// Bound by the matrix units where N and M are large (65536 x 2048 x 2048 bf16 570 - 640 us, 0.86 - 0.96 PFLOP/s, the sums of its slices 16 us; fp32 8192 x 1536 x 512 58 us and 7), by the
+// start and the end of a slice where they are small (16384 x 768 x 256 bf16 21 us and 5).  Tiles as large as the registers hold, so that LDS feeds them; bf16 as two workgroups
+// a compute unit, one of which multiplies while the other waits (one of 256 x 256: 685 us).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
