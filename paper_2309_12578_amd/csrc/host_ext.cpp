@@ -1261,24 +1261,40 @@ struct RotaryArgs {
     bool neighbours = false;
 };
 
+// Heads of x: [B, H, L, d], or [B, L, H d] with heads beside each other.
+struct Heads {
+    int64_t B, H, L, d, stride[3];   // strides of B, H, L
+    Heads(const at::Tensor& x, int64_t d_) : d(d_) {
+        const bool apart = x.dim() == 4;
+        B = x.size(0);
+        H = apart ? x.size(1) : x.size(2) / d;
+        L = x.size(apart ? 2 : 1);
+        stride[0] = x.stride(0);
+        stride[1] = apart ? x.stride(1) : d;
+        stride[2] = x.stride(apart ? 2 : 1);
+    }
+};
+
 // y as x lies, if that is without gaps.
 at::Tensor turn(const at::Tensor& x, const RotaryArgs& a, const at::Tensor& positions, bool back) {
     const at::Tensor y = x.is_non_overlapping_and_dense()
                              ? at::Tensor(at::detail::empty_strided_cuda(x.sizes(), x.strides(), x.scalar_type(), x.device()))
                              : new_like(x);
     if (x.numel() == 0) return y;
+    const int64_t d = 2 * a.turns.size(0);
+    const Heads from(x, d), to(y, d);
     spion_rotary_params p = {};
-    p.B = (int32_t)x.size(0);
-    p.H = (int32_t)x.size(1);
-    p.L = (int32_t)x.size(2);
-    p.d = (int32_t)x.size(3);
+    p.B = (int32_t)from.B;
+    p.H = (int32_t)from.H;
+    p.L = (int32_t)from.L;
+    p.d = (int32_t)d;
     p.rotated = (int32_t)a.rotated;
     p.axes = (int32_t)a.axes;
     p.dtype = dtype_code(x);
     p.position_bytes = positions.scalar_type() == at::kLong ? 8 : 4;
     for (int i = 0; i < 3; ++i) {
-        p.x_stride[i] = x.stride(i);
-        p.y_stride[i] = y.stride(i);
+        p.x_stride[i] = from.stride[i];
+        p.y_stride[i] = to.stride[i];
     }
     p.position_stride[0] = positions.stride(0);
     p.position_stride[1] = positions.dim() == 3 ? positions.stride(1) : 0;
@@ -1307,7 +1323,7 @@ struct RotaryBackward : public torch::autograd::Node {
         return differentiate("rotary cannot be differentiated twice", grads[0], [&] {
             const at::Device device = grads[0].device();
             const c10::DeviceGuard guard(device);
-            const at::Tensor g = grads[0].stride(3) == 1 ? grads[0] : grads[0].contiguous(), pos = positions.unpack();
+            const at::Tensor g = grads[0].stride(-1) == 1 ? grads[0] : grads[0].contiguous(), pos = positions.unpack();
             saved(pos.defined() && pos.device() == device && pos.layout() == at::kStrided && !transformed(pos) && pos.sizes() == at::IntArrayRef(position_sizes) &&
                       pos.scalar_type() == position_type, "rotary: a saved tensor is not the one that was saved");
             RotaryArgs a = args;
@@ -1319,7 +1335,7 @@ struct RotaryBackward : public torch::autograd::Node {
     }
 };
 
-// rotary(x, turns, axis_of, positions, axes, rotated, neighbours) -> y
+// rotary(x, turns, axis_of, positions, axes, rotated | None, neighbours) -> y
 PyObject* py_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!arg_count(n, 7, "rotary")) return nullptr;
     return guarded([&]() -> PyObject* {
@@ -1331,28 +1347,29 @@ PyObject* py_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
         args.turns = tensor_arg(a[1]);
         args.axis_of = tensor_arg(a[2]);
         args.axes = long_arg(a[4]);
-        args.rotated = long_arg(a[5]);
         args.neighbours = a[6] == Py_True;
         check_operand(positions, device);
         check_operand(args.turns, device);
         check_operand(args.axis_of, device);
         dtype_code(x);
-        if (x.dim() != 4) bad_value("rotary takes tensors of shape [B, H, L, head_dim]");
-        const int64_t d = x.size(3);
-        if (args.turns.dim() != 1 || 2 * args.turns.size(0) != d || args.turns.scalar_type() != at::kLong || !args.turns.is_contiguous() ||
-            args.axis_of.dim() != 1 || 2 * args.axis_of.size(0) != d || args.axis_of.scalar_type() != at::kByte || !args.axis_of.is_contiguous())
+        if (x.dim() != 4 && x.dim() != 3) bad_value("rotary takes tensors of shape [B, H, L, head_dim] or [B, L, H * head_dim]");
+        if (args.turns.dim() != 1 || args.turns.size(0) < 1 || args.turns.scalar_type() != at::kLong || !args.turns.is_contiguous() ||
+            args.axis_of.dim() != 1 || args.axis_of.size(0) != args.turns.size(0) || args.axis_of.scalar_type() != at::kByte || !args.axis_of.is_contiguous() ||
+            (x.dim() == 4 ? x.size(3) != 2 * args.turns.size(0) : x.size(2) % (2 * args.turns.size(0)) != 0))
             bad_value("the axes are not those of heads of this dimension");
-        if (args.rotated < 0 || args.rotated > x.size(1)) bad_value("heads must be a number of x's heads");
+        const Heads heads(x, 2 * args.turns.size(0));
+        args.rotated = a[5] == Py_None ? heads.H : long_arg(a[5]);
+        if (args.rotated < 0 || args.rotated > heads.H) bad_value("heads must be a number of x's heads");
         if ((positions.scalar_type() != at::kLong && positions.scalar_type() != at::kInt) || positions.dim() < 2 || positions.dim() > 3 ||
-            positions.size(0) != args.axes || positions.size(-1) != x.size(2) || (positions.dim() == 3 && positions.size(1) != x.size(0)))
+            positions.size(0) != args.axes || positions.size(-1) != heads.L || (positions.dim() == 3 && positions.size(1) != heads.B))
             bad_value("positions must be int32 or int64 [axes, L] or [axes, B, L]");
-        if (x.size(0) > 0x7fffffff || x.size(1) > 65535 || x.size(2) > 0x7fffffff) bad_value("rotary: too many heads or tokens");
+        if (heads.B > 0x7fffffff || heads.H > 65535 || heads.L > 0x7fffffff) bad_value("rotary: too many heads or tokens");
         const c10::DeviceGuard guard(device);
         const bool grad = torch::autograd::compute_requires_grad(x);
         at::Tensor y;
         {
             at::NoGradGuard no_grad;
-            y = turn(x.stride(3) == 1 ? x : x.contiguous(), args, positions, false);
+            y = turn(x.stride(-1) == 1 ? x : x.contiguous(), args, positions, false);
         }
         if (grad) {
             auto node = std::shared_ptr<RotaryBackward>(new RotaryBackward(), torch::autograd::deleteNode);

@@ -16,7 +16,7 @@ from . import binding as _b
 from .autograd import sparse_attention
 from .eight import Packed8, linear8, rms_norm
 from .extras import RelativeBuckets, _map_for, dropout_add
-from .rotary import RotaryAxes, rotary
+from .rotary import RotaryAxes
 
 HEAD_DIM = 64   # the only head dimension the kernels are built for
 
@@ -131,29 +131,29 @@ class SparseMHA(nn.Module):
         residual: with the "rms" norm, the stream that E, the branch of the sub-layer before, is to be added to.  The result then is (branch,
         stream), not their sum: the next sub-layer's E and residual."""
         B, L, D = E.shape
-        if positions is not None and self.turns is None:
+        w_qkv, w_o, norm, turns = self.w_qkv, self.w_o, self.norm, self.turns
+        if positions is not None and turns is None:
             raise ValueError("positions are for a sub-layer with rotary axes")
-        w_qkv, w_o = self.w_qkv, self.w_o
         attn_dropout = self.attn_dropout if self.training else 0.0
         plain = self.bias_table is None and lengths is None and attn_dropout == 0.0
         if not plain and flags:
             raise ValueError("flags are not supported together with a bias, lengths or dropout")
         S, R, checkpoint = None, E, None
-        if isinstance(self.norm, _RmsNorm):
+        if isinstance(norm, _RmsNorm):
             # a hook, or another forward, may change what the norm's codes stand for before the projection has it
-            shares = w_qkv.eight_bit and torch.is_grad_enabled() and not _hands_on(w_qkv) and not self.norm._forward_hooks
-            X, h, checkpoint = self.norm(E, residual, shares)
+            shares = w_qkv.eight_bit and torch.is_grad_enabled() and not _hands_on(w_qkv) and not norm._forward_hooks
+            X, h, checkpoint = norm(E, residual, shares)
             R = E if residual is None else h
         elif residual is not None:
             raise ValueError("a residual goes into the 'rms' norm only")
         else:
-            X = self.norm(E)
+            X = norm(E)
         qkv = w_qkv(X) if checkpoint is None else w_qkv(X, checkpoint)
         if qkv.is_cuda and not torch.compiler.is_compiling():
             host = _b._host or _b._native()
             if residual is None:
                 R = host.residual(E, X)   # E, its gradient added up in the norm's pass
-            if self.turns is not None:
+            if turns is not None:
                 qkv = self._turned(qkv, positions)
             # lines 4-7 for every head, on the heads as they lie in qkv
             index = (qkv, self.heads, pattern.row_ptr, pattern.col_idx, pattern.col_ptr, pattern.row_idx, pattern.bsr_pos,
@@ -165,7 +165,7 @@ class SparseMHA(nn.Module):
                 S = host.heads_attention_with(
                     *index, apart, self.bias_table, None if self.bias_table is None else _map_for(self.bias_table, self.buckets, L),
                     lengths, attn_dropout, rng, stream)
-        elif self.turns is not None:
+        elif turns is not None:
             qkv = self._turned(qkv, positions)
         if S is None:
             qkv = qkv.view(B, L, 3, self.heads, HEAD_DIM)
@@ -185,11 +185,10 @@ class SparseMHA(nn.Module):
 
     def _turned(self, qkv: torch.Tensor, positions: Optional[torch.Tensor]) -> torch.Tensor:
         """Queries and keys, the first two thirds of the heads beside each other in qkv, turned by their positions."""
-        B, L, D = qkv.shape
-        axes = self.rotary
+        count, neighbours = self._axes
         if positions is None:
-            if axes.count != 1:
-                raise ValueError("positions of %d axes are missing" % axes.count)
-            positions = torch.arange(L, device=qkv.device)[None]
-        heads = qkv.view(B, L, 3 * self.heads, HEAD_DIM).transpose(1, 2)
-        return rotary(heads, axes, positions, 2 * self.heads).transpose(1, 2).reshape(B, L, D)
+            if count != 1:
+                raise ValueError("positions of %d axes are missing" % count)
+            positions = torch.arange(qkv.shape[1], device=qkv.device)[None]
+        # (as `rotary`, without another RotaryAxes a call)
+        return (_b._host or _b._native()).rotary(qkv, self.turns.data, self.axis_of.data, positions, count, 2 * self.heads, neighbours)

@@ -129,6 +129,36 @@ def test_rotary_of_any_strides(sp, dtype):
         _near(dx, want, _rotary_tolerance(want, made_of, dtype))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rotary_of_heads_beside_each_other(sp, dtype):
+    """[B, L, H * head_dim] is the same as its heads one by one, with strides, gaps and odd addresses too."""
+    axes = sp.rotary_axes(48, (5, 9), device="cuda")
+    pos = torch.randint(-99, 99, (2, 3, 21), generator=torch.Generator("cuda").manual_seed(3), device="cuda")
+    apart = lambda t: t.unflatten(2, (-1, 48)).transpose(1, 2)
+    wide = _randn((3, 21, 5 * 48 + 7), dtype, 1)
+    for x in (wide[..., 7:].contiguous(), wide[..., :-7], wide[..., 3:-4], _randn((21, 3, 240), dtype, 2).transpose(0, 1), _randn((3, 240, 21), dtype, 2).transpose(1, 2),
+              wide[:1, :, :240].expand(3, -1, -1), wide[..., :0], wide[..., :48]):
+        for heads in (None, 0, x.shape[2] // 48):
+            leaf = x.detach().requires_grad_()
+            y = sp.rotary(leaf, axes, pos, heads)
+            want = sp.rotary(apart(x), axes, pos, heads)
+            assert y.shape == x.shape and torch.equal(apart(y), want) if x.numel() else y.shape == x.shape
+            for g in (_randn(x.shape, dtype, 4), torch.ones((), dtype=dtype, device="cuda").expand(x.shape)):
+                dx, = torch.autograd.grad(y, leaf, g, retain_graph=True)
+                assert dx.shape == x.shape and torch.equal(dx, _rotary_back(sp, apart, g, axes, pos, heads)) if x.numel() else dx.shape == x.shape
+    x = wide[..., 7:]
+    for call in (lambda: sp.rotary(wide, axes, pos), lambda: sp.rotary(x, axes, pos[:, :2]), lambda: sp.rotary(x, axes, pos, 6), lambda: sp.rotary(x, axes, pos, -1),
+                 lambda: sp.rotary(x, axes, pos[..., :20]), lambda: sp.rotary(x[0], axes, pos)):
+        with pytest.raises(ValueError):
+            call()
+
+
+def _rotary_back(sp, apart, g, axes, pos, heads):
+    leaf = apart(g).detach().requires_grad_()
+    dx, = torch.autograd.grad(sp.rotary(leaf, axes, pos, heads), leaf, apart(g))
+    return dx.transpose(1, 2).flatten(2)
+
+
 def test_rotary_of_any_axes(sp):
     """Axes beyond the last count as the last, any turns will do, and nothing is read that is not there."""
     g = torch.Generator().manual_seed(5)
