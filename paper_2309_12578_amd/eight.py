@@ -52,7 +52,8 @@ def pack8(x: torch.Tensor) -> Packed8:
 
 
 def unpack8(p: Packed8, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
-    """What p stands for, [..., size] of `dtype` (bf16 or fp32), rounded once; without a weight both hold it exactly."""
+    """What p stands for, [..., size] of `dtype` (bf16 or fp32), rounded once; without a weight both hold it exactly.  Not
+    differentiable."""
     return (_b._host or _b._native()).unpack8(p.codes, p.exponents, p.weight, p.size, _b._dtype_code(dtype))
 
 

@@ -61,7 +61,7 @@ def rotary_axes(head_dim: int, sections: Sequence[int], base: float = 10000.0, l
 
 def rotary(x: torch.Tensor, axes: RotaryAxes, positions: torch.Tensor, heads: Optional[int] = None) -> torch.Tensor:
     """x [B, H, L, head_dim], or [B, L, H * head_dim] with heads beside each other as a projection leaves them (bf16 or fp32; any strides, so that transposed views
-    of [B, L, H, head_dim] will do; the result lies as x does if x has no gaps), with the pairs (a, b) of its first `heads` heads (all of them if not given) turned by
+    of [B, L, H, head_dim] will do; the result lies as x does, if x has no gaps and heads are dense), with the pairs (a, b) of its first `heads` heads (all of them if not given) turned by
     t = position * frequency: (a cos t - b sin t, b cos t + a sin t); the others are copied, so that queries and keys in a joint projection's output are turned in one call.
     positions: int32 or int64 [axes, L], or [axes, B, L], of any sign; angles are exact to position * 2^-65 turns, then in fp32.  A pair that does not turn stays as it is,
     whatever it holds.  Differentiable with respect to x."""

@@ -40,6 +40,9 @@ class _RmsNorm(nn.Module):
         self.weight = nn.Parameter(torch.ones(dim, device=device, dtype=dtype))
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None, checkpoint: bool = False):
+        dtype = self.weight.dtype
+        if x.dtype != dtype and torch.is_autocast_enabled():   # in the weight's type, as LayerNorm under autocast in fp32
+            x, residual = x.to(dtype), None if residual is None else residual.to(dtype)
         return rms_norm(x, self.weight, residual, self.eps, checkpoint)
 
 

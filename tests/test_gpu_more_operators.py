@@ -614,6 +614,13 @@ def test_linear_asked_for_some_gradients_only(sp):
             assert torch.allclose(v, (dx, dw, db)[i], rtol=0, atol=float(20 * 2 * U * dy.abs().sum()))   # (the bias' alone by another sum)
     with torch.no_grad():
         assert torch.equal(sp.linear8(*full), torch.nn.functional.linear(x, w, b))
+    row = x[0, 0].clone().requires_grad_()   # one row, no leading dimension; a weight that is a view
+    y = sp.linear8(row, full[1], full[2])
+    assert y.shape == (24,) and torch.equal(torch.autograd.grad(y, full[2], dy[0, 0], retain_graph=True)[0], dy[0, 0])
+    assert [g.shape for g in torch.autograd.grad(y, [row, full[1]], dy[0, 0])] == [(70,), (24, 70)]
+    turned = w.t().contiguous().requires_grad_()
+    got = torch.autograd.grad(sp.linear8(x, turned.t()), turned, dy)[0]
+    assert torch.equal(got, torch.autograd.grad(sp.linear8(x, full[1]), full[1], dy)[0].t())
     empty = torch.zeros((0, 70), device="cuda", requires_grad=True)
     y = sp.linear8(empty, full[1], full[2])
     dx, dw, db = torch.autograd.grad(y, [empty, full[1], full[2]], torch.zeros_like(y))
@@ -856,8 +863,13 @@ def test_sub_layers_under_autocast(sp):
             e, r = m(E, pattern, residual=R)
             got = m(e, pattern, residual=R)
             dE, = torch.autograd.grad(got[0].float().sum(), E)
+            half_wide = m(E.bfloat16(), pattern, residual=R), m(E.bfloat16(), pattern)
         assert e.dtype == r.dtype == got[0].dtype == dE.dtype == torch.float32
         assert all((a - b).norm() <= 5e-2 * b.norm() for a, b in zip(got, want))
+        assert half_wide[0][0].dtype == half_wide[0][1].dtype == torch.float32 and (half_wide[0][1] - (E + R)).norm() <= 2.0 ** -8 * E.norm()
+        assert (half_wide[1] - m(E, pattern)).norm() <= 5e-2 * E.norm()
+        with pytest.raises(ValueError):   # without autocast types have to fit
+            m(E.bfloat16(), pattern)
 
 
 def test_what_the_sub_layer_keeps(sp):
