@@ -1662,7 +1662,7 @@ PyObject* py_rms_norm8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// The gradient of linear8: x's as a library product, the weight's and the bias' from the codes.
+// The gradient of linear8: x's as a library product unless it is small, the weight's and the bias' from the codes.
 struct Linear8Backward : public torch::autograd::Node {
     torch::autograd::SavedVariable codes, exponents, column, w;   // column: the weight of the codes, if they have one
     std::vector<int64_t> sizes;   // of x
@@ -1690,7 +1690,14 @@ struct Linear8Backward : public torch::autograd::Node {
             if (task_should_compute_output(0)) {
                 const at::Tensor W = w.unpack();
                 saved(W.defined() && W.device() == device && W.dim() == 2 && W.size(0) == N && W.size(1) == M && W.scalar_type() == type, other);
-                out[0] = at::mm(g, W).view(sizes);
+                if (W.is_contiguous() && !transformed(W) && spion_input_grad_suits((int32_t)rows, (int32_t)N, (int32_t)M)) {
+                    out[0] = new_tensor(sizes, type, device);
+                    const int rc = spion_input_grad(device_ptr(g), device_ptr(W), device_ptr(out[0]), (int32_t)rows, (int32_t)N, (int32_t)M, dtype_code(g),
+                                                    current_stream());
+                    if (rc != SPION_OK) throw SpionFailure{rc, "spion_input_grad"};
+                } else {
+                    out[0] = at::mm(g, W).view(sizes);
+                }
             }
             if (needs_w && rows > 0) {
                 Eight from;

@@ -723,6 +723,15 @@ int spion_weight_grad_eight(const void* dY, const int8_t* codes, const uint8_t* 
     return spion::launch_weight_grad_eight(a, dtype == SPION_BF16, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? SPION_OK : SPION_ERR_HIP;
 }
 
+int spion_input_grad_suits(int32_t rows, int32_t N, int32_t M) { return weight_grad_eight_ok(rows, N, M) && spion::input_grad_suits(rows, N, M); }
+
+int spion_input_grad(const void* dY, const void* W, void* dX, int32_t rows, int32_t N, int32_t M, int32_t dtype, void* hip_stream) {
+    if (!dY || !W || !dX) return SPION_ERR_NULL;
+    if (dtype != SPION_F32 && dtype != SPION_BF16) return SPION_ERR_DTYPE;
+    if (!weight_grad_eight_ok(rows, N, M)) return SPION_ERR_SHAPE;
+    return spion::launch_input_grad(dY, W, dX, rows, N, M, dtype == SPION_BF16, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? SPION_OK : SPION_ERR_HIP;
+}
+
 int spion_heads_attn_fwd(const void* qkv, void* S, float* LSE, const int32_t* row_ptr, const int32_t* col_idx, int32_t nnzb,
                          const spion_attn_params* p, void* room, size_t room_bytes, void* hip_stream) {
     if (!qkv || !S || !LSE || !row_ptr || !col_idx || !p) return SPION_ERR_NULL;

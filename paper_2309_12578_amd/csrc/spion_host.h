@@ -31,6 +31,11 @@ int spion_layer_norm_grad(const void* dy, const void* dr, const void* x, const v
                           void* dx, void* dw, void* db, int32_t rows, int32_t D, int32_t dtype, void* workspace,
                           size_t workspace_bytes, void* hip_stream);
 
+// dX [rows, M] = dY [rows, N] W [N, M], fp32 sums in a fixed order; fp32 or bf16, all contiguous.  1 <= N, M <= 2^20, 1 <= rows < 2^31 - 4096.
+// suits: 1 where that is to be preferred to a library product.
+int spion_input_grad_suits(int32_t rows, int32_t N, int32_t M);
+int spion_input_grad(const void* dY, const void* W, void* dX, int32_t rows, int32_t N, int32_t M, int32_t dtype, void* hip_stream);
+
 // Head split (split != 0) or merge: merged [B, L, n, H, 64] <-> tensors t[0 .. n - 1] [B, H, L, 64], n = 1 or 3, fp32 or
 // bf16, L a multiple of 4, fewer than 2^31 vectors of 16 bytes.
 int spion_heads(int32_t split, void* merged, void* const* t, int32_t B, int32_t L, int32_t H, int32_t n, int32_t dtype,

@@ -216,6 +216,9 @@ struct WeightGradEight {
 };
 size_t weight_grad_eight_workspace_bytes(int rows, int N, int M);
 hipError_t launch_weight_grad_eight(const WeightGradEight& a, bool is_bf16, hipStream_t st);
+// dX [rows, M] = dY [rows, N] W [N, M]; suits: where this is the shorter way
+bool input_grad_suits(int rows, int N, int M);
+hipError_t launch_input_grad(const void* dY, const void* W, void* dX, int rows, int N, int M, bool is_bf16, hipStream_t st);
 
 // projection_kernels.hip: dW [N, M] = dY^T X over `rows` rows, bf16, N and M multiples of 8
 size_t weight_grad_workspace_bytes(int rows, int N, int M);

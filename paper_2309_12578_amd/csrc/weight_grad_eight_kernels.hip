@@ -1,4 +1,4 @@
-// The weight's gradient of a projection whose input was kept in 8 bits (eight_bit.h): dW[n][m] = w[m] * sum over rows of dY[row][n] * code * 2^k,
+// Gradients of a projection whose input was kept in 8 bits (eight_bit.h).  The input's, where it is small: input_grad_kernel.  The weight's: dW[n][m] = w[m] * sum over rows of dY[row][n] * code * 2^k,
 // and beside it the bias' gradient, the column sums of dY.
 //
 // code * 2^k is exact in bf16, so X enters the product as it was kept, without a rounding.  An fp32 dY enters as the sum of three bf16 numbers, its
@@ -473,6 +473,90 @@ __global__ __launch_bounds__(256) void weight_grad_eight_sum_kernel(const float*
     }
 }
 
+// The input's gradient where it is small: dX [rows, M] = dY [rows, N] W [N, M], fp32 sums.  A workgroup has 32 x 32 outputs, its waves an eighth of the sum each, operands
+// straight from the L2s, a run of summands requested while the one before is multiplied.  The waves then add the eighths, in order, of two rows a half each.
+//
+// Where: a tile a compute unit at most, and sums of up to 2048.  The library's product then has 5 - 10 us on the GPU (fp32 and bf16, 255 x 512 x 512 6.7 and 6.9, 1024 x 768 x 256 7.7
+// and 6.9; at some sizes far more, 255 x 576 x 192 104 and 20, 130 x 640 x 128 49 and 11) and 18 on the host, this kernel 7 - 16 in fp32 and 5 - 10 in bf16 (7.4 and 5.2, 11.6
+// and 6.8; 10.4 and 6.7, 10.8 and 7.5) and 3 on the host, which sets the pace of such steps.  Beyond, the library's tiles win: 2000 x 1536 x 512 28 and 11, here 61 and 32.
+constexpr int kInputTile = 32, kInputWaves = 8, kInputTiles = 256, kInputSummands = 2048;
+
+template <typename T>
+__global__ __launch_bounds__(64 * kInputWaves) void input_grad_kernel(const T* __restrict__ dY, const T* __restrict__ W, T* __restrict__ dX, int rows, int N, int M,
+                                                                      int tiles_m) {
+    constexpr int EACH = sizeof(T) == 2 ? 8 : 4, PIECE = 2 * EACH, PIECES = 32 / PIECE;   // summands of a lane, of a piece; pieces of a run of 32
+    __shared__ float part[kInputWaves][16][64];
+    const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row0 = (int)(blockIdx.x / tiles_m) * kInputTile, col0 = (int)(blockIdx.x % tiles_m) * kInputTile, col = min(col0 + (lane & 31), M - 1);
+    const int pieces = (N + PIECE - 1) / PIECE, begin = wave * pieces / kInputWaves * PIECE, end = min(N, (wave + 1) * pieces / kInputWaves * PIECE);
+    const T *const a_row = dY + (size_t)min(row0 + (lane & 31), rows - 1) * N, *const b_column = W + col;
+    struct __attribute__((packed)) Each {
+        T v[EACH];
+    };
+    // A lane has EACH summands in a row of a piece, the other half of the wave the next: as both operands have them so, which ones an instruction takes does not matter.
+    struct Run {
+        T a[PIECES][EACH], b[PIECES][EACH];
+    };
+    auto fetch = [&](Run& r, int at) {
+        if (at + 32 <= end) {   // uniform
+#pragma unroll
+            for (int u = 0; u < PIECES; ++u) {
+                const int k = at + PIECE * u + EACH * half;
+                const Each q = *reinterpret_cast<const Each*>(a_row + k);
+#pragma unroll
+                for (int j = 0; j < EACH; ++j) r.a[u][j] = q.v[j];
+#pragma unroll
+                for (int j = 0; j < EACH; ++j) r.b[u][j] = b_column[(size_t)(k + j) * M];
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < PIECES; ++u)
+#pragma unroll
+                for (int j = 0; j < EACH; ++j) {
+                    const int k = at + PIECE * u + EACH * half + j;
+                    r.a[u][j] = k < end ? a_row[k] : (T)0.f;
+                    r.b[u][j] = k < end ? b_column[(size_t)k * M] : (T)0.f;
+                }
+        }
+    };
+    f32x16 acc;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+    auto multiply = [&](const Run& r) {
+#pragma unroll
+        for (int u = 0; u < PIECES; ++u) {
+            if constexpr (sizeof(T) == 2) {
+                bf16x8 a, b;
+#pragma unroll
+                for (int j = 0; j < EACH; ++j) a[j] = r.a[u][j], b[j] = r.b[u][j];
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc, 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int j = 0; j < EACH; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(r.a[u][j], r.b[u][j], acc, 0, 0, 0);
+            }
+        }
+    };
+    Run x, y;
+    fetch(x, begin);
+    for (int at = begin; at < end; at += 64) {
+        fetch(y, at + 32);
+        multiply(x);
+        fetch(x, at + 64);
+        multiply(y);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) part[wave][i][lane] = acc[i];
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < 16 / kInputWaves; ++n) {
+        const int i = 16 / kInputWaves * wave + n, row = row0 + 8 * (i / 4) + 4 * half + i % 4;
+        float v = part[0][i][lane];
+#pragma unroll
+        for (int w = 1; w < kInputWaves; ++w) v += part[w][i][lane];
+        if (row < rows && col0 + (lane & 31) < M) dX[(size_t)row * M + col] = (T)v;
+    }
+}
+
 // Slices of at least so many rows, and workgroups to aim at: two on a compute unit, or one where bf16 slices would have fewer than 512 rows, whose partial sums take
 // longer than what more of them save (256 and 512: 4096 x 512 x 512 22.3 and 25.5 us, 65536 x 128 x 128 20 and 24, 65536 x 512 x 512 68 and 61; fp32, 8192 x 1536 x 512,
 // 74 and 60).
@@ -548,5 +632,20 @@ static hipError_t launch_t(const WeightGradEight& a, hipStream_t st) {
     return hipGetLastError();
 }
 hipError_t launch_weight_grad_eight(const WeightGradEight& a, bool is_bf16, hipStream_t st) { return is_bf16 ? launch_t<bf16_t>(a, st) : launch_t<float>(a, st); }
+
+static long long input_tiles(int n) { return (n + (long long)kInputTile - 1) / kInputTile; }
+bool input_grad_suits(int rows, int N, int M) { return rows >= 1 && N <= kInputSummands && input_tiles(rows) * input_tiles(M) <= kInputTiles; }
+
+hipError_t launch_input_grad(const void* dY, const void* W, void* dX, int rows, int N, int M, bool is_bf16, hipStream_t st) {
+    const long long tiles_m = input_tiles(M), tiles = input_tiles(rows) * tiles_m;
+    if (tiles > 0x7fffffffll) return hipErrorInvalidValue;
+    auto launch = [&](auto kernel, auto type) {
+        typedef decltype(type) T;
+        kernel<<<dim3((unsigned)tiles), dim3(64 * kInputWaves), 0, st>>>(static_cast<const T*>(dY), static_cast<const T*>(W), static_cast<T*>(dX), rows, N, M, (int)tiles_m);
+    };
+    if (is_bf16) launch(input_grad_kernel<bf16_t>, bf16_t{});
+    else launch(input_grad_kernel<float>, float{});
+    return hipGetLastError();
+}
 
 }  // namespace spion

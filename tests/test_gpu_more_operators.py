@@ -532,7 +532,8 @@ def test_linear_against_the_formula(sp, dtype, rows, M, N, column):
     y = sp.linear8(*leaves, checkpoint=p)
     assert torch.equal(y, torch.nn.functional.linear(x, w, b))
     dx, dw, db = torch.autograd.grad(y, leaves, dy, retain_graph=True)
-    assert torch.equal(dx, torch.mm(dy, w))
+    want = torch.matmul(dy.double(), w.double())
+    _near(dx, want, _weight_tolerance(dy.t(), w, want, dtype, N))
     want = torch.matmul(dy.double().t(), values)
     _near(dw, want, _weight_tolerance(dy, values, want, dtype, rows, 3 if dtype == torch.float32 else 1) + U * want.abs())
     want = dy.double().sum(0)
@@ -541,6 +542,26 @@ def test_linear_against_the_formula(sp, dtype, rows, M, N, column):
     assert all(torch.equal(a, c) for a, c in zip((dx, dw, db), again))   # the same bits every time
     alone, = torch.autograd.grad(y, [w], dy, retain_graph=True)
     assert torch.equal(alone, dw)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,M,N", [(1, 1, 1), (1, 256, 768), (31, 33, 7), (33, 31, 17), (64, 65, 64), (70, 9, 1001), (255, 192, 576), (500, 512, 2048), (512, 512, 130),
+                                      (513, 512, 130), (40, 40, 2049), (8192, 32, 33), (8193, 32, 33)])
+def test_linear_input_gradient(sp, dtype, rows, M, N):
+    """Around where a library product takes over: at the sizes of a tile and of 256 of them, sums of up to 2048 and beyond; what is not finite stays in its row and column."""
+    x, w, dy = _randn((rows, M), dtype, 1).requires_grad_(), _randn((N, M), dtype, 2), _randn((rows, N), dtype, 3)
+    y = sp.linear8(x, w)
+    dx, = torch.autograd.grad(y, x, dy, retain_graph=True)
+    want = torch.matmul(dy.double(), w.double())
+    _near(dx, want, _weight_tolerance(dy.t(), w, want, dtype, N))
+    assert torch.equal(dx, torch.autograd.grad(y, x, dy, retain_graph=True)[0])
+    bad = dy.clone()
+    bad[-1, -1] = math.nan
+    got, = torch.autograd.grad(y, x, bad)
+    assert torch.equal(got[:-1], dx[:-1]) and torch.isnan(got[-1]).all()
+    w[0, -1] = math.inf
+    got, = torch.autograd.grad(sp.linear8(x, w), x, dy)
+    assert torch.equal(got[:, :-1], dx[:, :-1]) and not torch.isfinite(got[:, -1]).any()
 
 
 @pytest.mark.parametrize("dtype", TYPES)
