@@ -76,6 +76,12 @@ double double_arg(PyObject* o) {
     return v;
 }
 
+bool truth_arg(PyObject* o) {
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw python_error();
+    return v == 1;
+}
+
 void* current_stream() { return c10::hip::getCurrentHIPStream().stream(); }
 
 at::Tensor new_like(const at::Tensor& t) {
@@ -1347,7 +1353,7 @@ PyObject* py_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
         args.turns = tensor_arg(a[1]);
         args.axis_of = tensor_arg(a[2]);
         args.axes = long_arg(a[4]);
-        args.neighbours = a[6] == Py_True;
+        args.neighbours = truth_arg(a[6]);
         check_operand(positions, device);
         check_operand(args.turns, device);
         check_operand(args.axis_of, device);

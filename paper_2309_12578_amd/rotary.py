@@ -32,6 +32,7 @@ class RotaryAxes:
         pairs = (self.head_dim // 2,)
         if self.turns.dtype != torch.int64 or self.turns.shape != pairs or self.axis_of.dtype != torch.uint8 or self.axis_of.shape != pairs:
             raise ValueError("turns must be int64, axis_of uint8, both [head_dim / 2]")
+        object.__setattr__(self, "neighbours", bool(self.neighbours))   # (a NumPy truth value, or a number, too)
 
 
 def _turns(frequency: float) -> int:

@@ -202,6 +202,21 @@ def test_rotary_gradient_against_differences(sp):
         assert abs(d - dx[at].double()) <= 16 * U * 2 * (x.abs().max() + 1) * w.abs().max()
 
 
+@pytest.mark.parametrize("yes", [1, np.True_, 7])
+def test_rotary_pairs_neighbours_for_any_truth_value(sp, yes):
+    import dataclasses
+    x, pos = _randn((2, 3, 7, 64), torch.float32, 1).requires_grad_(), torch.arange(7, device="cuda")[None]
+    axes = sp.rotary_axes(64, (32,), neighbours=yes, device="cuda")
+    y = sp.rotary(x, axes, pos)
+    want, made_of = _rotary(x.detach(), dataclasses.replace(axes, neighbours=True), pos, 3)
+    _near(y.detach(), want, _rotary_tolerance(want, made_of, torch.float32))
+    assert not torch.equal(y, sp.rotary(x, dataclasses.replace(axes, neighbours=0), pos))
+    from paper_2309_12578_amd.binding import _native   # as the native call has it, whatever made the axes
+    again = _native().rotary(x, axes.turns, axes.axis_of, pos, 1, None, yes)
+    g = _randn(y.shape, torch.float32, 2)
+    assert torch.equal(again, y) and torch.equal(*[torch.autograd.grad(t, x, g)[0] for t in (y, again)])
+
+
 def test_rotary_past_32_bits(sp):
     axes = sp.rotary_axes(64, (32,), device="cuda")
     room = torch.zeros(2 ** 31 + 2 ** 20, dtype=torch.bfloat16, device="cuda")

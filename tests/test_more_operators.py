@@ -3,6 +3,7 @@ import ctypes
 import math
 from fractions import Fraction
 
+import numpy as np
 import pytest
 import torch
 
@@ -37,6 +38,16 @@ def test_axes_by_their_definition(head_dim, sections, base, ladder, neighbours):
 def test_axes_that_are_refused(arguments):
     with pytest.raises(ValueError):
         sp.rotary_axes(**arguments)
+
+
+@pytest.mark.parametrize("yes,no", [(True, False), (1, 0), (np.True_, np.False_), (torch.tensor(True), torch.tensor(0))])
+def test_pairing_by_any_truth_value(yes, no):
+    for given, want in ((yes, True), (no, False)):
+        axes = sp.rotary_axes(64, (32,), neighbours=given)
+        assert axes.neighbours is want and sp.RotaryAxes(64, 1, axes.turns, axes.axis_of, given).neighbours is want
+        assert sp.SparseMHA(64, 1, rotary=axes).rotary.neighbours is want
+    with pytest.raises(ValueError):
+        sp.rotary_axes(64, (32,), neighbours=np.zeros(2))
 
 
 def test_axes_and_packed_rows_are_looked_at():
