@@ -1607,7 +1607,7 @@ PyObject* py_rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::Tensor &x = tensor_arg(a[0]), &w = tensor_arg(a[1]);
         const at::Tensor residual = optional_arg(a[2]);
         const NormArgs args(x, w, residual, a[3]);
-        const bool checkpoint = PyObject_IsTrue(a[4]) == 1;
+        const bool checkpoint = truth_arg(a[4]);
         const c10::DeviceGuard guard(x.device());
         const bool grad = residual.defined() ? torch::autograd::compute_requires_grad(x, w, residual) : torch::autograd::compute_requires_grad(x, w);
         at::Tensor y = new_like(args.x), h, rstd;

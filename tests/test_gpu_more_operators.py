@@ -1024,6 +1024,14 @@ def test_calls_that_are_refused(sp):
             print("call %d was taken" % i)
 
 
+def test_norm_takes_any_truth_value_for_its_checkpoint(sp):
+    x, w = _randn((4, 64), torch.float32, 1), _randn((64,), torch.float32, 2)
+    for yes, no in ((True, False), (1, None), (np.True_, np.False_)):
+        assert sp.rms_norm(x, w, checkpoint=yes)[2] is not None and sp.rms_norm(x, w, checkpoint=no)[2] is None
+    with pytest.raises(ValueError):   # as Python's own `if`
+        sp.rms_norm(x, w, checkpoint=np.zeros(2))
+
+
 def test_gradients_that_are_refused(sp):
     inputs, _ = _steps(sp, torch.float32)
     x, a, w, r, W, b, g = inputs(1)
