@@ -61,14 +61,18 @@ class _Projection(nn.Linear):
         return super().forward(x) if y is None else y
 
 
+def _runs(module: nn.Module, forward) -> bool:
+    """Whether a call of the module runs that forward, neither a subclass's nor one set on the instance."""
+    return getattr(type(module), "forward", None) is forward and "forward" not in module.__dict__
+
+
 def _hands_on(projection: nn.Module) -> bool:
     """Whether code other than _Projection's is handed the projection's input or output (a hook, another forward): it may
     change them in place, also where no version counter tells, while the attention beside it has saved them."""
-    if getattr(type(projection), "forward", None) is not _Projection.forward:
+    if not _runs(projection, _Projection.forward):
         return True
     d = projection.__dict__
-    return bool(d["_forward_pre_hooks"] or d["_forward_hooks"] or "forward" in d or
-                _module._global_forward_pre_hooks or _module._global_forward_hooks)
+    return bool(d["_forward_pre_hooks"] or d["_forward_hooks"] or _module._global_forward_pre_hooks or _module._global_forward_hooks)
 
 
 class SparseMHA(nn.Module):
@@ -143,8 +147,9 @@ class SparseMHA(nn.Module):
             raise ValueError("flags are not supported together with a bias, lengths or dropout")
         S, R, checkpoint = None, E, None
         if isinstance(norm, _RmsNorm):
-            # a hook, or another forward, may change what the norm's codes stand for before the projection has it
-            shares = w_qkv.eight_bit and torch.is_grad_enabled() and not _hands_on(w_qkv) and not norm._forward_hooks
+            # a hook, or another forward, may change what the norm's codes stand for before the projection has it (global hooks: _hands_on)
+            shares = (w_qkv.eight_bit and torch.is_grad_enabled() and not _hands_on(w_qkv) and not norm._forward_hooks and
+                      _runs(norm, _RmsNorm.forward))
             X, h, checkpoint = norm(E, residual, shares)
             R = E if residual is None else h
         elif residual is not None:

@@ -888,6 +888,40 @@ def test_sub_layer_whose_norm_is_watched(sp, dtype, eight):
         sp.SparseMHA(128, 2, norm="rms", device="cuda", dtype=dtype)(E, pattern, positions=given["positions"])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("how", ["instance", "subclass", "global hook"])
+def test_sub_layer_whose_norm_is_another(sp, dtype, eight, how):
+    """A forward that changes the norm's result and hands on its codes: the projection keeps what it was handed, as if the norm's weight were twice as large."""
+    m, (E, R, *_), (pattern, _, _, given, gb), _ = _everything(sp, dtype, eight)
+    m.eval()
+    run = lambda: m(E, pattern, lengths=given["lengths"], positions=given["positions"], residual=R)[0]
+    own, kind = m.norm.forward, type(m.norm)
+
+    def doubled(*args, **kw):
+        out = own(*args, **kw)
+        return (out[0] * 2.0, *out[1:])
+    if how == "instance":
+        m.norm.forward = doubled
+    elif how == "subclass":
+        m.norm.__class__ = type("Doubled", (kind,), {"forward": lambda self, *args, **kw: doubled(*args, **kw)})
+    else:
+        hook = torch.nn.modules.module.register_module_forward_hook(
+            lambda mod, args, out: (out[0] * 2.0, *out[1:]) if mod is m.norm else None)
+    try:
+        dw, = torch.autograd.grad(run(), m.w_qkv.weight, gb)
+    finally:
+        if how == "global hook":
+            hook.remove()
+    m.norm.__dict__.pop("forward", None)
+    m.norm.__class__ = kind
+    with torch.no_grad():
+        m.norm.weight.mul_(2.0)
+    want, = torch.autograd.grad(run(), m.w_qkv.weight, gb)
+    # two ways to 8 bits, each with roundings of up to 2^-8 of a group's largest element
+    assert (dw.double() - want.double()).norm() <= (2 ** -6 if eight else 1e-5) * want.double().norm()
+
+
 def test_sub_layers_under_autocast(sp):
     """The stream stays in its type, the branch joins it."""
     pattern = _pattern(sp, _mask(4, 2), 32)
