@@ -148,8 +148,8 @@ class SparseMHA(nn.Module):
         S, R, checkpoint = None, E, None
         if isinstance(norm, _RmsNorm):
             # a hook, or another forward, may change what the norm's codes stand for before the projection has it (global hooks: _hands_on)
-            shares = (w_qkv.eight_bit and torch.is_grad_enabled() and not _hands_on(w_qkv) and not norm._forward_hooks and
-                      _runs(norm, _RmsNorm.forward))
+            shares = (not _hands_on(w_qkv) and w_qkv.eight_bit and torch.is_grad_enabled() and not norm._forward_hooks and
+                      _runs(norm, _RmsNorm.forward))   # (_hands_on first: the module in w_qkv's place may be any)
             X, h, checkpoint = norm(E, residual, shares)
             R = E if residual is None else h
         elif residual is not None:

@@ -922,6 +922,21 @@ def test_sub_layer_whose_norm_is_another(sp, dtype, eight, how):
     assert (dw.double() - want.double()).norm() <= (2 ** -6 if eight else 1e-5) * want.double().norm()
 
 
+@pytest.mark.parametrize("eight", [False, True])
+def test_sub_layer_whose_projection_is_another_module(sp, eight):
+    m, (E, R, *_), (pattern, _, _, given, gb), _ = _everything(sp, torch.float32, eight)
+    m.eval()
+    run = lambda: m(E, pattern, lengths=given["lengths"], positions=given["positions"], residual=R)
+    want, own = [t.detach() for t in run()], m.w_qkv
+    m.w_qkv = torch.nn.Linear(128, 384, device="cuda")
+    m.w_qkv.load_state_dict(own.state_dict())
+    got = run()
+    # fp32 with codes: x + residual is not rounded to 24 bits before it is squared and multiplied, without codes it is
+    assert torch.equal(got[1], want[1]) and (got[0].double() - want[0].double()).norm() <= 1e-5 * want[0].double().norm()
+    dw, = torch.autograd.grad(got[0], m.w_qkv.weight, gb)
+    assert dw.shape == (384, 128) and dw.any()
+
+
 def test_sub_layers_under_autocast(sp):
     """The stream stays in its type, the branch joins it."""
     pattern = _pattern(sp, _mask(4, 2), 32)
