@@ -79,7 +79,7 @@ def rms_norm8(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Te
 def linear8(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, checkpoint: Optional[Packed8] = None) -> torch.Tensor:
     """x weight^T + bias (bf16 or fp32, one type), whose graph keeps x in 8 bits: the weight's gradient is made from the codes, x's and the bias'
     are not touched by it.  checkpoint: codes that stand for x already, such as those of the norm before (the caller's word for it; shapes are
-    looked at); without it x is packed, if the weight needs a gradient."""
+    looked at); without it x is packed, if the weight needs a gradient.  Autocast changes no types here (SparseMHA casts for it)."""
     c = (None, None, None) if checkpoint is None else (checkpoint.codes, checkpoint.exponents, checkpoint.weight)
     if checkpoint is not None and checkpoint.size != (x.shape or (0,))[-1]:   # (the other sizes are the codes')
         raise ValueError("the checkpoint must have x's shape")

@@ -6,6 +6,7 @@ and lines 4-7 of Algorithm 5 (SDDMM, sparse softmax, SpMM for every head) are on
 """
 from __future__ import annotations
 
+import dataclasses
 from typing import Optional
 
 import torch
@@ -54,7 +55,13 @@ class _Projection(nn.Linear):
 
     def forward(self, x: torch.Tensor, checkpoint: Optional[Packed8] = None) -> torch.Tensor:
         if self.eight_bit:
-            return linear8(x, self.weight, self.bias, checkpoint)
+            weight, bias = self.weight, self.bias
+            if torch.is_autocast_enabled():   # in autocast's type, as nn.Linear; linear8 takes its operands' own
+                dtype = torch.get_autocast_dtype("cuda")
+                x, weight, bias = x.to(dtype), weight.to(dtype), None if bias is None else bias.to(dtype)
+                if checkpoint is not None and checkpoint.weight is not None:   # (a rounding of the codes' factors, 2^-9 of them in bf16, beside the codes' own 2^-8)
+                    checkpoint = dataclasses.replace(checkpoint, weight=checkpoint.weight.to(dtype))
+            return linear8(x, weight, bias, checkpoint)
         y = None
         if x.is_cuda and not torch.compiler.is_compiling():
             y = (_b._host or _b._native()).projection(x, self.weight, self.bias)

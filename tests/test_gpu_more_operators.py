@@ -957,6 +957,44 @@ def test_sub_layers_under_autocast(sp):
             m(E.bfloat16(), pattern)
 
 
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_sub_layer_in_8_bits_under_autocast(sp, norm, dtype):
+    """The projection runs in autocast's type as it does without the option, and what the graph keeps is no larger."""
+    pattern = _pattern(sp, _mask(4, 2), 32)
+    torch.manual_seed(1)
+    plain, eight = [sp.SparseMHA(128, 2, norm=norm, bias=True, rotary=sp.rotary_axes(64, (32,)), eight_bit=e, device="cuda", dtype=dtype) for e in (False, True)]
+    eight.load_state_dict(plain.state_dict())
+    with torch.no_grad():
+        for m in (plain, eight):
+            m.norm.weight.copy_(1 + 0.2 * _randn((128,), torch.float32, 3))
+    E, g = _randn((2, 128, 128), dtype, 1).requires_grad_(), _randn((2, 128, 128), torch.float32, 2)
+    results = []
+    for m in (plain, eight):
+        kept, types = {}, []
+
+        def keep(t):
+            kept[t.data_ptr()] = t.untyped_storage().nbytes()
+            assert t.numel() != 3 * E.numel() or t.dtype == torch.bfloat16
+            return t
+        with torch.autocast("cuda", dtype=torch.bfloat16):
+            with torch.autograd.graph.saved_tensors_hooks(keep, lambda t: t):
+                y = m(E, pattern)
+            results.append([y.detach(), *torch.autograd.grad(y, [E, *m.parameters()], g.to(y.dtype))])
+            hook = m.w_qkv.register_forward_hook(lambda mod, args, out: types.append(out.dtype))
+            m(E, pattern)
+            hook.remove()
+        assert types == [torch.bfloat16]
+        results[-1].append(sum(kept.values()))
+    kept, more = results[1].pop(), results[0].pop()
+    assert kept <= more
+    assert all(a.dtype == b.dtype and (a.double() - b.double()).norm() <= 2e-2 * b.double().norm() for a, b in zip(results[1], results[0]))
+    with torch.autocast("cuda", dtype=torch.float16), pytest.raises(ValueError):   # a type that the operators do not have
+        eight(E, pattern)
+    with torch.autocast("cuda", enabled=False):
+        assert eight(E, pattern).dtype == dtype
+
+
 def test_what_the_sub_layer_keeps(sp):
     """The norm's input and output, 4 bytes an element in bf16, are one byte and a little."""
     pattern = _pattern(sp, _mask(8, 2), 64)
