@@ -1770,6 +1770,7 @@ PyObject* py_linear8(PyObject*, PyObject* const* a, Py_ssize_t n) {
             at::NoGradGuard no_grad;
             const c10::impl::ExcludeDispatchKeyGuard no_autocast(c10::autocast_dispatch_keyset);
             y = at::linear(x, w, b.defined() ? std::optional<at::Tensor>(b) : std::nullopt);
+            if (y.is_view()) y = at::_unsafe_view(y, y.sizes());   // (of a product of matrices that is nobody else's: one made here may not be changed in place)
             if (keeps && !c.defined()) {
                 const at::Tensor xc = x.contiguous();
                 eight = Eight(xc);

@@ -663,6 +663,22 @@ def test_linear_asked_for_some_gradients_only(sp):
     assert y.shape == (0, 24) and dx.shape == (0, 70) and not dw.any() and not db.any()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lead", [(), (5,), (2, 5), (2, 3, 5)])
+@pytest.mark.parametrize("bias", [False, True])
+def test_linear_changed_in_place(sp, dtype, lead, bias):
+    """As torch's: its gradients do not go by the result."""
+    x, W, g = [_randn(s, dtype, k).requires_grad_(k < 2) for k, s in enumerate([(*lead, 64), (8, 64), (*lead, 8)])]
+    b = _randn((8,), dtype, 3).requires_grad_() if bias else None
+    leaves = [x, W] + ([b] if bias else [])
+    y = sp.linear8(x, W, b)
+    assert not y._is_view()
+    want = torch.autograd.grad(torch.relu(y), leaves, g)
+    y = sp.linear8(x, W, b)
+    torch.relu_(y)
+    assert all(torch.equal(p, q) for p, q in zip(torch.autograd.grad(y, leaves, g), want))
+
+
 def test_linear_past_32_bits(sp):
     rows, M = 2 ** 20 + 2 ** 10, 2048   # 2^31 codes and more; dY as many elements
     x = torch.zeros((rows, M), dtype=torch.bfloat16, device="cuda")
