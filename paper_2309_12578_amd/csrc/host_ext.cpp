@@ -668,6 +668,13 @@ PyObject* py_residual(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// x w^T + b, without gradients.  A view of the product (of matrices, which is nobody else's) becomes a tensor of its own: one made here may not be
+// changed in place.
+at::Tensor linear_of(const at::Tensor& x, const at::Tensor& w, const at::Tensor& b) {
+    const at::Tensor y = at::linear(x, w, b.defined() ? std::optional<at::Tensor>(b) : std::nullopt);
+    return y.is_view() ? at::_unsafe_view(y, y.sizes()) : y;
+}
+
 // projection(X, W, b | None) -> X W^T + b with the node above, or None where torch's own operator is to be called:
 // nothing to differentiate, types or sizes the kernel does not take, or more than plain tensors in play.  Weights of
 // more than 2^20 elements are torch's: with that many output tiles its product fills the machine.  Weight gradient,
@@ -690,7 +697,7 @@ PyObject* py_projection(PyObject*, PyObject* const* a, Py_ssize_t n) {
         at::Tensor y;
         {
             at::NoGradGuard no_grad;
-            y = at::linear(x, w, b.defined() ? std::optional<at::Tensor>(b) : std::nullopt);
+            y = linear_of(x, w, b);
         }
         auto node = std::shared_ptr<ProjectionBackward>(new ProjectionBackward(), torch::autograd::deleteNode);
         node->has_bias = b.defined();
@@ -1769,8 +1776,7 @@ PyObject* py_linear8(PyObject*, PyObject* const* a, Py_ssize_t n) {
         {
             at::NoGradGuard no_grad;
             const c10::impl::ExcludeDispatchKeyGuard no_autocast(c10::autocast_dispatch_keyset);
-            y = at::linear(x, w, b.defined() ? std::optional<at::Tensor>(b) : std::nullopt);
-            if (y.is_view()) y = at::_unsafe_view(y, y.sizes());   // (of a product of matrices that is nobody else's: one made here may not be changed in place)
+            y = linear_of(x, w, b);
             if (keeps && !c.defined()) {
                 const at::Tensor xc = x.contiguous();
                 eight = Eight(xc);

@@ -953,6 +953,24 @@ def test_sub_layer_whose_projection_is_another_module(sp, eight):
     assert dw.shape == (384, 128) and dw.any()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("eight", [False, True])
+def test_sub_layer_whose_projections_are_changed_in_place(sp, dtype, eight):
+    """By hooks, as torch's own module lets them."""
+    m, (E, R, *_), (pattern, _, _, given, gb), _ = _everything(sp, dtype, eight)
+    m.eval()
+    run = lambda: m(E, pattern, lengths=given["lengths"], positions=given["positions"], residual=R)[0]
+
+    def of(change):
+        hooks = [p.register_forward_hook(lambda mod, args, out: change(out)) for p in (m.w_qkv, m.w_o)]
+        y = run()
+        grads = torch.autograd.grad(y, list(m.parameters()), gb, allow_unused=True)
+        for h in hooks:
+            h.remove()
+        return [y.detach(), *grads]
+    assert all(torch.equal(a, b) for a, b in zip(of(lambda t: t.mul_(2.0)), of(lambda t: t * 2.0)))
+
+
 def test_sub_layers_under_autocast(sp):
     """The stream stays in its type, the branch joins it."""
     pattern = _pattern(sp, _mask(4, 2), 32)
