@@ -114,7 +114,11 @@ __global__ __launch_bounds__(RowThreads<LANES>::threads) void rms_norm_kernel(co
                                                                               const T* __restrict__ w, T* __restrict__ y, T* __restrict__ h,
                                                                               float* __restrict__ rstd, signed char* __restrict__ codes,
                                                                               uint8_t* __restrict__ exponents, long long rows, int D, double eps) {
-    typedef std::conditional_t<(CODES != kNoCodes && sizeof(T) == 4), double, float> S;   // (a sum of two bf16 numbers is exact in fp32, or off by 2^-24)
+    typedef std::conditional_t<(CODES != kNoCodes && sizeof(T) == 4), double, float> S;
+    // Of two bf16 numbers a sum is exact in fp32 unless they are some 17 binary orders apart (of normal data one element in 10^5).  Where codes are decided, a wave
+    // that has such an element takes its squares again, and that element's chunk its codes, from sums in 64 bits (16384 x 256 8.5 us, without that 7.6; 65536 x 4096 the
+    // same).
+    constexpr bool SUMS = CODES != kNoCodes && sizeof(T) == 2;
     constexpr int ROWS = RowThreads<LANES>::rows;
     __shared__ double shared[4][LANES > 64 ? LANES / 64 : 1];
     const int lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
@@ -140,13 +144,33 @@ __global__ __launch_bounds__(RowThreads<LANES>::threads) void rms_norm_kernel(co
         for (int k = 0; k < K; ++k) wv[k].opaque();   // else the weights are kept in fp32
         S s[K][8];
         double squares = 0.0;
+        unsigned rounded = 0;   // (of the wave) chunks with sums that fp32 does not hold
 #pragma unroll
-        for (int k = 0; k < K; ++k)
+        for (int k = 0; k < K; ++k) {
+            unsigned lost = 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 s[k][i] = residual ? (S)a[k].at(i) + (S)r[k].at(i) : (S)a[k].at(i);
+                if constexpr (SUMS)
+                    if (residual)
+                        lost |= __builtin_bit_cast(unsigned, (s[k][i] - a[k].at(i)) - r[k].at(i)) | __builtin_bit_cast(unsigned, (s[k][i] - r[k].at(i)) - a[k].at(i));
                 squares = fma((double)s[k][i], (double)s[k][i], squares);
             }
+            if (SUMS && __any(lost != 0)) rounded |= 1u << k;
+        }
+        if (SUMS && rounded) {
+            squares = 0.0;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                a[k].opaque();   // (else their numbers are kept in fp32)
+                r[k].opaque();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const double sum = (double)a[k].at(i) + (double)r[k].at(i);
+                    squares = fma(sum, sum, squares);
+                }
+            }
+        }
         if (first + step < rows) fetch(row + step);   // uniform
         const double inverse = inverse_root(row_sum<LANES>(squares, shared, turn) / D + eps);
         if (lane == 0 && has && rstd) rstd[row] = (float)inverse;
@@ -178,14 +202,23 @@ __global__ __launch_bounds__(RowThreads<LANES>::threads) void rms_norm_kernel(co
                 int exponent = group_exponent(exponent_byte(most));
                 Codes8 q;
                 unsure = !codes_of(q, z, exponent) || unsure;
-                if (__any(unsure)) {   // some 3 waves in 100
+                if (__any(unsure) || rounded >> k & 1) {   // some 3 waves in 100
                     double exact[8], largest = 0.0;
                     bool finite = true;
+                    Chunk<T> again_a, again_r;
+                    if (SUMS && residual) {   // (by now a and r are another row's)
+                        request<WHOLE>(again_a, x + min(row, rows - 1) * D, c, D);
+                        request<WHOLE>(again_r, residual + min(row, rows - 1) * D, c, D);
+                    }
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        S again = s[k][i];
-                        asm volatile("" : "+v"(again));   // else what the squares were made of is kept in 64 bits
-                        exact[i] = (double)again * inverse;
+                        if (SUMS && residual) {
+                            exact[i] = ((double)again_a.at(i) + (double)again_r.at(i)) * inverse;
+                        } else {
+                            S again = s[k][i];
+                            asm volatile("" : "+v"(again));   // else what the squares were made of is kept in 64 bits
+                            exact[i] = (double)again * inverse;
+                        }
                         if constexpr (CODES == kCodesOfY) exact[i] *= (double)wv[k].at(i);
                         largest = fmax(largest, fabs(exact[i]));
                         finite = finite && exact[i] == exact[i];

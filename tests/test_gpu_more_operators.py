@@ -403,6 +403,54 @@ def test_norm_codes_of_large_and_small_rows(sp, dtype, scale, weight):
         assert torch.equal(p.codes, codes) and torch.equal(p.exponents, exponents)
 
 
+def _row_of_mean_square_one():
+    """64 multiples of 1/128 with 8 bits each, whose squares' mean is 1 and whose first, 129/128, lies midway between two codes (of 1/64)."""
+    rest, row = 64 * 128 ** 2 - 129 ** 2, [129]
+    for left in range(63, 4, -1):
+        row.append(math.isqrt(rest // left))
+        rest -= row[-1] ** 2
+    for a in range(128, -1, -1):   # four squares make the rest
+        for b in range(math.isqrt(rest - a * a), -1, -1):
+            for c in range(math.isqrt(rest - a * a - b * b), -1, -1):
+                d = math.isqrt(rest - a * a - b * b - c * c)
+                if a * a + b * b + c * c + d * d == rest and max(b, c, d) < 200:
+                    return torch.tensor(row + [a, b, c, d], dtype=torch.float64) / 128
+
+
+@pytest.mark.parametrize("D", [64, 256, 1024, 4096, 16384])
+def test_norm_codes_of_sums_that_fp32_does_not_hold(sp, D):
+    """x + residual of two bf16 numbers far apart decides a tie: by what 64 bits hold of it."""
+    row = _row_of_mean_square_one()
+    assert float(row.square().sum()) == 64.0 and float(row.max()) <= 127 / 64 and torch.equal(row.bfloat16().double(), row)
+    x = row.bfloat16().cuda().repeat(D // 64).repeat(4, 1)
+    r = torch.zeros_like(x)
+    r[1, ::64], r[2, ::64] = 2.0 ** -26, -2.0 ** -26
+    r[3, D - 64] = 2.0 ** -26
+    x = torch.cat([x, r])   # the small ones in either operand
+    r = torch.cat([r, x[:4]])
+    w = torch.ones(D, dtype=torch.bfloat16, device="cuda")
+    codes, exponents, _ = _eight(_norm(x, w, r, 0.0)[2])
+    assert codes[:3, 0].tolist() == [64, 65, 64] and codes[3, D - 64] == 65
+    p = sp.rms_norm(x, w, r, 0.0, checkpoint=True)[2]
+    assert torch.equal(p.codes, codes) and torch.equal(p.exponents, exponents)
+    p, _ = sp.rms_norm8(x, w, r, 0.0)
+    assert torch.equal(p.codes, codes) and torch.equal(p.exponents, exponents)
+
+
+@pytest.mark.parametrize("D", [64, 100, 1024, 5000])
+def test_norm_codes_of_operands_of_all_magnitudes(sp, D):
+    of = torch.Generator("cuda").manual_seed(D)
+    x, r = [(torch.randn((2 ** 22 // D, D), generator=of, device="cuda") * torch.exp2(torch.randint(-20, 21, (2 ** 22 // D, D), generator=of, device="cuda").float())).bfloat16()
+            for _ in range(2)]
+    w = _randn((D,), torch.bfloat16, 3)
+    _, _, z, y = _norm(x, w, r)
+    y8, h, p = sp.rms_norm(x, w, r, EPS, checkpoint=True)
+    assert torch.equal(h, (x.double() + r.double()).bfloat16())
+    for p, want in ((p, z), (sp.rms_norm8(x, w, r, EPS)[0], y)):
+        codes, exponents, _ = _eight(want)
+        assert torch.equal(p.codes, codes) and torch.equal(p.exponents, exponents)
+
+
 def test_norm_gradients_against_differences(sp):
     x, w, r = [_randn(s, torch.float32, i).requires_grad_() for i, s in enumerate([(3, 70), (70,), (3, 70)])]
     a, b = _randn((3, 70), torch.float32, 8), _randn((3, 70), torch.float32, 9)
