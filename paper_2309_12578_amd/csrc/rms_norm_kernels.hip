@@ -173,6 +173,8 @@ __global__ __launch_bounds__(RowThreads<LANES>::threads) void rms_norm_kernel(co
         }
         if (first + step < rows) fetch(row + step);   // uniform
         const double inverse = inverse_root(row_sum<LANES>(squares, shared, turn) / D + eps);
+        // else fp32 holds it with fewer bits, or (a row that is not finite, or 0) not at all
+        const bool held = inverse >= 0x1p-126 && inverse <= (double)kMost;
         if (lane == 0 && has && rstd) rstd[row] = (float)inverse;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
@@ -187,8 +189,17 @@ __global__ __launch_bounds__(RowThreads<LANES>::threads) void rms_norm_kernel(co
             float z[8], most = 0.f;
             bool unsure = false;
 #pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] = (float)s[k][i] * (float)inverse;
+            if (__any(!held)) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    S again = s[k][i];
+                    asm volatile("" : "+v"(again));   // else what the squares were made of is kept in 64 bits
+                    z[i] = held ? z[i] : (float)((double)again * inverse);
+                }
+            }
+#pragma unroll
             for (int i = 0; i < 8; ++i) {
-                z[i] = (float)s[k][i] * (float)inverse;
                 v[i] = z[i] * wv[k].at(i);
                 if constexpr (CODES == kCodesOfY) {
                     z[i] = v[i];
@@ -197,8 +208,7 @@ __global__ __launch_bounds__(RowThreads<LANES>::threads) void rms_norm_kernel(co
                 most = fmaxf(most, fabsf(z[i]));
             }
             if constexpr (CODES != kNoCodes) {
-                // a row that is not finite has no finite 1 / rms, or 0; below 2^-126 fp32 holds it with fewer bits
-                unsure = unsure || !(inverse >= 0x1p-126 && inverse <= (double)kMost) || near_border(most);
+                unsure = unsure || !held || near_border(most);
                 int exponent = group_exponent(exponent_byte(most));
                 Codes8 q;
                 unsure = !codes_of(q, z, exponent) || unsure;
@@ -216,7 +226,7 @@ __global__ __launch_bounds__(RowThreads<LANES>::threads) void rms_norm_kernel(co
                             exact[i] = ((double)again_a.at(i) + (double)again_r.at(i)) * inverse;
                         } else {
                             S again = s[k][i];
-                            asm volatile("" : "+v"(again));   // else what the squares were made of is kept in 64 bits
+                            asm volatile("" : "+v"(again));   // (as above)
                             exact[i] = (double)again * inverse;
                         }
                         if constexpr (CODES == kCodesOfY) exact[i] *= (double)wv[k].at(i);

@@ -403,6 +403,23 @@ def test_norm_codes_of_large_and_small_rows(sp, dtype, scale, weight):
         assert torch.equal(p.codes, codes) and torch.equal(p.exponents, exponents)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [64, 100, 3000, 8192])
+@pytest.mark.parametrize("top", [2.0 ** -127, 2.0 ** -130, 2.0 ** -126, 2.0 ** 126, 2.0 ** 127])
+def test_norm_of_rows_whose_inverse_leaves_fp32(sp, dtype, D, top):
+    """Rows of subnormal numbers, and next to the largest: y is of ordinary size.  Some ordinary rows between them."""
+    x = torch.rand((9, D), generator=torch.Generator("cuda").manual_seed(1), device="cuda", dtype=torch.float64) * 1.9
+    x[::2] *= top
+    x, w = x.to(dtype), _randn((D,), dtype, 2)
+    for residual in (None, torch.zeros_like(x)):
+        for checkpoint in (False, True):
+            y, h, _ = sp.rms_norm(x, w, residual, 0.0, checkpoint)
+            want = _norm(x, w, residual, 0.0)[3]
+            assert torch.isfinite(want).all() and (h is None or torch.equal(h, x))
+            # z: three roundings, or one in 64 bits' place; the product with the weight
+            _near(y, want, half(dtype) * want.abs() + 4 * U * want.abs() + torch.finfo(torch.float32).tiny * torch.finfo(torch.float32).eps)
+
+
 def _row_of_mean_square_one():
     """64 multiples of 1/128 with 8 bits each, whose squares' mean is 1 and whose first, 129/128, lies midway between two codes (of 1/64)."""
     rest, row = 64 * 128 ** 2 - 129 ** 2, [129]
