@@ -536,8 +536,8 @@ hipError_t backward_t(const RmsNormGrad& a, hipStream_t st) {
 }
 
 // A chunk a thread, so that memory is met in order (65536 x 4096 to bf16, 8192 workgroups that go round, a chunk a thread at once 153 us, four 214; 65536 x 2048 from fp32
-// 129, so 115), up to 2^24 workgroups.
-unsigned chunk_grid(long long chunks) { return (unsigned)std::min<long long>((chunks + 255) / 256, 1 << 24); }
+// 129, so 115), up to the threads that a launch can have, 2^32 - 1.
+unsigned chunk_grid(long long chunks) { return (unsigned)std::min<long long>((chunks + 255) / 256, (1 << 24) - 1); }
 
 }  // namespace
 

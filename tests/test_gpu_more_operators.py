@@ -320,6 +320,22 @@ def test_eight_bits_past_32_bits(sp):
     assert torch.equal(y[-5:], x[-5:]) and not y[:5].any() and not p.codes[2 ** 20].any()
 
 
+def test_eight_bits_of_more_chunks_than_a_launch_has_threads(sp):
+    rows, D = 2 ** 15, 2 ** 20   # 2^32 chunks of 8
+    x = torch.ones((rows, D), dtype=torch.bfloat16, device="cuda")
+    x[0, ::3], x[-1, 1::5], x[-1, -64:] = -0.5, 0.25, 3.0
+    codes, exponents = torch.empty((rows, D), dtype=torch.int8, device="cuda"), torch.empty((rows, D // 64), dtype=torch.uint8, device="cuda")
+    sp.spion_pack_eight(x, codes, exponents, rows, D, sp.SPION_BF16)
+    ends = x[[0, -1]]
+    want = _eight(ends.double())
+    assert torch.equal(codes[[0, -1]], want[0]) and torch.equal(exponents[[0, -1]], want[1])
+    between = lambda t, v: all(bool((t[i:min(i + 1024, rows - 1)] == v).all()) for i in range(1, rows - 1, 1024))
+    assert between(codes, 64) and between(exponents, 121)
+    x.zero_()
+    sp.spion_unpack_eight(codes, exponents, None, x, rows, D, sp.SPION_BF16)
+    assert torch.equal(x[[0, -1]], ends) and between(x, 1.0)
+
+
 # ------------------------------------------------------------------------------------------------
 # root-mean-square norm
 # ------------------------------------------------------------------------------------------------
