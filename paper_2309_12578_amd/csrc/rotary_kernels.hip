@@ -18,7 +18,7 @@ namespace {
 
 constexpr int kRotaryTable = 2048, kRotaryTokens = 128;   // pairs of cosine and sine, and tokens, that a workgroup has room for
 
-// Of an eighth of a turn at most, either way, given in 2^-64 turns: the series, whose next terms are below 2^-29 of the results there.
+// Of an eighth of a turn at most, either way, given in 2^-64 turns: the series, whose next terms are below 2^-28.5 of the results there.
 __device__ __forceinline__ void sine_cosine(float turns, float& sine, float& cosine) {
     const float t = turns * 3.4061215800098876e-19f;   // 2 pi / 2^64
     const float q = t * t;
@@ -35,11 +35,11 @@ __device__ __forceinline__ void turn_pair(float& a, float& b, float2 u) {
 
 template <typename T, bool NEIGHBOURS>
 __global__ __launch_bounds__(256) void rotary_kernel(const T* __restrict__ x, T* __restrict__ y, const RotaryShape s, const long long* __restrict__ turns,
-                                                     const uint8_t* __restrict__ axis, const void* __restrict__ positions, int tokens) {
+                                                     const uint8_t* __restrict__ axis, const void* __restrict__ positions, int tokens, unsigned begin) {
     __shared__ float2 table[kRotaryTable];
     __shared__ long long place[kRotaryTokens][2];   // of the tokens in x and y
     const int pairs = s.d / 2, tid = threadIdx.x;
-    const unsigned first = blockIdx.x * (unsigned)tokens, total = (unsigned)s.B * (unsigned)s.L;   // (below 2^31)
+    const unsigned first = begin + blockIdx.x * (unsigned)tokens, total = (unsigned)s.B * (unsigned)s.L;   // (below 2^31)
     const int here = (int)min((unsigned)tokens, total - first);
     // A thread has every 256th of what follows, by numbers that are carried: no divisions.
     {
@@ -134,10 +134,12 @@ hipError_t launch_rotary(const void* x, void* y, const RotaryShape& s, const lon
     int tokens = std::min(kRotaryTokens, kRotaryTable / (s.d / 2));
     while (tokens > 1 && (total / tokens < 1024 || (long long)tokens * s.N * (s.d / 16) > most)) tokens /= 2;
     const long long grid = (total + tokens - 1) / tokens;
-    if (grid > 0x7fffffffll) return hipErrorInvalidValue;
+    constexpr long long kMostGroups = 1 << 23;   // of a launch, which can have 2^32 - 1 threads
     auto launch = [&](auto kernel, auto type) {
         typedef decltype(type) T;
-        kernel<<<dim3((unsigned)grid), dim3(256), 0, st>>>(static_cast<const T*>(x), static_cast<T*>(y), s, turns, axis, positions, tokens);
+        for (long long g = 0; g < grid; g += kMostGroups)
+            kernel<<<dim3((unsigned)std::min(grid - g, kMostGroups)), dim3(256), 0, st>>>(static_cast<const T*>(x), static_cast<T*>(y), s, turns, axis, positions, tokens,
+                                                                                         (unsigned)(g * tokens));
     };
     if (is_bf16) s.neighbours ? launch(rotary_kernel<bf16_t, true>, bf16_t{}) : launch(rotary_kernel<bf16_t, false>, bf16_t{});
     else s.neighbours ? launch(rotary_kernel<float, true>, float{}) : launch(rotary_kernel<float, false>, float{});

@@ -217,6 +217,23 @@ def test_rotary_pairs_neighbours_for_any_truth_value(sp, yes):
     assert torch.equal(again, y) and torch.equal(*[torch.autograd.grad(t, x, g)[0] for t in (y, again)])
 
 
+def test_rotary_of_more_tokens_than_a_launch_has_groups(sp):
+    B, L, d = 2, 2 ** 30 - 1, 16   # all but 2^31 tokens, 128 a workgroup
+    axes = sp.rotary_axes(d, (8,), device="cuda")
+    x = _randn((1, 1, 1, d), torch.bfloat16, 1).expand(B, 1, L, d)
+    n = 1000
+    pos = (torch.arange(n, dtype=torch.int32, device="cuda") * 7 - 3000).repeat(L // n + 1)[:L][None]
+    y = sp.rotary(x, axes, pos)
+    assert y.shape == x.shape and y.is_contiguous()
+    want, made_of = _rotary(x[:1, :, :n], axes, pos[:, :n], 1)
+    _near(y[:1, :, :n], want, _rotary_tolerance(want, made_of, torch.bfloat16))
+    some = y[0, 0, :n].reshape(1, n * d).clone()
+    for b in range(B):
+        whole = y[b, 0, :L // n * n].view(-1, n * d)
+        assert all(bool((whole[i:i + 2 ** 16] == some).all()) for i in range(0, whole.shape[0], 2 ** 16))
+        assert torch.equal(y[b, 0, L // n * n:].flatten(), some[0, :L % n * d])
+
+
 def test_rotary_past_32_bits(sp):
     axes = sp.rotary_axes(64, (32,), device="cuda")
     room = torch.zeros(2 ** 31 + 2 ** 20, dtype=torch.bfloat16, device="cuda")
