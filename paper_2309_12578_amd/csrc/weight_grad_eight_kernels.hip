@@ -111,7 +111,7 @@ __global__ __launch_bounds__(S::threads, 2) void weight_grad_eight_kernel(
     const int tiles = tiles_n * tiles_m, item = xcd_deal(blockIdx.x, 0, gridDim.x);
     const int slice = item / tiles, tile = item % tiles, tile_n = tile / tiles_m, tile_m = tile % tiles_m;
     const int n0 = tile_n * TN, m0 = tile_m * TM;
-    const int first = slice * slice_rows, end = min(rows, first + slice_rows);
+    const int first = slice * slice_rows, end = first + min(rows - first, slice_rows);   // (first + slice_rows may be 2^31)
     const int wave_n = wave / S::WM, wave_m = wave % S::WM;
 
     // dY into LDS in pieces of 1 KB

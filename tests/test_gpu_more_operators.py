@@ -792,6 +792,24 @@ def test_linear_past_32_bits(sp):
     _near(dw, want, _weight_tolerance(dy[some], values, want, torch.bfloat16, 1003))
 
 
+@pytest.mark.parametrize("N", [8, 1])
+def test_weight_gradient_of_the_most_rows(sp, N):
+    rows, M, n = 2 ** 31 - 4098, 64, 5000   # the last slice ends within its own length of 2^31
+    codes, exponents = torch.zeros((rows, M), dtype=torch.int8, device="cuda"), torch.full((rows, 1), 127, dtype=torch.uint8, device="cuda")
+    dy = torch.zeros((rows, N), dtype=torch.bfloat16, device="cuda")
+    of = torch.Generator("cuda").manual_seed(1)
+    for at in (0, rows // 2, rows - n):
+        codes[at:at + n] = torch.randint(-3, 4, (n, M), generator=of, device="cuda", dtype=torch.int8)
+        dy[at:at + n] = torch.randint(-2, 3, (n, N), generator=of, device="cuda").bfloat16()
+    want = sum(dy[at:at + n].double().t() @ codes[at:at + n].double() for at in (0, rows // 2, rows - n))
+    dW, db = torch.empty((N, M), dtype=torch.bfloat16, device="cuda"), torch.empty(N, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(sp.spion_weight_grad_eight_workspace_bytes(rows, N, M), dtype=torch.uint8, device="cuda")
+    sp.spion_weight_grad_eight(dy, codes, exponents, None, dW, db, rows, N, M, sp.SPION_BF16, ws)
+    assert torch.equal(dW, want.bfloat16())   # whole numbers below 2^24: exact sums
+    sums = sum(dy[at:at + n].double().sum(0) for at in (0, rows // 2, rows - n))
+    assert torch.equal(db, sums.bfloat16())
+
+
 # ------------------------------------------------------------------------------------------------
 # all of them
 # ------------------------------------------------------------------------------------------------
