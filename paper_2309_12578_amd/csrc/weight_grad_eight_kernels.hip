@@ -86,7 +86,8 @@ __device__ __forceinline__ void load_bytes(__amdgpu_buffer_rsrc_t from, unsigned
 template <typename T, typename S, bool WHOLE>
 __global__ __launch_bounds__(S::threads, 2) void weight_grad_eight_kernel(
     const T* __restrict__ dY, const signed char* __restrict__ codes, const uint8_t* __restrict__ exponents, const T* __restrict__ weight, T* __restrict__ dW,
-    float* __restrict__ partial, float* __restrict__ bias_partial, int rows, int N, int M, int slices, int slice_rows, int tiles_n, int tiles_m) {
+    float* __restrict__ partial, float* __restrict__ bias_partial, int rows, int N, int M, int slices, int slice_rows, int span_rows, int tiles_n,
+    int tiles_m) {
     constexpr int PLANES = Planes<T>::n, TN = S::TN, TM = S::TM, FN = S::FN, FM = S::FM, WAVES = S::threads / 64;
     constexpr bool ASYNC = WHOLE && PLANES == 1;
     struct Y {
@@ -111,20 +112,18 @@ __global__ __launch_bounds__(S::threads, 2) void weight_grad_eight_kernel(
     const int tiles = tiles_n * tiles_m, item = xcd_deal(blockIdx.x, 0, gridDim.x);
     const int slice = item / tiles, tile = item % tiles, tile_n = tile / tiles_m, tile_m = tile % tiles_m;
     const int n0 = tile_n * TN, m0 = tile_m * TM;
-    const int first = slice * slice_rows, end = first + min(rows - first, slice_rows);   // (first + slice_rows may be 2^31)
+    // the rows of a slice, in spans whose bytes have offsets of 31 bits
+    int first = slice * slice_rows;
+    const int slice_end = first + min(rows - first, slice_rows);   // (first + slice_rows may be 2^31)
+    int end = first + min(slice_end - first, span_rows);
     const int wave_n = wave / S::WM, wave_m = wave % S::WM;
 
     // dY into LDS in pieces of 1 KB
     constexpr int Y_SLOTS = TN / 8, Y_PIECE = 64 / Y_SLOTS, Y_PIECES = kStepRows / Y_PIECE / WAVES;   // rows of a piece, pieces of a wave
     unsigned y_off[Y_PIECES];
-#pragma unroll
-    for (int k = 0; k < Y_PIECES; ++k) {
-        const int row = (Y_PIECES * wave + k) * Y_PIECE + lane / Y_SLOTS;
-        y_off[k] = (unsigned)(row * N + n0 + slot_of(row, lane % Y_SLOTS) * 8) * (unsigned)sizeof(bf16_t);
-    }
     // the next 32 rows, each time
-    const auto y_rows = rows_between(dY, first, end, (size_t)N * sizeof(T)), x_rows = rows_between(codes, first, end, (size_t)pitch),
-               e_rows = rows_between(exponents, first, end, (size_t)(pitch / kGroup));
+    auto y_rows = rows_between(dY, first, end, (size_t)N * sizeof(T)), x_rows = rows_between(codes, first, end, (size_t)pitch),
+         e_rows = rows_between(exponents, first, end, (size_t)(pitch / kGroup));
     auto own = [&]() {   // the wave's number; computed from it anew each time: kept for every stage, the addresses would not fit the scalar registers
         int w = wave;
         asm volatile("" : "+s"(w));
@@ -143,7 +142,18 @@ __global__ __launch_bounds__(S::threads, 2) void weight_grad_eight_kernel(
     const int y_row = tid / Y_SLOTS, y_chunk = tid % Y_SLOTS, x_row = tid / (TM / 16), x_chunk = tid % (TM / 16);
     static_assert(Y_ROWS * Y_TIMES == kStepRows && S::threads / (TM / 16) == kStepRows && WAVES * Y_PIECES * Y_PIECE == kStepRows, "a step's pieces");
     const bool has_m = m0 + 16 * x_chunk < pitch;
-    unsigned x_off = (unsigned)(x_row * pitch + m0 + 16 * x_chunk);
+    unsigned x_off, v_off;
+    auto to_first = [&]() {
+        int t = tid;
+        asm volatile("" : "+v"(t));   // anew for each span: kept for the next one they would take registers throughout
+#pragma unroll
+        for (int k = 0; k < Y_PIECES; ++k) {
+            const int row = (Y_PIECES * wave + k) * Y_PIECE + (t & 63) / Y_SLOTS;
+            y_off[k] = (unsigned)(row * N + n0 + slot_of(row, (t & 63) % Y_SLOTS) * 8) * (unsigned)sizeof(bf16_t);
+        }
+        x_off = (unsigned)(t / (TM / 16) * pitch + m0 + 16 * (t % (TM / 16)));
+        v_off = (unsigned)(t / Y_SLOTS * N + n0 + 8 * (t % Y_SLOTS)) * (unsigned)sizeof(T);
+    };
     auto request_raw = [&](auto& to) {
         const int w = own();
         load_rows(x_rows, x_off, to.codes + 64 * w);
@@ -168,7 +178,6 @@ __global__ __launch_bounds__(S::threads, 2) void weight_grad_eight_kernel(
         int exponent;
     };
     constexpr bool RANGED = WHOLE && !ASYNC;
-    unsigned v_off = (unsigned)(y_row * N + n0 + 8 * y_chunk) * (unsigned)sizeof(T);
     auto request = [&](Rows& v, int at) {
         if constexpr (RANGED) {   // (fp32) the next 32 rows each time, by their range as above
 #pragma unroll
@@ -280,103 +289,114 @@ __global__ __launch_bounds__(S::threads, 2) void weight_grad_eight_kernel(
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    const int steps = (end - first + kStepRows - 1) / kStepRows;
-    if constexpr (ASYNC) {
-        // Step s reads ys[s % 3] and xs[s % 2], makes xs[(s + 1) % 2] from raw[(s + 1) % 3], and requests what two and three steps on takes into the stages
-        // that step s - 1 has read.  Of what is in flight at its start, the loads of step s - 1 may stay there: codes and exponents of s + 2, rows of s + 1.
-        static_assert(Y_PIECES == 2 || Y_PIECES == 4, "loads of a step");
-        auto step = [&](Y& y, Y& y_free, X& x, X& x_free, Raw& raw, Raw& raw_free) {
-            __builtin_amdgcn_s_waitcnt(Y_PIECES == 2 ? kWaitVm4 : kWaitVm6);
-            meet();
-            Operands o[2];
-            const uint4 q = raw.codes[tid];
-            const int e = raw.exponents[tid];
+    for (;;) {
+        to_first();
+        const int steps = (end - first + kStepRows - 1) / kStepRows;
+        if constexpr (ASYNC) {
+            // Step s reads ys[s % 3] and xs[s % 2], makes xs[(s + 1) % 2] from raw[(s + 1) % 3], and requests what two and three steps on takes into the stages
+            // that step s - 1 has read.  Of what is in flight at its start, the loads of step s - 1 may stay there: codes and exponents of s + 2, rows of s + 1.
+            static_assert(Y_PIECES == 2 || Y_PIECES == 4, "loads of a step");
+            auto step = [&](Y& y, Y& y_free, X& x, X& x_free, Raw& raw, Raw& raw_free) {
+                __builtin_amdgcn_s_waitcnt(Y_PIECES == 2 ? kWaitVm4 : kWaitVm6);
+                meet();
+                Operands o[2];
+                const uint4 q = raw.codes[tid];
+                const int e = raw.exponents[tid];
 #pragma unroll
-            for (int f = 0; f < FM; ++f) read_x(o[0], x, 0, f);
+                for (int f = 0; f < FM; ++f) read_x(o[0], x, 0, f);
 #pragma unroll
-            for (int f = 0; f < FN; ++f) read_y(o[0], y, 0, 0, f);
-            request_raw(raw_free);
-            request_y(y_free);
-            const float scale = eight_scale(e);
-            unsigned next[8];
-            __builtin_amdgcn_sched_barrier(0);
-            // each of the first products with some of the second's operands and of the next step's codes beside it
-#pragma unroll
-            for (int i = 0; i < FN * FM; ++i) {
-                multiply(o[0], i);
-                if (i < FM) read_x(o[1], x, 1, i);
-                else if (i < FM + FN) read_y(o[1], y, 0, 1, i - FM);
-#pragma unroll
-                for (int k = 0; k < 8 / (FN * FM); ++k) next[i * (8 / (FN * FM)) + k] = convert(q, scale, i * (8 / (FN * FM)) + k);
+                for (int f = 0; f < FN; ++f) read_y(o[0], y, 0, 0, f);
+                request_raw(raw_free);
+                request_y(y_free);
+                const float scale = eight_scale(e);
+                unsigned next[8];
                 __builtin_amdgcn_sched_barrier(0);
-            }
-            put_x(next, x_free);
+                // each of the first products with some of the second's operands and of the next step's codes beside it
 #pragma unroll
-            for (int i = 0; i < FN * FM; ++i) multiply(o[1], i);
-            if (wants_bias && turn == share) {
-                add_bias(o[0]);
-                add_bias(o[1]);
-            }
-            turn = turn + 1 == shares ? 0 : turn + 1;
-        };
-        request_raw(raw0);
-        request_raw(raw1);
-        request_y(ys0);
-        request_raw(raw2);
-        request_y(ys1);
-        __builtin_amdgcn_s_waitcnt(kWaitVm0);
-        unsigned x[8];
+                for (int i = 0; i < FN * FM; ++i) {
+                    multiply(o[0], i);
+                    if (i < FM) read_x(o[1], x, 1, i);
+                    else if (i < FM + FN) read_y(o[1], y, 0, 1, i - FM);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = convert(raw0.codes[tid], eight_scale(raw0.exponents[tid]), i);
-        put_x(x, xs0);
-        for (int s = 0; s < steps; s += 6) {
-            step(ys0, ys2, xs0, xs1, raw1, raw0);
-            if (s + 1 >= steps) break;
-            step(ys1, ys0, xs1, xs0, raw2, raw1);
-            if (s + 2 >= steps) break;
-            step(ys2, ys1, xs0, xs1, raw0, raw2);
-            if (s + 3 >= steps) break;
-            step(ys0, ys2, xs1, xs0, raw1, raw0);
-            if (s + 4 >= steps) break;
-            step(ys1, ys0, xs0, xs1, raw2, raw1);
-            if (s + 5 >= steps) break;
-            step(ys2, ys1, xs1, xs0, raw0, raw2);
-        }
-        __builtin_amdgcn_s_waitcnt(kWaitVm0);   // what was requested for steps that are not there
-    } else {
-        // rows are requested two steps before they are written to LDS, and three before they are multiplied
-        Rows va, vb;
-        auto step = [&](int s, Rows& v, Y& y, Y& y_free, X& x, X& x_free) {
-            const int at = first + s * kStepRows;
-            meet();
-            put(v, at + kStepRows, y_free, x_free);
-            request(v, at + 3 * kStepRows);
-            const bool sums = wants_bias && turn == share;
-#pragma unroll
-            for (int k = 0; k < kStepRows / 16; ++k) {
-                Operands o;
-#pragma unroll
-                for (int f = 0; f < FM; ++f) read_x(o, x, k, f);
-#pragma unroll
-                for (int p = 0; p < PLANES; ++p) {
-#pragma unroll
-                    for (int f = 0; f < FN; ++f) read_y(o, y, p, k, f);
-#pragma unroll
-                    for (int i = 0; i < FN * FM; ++i) multiply(o, i);
-                    if (sums) add_bias(o);
+                    for (int k = 0; k < 8 / (FN * FM); ++k) next[i * (8 / (FN * FM)) + k] = convert(q, scale, i * (8 / (FN * FM)) + k);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
+                put_x(next, x_free);
+#pragma unroll
+                for (int i = 0; i < FN * FM; ++i) multiply(o[1], i);
+                if (wants_bias && turn == share) {
+                    add_bias(o[0]);
+                    add_bias(o[1]);
+                }
+                turn = turn + 1 == shares ? 0 : turn + 1;
+            };
+            request_raw(raw0);
+            request_raw(raw1);
+            request_y(ys0);
+            request_raw(raw2);
+            request_y(ys1);
+            __builtin_amdgcn_s_waitcnt(kWaitVm0);
+            unsigned x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = convert(raw0.codes[tid], eight_scale(raw0.exponents[tid]), i);
+            put_x(x, xs0);
+            for (int s = 0; s < steps; s += 6) {
+                step(ys0, ys2, xs0, xs1, raw1, raw0);
+                if (s + 1 >= steps) break;
+                step(ys1, ys0, xs1, xs0, raw2, raw1);
+                if (s + 2 >= steps) break;
+                step(ys2, ys1, xs0, xs1, raw0, raw2);
+                if (s + 3 >= steps) break;
+                step(ys0, ys2, xs1, xs0, raw1, raw0);
+                if (s + 4 >= steps) break;
+                step(ys1, ys0, xs0, xs1, raw2, raw1);
+                if (s + 5 >= steps) break;
+                step(ys2, ys1, xs1, xs0, raw0, raw2);
             }
-            turn = turn + 1 == shares ? 0 : turn + 1;
-        };
-        request(va, first);
-        request(vb, first + kStepRows);
-        put(va, first, ys0, xs0);
-        request(va, first + 2 * kStepRows);
-        for (int s = 0; s < steps; s += 2) {
-            step(s, vb, ys0, ys1, xs0, xs1);
-            if (s + 1 >= steps) break;
-            step(s + 1, va, ys1, ys0, xs1, xs0);
+            __builtin_amdgcn_s_waitcnt(kWaitVm0);   // what was requested for steps that are not there
+        } else {
+            // rows are requested two steps before they are written to LDS, and three before they are multiplied
+            Rows va, vb;
+            auto step = [&](int s, Rows& v, Y& y, Y& y_free, X& x, X& x_free) {
+                const int at = first + s * kStepRows;
+                meet();
+                put(v, at + kStepRows, y_free, x_free);
+                request(v, at + 3 * kStepRows);
+                const bool sums = wants_bias && turn == share;
+#pragma unroll
+                for (int k = 0; k < kStepRows / 16; ++k) {
+                    Operands o;
+#pragma unroll
+                    for (int f = 0; f < FM; ++f) read_x(o, x, k, f);
+#pragma unroll
+                    for (int p = 0; p < PLANES; ++p) {
+#pragma unroll
+                        for (int f = 0; f < FN; ++f) read_y(o, y, p, k, f);
+#pragma unroll
+                        for (int i = 0; i < FN * FM; ++i) multiply(o, i);
+                        if (sums) add_bias(o);
+                    }
+                }
+                turn = turn + 1 == shares ? 0 : turn + 1;
+            };
+            request(va, first);
+            request(vb, first + kStepRows);
+            put(va, first, ys0, xs0);
+            request(va, first + 2 * kStepRows);
+            for (int s = 0; s < steps; s += 2) {
+                step(s, vb, ys0, ys1, xs0, xs1);
+                if (s + 1 >= steps) break;
+                step(s + 1, va, ys1, ys0, xs1, xs0);
+            }
         }
+        if (end == slice_end) break;
+        // the next span: the pipeline starts anew, the sums go on
+        first = end;
+        end = first + min(slice_end - first, span_rows);
+        y_rows = rows_between(dY, first, end, (size_t)N * sizeof(T));
+        x_rows = rows_between(codes, first, end, (size_t)pitch);
+        e_rows = rows_between(exponents, first, end, (size_t)(pitch / kGroup));
+        meet();   // what the span before has in LDS is read
     }
 
     // lane l has m = .. + l % 32 of rows n = .. + 8 (i / 4) + 4 (l / 32) + i % 4: whole lines
@@ -568,7 +588,7 @@ constexpr int kBigRows = 2048;
 
 struct Plan {
     int side_n = 128, side_m = 128;   // of a tile
-    int tiles_n, tiles_m, slices, slice_rows, shares;
+    int tiles_n, tiles_m, slices, slice_rows, span_rows, shares;
     size_t bias_at, total;   // bytes
     Plan(int rows, int N, int M, bool is_bf16, bool whole) {
         const long long pitch = eight_pitch(M);
@@ -584,7 +604,8 @@ struct Plan {
         if (is_bf16 && side_n == 128 && rows * tiles < (long long)kFewRows * kGroups) groups = kGroups / 2;
         slices = (int)std::max<long long>(1, std::min(groups / tiles, most));
         slice_rows = (int)((((long long)rows + slices - 1) / slices + kStepRows - 1) / kStepRows * kStepRows);
-        slice_rows = (int)std::min<long long>(slice_rows, (0x7fffffffll / std::max<long long>(4ll * N, pitch) - 4 * kStepRows) / kStepRows * kStepRows);   // 31 bits of offset
+        // 31 bits of offset, three steps beyond the last one's too
+        span_rows = (int)std::min<long long>(slice_rows, (0x7fffffffll / std::max<long long>((is_bf16 ? 2ll : 4ll) * N, pitch) - 4 * kStepRows) / kStepRows * kStepRows);
         slices = (int)(((long long)rows + slice_rows - 1) / slice_rows);
         shares = tiles_m * 2;
         bias_at = slices > 1 ? (size_t)slices * outputs * sizeof(float) : 0;
@@ -611,7 +632,7 @@ static hipError_t launch_t(const WeightGradEight& a, hipStream_t st) {
     const unsigned groups = (unsigned)p.slices * (unsigned)p.tiles_n * (unsigned)p.tiles_m;
     auto launch = [&](auto kernel, int threads) {
         kernel<<<dim3(groups), dim3(threads), 0, st>>>(static_cast<const T*>(a.dY), a.codes, a.exponents, weight, dW, partial, bias_partial, a.rows, a.N,
-                                                       a.M, p.slices, p.slice_rows, p.tiles_n, p.tiles_m);
+                                                       a.M, p.slices, p.slice_rows, p.span_rows, p.tiles_n, p.tiles_m);
     };
     typedef std::conditional_t<is_bf16, Wide, Large> Big;
     if (p.side_n == 256 && whole) launch(weight_grad_eight_kernel<T, Big, true>, Big::threads);

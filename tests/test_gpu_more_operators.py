@@ -792,6 +792,22 @@ def test_linear_past_32_bits(sp):
     _near(dw, want, _weight_tolerance(dy[some], values, want, torch.bfloat16, 1003))
 
 
+@pytest.mark.parametrize("dtype,rows,N,M", [
+    (torch.float32, 1000, 2 ** 20, 64), (torch.float32, 2100, 2 ** 20, 65), (torch.float32, 2100, 2 ** 20 - 1, 64),
+    (torch.bfloat16, 2000, 2 ** 20, 64), (torch.bfloat16, 2100, 2 ** 20, 65), (torch.bfloat16, 2000, 2 ** 20 - 4, 64), (torch.bfloat16, 1793, 2 ** 20 - 8, 128)])
+def test_weight_gradient_of_slices_longer_than_31_bits(sp, dtype, rows, N, M):
+    """Whole numbers, whose sums are exact in any order: every row is there once."""
+    of = torch.Generator("cuda").manual_seed(1)
+    P = (M + 63) // 64 * 64
+    codes, exponents = torch.randint(-3, 4, (rows, P), generator=of, device="cuda", dtype=torch.int8), torch.full((rows, P // 64), 127, dtype=torch.uint8, device="cuda")
+    dy = torch.randint(-2, 3, (rows, N), generator=of, device="cuda", dtype=torch.int8).to(dtype)
+    dW, db = torch.empty((N, M), dtype=dtype, device="cuda"), torch.empty(N, dtype=dtype, device="cuda")
+    ws = torch.empty(sp.spion_weight_grad_eight_workspace_bytes(rows, N, M), dtype=torch.uint8, device="cuda")
+    sp.spion_weight_grad_eight(dy, codes, exponents, None, dW, db, rows, N, M, sp.SPION_F32 if dtype == torch.float32 else sp.SPION_BF16, ws)
+    want = dy.float().t() @ codes[:, :M].float()
+    assert torch.equal(dW, want.to(dtype)) and torch.equal(db, dy.sum(0, dtype=torch.float32).to(dtype))
+
+
 @pytest.mark.parametrize("N", [8, 1])
 def test_weight_gradient_of_the_most_rows(sp, N):
     rows, M, n = 2 ** 31 - 4098, 64, 5000   # the last slice ends within its own length of 2^31

@@ -193,3 +193,9 @@ def test_weight_gradient_refuses():
     assert call(*good, dtype=3) == -3 and call(FAKE, ctypes.c_void_p(264), *good[2:]) == -5
     for bad in (dict(ws=NONE), dict(ws=ctypes.c_void_p(264)), dict(size=need - 1)):
         assert call(*good, **bad) == -4
+
+
+@pytest.mark.parametrize("rows,N,M", [(16384, 131072, 4096), (32768, 152064, 8192), (65536, 28672, 8192), (2 ** 30, 2 ** 13, 2 ** 13), (2 ** 20, 2 ** 20, 2 ** 16), (300, 2 ** 20, 64)])
+def test_weight_gradient_of_large_projections_needs_little_room(rows, N, M):
+    """Where dW has tiles enough to fill the machine, only the bias' sums: 2 numbers an output and 128 columns, a 16th of dW in bf16 (M up to 64: as much as dW)."""
+    assert sp.spion_weight_grad_eight_workspace_bytes(rows, N, M) <= 2 * 4 * N * ((M + 127) // 128)
