@@ -792,6 +792,31 @@ def test_linear_past_32_bits(sp):
     _near(dw, want, _weight_tolerance(dy[some], values, want, torch.bfloat16, 1003))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,M,N", [
+    (2049, 1100, 1000), (2100, 1100, 1003), (4097, 1024, 1032), (2048, 1088, 1024), (2047, 1100, 1000), (2080, 2048, 8192), (2111, 4096, 4096), (2049, 2050, 8200),
+    (9000, 130, 8200), (31, 130, 140), (33, 200, 136), (20000, 72, 40), (4127, 256, 768), (16385, 768, 776), (70001, 128, 129)])
+@pytest.mark.parametrize("column", [False, True])
+@pytest.mark.parametrize("aligned", [True, False])
+def test_weight_gradient_of_whole_numbers(sp, dtype, rows, M, N, column, aligned):
+    """Exact in any order: no row, column or step is left out or there twice.  Tiles of all sizes with remainders, one slice and many, with the bias' gradient."""
+    of = torch.Generator("cuda").manual_seed(rows)
+    code, P = sp.SPION_F32 if dtype == torch.float32 else sp.SPION_BF16, (M + 63) // 64 * 64
+    codes, exponents = torch.randint(-4, 5, (rows, P), generator=of, device="cuda", dtype=torch.int8), torch.full((rows, P // 64), 127, dtype=torch.uint8, device="cuda")
+    room = torch.randint(-3, 4, (rows * N + 1,), generator=of, device="cuda", dtype=torch.int8).to(dtype)
+    dy = (room[:-1] if aligned else room[1:]).view(rows, N)
+    weight = torch.randint(1, 8, (M,), generator=of, device="cuda").to(dtype) if column else None
+    dW, db = torch.empty((N, M), dtype=dtype, device="cuda"), torch.empty(N, dtype=dtype, device="cuda")
+    ws = torch.empty(sp.spion_weight_grad_eight_workspace_bytes(rows, N, M), dtype=torch.uint8, device="cuda")
+    sp.spion_weight_grad_eight(dy, codes, exponents, weight, dW, db, rows, N, M, code, ws)
+    want = torch.matmul(dy.double().t().contiguous(), codes[:, :M].double()) * (1 if weight is None else weight.double())
+    sums = dy.double().sum(0)
+    assert want.abs().max() < 2 ** 24 and torch.equal(dW, want.to(dtype)) and torch.equal(db, sums.to(dtype))
+    alone = torch.empty_like(dW)
+    sp.spion_weight_grad_eight(dy, codes, exponents, weight, alone, None, rows, N, M, code, ws)
+    assert torch.equal(alone, dW)
+
+
 @pytest.mark.parametrize("dtype,rows,N,M", [
     (torch.float32, 1000, 2 ** 20, 64), (torch.float32, 2100, 2 ** 20, 65), (torch.float32, 2100, 2 ** 20 - 1, 64),
     (torch.bfloat16, 2000, 2 ** 20, 64), (torch.bfloat16, 2100, 2 ** 20, 65), (torch.bfloat16, 2000, 2 ** 20 - 4, 64), (torch.bfloat16, 1793, 2 ** 20 - 8, 128)])
