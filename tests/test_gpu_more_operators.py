@@ -975,6 +975,36 @@ def test_sub_layer_is_the_same_with_its_residual_added_before(sp):
         m(E, pattern)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,M,N", [(16384, 256, 768), (255, 192, 576), (70, 130, 40)])
+def test_norm_and_projection_one_after_the_other(sp, dtype, rows, M, N):
+    """Between the two lie y and its gradient, tensors of the type, each rounded once; nothing else comes in.  With what one hands to the other as it is, each is
+    its formula in 64 bits, and together they are the two, to the bit."""
+    x, r, w, W, dy, dh = [_randn(s, dtype, k, v) for k, (s, v) in enumerate(
+        [((rows, M), 1), ((rows, M), 1), ((M,), 1), ((N, M), M ** -0.5), ((rows, N), 1), ((rows, M), 1)])]
+    leaves = [t.requires_grad_() for t in (x, r, w, W)]
+    y, h, p = sp.rms_norm(x, w, r, EPS, checkpoint=True)
+    z = sp.linear8(y, W, checkpoint=p)
+    dx, dr, dw, dW = torch.autograd.grad([z, h], leaves, [dy, dh])
+    held = y.detach().requires_grad_()   # as a program has it that runs them apart
+    alone = sp.linear8(held, W, checkpoint=p)
+    g, other = torch.autograd.grad(alone, [held, W], dy)
+    assert g.dtype == dtype and torch.equal(alone, z) and torch.equal(other, dW)
+    again, stream, _ = sp.rms_norm(x, w, r, EPS, checkpoint=True)
+    for a, b in zip(torch.autograd.grad([again, stream], [x, r, w], [g, dh]), (dx, dr, dw)):
+        assert torch.equal(a, b)
+    s, rstd, zz, want = _norm(x.detach(), w.detach(), r.detach())
+    # three roundings for z and one for its product, s off by one more
+    _near(y.detach(), want, half(dtype) * want.abs() + 5 * U * want.abs())
+    full = y.detach().double() @ W.detach().double().t()
+    _near(z.detach(), full, _weight_tolerance(y.detach().t(), W.detach().t(), full, dtype, M))
+    full = dy.double() @ W.detach().double()
+    _near(g, full, _weight_tolerance(dy.t(), W.detach(), full, dtype, N))
+    want, tol, want_w, tol_w = _norm_grad(g, dh, w.detach(), rstd, _eight(zz)[2], dtype)
+    _near(dx, want, tol)
+    _near(dw, want_w, tol_w)
+
+
 def _everything(sp, dtype, eight):
     """(module, leaves, contents of the step, step): bias, lengths, both dropouts, positions of several axes and a residual.  What a step returns is detached:
     a graph that lives, of the same leaves, would be in the way of a capture."""
