@@ -303,7 +303,7 @@ int spion_unpack_eight(const int8_t *codes, const uint8_t *exponents, const void
  * Root-mean-square norm over rows of D elements (1 <= D <= 16384; x, residual, weight, y, h, dy, dh, dx, dw of `dtype`; rstd fp32 [rows]):
  *   s = x + residual (residual may be NULL),  rstd = 1 / sqrt(mean s^2 + eps),  z = s rstd,  y = z weight,  h = s rounded.
  *   y, h, rstd, codes may be NULL: not wanted.  codes, exponents: z in 8 bits (as above), with SPION_NORM_CODES_OF_Y y.  Sums of squares, and what
- *   decides a code, are in 64 bits.
+ *   decides a code (x + residual too), are in 64 bits; y is off by four roundings in fp32 and one to its type.
  *   No result may overlap an operand.
  * Gradient:  dx = dh + rstd (weight dy - z mean(weight dy z)),  dw = sum of dy z.  It is the residual's too.  z from the codes (of z), or codes NULL and z = h rstd.
  *   dh may be NULL (none), dw may be NULL (not wanted).  fp32 sums in a fixed order.
@@ -320,7 +320,7 @@ int spion_rms_norm_grad(const void *dy, const void *dh, const void *h, const int
  * Gradients of a projection Y = X W^T + b whose input was kept in 8 bits:
  *   dW [N, M] = dY^T X,  X = code * 2^k * weight[column] (weight [M] or NULL: 1),  db [N] (or NULL) = column sums of dY.
  *   dY [rows, N], weight, dW, db of `dtype`; codes [rows, P], 16-byte aligned, exponents [rows, P / 64], as above with D = M.
- * The codes enter the product exactly, an fp32 dY as well; fp32 sums in a fixed order.  1 <= N, M <= 2^20, N * P <= 2^36, 1 <= rows < 2^31 - 4096.
+ * The codes enter the product exactly, an fp32 dY but for its bits below 2^-133; fp32 sums in a fixed order.  1 <= N, M <= 2^20, N * P <= 2^36, 1 <= rows < 2^31 - 4096.
  */
 size_t spion_weight_grad_eight_workspace_bytes(int32_t rows, int32_t N, int32_t M);
 int spion_weight_grad_eight(const void *dY, const int8_t *codes, const uint8_t *exponents, const void *weight, void *dW, void *db, int32_t rows,

@@ -7,8 +7,9 @@
 // (the sum over its lanes, the root) is shared by K times as many.  The sum of squares is in 64 bits, and so is all that decides a code: with a row's sum in
 // another order, or in 32 bits, one in 10^5 codes would be its neighbour.
 //
-// 65536 x 4096, bf16, with residual and codes: forward 440 - 455 us, 5.4 TB/s, backward from the codes 355 - 420 us, 4.5 - 5.3 TB/s (copies here reach 5.0 - 5.6).  16384 x 256:
-// 9.7 and 8.2 us, and 3.8 for the weight's sums.  With all of a code's arithmetic in 64 bits the forward pass took 523 us: 64 bits only where 32 cannot tell.
+// 65536 x 4096, bf16, with residual: forward with codes 440 - 465 us, 5.2 - 5.4 TB/s, without 406, 5.3; y in 8 bits only 349; backward from the codes 355 - 430, 4.4 - 5.3, from h 400,
+// 5.4 (copies here reach 5.0 - 5.6).  fp32, 16384 x 4096: 210, 195, 156; 160, 197.  bf16, 16384 x 256, with codes: 10.4 and 8.3 us, and 3.8 for the weight's sums.  With
+// all of a code's arithmetic in 64 bits the forward pass took 523 us: 64 bits only where 32 cannot tell.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

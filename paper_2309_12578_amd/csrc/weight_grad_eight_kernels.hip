@@ -2,9 +2,10 @@
 // and beside it the bias' gradient, the column sums of dY.
 //
 // code * 2^k is exact in bf16, so X enters the product as it was kept, without a rounding.  An fp32 dY enters as the sum of three bf16 numbers, its
-// significand's 24 bits by eights: three bf16 products, exact but for the sums, at 8 times the rate of the fp32 matrix instruction each.
+// significand's 24 bits by eights (but for bits below 2^-133, which bf16 does not have: of numbers below 2^-110): three bf16 products, exact but for the sums, at 8 times
+// the rate of the fp32 matrix instruction each.
 //
-// Bound by the matrix units where N and M are large (65536 x 2048 x 2048 bf16 570 - 640 us, 0.86 - 0.96 PFLOP/s, the sums of its slices 16 us; fp32 8192 x 1536 x 512 58 us and 7), by the
+// Bound by the matrix units where N and M are large (65536 x 2048 x 2048 bf16 540 - 630 us, 0.87 - 1.0 PFLOP/s, the sums of its slices 16 us; fp32 8192 x 1536 x 512 59 us and 7), by the
 // start and the end of a slice where they are small (16384 x 768 x 256 bf16 21 us and 5).  Tiles as large as the registers hold, so that LDS feeds them; bf16 as two workgroups
 // a compute unit, one of which multiplies while the other waits (one of 256 x 256: 685 us).
 #include <hip/hip_runtime.h>
@@ -82,7 +83,7 @@ __device__ __forceinline__ void load_bytes(__amdgpu_buffer_rsrc_t from, unsigned
 // bf16 and WHOLE (rows of dY aligned to 16 bytes): dY goes from memory straight into LDS, two steps ahead; codes and exponents too, three steps ahead, each lane's
 // to where it takes them from again.  (All by the same instruction, so that the counts that are waited for do not depend on how the compiler orders loads.)  Rows
 // behind the last come as zeros, codes and scales as well, by the range of the loads.
-// Else through registers, requested two steps ahead.
+// Else through registers, requested two steps ahead; where rows of dY are not aligned, by elements (bf16, with the sums, 16384 x 1000 x 768 46 us, x 1001 119).
 template <typename T, typename S, bool WHOLE>
 __global__ __launch_bounds__(S::threads, 2) void weight_grad_eight_kernel(
     const T* __restrict__ dY, const signed char* __restrict__ codes, const uint8_t* __restrict__ exponents, const T* __restrict__ weight, T* __restrict__ dW,

@@ -63,6 +63,7 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Ten
     z = s / sqrt(mean(s^2) + eps), y = z * weight and h = s, the stream that goes on (None without a residual).
     checkpoint: p is z in 8 bits with `weight` as its weight, so that it stands for y; the backward pass then takes z from p's codes and keeps
     neither x nor h, and `linear8` may keep the same codes (else p is None).
+    y is a tensor of x's type, and so is its gradient: in bf16 both are rounded on their way between the norm and what takes y.
     Differentiable with respect to x, weight and residual, through y and h."""
     y, h, codes, exponents = (_b._host or _b._native()).rms_norm(x, weight, residual, eps, checkpoint)
     return y, h, None if codes is None else _packed(codes, exponents, x.shape[-1], weight.detach())

@@ -59,7 +59,7 @@ class _Projection(nn.Linear):
             if torch.is_autocast_enabled():   # in autocast's type, as nn.Linear; linear8 takes its operands' own
                 dtype = torch.get_autocast_dtype("cuda")
                 x, weight, bias = x.to(dtype), weight.to(dtype), None if bias is None else bias.to(dtype)
-                if checkpoint is not None and checkpoint.weight is not None:   # (a rounding of the codes' factors, 2^-9 of them in bf16, beside the codes' own 2^-8)
+                if checkpoint is not None and checkpoint.weight is not None:   # (a rounding of the codes' factors, 2^-8 of them at most in bf16, beside the codes' own 2^-7)
                     checkpoint = dataclasses.replace(checkpoint, weight=checkpoint.weight.to(dtype))
             return linear8(x, weight, bias, checkpoint)
         y = None

@@ -1121,7 +1121,7 @@ def test_sub_layer_whose_norm_is_another(sp, dtype, eight, how):
     with torch.no_grad():
         m.norm.weight.mul_(2.0)
     want, = torch.autograd.grad(run(), m.w_qkv.weight, gb)
-    # two ways to 8 bits, each with roundings of up to 2^-8 of a group's largest element
+    # two ways to 8 bits, each with roundings of up to 2^-7 of a group's largest element
     assert (dw.double() - want.double()).norm() <= (2 ** -6 if eight else 1e-5) * want.double().norm()
 
 
