@@ -37,6 +37,8 @@ class Packed8:
 
 def _packed(codes: torch.Tensor, exponents: torch.Tensor, size: int, weight: Optional[torch.Tensor] = None) -> Packed8:
     """What an operator made, without the checks, which take 4 us, about as long as a call for a token."""
+    if torch.compiler.is_compiling():   # torch.compile follows how a dataclass is made, not this
+        return Packed8(codes, exponents, size, weight)
     p = object.__new__(Packed8)
     d = p.__dict__
     d["codes"], d["exponents"], d["size"], d["weight"] = codes, exponents, size, weight

@@ -1298,6 +1298,44 @@ def test_graphs_and_streams(sp, dtype):
     assert all(same(a, b) for a, b in zip(got, wants))
 
 
+@pytest.mark.parametrize("options", [dict(norm="rms"), dict(norm="rms", eight_bit=True), dict(eight_bit=True), dict(norm="rms", eight_bit=True, turned=True)])
+def test_sub_layer_in_a_compiled_program(sp, options):
+    """The operators break the graph and run as they are."""
+    torch._dynamo.reset()
+    options = dict(options)
+    if options.pop("turned", False):
+        options["rotary"] = sp.rotary_axes(64, (32,))
+    m, pattern = sp.SparseMHA(128, 2, device="cuda", **options), _pattern(sp, _mask(4, 2), 32)
+    E, g = _randn((2, 128, 128), torch.float32, 1).requires_grad_(), _randn((2, 128, 128), torch.float32, 2)
+    leaves = [E, *m.parameters()]
+    results = []
+    for run in (m, torch.compile(m, backend="eager")):
+        y = run(E, pattern)
+        results.append([y.detach(), *torch.autograd.grad(y, leaves, g)])
+    # the same operators but for the projections' weights, by other sums
+    assert all((a.double() - b.double()).norm() <= 1e-5 * a.double().norm() for a, b in zip(*results))
+    torch._dynamo.reset()
+
+
+def test_operators_in_a_compiled_program(sp):
+    torch._dynamo.reset()
+    axes, pos = sp.rotary_axes(64, (32,), device="cuda"), torch.arange(9, device="cuda")[None]
+
+    def step(x, w, r, W):
+        y, h, p = sp.rms_norm(x, w, r, checkpoint=True)
+        z = sp.rotary(sp.linear8(y, W, checkpoint=p), axes, pos)
+        with torch.no_grad():
+            v = sp.unpack8(sp.pack8(x)) + sp.unpack8(sp.rms_norm8(x, w)[0])
+        return z, h, v
+    x, w, r, W = [_randn(s, torch.float32, k).requires_grad_() for k, s in enumerate([(2, 9, 64), (64,), (2, 9, 64), (128, 64)])]
+    results = []
+    for run in (step, torch.compile(step, backend="eager")):
+        z, h, v = run(x, w, r, W)
+        results.append([z.detach(), h.detach(), v, *torch.autograd.grad([z, h], [x, w, r, W], [torch.ones_like(z), torch.ones_like(h)])])
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    torch._dynamo.reset()
+
+
 def test_calls_that_are_refused(sp):
     x, w, W = _randn((4, 64), torch.float32, 1), _randn((64,), torch.float32, 2), _randn((8, 64), torch.float32, 3)
     h4, axes = x.view(1, 2, 2, 64), sp.rotary_axes(64, (16, 16), device="cuda")
