@@ -42,7 +42,8 @@ class _RmsNorm(nn.Module):
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None, checkpoint: bool = False):
         dtype = self.weight.dtype
-        if x.dtype != dtype and torch.is_autocast_enabled():   # in the weight's type, as LayerNorm under autocast in fp32
+        if (x.dtype != dtype or residual is not None and residual.dtype != dtype) and torch.is_autocast_enabled():
+            # in the weight's type, as LayerNorm under autocast in fp32
             x, residual = x.to(dtype), None if residual is None else residual.to(dtype)
         return rms_norm(x, self.weight, residual, self.eps, checkpoint)
 

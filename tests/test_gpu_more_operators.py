@@ -1178,6 +1178,17 @@ def test_sub_layers_under_autocast(sp):
             m(E.bfloat16(), pattern)
 
 
+def test_sub_layer_under_autocast_takes_a_stream_of_another_type(sp):
+    """The branch and the stream each in any of the two types."""
+    m, pattern = sp.SparseMHA(128, 2, norm="rms", device="cuda"), _pattern(sp, _mask(4, 2), 32)
+    E, R = [_randn((2, 128, 128), torch.bfloat16, k) for k in (1, 2)]
+    with torch.autocast("cuda", dtype=torch.bfloat16):
+        results = [m(e, pattern, residual=r) for e in (E, E.float()) for r in (R, R.float())]
+    assert all(b.dtype == s.dtype == torch.float32 and torch.equal(b, results[-1][0]) and torch.equal(s, E.float() + R.float()) for b, s in results)
+    with pytest.raises(ValueError):
+        m(E.float(), pattern, residual=R)
+
+
 @pytest.mark.parametrize("norm", ["rms", "layer"])
 @pytest.mark.parametrize("dtype", TYPES)
 def test_sub_layer_in_8_bits_under_autocast(sp, norm, dtype):
